@@ -539,3 +539,12 @@ class SparseAdam:
         self.t += 1
         sparse_adam(self.table, grad, self.exp_avg, self.exp_avg_sq, self.t, self.lr, self.betas, self.eps,
                     touched=touched)
+
+
+# ---------------------------------------------------------------------------
+# The operators of the layer around the memory.
+
+from . import layer as _layer  # noqa: E402
+from .layer import *  # noqa: E402,F401,F403
+
+__all__ += _layer.__all__

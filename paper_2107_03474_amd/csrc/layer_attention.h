@@ -1,0 +1,382 @@
+// layer_attention.h -- part of liblram: what the attention kernels share.
+//
+// For a sequence of nq queries and nk keys, off = nk - nq; query i of head h sees key j if j < nk and, causal,
+// j <= i + off.  In units of log 2:
+//     z_ij = c q_i . k_j + t_h(j - i - off),  c = scale log2 e,  t_h the bias by distance, times log2 e
+//     p_ij = 2^(z_ij - m_i) / l_i,  o_i = sum_j p_ij v_j,  lse_i = m_i + log2 l_i
+//
+// The G = heads / kv_heads query heads that share a key head are rows of one matrix: packed row r of a sequence is query
+// r / G of the group's head r % G, so a few queries fill a tile, and a tile meets a key once for all G heads.
+//
+// Tiles.  Products run on the matrix cores as 32 x 32 blocks with K = 16 (fp32: eight steps of K = 2).  A lane's operand is
+// 8 elements: A row (lane & 31), k = 8 (lane >> 5) .. + 7, B column the same; a result's lane holds column lane & 31,
+// rows 8 (r >> 2) + 4 (lane >> 5) + (r & 3) for r < 16.  Scores are formed transposed (keys x rows), so a lane owns one row of
+// the softmax, and its 8 results r = 8 c .. 8 c + 7 are the B operand of the next product for keys 16 c .. 16 c + 15 as
+// they stand, with the k order (4 h + 0..3, 8 + 4 h + 0..3) that the other operand's loads follow (col_frag).
+
+#pragma once
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "layer_common.h"
+
+namespace {
+
+using f32x16 = float __attribute__((ext_vector_type(16)));
+using f32x8 = float __attribute__((ext_vector_type(8)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+using bf16x4 = __bf16 __attribute__((ext_vector_type(4)));
+using s16x4 = short __attribute__((ext_vector_type(4)));
+using Lds = __attribute__((address_space(3))) char*;
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int XCDS = 8;
+constexpr int ROWS = 32;     // packed rows (or keys) of a wave
+constexpr int KEYS = 64;     // keys of a tile in LDS
+constexpr int BIAS_PAD = 96;  // distances that a tile reaches past the last one with a bias of its own
+
+// Device-side view of a call.
+struct Args {
+  const void *q, *k, *v;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;  // strides in elements
+  const int32_t *start_q, *start_k, *used_k;
+  const void* rel_weight;
+  const int32_t* rel_bucket;
+  int64_t tq, tk;
+  int32_t heads, kv_heads, group, batch;
+  int32_t causal, buckets, reach;
+  int32_t rel_bf16;
+  int32_t slots;   // row (or key) tiles of all sequences, some of them empty
+  int32_t splits;  // pieces of the keys
+  int32_t piece;   // keys of a piece
+  float c;         // scale log2 e
+  float scale;
+};
+
+// A sequence's place.  The starts live in device memory, where no host check sees them: whatever they hold, no row
+// outside the tensors is addressed.
+struct Seq {
+  int64_t q0, k0;
+  int32_t nq, nk, cap;  // queries, keys, rows that the sequence has in k and v
+};
+
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); }
+
+// Sequence b; b = batch is the rows past the last sequence, which see nothing.  The first sequence starts at row 0.
+__device__ __forceinline__ Seq sequence(const Args& a, int b) {
+  Seq s;
+  s.q0 = b ? clamp64(a.start_q[b], 0, a.tq) : 0;
+  const int64_t q1 = b < a.batch ? clamp64(a.start_q[b + 1], s.q0, a.tq) : a.tq;
+  s.k0 = b ? clamp64(a.start_k[b], 0, a.tk) : 0;
+  const int64_t k1 = b < a.batch ? clamp64(a.start_k[b + 1], s.k0, a.tk) : a.tk;
+  s.nq = (int32_t)(q1 - s.q0);
+  s.cap = (int32_t)(k1 - s.k0);
+  s.nk = b < a.batch ? (a.used_k ? (int32_t)clamp64(a.used_k[b], 0, s.cap) : s.cap) : 0;
+  return s;
+}
+
+// Which sequence a tile belongs to, without knowing the lengths on the host: sequence b's tiles of `tile` units (scale
+// units per row) take the slots from start[b] scale / tile + b on, which leaves each at least as many as it needs and
+// ends before rows scale / tile + batch + 1.  Found by bisection; a slot past its sequence's last tile is empty.
+__device__ __forceinline__ int64_t first_slot(const int32_t* start, int64_t rows, int b, int scale, int tile) {
+  return (b ? clamp64(start[b], 0, rows) : 0) * scale / tile + b;
+}
+__device__ __forceinline__ int slot_sequence(const int32_t* start, int64_t rows, int batch, int scale, int tile,
+                                             int64_t slot) {
+  int lo = 0, hi = batch;  // the last b with first_slot(b) <= slot
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (first_slot(start, rows, mid, scale, tile) <= slot)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
+// Work item of a workgroup: workgroups go round the 8 dies in turn, and each die takes one contiguous range of items, so
+// that the tiles that read the same keys (or rows) share an L2.  -1: none.
+__device__ __forceinline__ int64_t work_item(int64_t total) {
+  const int64_t per = (total + XCDS - 1) / XCDS;
+  const int64_t w = (int64_t)(blockIdx.x % XCDS) * per + blockIdx.x / XCDS;
+  return blockIdx.x / XCDS < per && w < total ? w : -1;
+}
+inline unsigned work_grid(int64_t total) { return (unsigned)((total + XCDS - 1) / XCDS * XCDS); }
+
+template <typename T>
+struct Frag;
+template <>
+struct Frag<bf16> {
+  using type = bf16x8;
+};
+template <>
+struct Frag<float> {
+  using type = f32x8;
+};
+
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
+// Eight fp32 values as an operand (rounded to nearest even).
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type to_frag(f32x8 x) {
+  if constexpr (sizeof(T) == 4)
+    return x;
+  else
+    return __builtin_convertvector(x, bf16x8);
+}
+
+// The values of the lane and of its twin in the other half of the wave.
+struct Pair {
+  float lower, upper;
+};
+__device__ __forceinline__ Pair halves(float x) {
+  const int a = __builtin_bit_cast(int, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+  const unsigned lower = r[0], upper = r[1];
+  return {__builtin_bit_cast(float, lower), __builtin_bit_cast(float, upper)};
+}
+__device__ __forceinline__ float max_halves(float x) {
+  const Pair p = halves(x);
+  return fmaxf(p.lower, p.upper);
+}
+__device__ __forceinline__ float add_halves(float x) {
+  const Pair p = halves(x);
+  return p.lower + p.upper;
+}
+
+// A tile of rows x D elements in LDS, row-major, each row's 16-byte chunks permuted by an XOR of the row's low bits so
+// that neither a column of chunks (row_frag) nor four rows of 64 bytes (col_frag) meet in one bank.
+template <typename T, int D>
+struct Tile {
+  using F = typename Frag<T>::type;
+  static constexpr int ROW = D * (int)sizeof(T);  // bytes
+  static constexpr int CH = ROW / 16;
+  static constexpr int PER = 16 / (int)sizeof(T);  // elements of a chunk
+  static constexpr int STEPS = D / 16, BLOCKS = D / 32;
+
+  static __device__ __forceinline__ int swizzle(int row) {
+    const int b0 = row & 1, b1 = row >> 1 & 1, b2 = row >> 2 & 1, b3 = row >> 3 & 1;
+    if constexpr (sizeof(T) == 2 && CH == 16) return b1 << 3 | b0 << 2 | b3 << 1 | b2;
+    if constexpr (CH == 8) return b1 << 2 | b2 << 1 | b3;
+    if constexpr (CH == 4) return b2 << 1 | b3;
+    return b2 << 3 | b0 << 2 | b1 << 1 | b3;
+  }
+
+  // Addresses of a lane's operands, made once: A or B rows (row = the lane's row of the first block, the same for blocks
+  // at a multiple of 16 rows further on).
+  struct RowAddr {
+    uint32_t at[STEPS][sizeof(T) / 2];
+  };
+  static __device__ __forceinline__ RowAddr row_addr(int row) {
+    RowAddr r;
+    const int h = threadIdx.x >> 5 & 1;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+        r.at[s][i] = row * ROW + (((16 * s + 8 * h) / PER + i) ^ swizzle(row)) * 16;
+    return r;
+  }
+  // Row operand: 8 elements of the lane's row, k = 16 s + 8 h ...
+  static __device__ __forceinline__ F row_frag(Lds tile, const RowAddr& a, int s, int first_row) {
+    if constexpr (sizeof(T) == 2) {
+      return *(const __attribute__((address_space(3))) bf16x8*)(tile + a.at[s][0] + first_row * ROW);
+    } else {
+      const f32x4 x = *(const __attribute__((address_space(3))) f32x4*)(tile + a.at[s][0] + first_row * ROW);
+      const f32x4 y = *(const __attribute__((address_space(3))) f32x4*)(tile + a.at[s][1] + first_row * ROW);
+      return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+
+  // Column operand: column d = 32 block + (lane & 31) of the transposed tile, rows 16 c + (4 h + 0..3, 8 + 4 h + 0..3).
+  struct ColAddr {
+    uint32_t at[BLOCKS][2];
+  };
+  static __device__ __forceinline__ ColAddr col_addr() {
+    ColAddr r;
+    const int l = threadIdx.x & 63, h = l >> 5;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if constexpr (sizeof(T) == 2) {  // the transposing read: 16 lanes take 4 rows of 16 columns
+          const int row = 8 * u + 4 * h + (l >> 2 & 3), d = 32 * b + (l & 16) + 4 * (l & 3);
+          r.at[b][u] = row * ROW + (d / PER ^ swizzle(row)) * 16 + d % PER * 2;
+        } else {  // the first of the 4 rows; the others differ in the low bits of the swizzle
+          const int row = 8 * u + 4 * h, d = 32 * b + (l & 31);
+          r.at[b][u] = row * ROW + (d / PER ^ swizzle(row)) * 16 + d % PER * 4;
+        }
+      }
+    return r;
+  }
+  static __device__ __forceinline__ F col_frag(Lds tile, const ColAddr& a, int block, int c) {
+    if constexpr (sizeof(T) == 2) {
+      union {
+        s16x4 s[2];
+        bf16x8 f;
+      } u;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        u.s[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(tile + a.at[block][i] + 16 * c * ROW));
+      return u.f;
+    } else {
+      f32x8 f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t at = (a.at[block][i] + e * ROW) ^ (uint32_t)(swizzle(e) * 16);
+          f[4 * i + e] = *(const __attribute__((address_space(3))) float*)(tile + at + 16 * c * ROW);
+        }
+      return f;
+    }
+  }
+};
+
+// 16 bytes a lane from memory straight into LDS at dst + 16 lane; a lane whose offset lies past the resource's end
+// gets zeros.  Written out so that the compiler does not wait for it at the next read of any tile: the kernels wait
+// themselves (loads_left), before the barrier or the reads that need it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 is reserved, and written here all the same
+__device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t src, Lds dst, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"((uint32_t)(uintptr_t)dst), "v"(offset), "s"(src)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+}
+// Rows [row, row + N) of a head of k or v into a tile, by `waves` waves of which this is number `wave`; rows from `rows` on
+// become zeros.
+template <typename T, int D, int N, int WAVES>
+__device__ __forceinline__ void load_rows(const T* head, int64_t stride, int row, int rows, Lds tile, int wave) {
+  using Ti = Tile<T, D>;
+  const int left = rows - row;
+  const uint32_t bytes = left > 0 ? (uint32_t)(((left < N ? left : N) - 1) * stride + D) * (uint32_t)sizeof(T) : 0;
+  const auto src = resource(head + row * stride, bytes);
+  constexpr int LOADS = N * Ti::CH / 64 / WAVES;
+  static_assert(LOADS * 64 * WAVES == N * Ti::CH, "whole loads");
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int first = (wave * LOADS + i) * 64;  // chunk of lane 0
+    const int p = first + (threadIdx.x & 63);
+    const int r = p / Ti::CH, ch = (p % Ti::CH) ^ Ti::swizzle(r);
+    dma16(src, tile + first * 16, (uint32_t)(r * (int)stride + ch * Ti::PER) * (uint32_t)sizeof(T));
+  }
+}
+
+// The bias by distance of the group's heads, times log2 e, in LDS: [G][2 (reach + BIAS_PAD) + 1], constant past reach.
+__device__ __forceinline__ int bias_width(const Args& a) { return 2 * (a.reach + BIAS_PAD) + 1; }
+__device__ __forceinline__ float rel_weight(const Args& a, int head, int bucket) {
+  const int64_t at = (int64_t)head * a.buckets + bucket;
+  return a.rel_bf16 ? (float)((const bf16*)a.rel_weight)[at] : ((const float*)a.rel_weight)[at];
+}
+__device__ __forceinline__ int bucket_of(const Args& a, int d) {
+  d = d < -a.reach ? -a.reach : (d > a.reach ? a.reach : d);
+  const int b = a.rel_bucket[d + a.reach];
+  return b < 0 ? 0 : (b < a.buckets ? b : a.buckets - 1);  // device data: nothing outside the weights is addressed
+}
+__device__ __forceinline__ void fill_bias(const Args& a, int first_head, float* table, int threads) {
+  const int n = bias_width(a);
+  for (int i = threadIdx.x; i < a.group * n; i += threads)
+    table[i] = rel_weight(a, first_head + i / n, bucket_of(a, i % n - a.reach - BIAS_PAD)) * LOG2E;
+}
+
+// Waits of a wave: every load into LDS that it issued has arrived, all but the last N have, every read of LDS has.
+template <int N>
+__device__ __forceinline__ void loads_left() {
+  static_assert(N < 64, "the counter's range");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4 << 14));
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void loads_done() { loads_left<0>(); }
+__device__ __forceinline__ void reads_done() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("" ::: "memory");
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+
+int check_attention(const lram_attention& a, bool pointers) {
+  if (a.dtype != LRAM_F32 && a.dtype != LRAM_BF16) return LRAM_EDTYPE;
+  if (a.head_dim != 32 && a.head_dim != 64 && a.head_dim != 128) return LRAM_EDTYPE;
+  if (a.kv_heads < 1 || a.heads < 1 || a.heads % a.kv_heads || a.heads / a.kv_heads > 64 || a.heads > 65536)
+    return LRAM_EINVAL;
+  const int64_t G = a.heads / a.kv_heads;
+  if (a.batch < 0 || a.batch > 1 << 24 || (a.causal & ~1) || !(a.scale > 0) || !(a.scale < INFINITY))
+    return LRAM_EINVAL;
+  if (a.tq < 0 || a.tk < 0 || a.tk > INT32_MAX || a.tq > INT32_MAX / G || a.max_q < 0 || a.max_k < 0)
+    return LRAM_EINVAL;
+  // work items of every kernel (at most 64 pieces of tiles of 32 rows) stay below 2^31 workgroups of 256 threads
+  if (a.kv_heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 1) > (int64_t(1) << 24) - 16) return LRAM_EINVAL;
+  if (a.rel_weight) {
+    if (a.wdtype != LRAM_F32 && !(a.wdtype == LRAM_BF16 && a.dtype == LRAM_BF16)) return LRAM_EDTYPE;
+    if (!a.rel_bucket || a.rel_buckets < 1 || a.rel_buckets > 1024 || a.rel_reach < 0 || a.rel_reach > 4096 ||
+        G * (2 * (a.rel_reach + BIAS_PAD) + 1) > 4096)
+      return LRAM_EINVAL;
+    if (off_align(a.rel_weight, elem_size(a.wdtype)) || off_align(a.rel_bucket, 4)) return LRAM_EINVAL;
+  }
+  const int64_t per = 16 / (int64_t)elem_size(a.dtype);
+  for (int64_t row : {a.q_row, a.k_row, a.v_row})
+    if (row < a.head_dim || row > 1 << 22 || row % per) return LRAM_EINVAL;
+  for (int64_t head : {a.q_head, a.k_head, a.v_head})
+    if (head < 0 || head > INT64_MAX / 2 / a.heads || head % per) return LRAM_EINVAL;
+  if (!pointers) return LRAM_OK;
+  if (a.tq && (!a.q || off_align(a.q, 16))) return LRAM_EINVAL;
+  if (a.tk && (!a.k || !a.v || off_align(a.k, 16) || off_align(a.v, 16))) return LRAM_EINVAL;
+  if (a.batch && (!a.start_q || !a.start_k)) return LRAM_EINVAL;
+  if (off_align(a.start_q, 4) || off_align(a.start_k, 4) || off_align(a.used_k, 4)) return LRAM_EINVAL;
+  return LRAM_OK;
+}
+
+Args args_of(const lram_attention& a) {
+  Args x{};
+  x.q = a.q, x.k = a.k, x.v = a.v;
+  x.q_row = a.q_row, x.q_head = a.q_head, x.k_row = a.k_row, x.k_head = a.k_head, x.v_row = a.v_row, x.v_head = a.v_head;
+  x.start_q = a.start_q, x.start_k = a.start_k, x.used_k = a.used_k;
+  x.rel_weight = a.rel_weight, x.rel_bucket = a.rel_bucket;
+  x.tq = a.tq, x.tk = a.tk;
+  x.heads = a.heads, x.kv_heads = a.kv_heads, x.group = a.heads / a.kv_heads, x.batch = a.batch;
+  x.causal = a.causal, x.buckets = a.rel_buckets, x.reach = a.rel_reach, x.rel_bf16 = a.wdtype == LRAM_BF16;
+  x.scale = a.scale;
+  x.c = a.scale * LOG2E;
+  return x;
+}
+
+// More than 64 KB of a workgroup's LDS has to be asked for, once for a kernel and a device.
+int allow_lds(const void* kernel, size_t bytes) {
+  if (bytes <= 64 * 1024) return LRAM_OK;
+  const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  return e == hipSuccess ? LRAM_OK : layer_failed(e);
+}
+
+template <typename F>
+int by_kind(const lram_attention& a, F f) {
+  const auto width = [&](auto t, auto bias) {
+    switch (a.head_dim) {
+      case 32: return f(t, std::integral_constant<int, 32>(), bias);
+      case 64: return f(t, std::integral_constant<int, 64>(), bias);
+      default: return f(t, std::integral_constant<int, 128>(), bias);
+    }
+  };
+  const auto type = [&](auto bias) { return a.dtype == LRAM_F32 ? width(float(), bias) : width(bf16(), bias); };
+  return a.rel_weight ? type(std::true_type()) : type(std::false_type());
+}
+
+}  // namespace

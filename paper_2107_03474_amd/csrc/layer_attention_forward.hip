@@ -1,0 +1,510 @@
+// layer_attention_forward.hip -- part of liblram: attention over packed sequences, forward (see layer_attention.h for
+// the formulas and the tiles).
+//
+// k_attention: prompts.  A workgroup holds 128 packed rows, 32 to a wave, whose queries stay in registers; keys and values
+// pass through LDS in tiles of 64, the next tile's loads in flight while one is used.  One pass: running maximum m and
+// sum l a row, accumulators rescaled only when the maximum grows by more than 2^8 (the weights stay exact in that
+// range, and the branch is rarely taken).
+// k_attention_few: a few queries over many keys.  The four waves of a workgroup share the same 32 rows and take key
+// tiles in turn, each through LDS of its own without barriers, and join their sums at the end.
+// Where rows are few against the chip the keys are divided into pieces (either kernel) that k_attention_join joins.
+
+#include "layer_attention.h"
+
+namespace {
+
+constexpr int WAVES = 4, THREADS = WAVES * WAVE;
+constexpr int MAX_SPLITS = 64;
+constexpr float GROWTH = 8;  // log2 of how far weights may pass 1 before the sums are rescaled
+
+struct Out {
+  void* out;
+  void* residue;
+  float* lse;
+  float *part, *part_lse;  // [splits][tq heads][D], [splits][tq heads]
+};
+
+// A wave's running softmax over its 32 rows (a row to a lane and its twin in the other half).
+template <int D>
+struct Running {
+  f32x16 o[D / 32];
+  float m, l;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[b][r] = 0;
+    m = -INFINITY;
+    l = 0;
+  }
+};
+
+// N blocks of 32 keys from key j0 on, at `kt` and `vt` in LDS.  lim: the last key that the lane's row sees; masked: some row
+// of the wave does not see every key of the tile.  bias: the lane's row of the bias table at distance -(i + off) (or
+// null); bias_far: whether one value of it, `far`, serves the whole tile.
+template <typename T, int D, int N, bool BIAS>
+__device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::type (&q)[D / 16], Lds kt, Lds vt,
+                                       const typename Tile<T, D>::RowAddr& ka, const typename Tile<T, D>::ColAddr& va,
+                                       float c, int j0, int lim, bool masked, const float* bias, bool bias_far,
+                                       float far) {
+  using Ti = Tile<T, D>;
+  const int h = threadIdx.x >> 5 & 1;
+  f32x16 s[N];
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[b][r] = 0;
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+    for (int b = 0; b < N; ++b) s[b] = mma(Ti::row_frag(kt, ka, k, 32 * b), q[k], s[b]);
+  if constexpr (BIAS) {
+    if (bias_far) {
+#pragma unroll
+      for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], c, far);
+    } else {
+      const float* at = bias + j0 + 4 * h;
+#pragma unroll
+      for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], c, at[32 * b + 8 * (r >> 2) + (r & 3)]);
+    }
+  }
+  if (masked) {
+    const int last = lim - j0 - 4 * h;
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r >> 2) + (r & 3) <= last ? s[b][r] : -INFINITY;
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+  top = max_halves(top);
+  if constexpr (!BIAS) top *= c;
+  if (__builtin_amdgcn_ballot_w64(top > st.m + GROWTH)) {
+    const float m = fmaxf(st.m, top);
+    const float a = __builtin_amdgcn_exp2f(st.m - (m == -INFINITY ? 0.0f : m));
+    st.m = m;
+    st.l *= a;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[b][r] *= a;
+  }
+  const float m = st.m == -INFINITY ? 0.0f : st.m;
+  float l = 0;
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[b][r] = __builtin_amdgcn_exp2f(BIAS ? s[b][r] - m : fmaf(s[b][r], c, -m));
+      l += s[b][r];
+    }
+  st.l += l;
+#pragma unroll
+  for (int k = 0; k < 2 * N; ++k) {
+    f32x8 p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = s[k / 2][8 * (k % 2) + e];
+    const auto f = to_frag<T>(p);
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) st.o[b] = mma(Ti::col_frag(vt, va, b, k), f, st.o[b]);
+  }
+}
+
+// What a lane knows of its row.
+struct Row {
+  bool valid;
+  int i, g;  // query, head of the group
+};
+__device__ __forceinline__ Row row_of(const Args& a, const Seq& s, int row) {
+  Row r;
+  r.valid = row < s.nq * a.group;
+  r.i = row / a.group;
+  r.g = row - r.i * a.group;
+  return r;
+}
+template <typename T, int D>
+__device__ __forceinline__ void load_query(const Args& a, const T* base, int64_t row_stride, int64_t head_stride,
+                                           const Seq& s, int head, const Row& r, typename Frag<T>::type (&f)[D / 16]) {
+  using F = typename Frag<T>::type;
+  const T* p = base + (s.q0 + r.i) * row_stride + head * head_stride + 8 * (threadIdx.x >> 5 & 1);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    F z = {};
+    f[k] = r.valid ? *(const F*)(p + 16 * k) : z;
+  }
+}
+
+// The tiles of a workgroup: sequence, first packed row, key range.
+struct Work {
+  Seq s;
+  int hk, row0, split, kbeg, kend;
+};
+template <int M>
+__device__ __forceinline__ bool find_work(const Args& a, Work* w) {
+  const int64_t item = work_item((int64_t)a.kv_heads * a.slots * a.splits);
+  if (item < 0) return false;
+  w->hk = (int)(item / ((int64_t)a.slots * a.splits));
+  const int rest = (int)(item % ((int64_t)a.slots * a.splits));
+  w->split = rest % a.splits;
+  const int slot = a.slots - 1 - rest / a.splits;  // long causal rows first
+  const int b = slot_sequence(a.start_q, a.tq, a.batch, a.group, M, slot);
+  w->s = sequence(a, b);
+  const int64_t row0 = (slot - first_slot(a.start_q, a.tq, b, a.group, M)) * M;
+  if (row0 >= (int64_t)w->s.nq * a.group) return false;
+  w->row0 = (int)row0;
+  const int rows = w->s.nq * a.group;
+  const int last = (w->row0 + M < rows ? w->row0 + M : rows) - 1;
+  int end = w->s.nk;
+  if (a.causal) {
+    const int seen = last / a.group + w->s.nk - w->s.nq + 1;
+    end = seen < end ? (seen > 0 ? seen : 0) : end;
+  }
+  const int64_t from = (int64_t)w->split * a.piece;
+  w->kbeg = from < end ? (int)from : end;
+  w->kend = w->split == a.splits - 1 || from + a.piece > end ? end : (int)(from + a.piece);
+  return true;
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, f32x4 x) {
+  using V = T __attribute__((ext_vector_type(4)));
+  *(V*)p = __builtin_convertvector(x, V);
+}
+
+// Results of flat row `at` = (row of q) heads + head: 4 elements from d on.
+template <typename T, int D>
+__device__ __forceinline__ void put(const Args& a, const Out& o, int split, int64_t at, int d, f32x4 x) {
+  if (a.splits > 1) {
+    *(f32x4*)(o.part + ((int64_t)split * a.tq * a.heads + at) * D + d) = x;
+    return;
+  }
+  T* p = (T*)o.out + at * D + d;
+  store4<T>(p, x);
+  if constexpr (sizeof(T) == 2) {
+    if (o.residue) {
+      f32x4 left;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) left[e] = x[e] - (float)(T)x[e];
+      store4<T>((T*)o.residue + at * D + d, left);
+    }
+  }
+}
+__device__ __forceinline__ void put_lse(const Args& a, const Out& o, int split, int64_t at, float lse) {
+  if (a.splits > 1)
+    o.part_lse[(int64_t)split * a.tq * a.heads + at] = lse;
+  else if (o.lse)
+    o.lse[at] = lse;
+}
+
+// Waves per SIMD: two; one where LDS holds one workgroup a CU.
+template <typename T, int D>
+constexpr int waves_per_simd() { return 4 * KEYS * Tile<T, D>::ROW > 80 * 1024 ? 1 : 2; }
+
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention(Args a, Out o) {
+  using Ti = Tile<T, D>;
+  constexpr int M = WAVES * ROWS, BYTES = KEYS * Ti::ROW;
+  extern __shared__ __attribute__((aligned(256))) char smem[];
+  Lds lds = (Lds)smem;
+  Work w;
+  if (!find_work<M>(a, &w)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE;
+  const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
+  const Row r = row_of(a, w.s, first + (l & 31));
+  const int head = w.hk * G + r.g;
+  typename Frag<T>::type q[D / 16];
+  load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
+  // last key of the lane's row, and of the wave's first and last rows
+  const int lim = a.causal && r.valid ? min(r.i + off, w.s.nk - 1) : w.s.nk - 1;
+  const int i_first = first / G, i_last = (min(first + ROWS, rows) - 1) / G;
+  const int lim_first = a.causal ? min(i_first + off, w.s.nk - 1) : w.s.nk - 1;
+  const int lim_last = first >= rows ? -1 : (a.causal ? min(i_last + off, w.s.nk - 1) : w.s.nk - 1);
+  const float* bias = nullptr;
+  float near_far[2] = {0, 0};
+  if constexpr (BIAS) {
+    float* table = (float*)(smem + 4 * BYTES);
+    fill_bias(a, w.hk * G, table, THREADS);
+    bias = table + r.g * bias_width(a) + a.reach + BIAS_PAD - (r.i + off);
+    __syncthreads();
+    const float* mine = table + (r.valid ? r.g : 0) * bias_width(a);
+    near_far[0] = mine[0];
+    near_far[1] = mine[bias_width(a) - 1];
+  }
+  const typename Ti::RowAddr ka = Ti::row_addr(l & 31);
+  const typename Ti::ColAddr va = Ti::col_addr();
+  Running<D> st;
+  st.clear();
+  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.hk * a.k_head;
+  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.hk * a.v_head;
+  auto load = [&](int j0, int buf) {
+    load_rows<T, D, KEYS, WAVES>(kh, a.k_row, j0, w.s.nk, lds + buf * 2 * BYTES, wave);
+    load_rows<T, D, KEYS, WAVES>(vh, a.v_row, j0, w.s.nk, lds + buf * 2 * BYTES + BYTES, wave);
+  };
+  if (w.kbeg < w.kend) load(w.kbeg, 0);
+  int buf = 0;
+  for (int j0 = w.kbeg; j0 < w.kend; j0 += KEYS, buf ^= 1) {
+    loads_done();
+    __syncthreads();  // this tile is whole, and every wave has left the other buffer
+    if (j0 + KEYS < w.kend) load(j0 + KEYS, buf ^ 1);
+    if (j0 > lim_last) continue;
+    const bool masked = j0 + KEYS - 1 > lim_first;
+    bool whole = false;
+    float far = 0;
+    if constexpr (BIAS) {
+      const bool below = j0 + KEYS - 1 - (i_first + off) <= -a.reach, above = j0 - (i_last + off) >= a.reach;
+      whole = below || above;
+      far = near_far[above];
+    }
+    attend<T, D, KEYS / 32, BIAS>(st, q, lds + buf * 2 * BYTES, lds + buf * 2 * BYTES + BYTES, ka, va, a.c, j0, lim,
+                                  masked, bias, whole, far);
+  }
+  if (!r.valid) return;
+  const float sum = add_halves(st.l), inv = sum == 0 ? 0.0f : 1.0f / sum;
+  const int64_t at = (w.s.q0 + r.i) * a.heads + head;
+  if (l < 32) put_lse(a, o, w.split, at, sum == 0 ? -INFINITY : st.m + __builtin_amdgcn_logf(sum));
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = st.o[b][4 * u + e] * inv;
+      put<T, D>(a, o, w.split, at, 32 * b + 8 * u + 4 * (l >> 5), x);
+    }
+}
+
+// Buffers of a wave's key and value tiles in k_attention_few: two where LDS holds them.
+template <typename T, int D>
+constexpr int few_stages() { return WAVES * 2 * 2 * 32 * Tile<T, D>::ROW <= 128 * 1024 ? 2 : 1; }
+template <typename T, int D>
+constexpr int few_bytes() { return WAVES * few_stages<T, D>() * 2 * 32 * Tile<T, D>::ROW; }
+
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
+  using Ti = Tile<T, D>;
+  constexpr int N = 32, BYTES = N * Ti::ROW, STAGES = few_stages<T, D>();
+  constexpr int LOADS = 2 * N * Ti::CH / 64;  // of a tile of keys and values
+  extern __shared__ __attribute__((aligned(256))) char smem[];
+  Work w;
+  if (!find_work<ROWS>(a, &w)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE;
+  Lds lds = (Lds)smem + wave * STAGES * 2 * BYTES;
+  const int G = a.group, off = w.s.nk - w.s.nq, rows = w.s.nq * G;
+  const Row r = row_of(a, w.s, w.row0 + (l & 31));
+  const int head = w.hk * G + r.g;
+  typename Frag<T>::type q[D / 16];
+  load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
+  const int lim = a.causal && r.valid ? min(r.i + off, w.s.nk - 1) : w.s.nk - 1;
+  const int i_first = w.row0 / G, i_last = (min(w.row0 + ROWS, rows) - 1) / G;
+  const int lim_first = a.causal ? min(i_first + off, w.s.nk - 1) : w.s.nk - 1;
+  const float* bias = nullptr;
+  float near_far[2] = {0, 0};
+  if constexpr (BIAS) {
+    float* table = (float*)(smem + few_bytes<T, D>());
+    fill_bias(a, w.hk * G, table, THREADS);
+    bias = table + r.g * bias_width(a) + a.reach + BIAS_PAD - (r.i + off);
+    __syncthreads();
+    const float* mine = table + (r.valid ? r.g : 0) * bias_width(a);
+    near_far[0] = mine[0];
+    near_far[1] = mine[bias_width(a) - 1];
+  }
+  const typename Ti::RowAddr ka = Ti::row_addr(l & 31);
+  const typename Ti::ColAddr va = Ti::col_addr();
+  Running<D> st;
+  st.clear();
+  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.hk * a.k_head;
+  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.hk * a.v_head;
+  auto load = [&](int j0, int buf) {
+    load_rows<T, D, N, 1>(kh, a.k_row, j0, w.s.nk, lds + buf * 2 * BYTES, 0);
+    load_rows<T, D, N, 1>(vh, a.v_row, j0, w.s.nk, lds + buf * 2 * BYTES + BYTES, 0);
+  };
+  const int step = WAVES * N;
+  int j0 = w.kbeg + wave * N;
+  if (STAGES == 2 && j0 < w.kend) load(j0, 0);
+  for (int buf = 0; j0 < w.kend; j0 += step, buf ^= STAGES - 1) {
+    reads_done();  // of the buffer that is loaded next
+    if (STAGES == 1) load(j0, 0);
+    const bool more = STAGES == 2 && j0 + step < w.kend;
+    if (more) {
+      load(j0 + step, buf ^ 1);
+      loads_left<LOADS>();
+    } else {
+      loads_left<0>();
+    }
+    const bool masked = j0 + N - 1 > lim_first;
+    bool whole = false;
+    float far = 0;
+    if constexpr (BIAS) {
+      const bool below = j0 + N - 1 - (i_first + off) <= -a.reach, above = j0 - (i_last + off) >= a.reach;
+      whole = below || above;
+      far = near_far[above];
+    }
+    attend<T, D, N / 32, BIAS>(st, q, lds + buf * 2 * BYTES, lds + buf * 2 * BYTES + BYTES, ka, va, a.c, j0, lim,
+                               masked, bias, whole, far);
+  }
+  // join the waves: maxima and sums, then the scaled accumulators, through LDS
+  constexpr int PITCH = D * 4 + 16;
+  static_assert(WAVES * ROWS * PITCH + 2 * WAVES * ROWS * 4 <= few_bytes<T, D>() || D == 32, "the join fits");
+  float* ml = (float*)(smem + WAVES * ROWS * PITCH);
+  const float mine = add_halves(st.l);
+  __syncthreads();
+  if (l < 32) {
+    ml[wave * ROWS + l] = st.m;
+    ml[(WAVES + wave) * ROWS + l] = mine;
+  }
+  __syncthreads();
+  float m = -INFINITY, sum = 0;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) m = fmaxf(m, ml[v * ROWS + (l & 31)]);
+  const float m0 = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v)
+    sum += ml[(WAVES + v) * ROWS + (l & 31)] * __builtin_amdgcn_exp2f(ml[v * ROWS + (l & 31)] - m0);
+  const float f = sum == 0 ? 0.0f : __builtin_amdgcn_exp2f(st.m - m0) / sum;
+  const int64_t at = (w.s.q0 + r.i) * a.heads + head;
+  if (wave == 0 && l < 32 && r.valid) put_lse(a, o, w.split, at, sum == 0 ? -INFINITY : m + __builtin_amdgcn_logf(sum));
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = st.o[b][4 * u + e] * f;
+      *(f32x4*)(smem + (wave * ROWS + (l & 31)) * PITCH + (32 * b + 8 * u + 4 * (l >> 5)) * 4) = x;
+    }
+  __syncthreads();
+  for (int t = threadIdx.x; t < ROWS * D / 4; t += THREADS) {
+    const int row = t / (D / 4), d = t % (D / 4) * 4;
+    const Row rr = row_of(a, w.s, w.row0 + row);
+    if (!rr.valid) continue;
+    f32x4 x = *(const f32x4*)(smem + row * PITCH + d * 4);
+#pragma unroll
+    for (int v = 1; v < WAVES; ++v) {
+      const f32x4 y = *(const f32x4*)(smem + (v * ROWS + row) * PITCH + d * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[e];
+    }
+    put<T, D>(a, o, w.split, (w.s.q0 + rr.i) * a.heads + w.hk * G + rr.g, d, x);
+  }
+}
+
+// The pieces of a flat row joined: a row to D / 4 lanes.
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS) void k_attention_join(Args a, Out o) {
+  constexpr int PER = D / 4;  // lanes of a row
+  const int64_t n = a.tq * a.heads;
+  const int64_t at = ((int64_t)blockIdx.x * THREADS + threadIdx.x) / PER;
+  const int d = threadIdx.x % PER * 4;
+  if (at >= n) return;
+  float m = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, o.part_lse[s * n + at]);
+  const float m0 = m == -INFINITY ? 0.0f : m;
+  float sum = 0;
+  f32x4 x = {0, 0, 0, 0};
+  for (int s = 0; s < a.splits; ++s) {
+    const float lse = o.part_lse[s * n + at];
+    if (lse == -INFINITY) continue;  // a piece without keys
+    const float f = __builtin_amdgcn_exp2f(lse - m0);
+    sum += f;
+    const f32x4 y = *(const f32x4*)(o.part + (s * n + at) * D + d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], f, x[e]);
+  }
+  const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] *= inv;
+  a.splits = 1;
+  put<T, D>(a, o, 0, at, d, x);
+  if (d == 0) put_lse(a, o, 0, at, sum == 0 ? -INFINITY : m + __builtin_amdgcn_logf(sum));
+}
+
+struct Plan {
+  bool few;
+  int slots, splits, piece;
+};
+
+// Few rows: a sequence's packed rows fit one wave.  Pieces of the keys: as many as give the chip about four
+// workgroups a CU, none shorter than 256 keys.
+Plan plan_of(const lram_attention& a) {
+  Plan p;
+  const int64_t G = a.heads / a.kv_heads;
+  p.few = a.max_q * G <= ROWS;
+  const int tile = p.few ? ROWS : WAVES * ROWS;
+  p.slots = (int)(a.tq * G / tile + a.batch + 1);
+  const int64_t work = (int64_t)a.kv_heads * a.batch * std::max<int64_t>(1, (a.max_q * G + tile - 1) / tile);
+  const int64_t real = std::min<int64_t>(work, (int64_t)a.kv_heads * p.slots);
+  int64_t splits = real > 0 ? (p.few ? 1024 : 512) / real : 1;
+  splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + 255) / 256});
+  if (splits < 1) splits = 1;
+  p.piece = (int)std::min<int64_t>(((a.max_k + splits - 1) / splits + 127) / 128 * 128, INT32_MAX / 2);
+  if (p.piece < 128) p.piece = 128;
+  p.splits = (int)std::min<int64_t>(splits, std::max<int64_t>(1, (a.max_k + p.piece - 1) / p.piece));
+  return p;
+}
+
+size_t workspace_of(const lram_attention& a, const Plan& p) {
+  return p.splits > 1 ? (size_t)p.splits * a.tq * a.heads * (a.head_dim + 1) * 4 : 0;
+}
+
+template <typename T, int D, bool BIAS>
+int go(Args x, const Out& o, const Plan& p, hipStream_t s) {
+  const unsigned grid = work_grid((int64_t)x.kv_heads * x.slots * x.splits);
+  const size_t table = BIAS ? (size_t)x.group * (2 * (x.reach + BIAS_PAD) + 1) * 4 : 0;
+  const auto launch = [&](auto kernel, size_t bytes) {
+    if (int rc = allow_lds((const void*)kernel, bytes)) return rc;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(THREADS), bytes, s, x, o);
+    return layer_launched();
+  };
+  int rc;
+  if (p.few)
+    rc = launch(k_attention_few<T, D, BIAS>,
+                std::max<size_t>(few_bytes<T, D>(), WAVES * ROWS * (D * 4 + 16 + 8)) + table);
+  else
+    rc = launch(k_attention<T, D, BIAS>, (size_t)4 * KEYS * Tile<T, D>::ROW + table);
+  if (rc || x.splits == 1) return rc;
+  const int64_t threads = x.tq * x.heads * (D / 4);
+  hipLaunchKernelGGL((k_attention_join<T, D>), dim3((unsigned)((threads + THREADS - 1) / THREADS)), dim3(THREADS), 0, s,
+                     x, o);
+  return layer_launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int lram_attention_forward_workspace_bytes(const lram_attention* a, size_t* bytes) {
+  if (!a || !bytes) return LRAM_EINVAL;
+  if (int rc = check_attention(*a, false)) return rc;
+  *bytes = a->tq ? workspace_of(*a, plan_of(*a)) : 0;
+  return LRAM_OK;
+}
+
+int lram_attention_forward(const lram_attention* a, void* out, float* lse, void* residue, void* workspace,
+                           size_t ws_bytes, void* stream) {
+  if (!a) return LRAM_EINVAL;
+  if (int rc = check_attention(*a, true)) return rc;
+  if (a->tq == 0) return LRAM_OK;
+  if (!out || off_align(out, 16) || off_align(residue, 16) || off_align(lse, 4)) return LRAM_EINVAL;
+  if (residue && a->dtype != LRAM_BF16) return LRAM_EDTYPE;
+  const Plan p = plan_of(*a);
+  const size_t need = workspace_of(*a, p);
+  if (need && (!workspace || off_align(workspace, 16) || ws_bytes < need)) return LRAM_EWORKSPACE;
+  Args x = args_of(*a);
+  x.slots = p.slots;
+  x.splits = p.splits;
+  x.piece = p.piece;
+  Out o{out, residue, lse, (float*)workspace, nullptr};
+  o.part_lse = o.part ? o.part + (size_t)p.splits * a->tq * a->heads * a->head_dim : nullptr;
+  return by_kind(*a, [&](auto t, auto d, auto bias) {
+    return go<decltype(t), decltype(d)::value, decltype(bias)::value>(x, o, p, (hipStream_t)stream);
+  });
+}
+
+}  // extern "C"

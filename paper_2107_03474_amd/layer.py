@@ -1,0 +1,302 @@
+"""The operators around the lattice memory in a transformer layer: layer norm (with the residual add in front of it),
+attention over packed sequences, and the learned relative position bias inside it.
+
+As in the package's other calls, this module only marshals torch tensors and the current HIP stream into the C ABI
+(``include/lram_layer.h``); the work is done by the library's HIP kernels, and there is no fallback.  Gradients come in
+their inputs' types, rounded once from fp32.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import NamedTuple, Optional, Sequence, Tuple
+
+import torch
+
+from . import BF16, F32, LramError, _dev, _stream
+from . import load as _load_library
+
+__all__ = ["layer_norm_forward", "layer_norm_backward", "layer_norm", "Packed", "pack", "RelativeBias",
+           "relative_buckets", "AttentionSaved", "attention_forward"]
+
+_P, _I64, _I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
+
+
+class _Attention(ctypes.Structure):
+    """lram_attention"""
+    _fields_ = ([(n, _I32) for n in ("dtype", "wdtype", "heads", "kv_heads", "head_dim", "batch", "causal")] +
+                [("scale", ctypes.c_float)] + [(n, _I64) for n in ("tq", "tk", "max_q", "max_k")] +
+                [(n, _P) for n in ("q", "k", "v")] +
+                [(n, _I64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head")] +
+                [(n, _P) for n in ("start_q", "start_k", "used_k", "rel_weight", "rel_bucket")] +
+                [("rel_buckets", _I32), ("rel_reach", _I32)])
+
+
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        lib = _load_library()
+        I, SZ, SZP = ctypes.c_int, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+        A = ctypes.POINTER(_Attention)
+        lib.lram_layer_last_hip_error.restype = I
+        lib.lram_layer_norm_forward.argtypes = [_P, _P, _P, _P, I, I, _I64, _I64, ctypes.c_double, _P, _P, _P, _P, _P]
+        lib.lram_layer_norm_backward_workspace_bytes.argtypes = [_I64, _I64, I, SZP]
+        lib.lram_layer_norm_backward.argtypes = [_P, _P, _P, _P, _P, _P, I, I, _I64, _I64, _P, _P, _P, _P, SZ, _P]
+        lib.lram_attention_forward_workspace_bytes.argtypes = [A, SZP]
+        lib.lram_attention_forward.argtypes = [A, _P, _P, _P, _P, SZ, _P]
+        _lib = lib
+    return _lib
+
+
+def _check(rc: int):
+    if rc != 0:
+        lib = _library()
+        msg = lib.lram_strerror(rc).decode()
+        if rc == 6:
+            msg += " (hipError %d)" % lib.lram_layer_last_hip_error()
+        raise LramError(msg)
+
+
+def _type(t: torch.Tensor, name: str) -> int:
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise LramError("%s must be float32 or bfloat16" % name)
+
+
+def _scratch(nbytes: int, workspace: Optional[torch.Tensor], like: torch.Tensor):
+    """(pointer, bytes, tensor to keep until the launch) of a call's workspace."""
+    if workspace is None:
+        if not nbytes:
+            return None, 0, None
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    return _dev(workspace, "workspace", like=like), workspace.numel() * workspace.element_size(), workspace
+
+
+# ---------------------------------------------------------------------------
+# Layer norm.
+
+def _norm_args(x: torch.Tensor, weight: torch.Tensor, name: str):
+    if x.dim() < 1:
+        raise LramError("%s must be [..., width]" % name)
+    width = x.shape[-1]
+    rows = x.numel() // width if width else 0
+    if weight.dtype not in (x.dtype, torch.float32):
+        raise LramError("weight must be float32 or of %s's type" % name)
+    return rows, width, _type(x, name), _type(weight, "weight")
+
+
+def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, eps: float = 1e-5,
+                       residual: Optional[torch.Tensor] = None):
+    """(y, h, mean, rstd): h = x + residual in x's type (x itself without a residual), y its layer norm over the last
+    dimension, and the rows' statistics (fp32 [...]) for the backward."""
+    lib = _library()
+    rows, width, dt, wt = _norm_args(x, weight, "x")
+    y = torch.empty_like(x)
+    h = x if residual is None else torch.empty_like(x)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    _check(lib.lram_layer_norm_forward(
+        _dev(x, "x"), None if residual is None else _dev(residual, "residual", x.dtype, x.shape, like=x),
+        _dev(weight, "weight", shape=(width,), like=x), _dev(bias, "bias", weight.dtype, (width,), like=x), dt, wt, rows,
+        width, float(eps), None if residual is None else h.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+        _stream(x)))
+    return y, h, mean, rstd
+
+
+def layer_norm_backward(h: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                        grad_y: torch.Tensor, grad_h: Optional[torch.Tensor] = None, want_grad_weight: bool = True,
+                        workspace: Optional[torch.Tensor] = None):
+    """(grad_x, grad_weight, grad_bias) from what ``layer_norm_forward`` returned.  grad_h: the gradient that reaches h
+    besides (the residual stream's); grad_x is that of x and of residual alike.  The weights' are None unless
+    want_grad_weight."""
+    lib = _library()
+    rows, width, dt, wt = _norm_args(h, weight, "h")
+    f32, lead = torch.float32, h.shape[:-1]
+    gx = torch.empty_like(h)
+    gw = torch.empty_like(weight) if want_grad_weight else None
+    gb = torch.empty_like(weight) if want_grad_weight else None
+    n = ctypes.c_size_t(0)
+    if want_grad_weight and workspace is None:
+        _check(lib.lram_layer_norm_backward_workspace_bytes(rows, width, dt, ctypes.byref(n)))
+    ws, ws_bytes, _keep = _scratch(n.value, workspace, h)
+    _check(lib.lram_layer_norm_backward(
+        _dev(h, "h"), _dev(weight, "weight", shape=(width,), like=h), _dev(mean, "mean", f32, lead, like=h),
+        _dev(rstd, "rstd", f32, lead, like=h), _dev(grad_y, "grad_y", h.dtype, h.shape, like=h),
+        None if grad_h is None else _dev(grad_h, "grad_h", h.dtype, h.shape, like=h), dt, wt, rows, width,
+        gx.data_ptr(), None if gw is None else gw.data_ptr(), None if gb is None else gb.data_ptr(), ws, ws_bytes,
+        _stream(h)))
+    return gx, gw, gb
+
+
+class LayerNorm(torch.autograd.Function):
+    """Autograd wrapper: (y, h)."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, eps):
+        x = x.contiguous()
+        residual = None if residual is None else residual.contiguous()
+        y, h, mean, rstd = layer_norm_forward(x, weight.contiguous(), bias.contiguous(), eps, residual)
+        ctx.save_for_backward(h, weight.contiguous(), mean, rstd)
+        ctx.residual = residual is not None
+        ctx.set_materialize_grads(False)
+        if residual is None:
+            return y, None
+        return y, h
+
+    @staticmethod
+    def backward(ctx, gy, gh):
+        h, weight, mean, rstd = ctx.saved_tensors
+        if gy is None:
+            return gh, gh if ctx.residual else None, None, None, None
+        gx, gw, gb = layer_norm_backward(h, weight, mean, rstd, gy.contiguous(),
+                                         None if gh is None else gh.contiguous(),
+                                         want_grad_weight=ctx.needs_input_grad[2] or ctx.needs_input_grad[3])
+        return gx, gx if ctx.residual else None, gw, gb, None
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, eps: float = 1e-5,
+               residual: Optional[torch.Tensor] = None):
+    """The layer norm of x, differentiable; with a residual (y, h): the norm of h = x + residual, and h."""
+    y, h = LayerNorm.apply(x, residual, weight, bias, float(eps))
+    return y if residual is None else (y, h)
+
+
+# ---------------------------------------------------------------------------
+# Attention over packed sequences.
+
+class Packed(NamedTuple):
+    """Where a batch's sequences lie (int32 device tensors): sequence b has the rows start_q[b] ... start_q[b + 1] - 1 of
+    q and start_k[b] ... start_k[b + 1] - 1 of k and v, of the latter only the first used_k[b] where used_k is given (a
+    cache).  max_q and max_k: the longest expected; what exceeds them costs time, not results."""
+    start_q: torch.Tensor
+    start_k: torch.Tensor
+    max_q: int
+    max_k: int
+    used_k: Optional[torch.Tensor] = None
+
+
+def pack(queries: Sequence[int], keys: Optional[Sequence[int]] = None, capacity: int = 0, device="cuda") -> Packed:
+    """The plan of sequences of these lengths, packed one after the other; keys: their keys' lengths (the queries' by
+    default); capacity: rows that a cache holds for every sequence, of which ``keys`` are used."""
+    keys = queries if keys is None else keys
+    if len(queries) != len(keys) or any(n < 0 for n in queries) or any(n < 0 for n in keys):
+        raise LramError("queries and keys must be lengths of the same sequences")
+    if capacity and any(n > capacity for n in keys):
+        raise LramError("a sequence has more keys than the cache holds for it")
+
+    def starts(lengths):
+        at = [0]
+        for n in lengths:
+            at.append(at[-1] + int(n))
+        if at[-1] >= 1 << 31:
+            raise LramError("2^31 rows or more")
+        return torch.tensor(at, dtype=torch.int32).to(device)
+
+    return Packed(starts(queries), starts([capacity] * len(keys) if capacity else keys), max(queries, default=0),
+                  max(keys, default=0), torch.tensor(list(keys), dtype=torch.int32).to(device) if capacity else None)
+
+
+class RelativeBias(NamedTuple):
+    """Learned bias of a query-key pair by head and bucket of their distance: weight [heads, buckets] (q's type or
+    fp32), bucket [2 reach + 1] int32 (``relative_buckets``): the bucket of key minus query = -reach ... reach, the ends
+    aligned; longer distances take the last one's."""
+    weight: torch.Tensor
+    bucket: torch.Tensor
+
+
+def relative_buckets(buckets: int, reach: int, both: bool = True, device="cuda") -> torch.Tensor:
+    """Buckets of the distances -reach ... reach: half of a side's one distance each, the others growing as powers up to
+    reach; ``both``: half of the buckets for keys behind the query, else none (a key behind it counts as distance 0)."""
+    side = buckets // 2 if both else buckets
+    near = max(side // 2, 1)
+    n = side - near
+    if buckets < 1 or side < 1 or reach < near:
+        raise LramError("relative_buckets needs buckets >= 1 (2 for both sides) and reach >= half of a side's buckets")
+
+    def one(a):  # near + floor(log(a / near) / log(reach / near) n), at most side - 1, in whole numbers
+        return a if a < near else near + sum(a ** n * near ** c >= near ** n * reach ** c for c in range(1, n))
+
+    got = [min(one(abs(d) if both else max(-d, 0)), side - 1) + (side if both and d > 0 else 0)
+           for d in range(-reach, reach + 1)]
+    return torch.tensor(got, dtype=torch.int32).to(device)
+
+
+class AttentionSaved(NamedTuple):
+    """What ``attention_backward`` needs beside the result: lse [rows, heads] fp32 (log2 of the softmax sums) and, bf16,
+    the part of the result that its rounding left out."""
+    lse: torch.Tensor
+    residue: Optional[torch.Tensor]
+
+
+def _heads(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None):
+    """(pointer, row stride, head stride) of a [rows, heads, head_dim] tensor whose last dimension is dense."""
+    if not t.is_cuda:
+        raise LramError("%s must be a GPU tensor" % name)
+    if t.dim() != 3:
+        raise LramError("%s must be [rows, heads, head_dim]" % name)
+    if like is not None and (t.device != like.device or t.dtype != like.dtype or t.shape[2] != like.shape[2]):
+        raise LramError("%s must have q's device, type and head_dim" % name)
+    if t.stride(2) != 1 and t.numel():
+        raise LramError("%s must be dense along head_dim" % name)
+    # a dimension of size 0 or 1 has no stride to speak of
+    row = t.stride(0) if t.shape[0] > 1 else max(t.shape[1] * t.shape[2], t.shape[2])
+    return t.data_ptr(), row, t.stride(1) if t.shape[1] > 1 else t.shape[2]
+
+
+def _describe(q, k, v, seqs: Packed, causal, scale, rel: Optional[RelativeBias]):
+    qp, q_row, q_head = _heads(q, "q")
+    kp, k_row, k_head = _heads(k, "k", q)
+    vp, v_row, v_head = _heads(v, "v", q)
+    if k.shape != v.shape:
+        raise LramError("k and v must have the same shape")
+    batch = seqs.start_q.numel() - 1
+    if batch < 0:
+        raise LramError("start_q must be [batch + 1]")
+    i32 = torch.int32
+    a = _Attention(
+        dtype=_type(q, "q"), heads=q.shape[1], kv_heads=k.shape[1], head_dim=q.shape[2], batch=batch,
+        causal=int(bool(causal)), scale=1.0 / math.sqrt(max(q.shape[2], 1)) if scale is None else float(scale),
+        tq=q.shape[0], tk=k.shape[0], max_q=int(seqs.max_q), max_k=int(seqs.max_k), q=qp, k=kp, v=vp, q_row=q_row,
+        q_head=q_head, k_row=k_row, k_head=k_head, v_row=v_row, v_head=v_head,
+        start_q=_dev(seqs.start_q, "start_q", i32, (batch + 1,), like=q),
+        start_k=_dev(seqs.start_k, "start_k", i32, (batch + 1,), like=q),
+        used_k=None if seqs.used_k is None else _dev(seqs.used_k, "used_k", i32, (batch,), like=q))
+    if rel is not None:
+        if rel.weight.dim() != 2 or rel.bucket.dim() != 1 or rel.bucket.numel() % 2 != 1:
+            raise LramError("a relative bias has weight [heads, buckets] and bucket [2 reach + 1]")
+        if rel.weight.dtype not in (q.dtype, torch.float32):
+            raise LramError("the relative bias's weight must be float32 or of q's type")
+        a.rel_weight = _dev(rel.weight, "rel.weight", shape=(q.shape[1], rel.weight.shape[1]), like=q)
+        a.rel_bucket = _dev(rel.bucket, "rel.bucket", i32, like=q)
+        a.wdtype = _type(rel.weight, "rel.weight")
+        a.rel_buckets, a.rel_reach = rel.weight.shape[1], rel.bucket.numel() // 2
+    return a
+
+
+def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Packed, causal: bool = False,
+                      scale: Optional[float] = None, rel: Optional[RelativeBias] = None, save: bool = False,
+                      workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[AttentionSaved]]:
+    """(out, saved): softmax(scale q k^T + bias) v of packed sequences, q [rows, heads, head_dim], k and v [rows, kv_heads,
+    head_dim] (any row and head strides; head_dim 32, 64 or 128; scale 1 / sqrt(head_dim) by default).  The ends of a
+    sequence's queries and keys are aligned, and ``causal`` queries see no key past theirs.  saved (with ``save``): for
+    ``attention_backward``."""
+    lib = _library()
+    a = _describe(q, k, v, seqs, causal, scale, rel)
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    saved = None
+    if save:
+        saved = AttentionSaved(torch.empty(q.shape[:2], dtype=torch.float32, device=q.device),
+                               torch.empty_like(out) if q.dtype == torch.bfloat16 else None)
+    n = ctypes.c_size_t(0)
+    if workspace is None:
+        _check(lib.lram_attention_forward_workspace_bytes(ctypes.byref(a), ctypes.byref(n)))
+    ws, ws_bytes, _keep = _scratch(n.value, workspace, q)
+    _check(lib.lram_attention_forward(
+        ctypes.byref(a), out.data_ptr(), saved.lse.data_ptr() if save else None,
+        saved.residue.data_ptr() if save and saved.residue is not None else None, ws, ws_bytes, _stream(q)))
+    return out, saved
