@@ -79,7 +79,7 @@ typedef struct {
   int32_t batch;              /* sequences, at least 0 */
   int32_t causal;             /* 0 or 1 */
   float scale;                /* finite, > 0 */
-  int64_t tq, tk;             /* rows of q, of k and v; tq heads / kv_heads < 2^31, tk < 2^31 */
+  int64_t tq, tk;             /* rows of q, of k and v; tq heads / kv_heads <= 2^30, tk < 2^31 */
   int64_t max_q, max_k;
   const void *q, *k, *v;      /* [tq][heads][head_dim], [tk][kv_heads][head_dim] with the strides below */
   int64_t q_row, q_head, k_row, k_head, v_row, v_head; /* in elements: multiples of 16 bytes, rows at least head_dim
@@ -103,6 +103,18 @@ typedef struct {
 int lram_attention_forward_workspace_bytes(const lram_attention* a, size_t* bytes);
 int lram_attention_forward(const lram_attention* a, void* out, float* lse, void* residue, void* workspace,
                            size_t ws_bytes, void* stream);
+
+/*
+ * lram_attention_backward -- gradients of <grad_out, out>, from the same arguments and what the forward wrote:
+ *   grad_q [tq][heads][head_dim], grad_k, grad_v [tk][kv_heads][head_dim]  dense, in dtype, overwritten (rows that no
+ *          query meets, those of a cache past used_k among them: zeros)
+ *   grad_rel [heads][rel_buckets] in wdtype, overwritten; given exactly where rel_weight is
+ *   residue  nullable (the forward's).
+ */
+int lram_attention_backward_workspace_bytes(const lram_attention* a, size_t* bytes);
+int lram_attention_backward(const lram_attention* a, const void* out, const void* residue, const float* lse,
+                            const void* grad_out, void* grad_q, void* grad_k, void* grad_v, void* grad_rel,
+                            void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

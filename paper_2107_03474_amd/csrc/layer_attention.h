@@ -36,6 +36,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr int XCDS = 8;
 constexpr int ROWS = 32;     // packed rows (or keys) of a wave
 constexpr int KEYS = 64;     // keys of a tile in LDS
+constexpr int WAVES = 4, THREADS = WAVES * WAVE;
 constexpr int BIAS_PAD = 96;  // distances that a tile reaches past the last one with a bias of its own
 
 // Device-side view of a call.
@@ -246,16 +247,14 @@ struct Tile {
 
 // 16 bytes a lane from memory straight into LDS at dst + 16 lane; a lane whose offset lies past the resource's end
 // gets zeros.  Written out so that the compiler does not wait for it at the next read of any tile: the kernels wait
-// themselves (loads_left), before the barrier or the reads that need it.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"  // m0 is reserved, and written here all the same
+// themselves (loads_left), before the barrier or the reads that need it.  m0, the destination's register, holds nothing
+// else in these kernels.
 __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t src, Lds dst, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"((uint32_t)(uintptr_t)dst), "v"(offset), "s"(src)
-               : "memory", "m0");
+               : "memory");
 }
-#pragma clang diagnostic pop
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 }
@@ -310,6 +309,73 @@ __device__ __forceinline__ void reads_done() {
   asm volatile("" ::: "memory");
 }
 
+// What a lane knows of its row.
+struct Row {
+  bool valid;
+  int i, g;  // query, head of the group
+};
+__device__ __forceinline__ Row row_of(const Args& a, const Seq& s, int row) {
+  Row r;
+  r.valid = row < s.nq * a.group;
+  r.i = row / a.group;
+  r.g = row - r.i * a.group;
+  return r;
+}
+template <typename T, int D>
+__device__ __forceinline__ void load_query(const Args& a, const T* base, int64_t row_stride, int64_t head_stride,
+                                           const Seq& s, int head, const Row& r, typename Frag<T>::type (&f)[D / 16]) {
+  using F = typename Frag<T>::type;
+  const T* p = base + (s.q0 + r.i) * row_stride + head * head_stride + 8 * (threadIdx.x >> 5 & 1);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    F z = {};
+    f[k] = r.valid ? *(const F*)(p + 16 * k) : z;
+  }
+}
+
+// The tile of a workgroup: sequence, first packed row, key range (find_work: false for an empty slot, slot = -1 for no slot
+// at all).
+struct Work {
+  Seq s;
+  int hk, slot, row0, split, kbeg, kend;
+};
+template <int M>
+__device__ __forceinline__ bool find_work(const Args& a, Work* w) {
+  w->slot = -1;
+  const int64_t item = work_item((int64_t)a.kv_heads * a.slots * a.splits);
+  if (item < 0) return false;
+  w->hk = (int)(item / ((int64_t)a.slots * a.splits));
+  const int rest = (int)(item % ((int64_t)a.slots * a.splits));
+  w->split = rest % a.splits;
+  const int slot = w->slot = a.slots - 1 - rest / a.splits;  // long causal rows first
+  const int b = slot_sequence(a.start_q, a.tq, a.batch, a.group, M, slot);
+  w->s = sequence(a, b);
+  const int64_t row0 = (slot - first_slot(a.start_q, a.tq, b, a.group, M)) * M;
+  if (row0 >= (int64_t)w->s.nq * a.group) return false;
+  w->row0 = (int)row0;
+  const int rows = w->s.nq * a.group;
+  const int last = (w->row0 + M < rows ? w->row0 + M : rows) - 1;
+  int end = w->s.nk;
+  if (a.causal) {
+    const int seen = last / a.group + w->s.nk - w->s.nq + 1;
+    end = seen < end ? (seen > 0 ? seen : 0) : end;
+  }
+  const int64_t from = (int64_t)w->split * a.piece;
+  w->kbeg = from < end ? (int)from : end;
+  w->kend = w->split == a.splits - 1 || from + a.piece > end ? end : (int)(from + a.piece);
+  return true;
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, f32x4 x) {
+  using V = T __attribute__((ext_vector_type(4)));
+  *(V*)p = __builtin_convertvector(x, V);
+}
+
+// Waves per SIMD: two; one where LDS holds one workgroup a CU.
+template <typename T, int D>
+constexpr int waves_per_simd() { return 4 * KEYS * Tile<T, D>::ROW > 80 * 1024 ? 1 : 2; }
+
 // ---------------------------------------------------------------------------
 // Host side.
 
@@ -321,7 +387,7 @@ int check_attention(const lram_attention& a, bool pointers) {
   const int64_t G = a.heads / a.kv_heads;
   if (a.batch < 0 || a.batch > 1 << 24 || (a.causal & ~1) || !(a.scale > 0) || !(a.scale < INFINITY))
     return LRAM_EINVAL;
-  if (a.tq < 0 || a.tk < 0 || a.tk > INT32_MAX || a.tq > INT32_MAX / G || a.max_q < 0 || a.max_k < 0)
+  if (a.tq < 0 || a.tk < 0 || a.tk > INT32_MAX || a.tq > (1 << 30) / G || a.max_q < 0 || a.max_k < 0)
     return LRAM_EINVAL;
   // work items of every kernel (at most 64 pieces of tiles of 32 rows) stay below 2^31 workgroups of 256 threads
   if (a.kv_heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 1) > (int64_t(1) << 24) - 16) return LRAM_EINVAL;

@@ -1,0 +1,547 @@
+// layer_attention_backward.hip -- part of liblram: attention over packed sequences, backward (see layer_attention.h for
+// the formulas and the tiles).
+//
+//     p_ij = 2^(z_ij - lse_i),  dv_j = sum_i p_ij do_i,  ds_ij = p_ij (do_i . v_j - delta_i),  delta_i = do_i . o_i
+//     dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dW_h(d) = sum over j - i - off = d of ds_ij
+//
+// Two kernels, each forming p again, so that every sum has one owner and one order: k_attention_dq keeps 128 packed
+// rows and walks over the keys (scores transposed, as in the forward pass), k_attention_dkv keeps 128 keys and walks over
+// the packed rows, the G heads of its group among them.  Seven products instead of the five of a single kernel, whose dq
+// would be added up in memory by atomics, in an order that varies.  p and ds are rounded to the operands' type.
+//
+// The bias's gradient: k_attention_dq adds ds by distance in LDS, one table to a wave, the two halves of the wave one
+// after the other (inside a half no two lanes meet in an entry, so the order is fixed); tiles past reach go into a
+// register.  A workgroup leaves one row of sums by distance, and k_relative_grad adds the rows and gathers the buckets.
+
+#include "layer_attention.h"
+
+namespace {
+
+struct Grads {
+  const void *out, *residue, *grad_out;
+  const float* lse;
+  void *gq, *gk, *gv, *grel;
+  float *delta, *rel;  // workspace: [tq heads], [slots][heads][2 reach + 1]
+};
+
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention_dq(Args a, Grads o) {
+  using Ti = Tile<T, D>;
+  using F = typename Frag<T>::type;
+  constexpr int M = WAVES * ROWS, BYTES = KEYS * Ti::ROW;
+  extern __shared__ __attribute__((aligned(256))) char smem[];
+  Lds lds = (Lds)smem;
+  Work w;
+  const bool found = find_work<M>(a, &w);
+  if constexpr (BIAS) {
+    if (!found) {  // an empty slot's sums are zero
+      if (w.slot >= 0)
+        for (int t = threadIdx.x; t < a.group * (2 * a.reach + 1); t += THREADS)
+          o.rel[((int64_t)w.slot * a.heads + w.hk * a.group) * (2 * a.reach + 1) + t] = 0;
+      return;
+    }
+  } else {
+    if (!found) return;
+  }
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
+  const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
+  const Row r = row_of(a, w.s, first + (l & 31));
+  const int head = w.hk * G + r.g;
+  const int64_t at = (w.s.q0 + r.i) * a.heads + head;
+  F q[D / 16], g[D / 16];
+  load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
+  load_query<T, D>(a, (const T*)o.grad_out, (int64_t)a.heads * D, D, w.s, head, r, g);
+  float delta = 0, lse = 0;
+  {
+    F x[D / 16];
+    load_query<T, D>(a, (const T*)o.out, (int64_t)a.heads * D, D, w.s, head, r, x);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)g[k][e], (float)x[k][e], delta);
+    if (o.residue) {
+      load_query<T, D>(a, (const T*)o.residue, (int64_t)a.heads * D, D, w.s, head, r, x);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf((float)g[k][e], (float)x[k][e], delta);
+    }
+    delta = add_halves(delta);
+    if (r.valid) {
+      lse = o.lse[at];
+      if (l < 32) o.delta[at] = delta;
+    }
+  }
+  const int lim = a.causal && r.valid ? min(r.i + off, w.s.nk - 1) : w.s.nk - 1;
+  const int i_first = first / G, i_last = (min(first + ROWS, rows) - 1) / G;
+  const int lim_first = a.causal ? min(i_first + off, w.s.nk - 1) : w.s.nk - 1;
+  const int lim_last = first >= rows ? -1 : (a.causal ? min(i_last + off, w.s.nk - 1) : w.s.nk - 1);
+  const float* bias = nullptr;
+  float* hist = nullptr;  // the wave's table of sums, at the lane's row as `bias` is
+  float near_far[2] = {0, 0}, far_sum[2] = {0, 0};
+  const int width = bias_width(a);
+  float* const table = (float*)(smem + 4 * BYTES);
+  float* const sums = table + G * width;  // [WAVES][G][width]
+  if constexpr (BIAS) {
+    fill_bias(a, w.hk * G, table, THREADS);
+    for (int t = threadIdx.x; t < WAVES * G * width; t += THREADS) sums[t] = 0;
+    const int shift = a.reach + BIAS_PAD - (r.i + off), gi = r.valid ? r.g : 0;
+    bias = table + r.g * width + shift;
+    hist = sums + (wave * G + r.g) * width + shift;
+    __syncthreads();
+    near_far[0] = table[gi * width];
+    near_far[1] = table[gi * width + width - 1];
+  }
+  const typename Ti::RowAddr ka = Ti::row_addr(l & 31);
+  const typename Ti::ColAddr ca = Ti::col_addr();
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[b][e] = 0;
+  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.hk * a.k_head;
+  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.hk * a.v_head;
+  auto load = [&](int j0, int buf) {
+    load_rows<T, D, KEYS, WAVES>(kh, a.k_row, j0, w.s.nk, lds + buf * 2 * BYTES, wave);
+    load_rows<T, D, KEYS, WAVES>(vh, a.v_row, j0, w.s.nk, lds + buf * 2 * BYTES + BYTES, wave);
+  };
+  if (w.kbeg < w.kend) load(w.kbeg, 0);
+  int buf = 0;
+  for (int j0 = w.kbeg; j0 < w.kend; j0 += KEYS, buf ^= 1) {
+    loads_done();
+    __syncthreads();
+    if (j0 + KEYS < w.kend) load(j0 + KEYS, buf ^ 1);
+    const Lds kt = lds + buf * 2 * BYTES, vt = kt + BYTES;
+#pragma unroll
+    for (int b = 0; b < KEYS / 32; ++b) {
+      const int j = j0 + 32 * b;
+      if (j > lim_last) continue;
+      f32x16 s, dp;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) s = mma(Ti::row_frag(kt, ka, k, 32 * b), q[k], s);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) dp = mma(Ti::row_frag(vt, ka, k, 32 * b), g[k], dp);
+      bool whole = true, above = false;
+      float far = 0;
+      if constexpr (BIAS) {
+        above = j - (i_last + off) >= a.reach;
+        whole = above || j + 31 - (i_first + off) <= -a.reach;
+        far = near_far[above];
+      }
+      if (whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.c, far - lse));
+      } else {
+        const float* t = bias + j + 4 * h;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.c, t[8 * (e >> 2) + (e & 3)]) - lse);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] *= dp[e] - delta;
+      if (j + 31 > lim_first) {
+        const int last = lim - j - 4 * h;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) <= last ? s[e] : 0.0f;
+      }
+      if constexpr (BIAS) {
+        if (whole) {
+          float sum = 0;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum += s[e];
+          far_sum[0] += above ? 0.0f : sum;
+          far_sum[1] += above ? sum : 0.0f;
+        } else {
+          float* t = hist + j + 4 * h;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            asm volatile("" ::: "memory");  // one half of the wave, then the other
+            if (r.valid && h == half)
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                __hip_atomic_fetch_add(t + 8 * (e >> 2) + (e & 3), s[e], __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_WORKGROUP);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        f32x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = s[8 * k + e];
+        const auto f = to_frag<T>(p);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) acc[d] = mma(Ti::col_frag(kt, ca, d, 2 * b + k), f, acc[d]);
+      }
+    }
+  }
+  if (r.valid) {
+    T* p = (T*)o.gq + at * D + 4 * h;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        f32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = acc[b][4 * u + e] * a.scale;
+        store4<T>(p + 32 * b + 8 * u, x);
+      }
+  }
+  if constexpr (BIAS) {
+    // the waves' tables added up, then the entries past reach, with the far tiles' sums, into the last one's
+    __syncthreads();
+    for (int t = threadIdx.x; t < G * width; t += THREADS) {
+      float x = 0;
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) x += sums[v * G * width + t];
+      sums[t] = x;
+    }
+    float* const lane = (float*)smem;  // [2][THREADS]; the tiles are done with
+    lane[threadIdx.x] = far_sum[0];
+    lane[THREADS + threadIdx.x] = far_sum[1];
+    __syncthreads();
+    const int n = 2 * a.reach + 1;
+    float* const row = o.rel + ((int64_t)w.slot * a.heads + w.hk * G) * n;
+    for (int t = threadIdx.x; t < G * n; t += THREADS) {
+      const int gi = t / n, d = t % n;
+      if (d > 0 && d < n - 1) row[t] = sums[gi * width + BIAS_PAD + d];
+    }
+    for (int t = wave; t < 2 * G; t += WAVES) {
+      const int gi = t / 2, side = t % 2;
+      if (a.reach == 0 && side) continue;  // one entry in all
+      float x = 0;
+      for (int e = l; e < THREADS; e += WAVE) {
+        const int lr = w.row0 + e / WAVE * ROWS + (e & 31);
+        if (lr % G == gi) x += lane[side * THREADS + e] + (a.reach == 0 ? lane[THREADS + e] : 0.0f);
+      }
+      const int entries = a.reach == 0 ? width : BIAS_PAD + 1;
+      for (int e = l; e < entries; e += WAVE) x += sums[gi * width + (side ? width - entries : 0) + e];
+      x = wave_sum(x);
+      if (l == 0) row[gi * n + (side ? n - 1 : 0)] = x;
+    }
+  }
+}
+
+// 16 bytes a lane from the lane's address straight into LDS at dst + 16 lane (see dma16).
+__device__ __forceinline__ void dma16_from(const void* src, Lds dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"((uint32_t)(uintptr_t)dst), "v"(src)
+               : "memory");
+}
+
+constexpr int TROWS = 64;  // packed rows of a tile in k_attention_dkv
+// What it keeps of a row: delta, lse, lse less the bias below and above reach, and where distance 0 to key 0 stands in the
+// bias table.
+enum { DELTA, LSE, BELOW, ABOVE, BASE, STATS };
+
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention_dkv(Args a, Grads o) {
+  using Ti = Tile<T, D>;
+  using F = typename Frag<T>::type;
+  constexpr int N = WAVES * 32, BYTES = TROWS * Ti::ROW, LOADS = TROWS * Ti::CH / 64 / WAVES;
+  extern __shared__ __attribute__((aligned(256))) char smem[];
+  Lds lds = (Lds)smem;
+  const int64_t item = work_item((int64_t)a.kv_heads * a.slots);
+  if (item < 0) return;
+  const int hk = (int)(item / a.slots), slot = (int)(item % a.slots);
+  const int b = slot_sequence(a.start_k, a.tk, a.batch, 1, N, slot);
+  const Seq s = sequence(a, b);
+  const int64_t from = (slot - first_slot(a.start_k, a.tk, b, 1, N)) * N;
+  if (from >= s.cap) return;
+  const int j0 = (int)from;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
+  const int G = a.group, off = s.nk - s.nq, rows = s.nq * G;
+  const int jw = j0 + 32 * wave, j = jw + (l & 31);
+  const bool valid = j < s.nk;
+  // keys from row_of_key on see the lane's key (causal)
+  const auto first_row = [&](int key) { return a.causal ? max(key - off, 0) * G : 0; };
+  const int seen_from = first_row(j);
+  const int begin = j0 < s.nk ? first_row(j0) : rows;
+
+  F k[D / 16], v[D / 16];
+  {
+    const T* kp = (const T*)a.k + (s.k0 + j) * a.k_row + hk * a.k_head + 8 * h;
+    const T* vp = (const T*)a.v + (s.k0 + j) * a.v_row + hk * a.v_head + 8 * h;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+      F z = {};
+      k[t] = valid ? *(const F*)(kp + 16 * t) : z;
+      v[t] = valid ? *(const F*)(vp + 16 * t) : z;
+    }
+  }
+  // beside the tiles: [2][STATS][TROWS], then the bias table
+  float* const stats = (float*)(smem + 4 * BYTES);
+  float* const table = stats + 2 * STATS * TROWS;
+  const int width = bias_width(a);
+  if constexpr (BIAS) {
+    fill_bias(a, hk * G, table, THREADS);
+    __syncthreads();
+  }
+  const typename Ti::RowAddr ra = Ti::row_addr(l & 31);
+  const typename Ti::ColAddr ca = Ti::col_addr();
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dk[t][e] = dv[t][e] = 0;
+
+  const T* const qh = (const T*)a.q + s.q0 * a.q_row + (int64_t)hk * G * a.q_head;
+  const T* const gh = (const T*)o.grad_out + (s.q0 * a.heads + hk * G) * D;
+  const float* const lse_h = o.lse + s.q0 * a.heads + hk * G;
+  const float* const delta_h = o.delta + s.q0 * a.heads + hk * G;
+  const int inv = 65536 / G + 1;  // x / G = x inv >> 16 for x < 128, G <= 64
+  // packed row t of a tile from row r0 on, i0 = r0 / G: (query, head of the group); past the last row its last one
+  const auto split_row = [&](int r0, int i0, int t, int* i, int* g) {
+    t = min(t, rows - 1 - r0);
+    const int x = r0 - i0 * G + t, di = x * inv >> 16;
+    *i = i0 + di;
+    *g = x - di * G;
+  };
+  const auto load = [&](int r0, int buf) {
+    const int i0 = r0 / G;
+#pragma unroll
+    for (int n = 0; n < LOADS; ++n) {
+      const int c = (wave * LOADS + n) * 64, p = c + l, r = p / Ti::CH;
+      const int ch = (p % Ti::CH) ^ Ti::swizzle(r);
+      int i, g;
+      split_row(r0, i0, r, &i, &g);
+      const Lds to = lds + buf * 2 * BYTES + c * 16;
+      dma16_from(qh + (int64_t)i * a.q_row + (int64_t)g * a.q_head + ch * Ti::PER, to);
+      dma16_from(gh + ((int64_t)i * a.heads + g) * D + ch * Ti::PER, to + BYTES);
+    }
+  };
+  // A tile's statistics, a row to a thread of the first wave: loaded with the tile before, written when it is done.
+  // A row past the last one gets lse = inf, and with it p = 0.
+  float st_lse = 0, st_delta = 0;
+  const auto load_stats = [&](int r0) {
+    int i, g;
+    split_row(r0, r0 / G, l, &i, &g);
+    st_lse = r0 + l < rows ? lse_h[(int64_t)i * a.heads + g] : INFINITY;
+    st_delta = delta_h[(int64_t)i * a.heads + g];
+  };
+  const auto put_stats = [&](int r0, int buf) {
+    float* to = stats + buf * STATS * TROWS + l;
+    to[DELTA * TROWS] = st_delta;
+    to[LSE * TROWS] = st_lse;
+    if constexpr (BIAS) {
+      int i, g;
+      split_row(r0, r0 / G, l, &i, &g);
+      to[BELOW * TROWS] = st_lse - table[g * width];
+      to[ABOVE * TROWS] = st_lse - table[g * width + width - 1];
+      ((int*)to)[BASE * TROWS] = g * width + a.reach + BIAS_PAD - (i + off);
+    }
+  };
+  if (begin < rows) {
+    load(begin, 0);
+    if (wave == 0) {
+      load_stats(begin);
+      put_stats(begin, 0);
+    }
+  }
+  int buf = 0;
+  for (int r0 = begin; r0 < rows; r0 += TROWS, buf ^= 1) {
+    loads_done();
+    __syncthreads();
+    const bool more = r0 + TROWS < rows;
+    if (more) {
+      load(r0 + TROWS, buf ^ 1);
+      if (wave == 0) load_stats(r0 + TROWS);
+    }
+    const Lds qt = lds + buf * 2 * BYTES, gt = qt + BYTES;
+    const float* const st = stats + buf * STATS * TROWS + 4 * h;
+#pragma unroll
+    for (int rb = 0; rb < TROWS / 32; ++rb) {
+      // rows that none of the wave's keys meets
+      if (jw >= s.nk || r0 + 32 * rb + 31 < first_row(jw) || r0 + 32 * rb >= rows) continue;
+      int use = LSE;  // past reach one value of a row's bias serves the whole block, and is in the row's statistic
+      if constexpr (BIAS) {
+        const int i_first = (r0 + 32 * rb) / G, i_last = (min(r0 + 32 * rb + 32, rows) - 1) / G;
+        if (jw + 31 - (i_first + off) <= -a.reach) use = BELOW;
+        if (jw - (i_last + off) >= a.reach) use = ABOVE;
+      }
+      const bool near = BIAS && use == LSE;
+      f32x16 p, ds;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[e] = ds[e] = 0;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) p = mma(Ti::row_frag(qt, ra, t, 32 * rb), k[t], p);
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) ds = mma(Ti::row_frag(gt, ra, t, 32 * rb), v[t], ds);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const f32x4 lse = *(const f32x4*)(st + use * TROWS + 32 * rb + 8 * u);
+        if (near) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int at = ((const int*)st)[BASE * TROWS + 32 * rb + 8 * u + e] + j;
+            p[4 * u + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * u + e], a.c, table[at]) - lse[e]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[4 * u + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * u + e], a.c, -lse[e]));
+        }
+        const f32x4 delta = *(const f32x4*)(st + DELTA * TROWS + 32 * rb + 8 * u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ds[4 * u + e] = p[4 * u + e] * (ds[4 * u + e] - delta[e]);
+      }
+      if (a.causal && r0 + 32 * rb < first_row(jw + 31)) {
+        const int need = seen_from - (r0 + 32 * rb) - 4 * h;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const bool sees = 8 * (e >> 2) + (e & 3) >= need;
+          p[e] = sees ? p[e] : 0.0f;
+          ds[e] = sees ? ds[e] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        f32x8 x, y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] = p[8 * c + e];
+          y[e] = ds[8 * c + e];
+        }
+        const auto fx = to_frag<T>(x), fy = to_frag<T>(y);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) dv[t] = mma(Ti::col_frag(gt, ca, t, 2 * rb + c), fx, dv[t]);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) dk[t] = mma(Ti::col_frag(qt, ca, t, 2 * rb + c), fy, dk[t]);
+      }
+    }
+    if (more && wave == 0) put_stats(r0 + TROWS, buf ^ 1);
+  }
+  if (j >= s.cap) return;
+  const int64_t at = ((s.k0 + j) * a.kv_heads + hk) * D + 4 * h;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      f32x4 x, y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {  // rows of a cache past the sequence's keys: zeros
+        x[e] = valid ? dk[t][4 * u + e] * a.scale : 0.0f;
+        y[e] = valid ? dv[t][4 * u + e] : 0.0f;
+      }
+      store4<T>((T*)o.gk + at + 32 * t + 8 * u, x);
+      store4<T>((T*)o.gv + at + 32 * t + 8 * u, y);
+    }
+}
+
+// A head's sums by distance over all slots, and its buckets' from them; a workgroup to a head.
+constexpr int REL_THREADS = 1024;
+template <typename W>
+__global__ __launch_bounds__(REL_THREADS) void k_relative_grad(Args a, const float* rel, W* grad) {
+  constexpr int COLS = 128, PARTS = REL_THREADS / COLS;
+  extern __shared__ float sum[];  // [n], then [PARTS][COLS]
+  const int n = 2 * a.reach + 1, head = blockIdx.x;
+  float* const part = sum + n;
+  const int c = threadIdx.x % COLS, p = threadIdx.x / COLS;
+  for (int d0 = 0; d0 < n; d0 += COLS) {
+    float x = 0;
+    if (d0 + c < n)
+#pragma unroll 8
+      for (int s = p; s < a.slots; s += PARTS) x += rel[((int64_t)s * a.heads + head) * n + d0 + c];
+    part[p * COLS + c] = x;
+    __syncthreads();
+    if (p == 0 && d0 + c < n) {
+#pragma unroll
+      for (int t = 1; t < PARTS; ++t) x += part[t * COLS + c];
+      sum[d0 + c] = x;
+    }
+    __syncthreads();
+  }
+  const int wave = threadIdx.x / WAVE, l = threadIdx.x % WAVE;
+  for (int k = wave; k < a.buckets; k += REL_THREADS / WAVE) {
+    float x = 0;
+    for (int d = l; d < n; d += WAVE) x += bucket_of(a, d - a.reach) == k ? sum[d] : 0.0f;
+    x = wave_sum(x);
+    if (l == 0) grad[(int64_t)head * a.buckets + k] = (W)x;
+  }
+}
+
+int row_slots(const lram_attention& a) {
+  return (int)(a.tq * (a.heads / a.kv_heads) / (WAVES * ROWS) + a.batch + 1);
+}
+
+struct Space {
+  size_t delta, rel, total;  // floats
+};
+Space space_of(const lram_attention& a) {
+  Space s;
+  s.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
+  s.rel = a.rel_weight ? (size_t)row_slots(a) * a.heads * (2 * a.rel_reach + 1) : 0;
+  s.total = s.delta + s.rel;
+  return s;
+}
+
+template <typename T, int D, bool BIAS>
+int go(Args x, const Grads& g, const lram_attention& d, hipStream_t s) {
+  const size_t table = BIAS ? (size_t)x.group * (2 * (x.reach + BIAS_PAD) + 1) * 4 : 0;
+  const size_t tiles = (size_t)4 * KEYS * Tile<T, D>::ROW;
+  const auto launch = [&](auto kernel, size_t bytes) {
+    if (int rc = allow_lds((const void*)kernel, bytes)) return rc;
+    hipLaunchKernelGGL(kernel, dim3(work_grid((int64_t)x.kv_heads * x.slots)), dim3(THREADS), bytes, s, x, g);
+    return layer_launched();
+  };
+  if (x.tq) {
+    x.slots = row_slots(d);
+    if (int rc = launch(k_attention_dq<T, D, BIAS>, tiles + table * (1 + WAVES))) return rc;
+  }
+  if (x.tk) {
+    x.slots = (int)(x.tk / (WAVES * 32) + x.batch + 1);
+    static_assert(TROWS == KEYS, "the tiles' bytes");
+    if (int rc = launch(k_attention_dkv<T, D, BIAS>, tiles + 2 * STATS * TROWS * 4 + table)) return rc;
+  }
+  if constexpr (BIAS) {
+    x.slots = x.tq ? row_slots(d) : 0;
+    const size_t bytes = (size_t)(2 * x.reach + 1 + REL_THREADS) * 4;
+    const auto finish = [&](auto w) {
+      using W = decltype(w);
+      hipLaunchKernelGGL(k_relative_grad<W>, dim3(x.heads), dim3(REL_THREADS), bytes, s, x, (const float*)g.rel,
+                         (W*)g.grel);
+      return layer_launched();
+    };
+    return d.wdtype == LRAM_BF16 ? finish(bf16()) : finish(float());
+  }
+  return LRAM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lram_attention_backward_workspace_bytes(const lram_attention* a, size_t* bytes) {
+  if (!a || !bytes) return LRAM_EINVAL;
+  if (int rc = check_attention(*a, false)) return rc;
+  *bytes = space_of(*a).total * 4;
+  return LRAM_OK;
+}
+
+int lram_attention_backward(const lram_attention* a, const void* out, const void* residue, const float* lse,
+                            const void* grad_out, void* grad_q, void* grad_k, void* grad_v, void* grad_rel,
+                            void* workspace, size_t ws_bytes, void* stream) {
+  if (!a) return LRAM_EINVAL;
+  if (int rc = check_attention(*a, true)) return rc;
+  if (a->tq && (!out || !lse || !grad_out || !grad_q)) return LRAM_EINVAL;
+  if (a->tk && (!grad_k || !grad_v)) return LRAM_EINVAL;
+  if ((a->rel_weight != nullptr) != (grad_rel != nullptr)) return LRAM_EINVAL;
+  if (off_align(out, 16) || off_align(residue, 16) || off_align(grad_out, 16) || off_align(grad_q, 16) ||
+      off_align(grad_k, 16) || off_align(grad_v, 16) || off_align(lse, 4) ||
+      off_align(grad_rel, elem_size(a->wdtype)))
+    return LRAM_EINVAL;
+  if (residue && a->dtype != LRAM_BF16) return LRAM_EDTYPE;
+  const Space sp = space_of(*a);
+  if (sp.total && (!workspace || off_align(workspace, 16) || ws_bytes < sp.total * 4)) return LRAM_EWORKSPACE;
+  Args x = args_of(*a);
+  x.splits = 1;
+  const Grads g{out, residue, grad_out, lse, grad_q, grad_k, grad_v, grad_rel, (float*)workspace,
+                (float*)workspace + sp.delta};
+  return by_kind(*a, [&](auto t, auto d, auto bias) {
+    return go<decltype(t), decltype(d)::value, decltype(bias)::value>(x, g, *a, (hipStream_t)stream);
+  });
+}
+
+}  // extern "C"

@@ -13,7 +13,6 @@
 
 namespace {
 
-constexpr int WAVES = 4, THREADS = WAVES * WAVE;
 constexpr int MAX_SPLITS = 64;
 constexpr float GROWTH = 8;  // log2 of how far weights may pass 1 before the sums are rescaled
 
@@ -117,67 +116,6 @@ __device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::t
   }
 }
 
-// What a lane knows of its row.
-struct Row {
-  bool valid;
-  int i, g;  // query, head of the group
-};
-__device__ __forceinline__ Row row_of(const Args& a, const Seq& s, int row) {
-  Row r;
-  r.valid = row < s.nq * a.group;
-  r.i = row / a.group;
-  r.g = row - r.i * a.group;
-  return r;
-}
-template <typename T, int D>
-__device__ __forceinline__ void load_query(const Args& a, const T* base, int64_t row_stride, int64_t head_stride,
-                                           const Seq& s, int head, const Row& r, typename Frag<T>::type (&f)[D / 16]) {
-  using F = typename Frag<T>::type;
-  const T* p = base + (s.q0 + r.i) * row_stride + head * head_stride + 8 * (threadIdx.x >> 5 & 1);
-#pragma unroll
-  for (int k = 0; k < D / 16; ++k) {
-    F z = {};
-    f[k] = r.valid ? *(const F*)(p + 16 * k) : z;
-  }
-}
-
-// The tiles of a workgroup: sequence, first packed row, key range.
-struct Work {
-  Seq s;
-  int hk, row0, split, kbeg, kend;
-};
-template <int M>
-__device__ __forceinline__ bool find_work(const Args& a, Work* w) {
-  const int64_t item = work_item((int64_t)a.kv_heads * a.slots * a.splits);
-  if (item < 0) return false;
-  w->hk = (int)(item / ((int64_t)a.slots * a.splits));
-  const int rest = (int)(item % ((int64_t)a.slots * a.splits));
-  w->split = rest % a.splits;
-  const int slot = a.slots - 1 - rest / a.splits;  // long causal rows first
-  const int b = slot_sequence(a.start_q, a.tq, a.batch, a.group, M, slot);
-  w->s = sequence(a, b);
-  const int64_t row0 = (slot - first_slot(a.start_q, a.tq, b, a.group, M)) * M;
-  if (row0 >= (int64_t)w->s.nq * a.group) return false;
-  w->row0 = (int)row0;
-  const int rows = w->s.nq * a.group;
-  const int last = (w->row0 + M < rows ? w->row0 + M : rows) - 1;
-  int end = w->s.nk;
-  if (a.causal) {
-    const int seen = last / a.group + w->s.nk - w->s.nq + 1;
-    end = seen < end ? (seen > 0 ? seen : 0) : end;
-  }
-  const int64_t from = (int64_t)w->split * a.piece;
-  w->kbeg = from < end ? (int)from : end;
-  w->kend = w->split == a.splits - 1 || from + a.piece > end ? end : (int)(from + a.piece);
-  return true;
-}
-
-template <typename T>
-__device__ __forceinline__ void store4(T* p, f32x4 x) {
-  using V = T __attribute__((ext_vector_type(4)));
-  *(V*)p = __builtin_convertvector(x, V);
-}
-
 // Results of flat row `at` = (row of q) heads + head: 4 elements from d on.
 template <typename T, int D>
 __device__ __forceinline__ void put(const Args& a, const Out& o, int split, int64_t at, int d, f32x4 x) {
@@ -202,10 +140,6 @@ __device__ __forceinline__ void put_lse(const Args& a, const Out& o, int split, 
   else if (o.lse)
     o.lse[at] = lse;
 }
-
-// Waves per SIMD: two; one where LDS holds one workgroup a CU.
-template <typename T, int D>
-constexpr int waves_per_simd() { return 4 * KEYS * Tile<T, D>::ROW > 80 * 1024 ? 1 : 2; }
 
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention(Args a, Out o) {

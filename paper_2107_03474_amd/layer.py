@@ -17,7 +17,7 @@ from . import BF16, F32, LramError, _dev, _stream
 from . import load as _load_library
 
 __all__ = ["layer_norm_forward", "layer_norm_backward", "layer_norm", "Packed", "pack", "RelativeBias",
-           "relative_buckets", "AttentionSaved", "attention_forward"]
+           "relative_buckets", "AttentionSaved", "attention_forward", "attention_backward", "attention"]
 
 _P, _I64, _I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
 
@@ -47,6 +47,8 @@ def _library():
         lib.lram_layer_norm_backward.argtypes = [_P, _P, _P, _P, _P, _P, I, I, _I64, _I64, _P, _P, _P, _P, SZ, _P]
         lib.lram_attention_forward_workspace_bytes.argtypes = [A, SZP]
         lib.lram_attention_forward.argtypes = [A, _P, _P, _P, _P, SZ, _P]
+        lib.lram_attention_backward_workspace_bytes.argtypes = [A, SZP]
+        lib.lram_attention_backward.argtypes = [A, _P, _P, _P, _P, _P, _P, _P, _P, _P, SZ, _P]
         _lib = lib
     return _lib
 
@@ -300,3 +302,57 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: P
         ctypes.byref(a), out.data_ptr(), saved.lse.data_ptr() if save else None,
         saved.residue.data_ptr() if save and saved.residue is not None else None, ws, ws_bytes, _stream(q)))
     return out, saved
+
+
+def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Packed, out: torch.Tensor,
+                       saved: AttentionSaved, grad_out: torch.Tensor, causal: bool = False,
+                       scale: Optional[float] = None, rel: Optional[RelativeBias] = None,
+                       workspace: Optional[torch.Tensor] = None):
+    """(grad_q, grad_k, grad_v, grad_rel) from what ``attention_forward`` returned (with ``save`` and the same
+    arguments); grad_rel, of the bias's weight, is None without one.  Rows of k and v that no query may see get zeros."""
+    lib = _library()
+    a = _describe(q, k, v, seqs, causal, scale, rel)
+    gq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    gk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    gv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    grel = None if rel is None else torch.empty_like(rel.weight)
+    n = ctypes.c_size_t(0)
+    if workspace is None:
+        _check(lib.lram_attention_backward_workspace_bytes(ctypes.byref(a), ctypes.byref(n)))
+    ws, ws_bytes, _keep = _scratch(n.value, workspace, q)
+    _check(lib.lram_attention_backward(
+        ctypes.byref(a), _dev(out, "out", q.dtype, q.shape, like=q),
+        None if saved.residue is None else _dev(saved.residue, "saved.residue", q.dtype, q.shape, like=q),
+        _dev(saved.lse, "saved.lse", torch.float32, q.shape[:2], like=q),
+        _dev(grad_out, "grad_out", q.dtype, q.shape, like=q), gq.data_ptr(), gk.data_ptr(), gv.data_ptr(),
+        None if grel is None else grel.data_ptr(), ws, ws_bytes, _stream(q)))
+    return gq, gk, gv, grel
+
+
+class Attention(torch.autograd.Function):
+    """Autograd wrapper of attention over packed sequences."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, weight, bucket, seqs, causal, scale):
+        rel = None if weight is None else RelativeBias(weight.contiguous(), bucket)
+        out, saved = attention_forward(q, k, v, seqs, causal, scale, rel, save=True)
+        ctx.save_for_backward(q, k, v, out, saved.lse, saved.residue, None if rel is None else rel.weight, bucket,
+                              seqs.start_q, seqs.start_k, seqs.used_k)
+        ctx.rest = (seqs.max_q, seqs.max_k, causal, scale)
+        return out
+
+    @staticmethod
+    def backward(ctx, g):
+        q, k, v, out, lse, residue, weight, bucket, start_q, start_k, used_k = ctx.saved_tensors
+        max_q, max_k, causal, scale = ctx.rest
+        rel = None if weight is None else RelativeBias(weight, bucket)
+        gq, gk, gv, grel = attention_backward(q, k, v, Packed(start_q, start_k, max_q, max_k, used_k), out,
+                                              AttentionSaved(lse, residue), g.contiguous(), causal, scale, rel)
+        return gq, gk, gv, grel, None, None, None, None
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Packed, causal: bool = False,
+              scale: Optional[float] = None, rel: Optional[RelativeBias] = None) -> torch.Tensor:
+    """``attention_forward``'s result, differentiable in q, k, v and the bias's weight."""
+    return Attention.apply(q, k, v, None if rel is None else rel.weight, None if rel is None else rel.bucket, seqs,
+                           bool(causal), scale)
