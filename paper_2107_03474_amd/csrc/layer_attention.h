@@ -5,8 +5,9 @@
 //     z_ij = c q_i . k_j + t_h(j - i - off),  c = scale log2 e,  t_h the bias by distance, times log2 e
 //     p_ij = 2^(z_ij - m_i) / l_i,  o_i = sum_j p_ij v_j,  lse_i = m_i + log2 l_i
 //
-// The G = heads / kv_heads query heads that share a key head are rows of one matrix: packed row r of a sequence is query
-// r / G of the group's head r % G, so a few queries fill a tile, and a tile meets a key once for all G heads.
+// The heads / kv_heads query heads that share a key head are rows of one matrix: with G = heads / kv_heads, packed row r of a
+// sequence is query r / G of head r % G of the group, so a few queries fill a tile, and a tile meets a key once for all
+// G heads.  Row tiles of prompts with a bias keep to one head (G = 1): its rows' distances to a key are consecutive.
 //
 // Tiles.  Products run on the matrix cores as 32 x 32 blocks with K = 16 (fp32: eight steps of K = 2).  A lane's operand is
 // 8 elements: A row (lane & 31), k = 8 (lane >> 5) .. + 7, B column the same; a result's lane holds column lane & 31,
@@ -33,7 +34,6 @@ using s16x4 = short __attribute__((ext_vector_type(4)));
 using Lds = __attribute__((address_space(3))) char*;
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int XCDS = 8;
 constexpr int ROWS = 32;     // packed rows (or keys) of a wave
 constexpr int KEYS = 64;     // keys of a tile in LDS
 constexpr int WAVES = 4, THREADS = WAVES * WAVE;
@@ -47,7 +47,9 @@ struct Args {
   const void* rel_weight;
   const int32_t* rel_bucket;
   int64_t tq, tk;
-  int32_t heads, kv_heads, group, batch;
+  int32_t heads, kv_heads, batch;
+  int32_t ratio;  // heads of a key head
+  int32_t group;  // of them, those packed in a tile: ratio or 1
   int32_t causal, buckets, reach;
   int32_t rel_bf16;
   int32_t slots;   // row (or key) tiles of all sequences, some of them empty
@@ -98,14 +100,18 @@ __device__ __forceinline__ int slot_sequence(const int32_t* start, int64_t rows,
   return lo;
 }
 
-// Work item of a workgroup: workgroups go round the 8 dies in turn, and each die takes one contiguous range of items, so
-// that the tiles that read the same keys (or rows) share an L2.  -1: none.
-__device__ __forceinline__ int64_t work_item(int64_t total) {
-  const int64_t per = (total + XCDS - 1) / XCDS;
-  const int64_t w = (int64_t)(blockIdx.x % XCDS) * per + blockIdx.x / XCDS;
-  return blockIdx.x / XCDS < per && w < total ? w : -1;
+// Workgroups go round the 8 dies in turn, and neighbours in the grid are different heads: with 8 key heads, or a divisor or
+// multiple of 8, the tiles that read the same keys run on the same die and share its L2, and every die gets long and
+// short tiles alike.  Packed head n (of heads / group) of the grid's order:
+struct Heads {
+  int kv, first;  // key head, first query head
+};
+__device__ __forceinline__ Heads heads_of(const Args& a, int n) {
+  Heads h;
+  h.kv = n % a.kv_heads;
+  h.first = h.kv * a.ratio + n / a.kv_heads * a.group;
+  return h;
 }
-inline unsigned work_grid(int64_t total) { return (unsigned)((total + XCDS - 1) / XCDS * XCDS); }
 
 template <typename T>
 struct Frag;
@@ -173,54 +179,34 @@ struct Tile {
     return b2 << 3 | b0 << 2 | b1 << 1 | b3;
   }
 
-  // Addresses of a lane's operands, made once: A or B rows (row = the lane's row of the first block, the same for blocks
-  // at a multiple of 16 rows further on).
-  struct RowAddr {
-    uint32_t at[STEPS][sizeof(T) / 2];
-  };
-  static __device__ __forceinline__ RowAddr row_addr(int row) {
-    RowAddr r;
+  // A lane's operand addresses are a base and, since the swizzle is linear in the row's bits, an XOR with a constant.
+  // Row operand: 8 elements of the lane's row, k = 16 s + 8 h ..., of the block that starts at first_row (a multiple of 16).
+  static __device__ __forceinline__ uint32_t row_base(int row) {
     const int h = threadIdx.x >> 5 & 1;
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-        r.at[s][i] = row * ROW + (((16 * s + 8 * h) / PER + i) ^ swizzle(row)) * 16;
-    return r;
+    return row * ROW + (8 * h / PER ^ swizzle(row)) * 16;
   }
-  // Row operand: 8 elements of the lane's row, k = 16 s + 8 h ...
-  static __device__ __forceinline__ F row_frag(Lds tile, const RowAddr& a, int s, int first_row) {
+  static __device__ __forceinline__ F row_frag(Lds tile, uint32_t base, int s, int first_row) {
     if constexpr (sizeof(T) == 2) {
-      return *(const __attribute__((address_space(3))) bf16x8*)(tile + a.at[s][0] + first_row * ROW);
+      return *(const __attribute__((address_space(3))) bf16x8*)(tile + (base ^ s * 32) + first_row * ROW);
     } else {
-      const f32x4 x = *(const __attribute__((address_space(3))) f32x4*)(tile + a.at[s][0] + first_row * ROW);
-      const f32x4 y = *(const __attribute__((address_space(3))) f32x4*)(tile + a.at[s][1] + first_row * ROW);
+      const f32x4 x = *(const __attribute__((address_space(3))) f32x4*)(tile + (base ^ s * 64) + first_row * ROW);
+      const f32x4 y = *(const __attribute__((address_space(3))) f32x4*)(tile + (base ^ (s * 64 + 16)) + first_row * ROW);
       return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
 
   // Column operand: column d = 32 block + (lane & 31) of the transposed tile, rows 16 c + (4 h + 0..3, 8 + 4 h + 0..3).
-  struct ColAddr {
-    uint32_t at[BLOCKS][2];
-  };
-  static __device__ __forceinline__ ColAddr col_addr() {
-    ColAddr r;
+  static __device__ __forceinline__ uint32_t col_base() {
     const int l = threadIdx.x & 63, h = l >> 5;
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if constexpr (sizeof(T) == 2) {  // the transposing read: 16 lanes take 4 rows of 16 columns
-          const int row = 8 * u + 4 * h + (l >> 2 & 3), d = 32 * b + (l & 16) + 4 * (l & 3);
-          r.at[b][u] = row * ROW + (d / PER ^ swizzle(row)) * 16 + d % PER * 2;
-        } else {  // the first of the 4 rows; the others differ in the low bits of the swizzle
-          const int row = 8 * u + 4 * h, d = 32 * b + (l & 31);
-          r.at[b][u] = row * ROW + (d / PER ^ swizzle(row)) * 16 + d % PER * 4;
-        }
-      }
-    return r;
+    if constexpr (sizeof(T) == 2) {  // the transposing read: 16 lanes take 4 rows of 16 columns
+      const int row = 4 * h + (l >> 2 & 3), d = (l & 16) + 4 * (l & 3);
+      return row * ROW + (d / PER ^ swizzle(row)) * 16 + d % PER * 2;
+    } else {
+      const int row = 4 * h, d = l & 31;
+      return row * ROW + (d / PER ^ swizzle(row)) * 16 + d % PER * 4;
+    }
   }
-  static __device__ __forceinline__ F col_frag(Lds tile, const ColAddr& a, int block, int c) {
+  static __device__ __forceinline__ F col_frag(Lds tile, uint32_t base, int block, int c) {
     if constexpr (sizeof(T) == 2) {
       union {
         s16x4 s[2];
@@ -228,18 +214,17 @@ struct Tile {
       } u;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        u.s[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(tile + a.at[block][i] + 16 * c * ROW));
+        u.s[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(
+            tile + (base ^ (32 * block / PER ^ swizzle(8 * i)) * 16) + (16 * c + 8 * i) * ROW));
       return u.f;
     } else {
       f32x8 f;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t at = (a.at[block][i] + e * ROW) ^ (uint32_t)(swizzle(e) * 16);
-          f[4 * i + e] = *(const __attribute__((address_space(3))) float*)(tile + at + 16 * c * ROW);
-        }
+        for (int e = 0; e < 4; ++e)
+          f[4 * i + e] = *(const __attribute__((address_space(3))) float*)(
+              tile + (base ^ (32 * block / PER ^ swizzle(8 * i + e)) * 16) + (16 * c + 8 * i + e) * ROW);
       return f;
     }
   }
@@ -288,9 +273,9 @@ __device__ __forceinline__ int bucket_of(const Args& a, int d) {
   const int b = a.rel_bucket[d + a.reach];
   return b < 0 ? 0 : (b < a.buckets ? b : a.buckets - 1);  // device data: nothing outside the weights is addressed
 }
-__device__ __forceinline__ void fill_bias(const Args& a, int first_head, float* table, int threads) {
+__device__ __forceinline__ void fill_bias(const Args& a, int first_head, int heads, float* table) {
   const int n = bias_width(a);
-  for (int i = threadIdx.x; i < a.group * n; i += threads)
+  for (int i = threadIdx.x; i < heads * n; i += THREADS)
     table[i] = rel_weight(a, first_head + i / n, bucket_of(a, i % n - a.reach - BIAS_PAD)) * LOG2E;
 }
 
@@ -333,21 +318,19 @@ __device__ __forceinline__ void load_query(const Args& a, const T* base, int64_t
   }
 }
 
-// The tile of a workgroup: sequence, first packed row, key range (find_work: false for an empty slot, slot = -1 for no slot
-// at all).
+// The tile of a workgroup: sequence, first packed row, key range (find_work: false for an empty slot).  The grid
+// is slots x splits x packed heads, the last fastest.
 struct Work {
   Seq s;
-  int hk, slot, row0, split, kbeg, kend;
+  Heads head;
+  int slot, row0, split, kbeg, kend;
 };
 template <int M>
 __device__ __forceinline__ bool find_work(const Args& a, Work* w) {
-  w->slot = -1;
-  const int64_t item = work_item((int64_t)a.kv_heads * a.slots * a.splits);
-  if (item < 0) return false;
-  w->hk = (int)(item / ((int64_t)a.slots * a.splits));
-  const int rest = (int)(item % ((int64_t)a.slots * a.splits));
-  w->split = rest % a.splits;
-  const int slot = w->slot = a.slots - 1 - rest / a.splits;  // long causal rows first
+  const unsigned n = a.heads / a.group;
+  w->head = heads_of(a, blockIdx.x % n);
+  w->split = blockIdx.x / n % a.splits;
+  const int slot = w->slot = a.slots - 1 - (int)(blockIdx.x / n / a.splits);  // long causal rows first
   const int b = slot_sequence(a.start_q, a.tq, a.batch, a.group, M, slot);
   w->s = sequence(a, b);
   const int64_t row0 = (slot - first_slot(a.start_q, a.tq, b, a.group, M)) * M;
@@ -390,7 +373,7 @@ int check_attention(const lram_attention& a, bool pointers) {
   if (a.tq < 0 || a.tk < 0 || a.tk > INT32_MAX || a.tq > (1 << 30) / G || a.max_q < 0 || a.max_k < 0)
     return LRAM_EINVAL;
   // work items of every kernel (at most 64 pieces of tiles of 32 rows) stay below 2^31 workgroups of 256 threads
-  if (a.kv_heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 1) > (int64_t(1) << 24) - 16) return LRAM_EINVAL;
+  if (a.heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 1) > (int64_t(1) << 24)) return LRAM_EINVAL;
   if (a.rel_weight) {
     if (a.wdtype != LRAM_F32 && !(a.wdtype == LRAM_BF16 && a.dtype == LRAM_BF16)) return LRAM_EDTYPE;
     if (!a.rel_bucket || a.rel_buckets < 1 || a.rel_buckets > 1024 || a.rel_reach < 0 || a.rel_reach > 4096 ||
@@ -418,7 +401,7 @@ Args args_of(const lram_attention& a) {
   x.start_q = a.start_q, x.start_k = a.start_k, x.used_k = a.used_k;
   x.rel_weight = a.rel_weight, x.rel_bucket = a.rel_bucket;
   x.tq = a.tq, x.tk = a.tk;
-  x.heads = a.heads, x.kv_heads = a.kv_heads, x.group = a.heads / a.kv_heads, x.batch = a.batch;
+  x.heads = a.heads, x.kv_heads = a.kv_heads, x.ratio = x.group = a.heads / a.kv_heads, x.batch = a.batch;
   x.causal = a.causal, x.buckets = a.rel_buckets, x.reach = a.rel_reach, x.rel_bf16 = a.wdtype == LRAM_BF16;
   x.scale = a.scale;
   x.c = a.scale * LOG2E;

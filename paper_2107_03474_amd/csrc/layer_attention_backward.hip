@@ -9,20 +9,47 @@
 // the packed rows, the G heads of its group among them.  Seven products instead of the five of a single kernel, whose dq
 // would be added up in memory by atomics, in an order that varies.  p and ds are rounded to the operands' type.
 //
-// The bias's gradient: k_attention_dq adds ds by distance in LDS, one table to a wave, the two halves of the wave one
-// after the other (inside a half no two lanes meet in an entry, so the order is fixed); tiles past reach go into a
+// The bias's gradient: k_attention_dq adds up the diagonals of its 32 x 32 blocks of ds.  Rows are lanes and keys registers, so
+// a sum that moves on by one lane with every key collects a diagonal in a lane (diagonals); 8 keys' sums then go to the
+// wave's own table in LDS (one instruction, no two lanes in an entry: the order is fixed).  Blocks past reach go into a
 // register.  A workgroup leaves one row of sums by distance, and k_relative_grad adds the rows and gathers the buckets.
 
 #include "layer_attention.h"
 
 namespace {
 
+// The value of the lane before, going round the wave.
+__device__ __forceinline__ float next_lane(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x13c, 0xf, 0xf, false));
+}
+
 struct Grads {
   const void *out, *residue, *grad_out;
   const float* lse;
   void *gq, *gk, *gv, *grel;
-  float *delta, *rel;  // workspace: [tq heads], [slots][heads][2 reach + 1]
+  float *delta, *rel, *part;  // workspace: [tq heads], [slots][heads][2 reach + 1], [pieces][tk][kv_heads][2][D]
 };
+
+// Eight keys of 32 rows (a row to a lane, key 4 h + e in argument e) summed along the diagonals: lane p < 39 of the result
+// holds the sum over lane c's key k with c + 7 - k = p.
+__device__ __forceinline__ float diagonals(float k0, float k1, float k2, float k3) {
+  const float keys[4] = {k0, k1, k2, k3};
+  float half[2] = {0, 0};  // keys 0..3 and 4..7: the lower and the upper half's lanes, each with zeros beside them
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, keys[e]), 0, false, false);
+    const unsigned lower = r[0], upper = r[1];
+    if (e) {
+      half[0] = next_lane(half[0]);
+      half[1] = next_lane(half[1]);
+    }
+    half[0] += __builtin_bit_cast(float, lower);
+    half[1] += __builtin_bit_cast(float, upper);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) half[0] = next_lane(half[0]);
+  return half[0] + half[1];
+}
 
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention_dq(Args a, Grads o) {
@@ -32,21 +59,16 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   extern __shared__ __attribute__((aligned(256))) char smem[];
   Lds lds = (Lds)smem;
   Work w;
-  const bool found = find_work<M>(a, &w);
-  if constexpr (BIAS) {
-    if (!found) {  // an empty slot's sums are zero
-      if (w.slot >= 0)
-        for (int t = threadIdx.x; t < a.group * (2 * a.reach + 1); t += THREADS)
-          o.rel[((int64_t)w.slot * a.heads + w.hk * a.group) * (2 * a.reach + 1) + t] = 0;
-      return;
-    }
-  } else {
-    if (!found) return;
+  if (!find_work<M>(a, &w)) {
+    if constexpr (BIAS)  // an empty slot's sums are zero
+      for (int t = threadIdx.x; t < 2 * a.reach + 1; t += THREADS)
+        o.rel[((int64_t)w.slot * a.heads + w.head.first) * (2 * a.reach + 1) + t] = 0;
+    return;
   }
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
   const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, first + (l & 31));
-  const int head = w.hk * G + r.g;
+  const int head = w.head.first + r.g;
   const int64_t at = (w.s.q0 + r.i) * a.heads + head;
   F q[D / 16], g[D / 16];
   load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
@@ -76,31 +98,29 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const int i_first = first / G, i_last = (min(first + ROWS, rows) - 1) / G;
   const int lim_first = a.causal ? min(i_first + off, w.s.nk - 1) : w.s.nk - 1;
   const int lim_last = first >= rows ? -1 : (a.causal ? min(i_last + off, w.s.nk - 1) : w.s.nk - 1);
+  // with a bias G = 1: the lane's row is query i of one head
   const float* bias = nullptr;
-  float* hist = nullptr;  // the wave's table of sums, at the lane's row as `bias` is
-  float near_far[2] = {0, 0}, far_sum[2] = {0, 0};
+  float far_bias[2] = {0, 0}, far_sum[2] = {0, 0};
   const int width = bias_width(a);
   float* const table = (float*)(smem + 4 * BYTES);
-  float* const sums = table + G * width;  // [WAVES][G][width]
+  float* const sums = table + width;         // [WAVES][width]
+  float* const mine = sums + wave * width;
   if constexpr (BIAS) {
-    fill_bias(a, w.hk * G, table, THREADS);
-    for (int t = threadIdx.x; t < WAVES * G * width; t += THREADS) sums[t] = 0;
-    const int shift = a.reach + BIAS_PAD - (r.i + off), gi = r.valid ? r.g : 0;
-    bias = table + r.g * width + shift;
-    hist = sums + (wave * G + r.g) * width + shift;
+    fill_bias(a, w.head.first, 1, table);
+    for (int t = threadIdx.x; t < WAVES * width; t += THREADS) sums[t] = 0;
+    bias = table + a.reach + BIAS_PAD - (r.i + off);
     __syncthreads();
-    near_far[0] = table[gi * width];
-    near_far[1] = table[gi * width + width - 1];
+    far_bias[0] = table[0];
+    far_bias[1] = table[width - 1];
   }
-  const typename Ti::RowAddr ka = Ti::row_addr(l & 31);
-  const typename Ti::ColAddr ca = Ti::col_addr();
+  const uint32_t ka = Ti::row_base(l & 31), ca = Ti::col_base();
   f32x16 acc[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[b][e] = 0;
-  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.hk * a.k_head;
-  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.hk * a.v_head;
+  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.head.kv * a.k_head;
+  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.head.kv * a.v_head;
   auto load = [&](int j0, int buf) {
     load_rows<T, D, KEYS, WAVES>(kh, a.k_row, j0, w.s.nk, lds + buf * 2 * BYTES, wave);
     load_rows<T, D, KEYS, WAVES>(vh, a.v_row, j0, w.s.nk, lds + buf * 2 * BYTES + BYTES, wave);
@@ -128,7 +148,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       if constexpr (BIAS) {
         above = j - (i_last + off) >= a.reach;
         whole = above || j + 31 - (i_first + off) <= -a.reach;
-        far = near_far[above];
+        far = far_bias[above];
       }
       if (whole) {
 #pragma unroll
@@ -154,15 +174,13 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
           far_sum[0] += above ? 0.0f : sum;
           far_sum[1] += above ? sum : 0.0f;
         } else {
-          float* t = hist + j + 4 * h;
+          // entry of distance (j + 8 u) - (first + off), and lane p holds the distance 7 - p more
+          float* const t = mine + a.reach + BIAS_PAD + j - (first + off) + 7 - l;
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            asm volatile("" ::: "memory");  // one half of the wave, then the other
-            if (r.valid && h == half)
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                __hip_atomic_fetch_add(t + 8 * (e >> 2) + (e & 3), s[e], __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_WORKGROUP);
+          for (int u = 0; u < 4; ++u) {
+            const float sum = diagonals(s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]);
+            if (l < 39)
+              __hip_atomic_fetch_add(t + 8 * u, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
           }
         }
       }
@@ -190,36 +208,29 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       }
   }
   if constexpr (BIAS) {
-    // the waves' tables added up, then the entries past reach, with the far tiles' sums, into the last one's
+    // the waves' tables added up, then the entries past reach, with the far blocks' sums, into the last one's
     __syncthreads();
-    for (int t = threadIdx.x; t < G * width; t += THREADS) {
+    for (int t = threadIdx.x; t < width; t += THREADS) {
       float x = 0;
 #pragma unroll
-      for (int v = 0; v < WAVES; ++v) x += sums[v * G * width + t];
+      for (int v = 0; v < WAVES; ++v) x += sums[v * width + t];
       sums[t] = x;
     }
-    float* const lane = (float*)smem;  // [2][THREADS]; the tiles are done with
-    lane[threadIdx.x] = far_sum[0];
-    lane[THREADS + threadIdx.x] = far_sum[1];
-    __syncthreads();
-    const int n = 2 * a.reach + 1;
-    float* const row = o.rel + ((int64_t)w.slot * a.heads + w.hk * G) * n;
-    for (int t = threadIdx.x; t < G * n; t += THREADS) {
-      const int gi = t / n, d = t % n;
-      if (d > 0 && d < n - 1) row[t] = sums[gi * width + BIAS_PAD + d];
+    float* const far = (float*)smem;  // [2][WAVES]; the tiles are done with
+    const float below = wave_sum(far_sum[0]), above = wave_sum(far_sum[1]);
+    if (l == 0) {
+      far[wave] = below;
+      far[WAVES + wave] = above;
     }
-    for (int t = wave; t < 2 * G; t += WAVES) {
-      const int gi = t / 2, side = t % 2;
-      if (a.reach == 0 && side) continue;  // one entry in all
-      float x = 0;
-      for (int e = l; e < THREADS; e += WAVE) {
-        const int lr = w.row0 + e / WAVE * ROWS + (e & 31);
-        if (lr % G == gi) x += lane[side * THREADS + e] + (a.reach == 0 ? lane[THREADS + e] : 0.0f);
-      }
-      const int entries = a.reach == 0 ? width : BIAS_PAD + 1;
-      for (int e = l; e < entries; e += WAVE) x += sums[gi * width + (side ? width - entries : 0) + e];
+    __syncthreads();
+    const int n = 2 * a.reach + 1, ends = a.reach == 0 ? width : BIAS_PAD + 1;
+    float* const row = o.rel + ((int64_t)w.slot * a.heads + head) * n;
+    for (int t = 1 + threadIdx.x; t < n - 1; t += THREADS) row[t] = sums[BIAS_PAD + t];
+    if (wave < 2 && wave < n) {  // reach 0: one entry in all
+      float x = l < WAVES ? far[wave * WAVES + l] + (n == 1 ? far[WAVES + l] : 0.0f) : 0.0f;
+      for (int e = l; e < ends; e += WAVE) x += sums[(wave ? width - ends : 0) + e];
       x = wave_sum(x);
-      if (l == 0) row[gi * n + (side ? n - 1 : 0)] = x;
+      if (l == 0) row[wave ? n - 1 : 0] = x;
     }
   }
 }
@@ -232,36 +243,72 @@ __device__ __forceinline__ void dma16_from(const void* src, Lds dst) {
                : "memory");
 }
 
-constexpr int TROWS = 64;  // packed rows of a tile in k_attention_dkv
+// k_attention_dkv: a wave's 32 keys stay in registers, and so do their values while a row of them takes 128 bytes; longer
+// ones stay in LDS, where the tiles are then half as long.  (2 x 8,192 causal tokens, 32/8 heads of 128, bf16: values in
+// registers, tiles of 64 rows 4.28 ms with 76 registers spilled; in LDS, tiles of 32 rows 2.47 ms.  32 x 256 tokens, 8
+// heads of 64: 39 and 42 us.)
+template <typename T, int D>
+constexpr bool values_in_lds() { return Tile<T, D>::ROW >= 256; }
+template <typename T, int D>
+constexpr int tile_rows() { return values_in_lds<T, D>() ? 32 : 64; }  // packed rows
+constexpr int DKV_KEYS = WAVES * 32;
+template <typename T, int D>
+constexpr int dkv_bytes() {
+  return 4 * tile_rows<T, D>() * Tile<T, D>::ROW + (values_in_lds<T, D>() ? DKV_KEYS * Tile<T, D>::ROW : 0);
+}
+template <typename T, int D>
+constexpr int dkv_waves() { return dkv_bytes<T, D>() > 72 * 1024 ? 1 : 2; }  // a SIMD
 // What it keeps of a row: delta, lse, lse less the bias below and above reach, and where distance 0 to key 0 stands in the
 // bias table.
 enum { DELTA, LSE, BELOW, ABOVE, BASE, STATS };
 
+// The key tile of a workgroup and its piece of the packed rows.
+struct KeyWork {
+  Seq s;
+  int j0, rows, begin, end;  // begin >= end: no row of the piece meets a key of the tile
+};
+// Packed rows from first_row on see the key (causal).
+__device__ __forceinline__ int first_row(const Args& a, const Seq& s, int key) {
+  return a.causal ? max(key - (s.nk - s.nq), 0) * a.ratio : 0;
+}
+__device__ __forceinline__ bool key_work(const Args& a, int slot, int piece, KeyWork* w) {
+  const int b = slot_sequence(a.start_k, a.tk, a.batch, 1, DKV_KEYS, slot);
+  w->s = sequence(a, b);
+  const int64_t from = (slot - first_slot(a.start_k, a.tk, b, 1, DKV_KEYS)) * DKV_KEYS;
+  if (from >= w->s.cap) return false;
+  w->j0 = (int)from;
+  w->rows = w->s.nq * a.ratio;
+  w->begin = w->j0 < w->s.nk ? first_row(a, w->s, w->j0) : w->rows;
+  w->end = w->rows;
+  const int64_t lo = (int64_t)piece * a.piece, hi = lo + a.piece;
+  if (w->begin < lo) w->begin = (int)(lo < w->rows ? lo : w->rows);
+  if (piece < a.splits - 1 && hi < w->end) w->end = (int)hi;
+  return true;
+}
+
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention_dkv(Args a, Grads o) {
+__global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(Args a, Grads o) {
   using Ti = Tile<T, D>;
   using F = typename Frag<T>::type;
-  constexpr int N = WAVES * 32, BYTES = TROWS * Ti::ROW, LOADS = TROWS * Ti::CH / 64 / WAVES;
+  constexpr int TROWS = tile_rows<T, D>(), BYTES = TROWS * Ti::ROW, LOADS = TROWS * Ti::CH / 64 / WAVES;
+  constexpr bool VLDS = values_in_lds<T, D>();
   extern __shared__ __attribute__((aligned(256))) char smem[];
   Lds lds = (Lds)smem;
-  const int64_t item = work_item((int64_t)a.kv_heads * a.slots);
-  if (item < 0) return;
-  const int hk = (int)(item / a.slots), slot = (int)(item % a.slots);
-  const int b = slot_sequence(a.start_k, a.tk, a.batch, 1, N, slot);
-  const Seq s = sequence(a, b);
-  const int64_t from = (slot - first_slot(a.start_k, a.tk, b, 1, N)) * N;
-  if (from >= s.cap) return;
-  const int j0 = (int)from;
+  const int hk = blockIdx.x % a.kv_heads, piece = blockIdx.x / a.kv_heads % a.splits;
+  const int slot = blockIdx.x / a.kv_heads / a.splits;  // the first keys, which most rows see, first
+  KeyWork w;
+  if (!key_work(a, slot, piece, &w)) return;
+  if (a.splits > 1 && w.begin >= w.end) return;  // k_attention_dkv_join leaves it out
+  const Seq& s = w.s;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
-  const int G = a.group, off = s.nk - s.nq, rows = s.nq * G;
-  const int jw = j0 + 32 * wave, j = jw + (l & 31);
+  const int G = a.ratio, off = s.nk - s.nq, rows = w.rows;
+  const int jw = w.j0 + 32 * wave, j = jw + (l & 31);
   const bool valid = j < s.nk;
-  // keys from row_of_key on see the lane's key (causal)
-  const auto first_row = [&](int key) { return a.causal ? max(key - off, 0) * G : 0; };
-  const int seen_from = first_row(j);
-  const int begin = j0 < s.nk ? first_row(j0) : rows;
-
-  F k[D / 16], v[D / 16];
+  const int seen_from = first_row(a, s, j), wave_from = first_row(a, s, jw), wave_all = first_row(a, s, jw + 31);
+  F k[D / 16], v[VLDS ? 1 : D / 16];
+  const Lds vt = lds + 4 * BYTES;
+  if (VLDS && w.begin < w.end)
+    load_rows<T, D, DKV_KEYS, WAVES>((const T*)a.v + s.k0 * a.v_row + hk * a.v_head, a.v_row, w.j0, s.nk, vt, wave);
   {
     const T* kp = (const T*)a.k + (s.k0 + j) * a.k_row + hk * a.k_head + 8 * h;
     const T* vp = (const T*)a.v + (s.k0 + j) * a.v_row + hk * a.v_head + 8 * h;
@@ -269,19 +316,18 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
     for (int t = 0; t < D / 16; ++t) {
       F z = {};
       k[t] = valid ? *(const F*)(kp + 16 * t) : z;
-      v[t] = valid ? *(const F*)(vp + 16 * t) : z;
+      if constexpr (!VLDS) v[t] = valid ? *(const F*)(vp + 16 * t) : z;
     }
   }
   // beside the tiles: [2][STATS][TROWS], then the bias table
-  float* const stats = (float*)(smem + 4 * BYTES);
+  float* const stats = (float*)(smem + dkv_bytes<T, D>());
   float* const table = stats + 2 * STATS * TROWS;
   const int width = bias_width(a);
   if constexpr (BIAS) {
-    fill_bias(a, hk * G, table, THREADS);
+    fill_bias(a, hk * G, G, table);
     __syncthreads();
   }
-  const typename Ti::RowAddr ra = Ti::row_addr(l & 31);
-  const typename Ti::ColAddr ca = Ti::col_addr();
+  uint32_t ra = Ti::row_base(l & 31), ca = Ti::col_base();
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int t = 0; t < D / 32; ++t)
@@ -314,12 +360,12 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
     }
   };
   // A tile's statistics, a row to a thread of the first wave: loaded with the tile before, written when it is done.
-  // A row past the last one gets lse = inf, and with it p = 0.
+  // A row past the piece's last one gets lse = inf, and with it p = 0.
   float st_lse = 0, st_delta = 0;
   const auto load_stats = [&](int r0) {
     int i, g;
     split_row(r0, r0 / G, l, &i, &g);
-    st_lse = r0 + l < rows ? lse_h[(int64_t)i * a.heads + g] : INFINITY;
+    st_lse = r0 + l < w.end ? lse_h[(int64_t)i * a.heads + g] : INFINITY;
     st_delta = delta_h[(int64_t)i * a.heads + g];
   };
   const auto put_stats = [&](int r0, int buf) {
@@ -334,28 +380,30 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       ((int*)to)[BASE * TROWS] = g * width + a.reach + BIAS_PAD - (i + off);
     }
   };
-  if (begin < rows) {
-    load(begin, 0);
-    if (wave == 0) {
-      load_stats(begin);
-      put_stats(begin, 0);
+  const bool keeper = wave == 0 && l < TROWS;
+  if (w.begin < w.end) {
+    load(w.begin, 0);
+    if (keeper) {
+      load_stats(w.begin);
+      put_stats(w.begin, 0);
     }
   }
   int buf = 0;
-  for (int r0 = begin; r0 < rows; r0 += TROWS, buf ^= 1) {
+  for (int r0 = w.begin; r0 < w.end; r0 += TROWS, buf ^= 1) {
     loads_done();
     __syncthreads();
-    const bool more = r0 + TROWS < rows;
+    const bool more = r0 + TROWS < w.end;
     if (more) {
       load(r0 + TROWS, buf ^ 1);
-      if (wave == 0) load_stats(r0 + TROWS);
+      if (keeper) load_stats(r0 + TROWS);
     }
+    asm volatile("" : "+v"(ra), "+v"(ca));  // the addresses are formed at their use: kept, they would not fit the registers
     const Lds qt = lds + buf * 2 * BYTES, gt = qt + BYTES;
     const float* const st = stats + buf * STATS * TROWS + 4 * h;
 #pragma unroll
     for (int rb = 0; rb < TROWS / 32; ++rb) {
       // rows that none of the wave's keys meets
-      if (jw >= s.nk || r0 + 32 * rb + 31 < first_row(jw) || r0 + 32 * rb >= rows) continue;
+      if (jw >= s.nk || r0 + 32 * rb + 31 < wave_from || r0 + 32 * rb >= w.end) continue;
       int use = LSE;  // past reach one value of a row's bias serves the whole block, and is in the row's statistic
       if constexpr (BIAS) {
         const int i_first = (r0 + 32 * rb) / G, i_last = (min(r0 + 32 * rb + 32, rows) - 1) / G;
@@ -369,7 +417,12 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
 #pragma unroll
       for (int t = 0; t < D / 16; ++t) p = mma(Ti::row_frag(qt, ra, t, 32 * rb), k[t], p);
 #pragma unroll
-      for (int t = 0; t < D / 16; ++t) ds = mma(Ti::row_frag(gt, ra, t, 32 * rb), v[t], ds);
+      for (int t = 0; t < D / 16; ++t) {
+        if constexpr (VLDS)
+          ds = mma(Ti::row_frag(gt, ra, t, 32 * rb), Ti::row_frag(vt, ra, t, 32 * wave), ds);
+        else
+          ds = mma(Ti::row_frag(gt, ra, t, 32 * rb), v[t], ds);
+      }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const f32x4 lse = *(const f32x4*)(st + use * TROWS + 32 * rb + 8 * u);
@@ -387,7 +440,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
 #pragma unroll
         for (int e = 0; e < 4; ++e) ds[4 * u + e] = p[4 * u + e] * (ds[4 * u + e] - delta[e]);
       }
-      if (a.causal && r0 + 32 * rb < first_row(jw + 31)) {
+      if (r0 + 32 * rb < wave_all) {
         const int need = seen_from - (r0 + 32 * rb) - 4 * h;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -411,7 +464,25 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
         for (int t = 0; t < D / 32; ++t) dk[t] = mma(Ti::col_frag(qt, ca, t, 2 * rb + c), fy, dk[t]);
       }
     }
-    if (more && wave == 0) put_stats(r0 + TROWS, buf ^ 1);
+    if (more && keeper) put_stats(r0 + TROWS, buf ^ 1);
+  }
+  if (a.splits > 1) {
+    if (j >= s.nk) return;
+    float* const to = o.part + (((int64_t)piece * a.tk + s.k0 + j) * a.kv_heads + hk) * 2 * D + 4 * h;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        f32x4 x, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = dk[t][4 * u + e] * a.scale;
+          y[e] = dv[t][4 * u + e];
+        }
+        *(f32x4*)(to + 32 * t + 8 * u) = x;
+        *(f32x4*)(to + D + 32 * t + 8 * u) = y;
+      }
+    return;
   }
   if (j >= s.cap) return;
   const int64_t at = ((s.k0 + j) * a.kv_heads + hk) * D + 4 * h;
@@ -428,6 +499,36 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       store4<T>((T*)o.gk + at + 32 * t + 8 * u, x);
       store4<T>((T*)o.gv + at + 32 * t + 8 * u, y);
     }
+}
+
+// The pieces of a key tile's gradients added up, in their order; a workgroup to a tile and key head.
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o) {
+  const int hk = blockIdx.x % a.kv_heads, slot = blockIdx.x / a.kv_heads;
+  KeyWork w;
+  if (!key_work(a, slot, 0, &w)) return;
+  int used[2] = {a.splits, 0};  // pieces with rows for the tile: one range
+  for (int p = 0; p < a.splits; ++p) {
+    KeyWork x;
+    key_work(a, slot, p, &x);
+    if (x.begin < x.end) {
+      used[0] = min(used[0], p);
+      used[1] = p + 1;
+    }
+  }
+  const int keys = min(DKV_KEYS, w.s.cap - w.j0);
+  for (int t = threadIdx.x; t < keys * (2 * D / 4); t += THREADS) {
+    const int j = w.j0 + t / (2 * D / 4), d = t % (2 * D / 4) * 4;
+    const int64_t at = (w.s.k0 + j) * a.kv_heads + hk;
+    f32x4 x = {0, 0, 0, 0};
+    if (j < w.s.nk)
+      for (int p = used[0]; p < used[1]; ++p) {
+        const f32x4 y = *(const f32x4*)(o.part + ((int64_t)p * a.tk * a.kv_heads + at) * 2 * D + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += y[e];
+      }
+    store4<T>((d < D ? (T*)o.gk + d : (T*)o.gv + d - D) + at * D, x);
+  }
 }
 
 // A head's sums by distance over all slots, and its buckets' from them; a workgroup to a head.
@@ -462,41 +563,57 @@ __global__ __launch_bounds__(REL_THREADS) void k_relative_grad(Args a, const flo
   }
 }
 
-int row_slots(const lram_attention& a) {
-  return (int)(a.tq * (a.heads / a.kv_heads) / (WAVES * ROWS) + a.batch + 1);
-}
-
-struct Space {
-  size_t delta, rel, total;  // floats
+// How the two kernels divide the work.  Packed rows come in pieces where the key tiles are few against the chip (about
+// four workgroups a CU are wanted), none shorter than 1,024 rows.
+struct Plan {
+  int group, row_slots, key_slots, pieces, piece;
+  size_t delta, rel, part;  // floats of workspace
 };
-Space space_of(const lram_attention& a) {
-  Space s;
-  s.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
-  s.rel = a.rel_weight ? (size_t)row_slots(a) * a.heads * (2 * a.rel_reach + 1) : 0;
-  s.total = s.delta + s.rel;
-  return s;
+Plan plan_of(const lram_attention& a) {
+  Plan p;
+  const int64_t G = a.heads / a.kv_heads;
+  p.group = a.rel_weight ? 1 : (int)G;
+  p.row_slots = (int)(a.tq * p.group / (WAVES * ROWS) + a.batch + 1);
+  p.key_slots = (int)(a.tk / DKV_KEYS + a.batch + 1);
+  const int64_t tiles = std::min<int64_t>((int64_t)a.batch * ((a.max_k + DKV_KEYS - 1) / DKV_KEYS), p.key_slots);
+  const int64_t rows = a.max_q * G;
+  int64_t pieces = tiles > 0 ? 1024 / (tiles * a.kv_heads) : 1;
+  pieces = std::max<int64_t>(1, std::min<int64_t>({pieces, (rows + 1023) / 1024, 16}));
+  p.piece = (int)std::min<int64_t>((rows / pieces + 64) / 64 * 64, 1 << 30);
+  p.pieces = (int)std::max<int64_t>(1, std::min(pieces, (rows + p.piece - 1) / p.piece));
+  p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
+  p.rel = a.rel_weight ? ((size_t)p.row_slots * a.heads * (2 * a.rel_reach + 1) + 3) / 4 * 4 : 0;
+  p.part = p.pieces > 1 ? (size_t)p.pieces * a.tk * a.kv_heads * 2 * a.head_dim : 0;
+  return p;
 }
 
 template <typename T, int D, bool BIAS>
-int go(Args x, const Grads& g, const lram_attention& d, hipStream_t s) {
-  const size_t table = BIAS ? (size_t)x.group * (2 * (x.reach + BIAS_PAD) + 1) * 4 : 0;
-  const size_t tiles = (size_t)4 * KEYS * Tile<T, D>::ROW;
-  const auto launch = [&](auto kernel, size_t bytes) {
+int go(Args x, const Grads& g, const lram_attention& d, const Plan& p, hipStream_t s) {
+  const size_t width = BIAS ? (size_t)(2 * (x.reach + BIAS_PAD) + 1) * 4 : 0;
+  const auto launch = [&](auto kernel, int64_t grid, size_t bytes) {
     if (int rc = allow_lds((const void*)kernel, bytes)) return rc;
-    hipLaunchKernelGGL(kernel, dim3(work_grid((int64_t)x.kv_heads * x.slots)), dim3(THREADS), bytes, s, x, g);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(THREADS), bytes, s, x, g);
     return layer_launched();
   };
   if (x.tq) {
-    x.slots = row_slots(d);
-    if (int rc = launch(k_attention_dq<T, D, BIAS>, tiles + table * (1 + WAVES))) return rc;
+    x.group = p.group;
+    x.slots = p.row_slots;
+    if (int rc = launch(k_attention_dq<T, D, BIAS>, (int64_t)(x.heads / x.group) * x.slots,
+                        (size_t)4 * KEYS * Tile<T, D>::ROW + width * (1 + WAVES)))
+      return rc;
   }
   if (x.tk) {
-    x.slots = (int)(x.tk / (WAVES * 32) + x.batch + 1);
-    static_assert(TROWS == KEYS, "the tiles' bytes");
-    if (int rc = launch(k_attention_dkv<T, D, BIAS>, tiles + 2 * STATS * TROWS * 4 + table)) return rc;
+    x.slots = p.key_slots;
+    x.splits = p.pieces;
+    x.piece = p.piece;
+    if (int rc = launch(k_attention_dkv<T, D, BIAS>, (int64_t)x.kv_heads * x.slots * x.splits,
+                        dkv_bytes<T, D>() + 2 * STATS * tile_rows<T, D>() * 4 + width * x.ratio))
+      return rc;
+    if (x.splits > 1)
+      if (int rc = launch(k_attention_dkv_join<T, D>, (int64_t)x.kv_heads * x.slots, 0)) return rc;
   }
   if constexpr (BIAS) {
-    x.slots = x.tq ? row_slots(d) : 0;
+    x.slots = x.tq ? p.row_slots : 0;
     const size_t bytes = (size_t)(2 * x.reach + 1 + REL_THREADS) * 4;
     const auto finish = [&](auto w) {
       using W = decltype(w);
@@ -516,7 +633,8 @@ extern "C" {
 int lram_attention_backward_workspace_bytes(const lram_attention* a, size_t* bytes) {
   if (!a || !bytes) return LRAM_EINVAL;
   if (int rc = check_attention(*a, false)) return rc;
-  *bytes = space_of(*a).total * 4;
+  const Plan p = plan_of(*a);
+  *bytes = (p.delta + p.rel + p.part) * 4;
   return LRAM_OK;
 }
 
@@ -533,14 +651,16 @@ int lram_attention_backward(const lram_attention* a, const void* out, const void
       off_align(grad_rel, elem_size(a->wdtype)))
     return LRAM_EINVAL;
   if (residue && a->dtype != LRAM_BF16) return LRAM_EDTYPE;
-  const Space sp = space_of(*a);
-  if (sp.total && (!workspace || off_align(workspace, 16) || ws_bytes < sp.total * 4)) return LRAM_EWORKSPACE;
+  const Plan p = plan_of(*a);
+  const size_t need = (p.delta + p.rel + p.part) * 4;
+  if (need && (!workspace || off_align(workspace, 16) || ws_bytes < need)) return LRAM_EWORKSPACE;
   Args x = args_of(*a);
   x.splits = 1;
-  const Grads g{out, residue, grad_out, lse, grad_q, grad_k, grad_v, grad_rel, (float*)workspace,
-                (float*)workspace + sp.delta};
+  float* const ws = (float*)workspace;
+  const Grads g{out, residue, grad_out, lse, grad_q, grad_k, grad_v, grad_rel, ws, ws + p.delta,
+                ws + p.delta + p.rel};
   return by_kind(*a, [&](auto t, auto d, auto bias) {
-    return go<decltype(t), decltype(d)::value, decltype(bias)::value>(x, g, *a, (hipStream_t)stream);
+    return go<decltype(t), decltype(d)::value, decltype(bias)::value>(x, g, *a, p, (hipStream_t)stream);
   });
 }
 

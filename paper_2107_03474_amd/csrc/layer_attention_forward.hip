@@ -43,8 +43,7 @@ struct Running {
 // null); bias_far: whether one value of it, `far`, serves the whole tile.
 template <typename T, int D, int N, bool BIAS>
 __device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::type (&q)[D / 16], Lds kt, Lds vt,
-                                       const typename Tile<T, D>::RowAddr& ka, const typename Tile<T, D>::ColAddr& va,
-                                       float c, int j0, int lim, bool masked, const float* bias, bool bias_far,
+                                       uint32_t ka, uint32_t va, float c, int j0, int lim, bool masked, const float* bias, bool bias_far,
                                        float far) {
   using Ti = Tile<T, D>;
   const int h = threadIdx.x >> 5 & 1;
@@ -152,7 +151,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE;
   const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, first + (l & 31));
-  const int head = w.hk * G + r.g;
+  const int head = w.head.first + r.g;
   typename Frag<T>::type q[D / 16];
   load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
   // last key of the lane's row, and of the wave's first and last rows
@@ -164,19 +163,18 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   float near_far[2] = {0, 0};
   if constexpr (BIAS) {
     float* table = (float*)(smem + 4 * BYTES);
-    fill_bias(a, w.hk * G, table, THREADS);
+    fill_bias(a, w.head.first, G, table);
     bias = table + r.g * bias_width(a) + a.reach + BIAS_PAD - (r.i + off);
     __syncthreads();
     const float* mine = table + (r.valid ? r.g : 0) * bias_width(a);
     near_far[0] = mine[0];
     near_far[1] = mine[bias_width(a) - 1];
   }
-  const typename Ti::RowAddr ka = Ti::row_addr(l & 31);
-  const typename Ti::ColAddr va = Ti::col_addr();
+  const uint32_t ka = Ti::row_base(l & 31), va = Ti::col_base();
   Running<D> st;
   st.clear();
-  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.hk * a.k_head;
-  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.hk * a.v_head;
+  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.head.kv * a.k_head;
+  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.head.kv * a.v_head;
   auto load = [&](int j0, int buf) {
     load_rows<T, D, KEYS, WAVES>(kh, a.k_row, j0, w.s.nk, lds + buf * 2 * BYTES, wave);
     load_rows<T, D, KEYS, WAVES>(vh, a.v_row, j0, w.s.nk, lds + buf * 2 * BYTES + BYTES, wave);
@@ -232,7 +230,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
   Lds lds = (Lds)smem + wave * STAGES * 2 * BYTES;
   const int G = a.group, off = w.s.nk - w.s.nq, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, w.row0 + (l & 31));
-  const int head = w.hk * G + r.g;
+  const int head = w.head.first + r.g;
   typename Frag<T>::type q[D / 16];
   load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
   const int lim = a.causal && r.valid ? min(r.i + off, w.s.nk - 1) : w.s.nk - 1;
@@ -242,19 +240,18 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
   float near_far[2] = {0, 0};
   if constexpr (BIAS) {
     float* table = (float*)(smem + few_bytes<T, D>());
-    fill_bias(a, w.hk * G, table, THREADS);
+    fill_bias(a, w.head.first, G, table);
     bias = table + r.g * bias_width(a) + a.reach + BIAS_PAD - (r.i + off);
     __syncthreads();
     const float* mine = table + (r.valid ? r.g : 0) * bias_width(a);
     near_far[0] = mine[0];
     near_far[1] = mine[bias_width(a) - 1];
   }
-  const typename Ti::RowAddr ka = Ti::row_addr(l & 31);
-  const typename Ti::ColAddr va = Ti::col_addr();
+  const uint32_t ka = Ti::row_base(l & 31), va = Ti::col_base();
   Running<D> st;
   st.clear();
-  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.hk * a.k_head;
-  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.hk * a.v_head;
+  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.head.kv * a.k_head;
+  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.head.kv * a.v_head;
   auto load = [&](int j0, int buf) {
     load_rows<T, D, N, 1>(kh, a.k_row, j0, w.s.nk, lds + buf * 2 * BYTES, 0);
     load_rows<T, D, N, 1>(vh, a.v_row, j0, w.s.nk, lds + buf * 2 * BYTES + BYTES, 0);
@@ -325,7 +322,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] += y[e];
     }
-    put<T, D>(a, o, w.split, (w.s.q0 + rr.i) * a.heads + w.hk * G + rr.g, d, x);
+    put<T, D>(a, o, w.split, (w.s.q0 + rr.i) * a.heads + w.head.first + rr.g, d, x);
   }
 }
 
@@ -361,7 +358,7 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(Args a, Out o) {
 
 struct Plan {
   bool few;
-  int slots, splits, piece;
+  int group, slots, splits, piece;
 };
 
 // Few rows: a sequence's packed rows fit one wave.  Pieces of the keys: as many as give the chip about four
@@ -371,9 +368,11 @@ Plan plan_of(const lram_attention& a) {
   const int64_t G = a.heads / a.kv_heads;
   p.few = a.max_q * G <= ROWS;
   const int tile = p.few ? ROWS : WAVES * ROWS;
-  p.slots = (int)(a.tq * G / tile + a.batch + 1);
-  const int64_t work = (int64_t)a.kv_heads * a.batch * std::max<int64_t>(1, (a.max_q * G + tile - 1) / tile);
-  const int64_t real = std::min<int64_t>(work, (int64_t)a.kv_heads * p.slots);
+  p.group = a.rel_weight && !p.few ? 1 : (int)G;
+  p.slots = (int)(a.tq * p.group / tile + a.batch + 1);
+  const int64_t heads = a.heads / p.group;
+  const int64_t work = heads * a.batch * std::max<int64_t>(1, (a.max_q * p.group + tile - 1) / tile);
+  const int64_t real = std::min<int64_t>(work, heads * p.slots);
   int64_t splits = real > 0 ? (p.few ? 1024 : 512) / real : 1;
   splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + 255) / 256});
   if (splits < 1) splits = 1;
@@ -389,7 +388,7 @@ size_t workspace_of(const lram_attention& a, const Plan& p) {
 
 template <typename T, int D, bool BIAS>
 int go(Args x, const Out& o, const Plan& p, hipStream_t s) {
-  const unsigned grid = work_grid((int64_t)x.kv_heads * x.slots * x.splits);
+  const unsigned grid = (unsigned)(x.heads / x.group) * x.slots * x.splits;
   const size_t table = BIAS ? (size_t)x.group * (2 * (x.reach + BIAS_PAD) + 1) * 4 : 0;
   const auto launch = [&](auto kernel, size_t bytes) {
     if (int rc = allow_lds((const void*)kernel, bytes)) return rc;
@@ -431,6 +430,7 @@ int lram_attention_forward(const lram_attention* a, void* out, float* lse, void*
   const size_t need = workspace_of(*a, p);
   if (need && (!workspace || off_align(workspace, 16) || ws_bytes < need)) return LRAM_EWORKSPACE;
   Args x = args_of(*a);
+  x.group = p.group;
   x.slots = p.slots;
   x.splits = p.splits;
   x.piece = p.piece;
