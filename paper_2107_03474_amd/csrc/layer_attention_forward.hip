@@ -362,7 +362,7 @@ struct Plan {
 };
 
 // Few rows: a sequence's packed rows fit one wave.  Pieces of the keys: as many as give the chip about four
-// workgroups a CU, none shorter than 256 keys.
+// workgroups a CU, none shorter than 1,024 keys.
 Plan plan_of(const lram_attention& a) {
   Plan p;
   const int64_t G = a.heads / a.kv_heads;
@@ -374,7 +374,7 @@ Plan plan_of(const lram_attention& a) {
   const int64_t work = heads * a.batch * std::max<int64_t>(1, (a.max_q * p.group + tile - 1) / tile);
   const int64_t real = std::min<int64_t>(work, heads * p.slots);
   int64_t splits = real > 0 ? (p.few ? 1024 : 512) / real : 1;
-  splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + 255) / 256});
+  splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + 1023) / 1024});
   if (splits < 1) splits = 1;
   p.piece = (int)std::min<int64_t>(((a.max_k + splits - 1) / splits + 127) / 128 * 128, INT32_MAX / 2);
   if (p.piece < 128) p.piece = 128;

@@ -13,7 +13,7 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
-from . import BF16, F32, LramError, _dev, _stream
+from . import BF16, F32, LramError, _dev
 from . import load as _load_library
 
 __all__ = ["layer_norm_forward", "layer_norm_backward", "layer_norm", "Packed", "pack", "RelativeBias",
@@ -70,6 +70,20 @@ def _type(t: torch.Tensor, name: str) -> int:
     raise LramError("%s must be float32 or bfloat16" % name)
 
 
+# Small calls are bound by what happens on the host, so the checks below come cheapest first.
+
+def _stream(device: torch.device) -> int:
+    """The current stream of the device (the raw handle: torch's stream object costs 2 us to make)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _ptr(t: torch.Tensor, name: str, dtype: torch.dtype, shape, like: torch.Tensor) -> int:
+    """Device address of a contiguous tensor of this type and shape on like's device."""
+    if not (t.dtype is dtype and t.shape == shape and t.device == like.device and t.is_contiguous() and t.is_cuda):
+        _dev(t, name, dtype, shape, like=like)  # says what is wrong
+    return t.data_ptr()
+
+
 def _scratch(nbytes: int, workspace: Optional[torch.Tensor], like: torch.Tensor):
     """(pointer, bytes, tensor to keep until the launch) of a call's workspace."""
     if workspace is None:
@@ -85,11 +99,12 @@ def _scratch(nbytes: int, workspace: Optional[torch.Tensor], like: torch.Tensor)
 def _norm_args(x: torch.Tensor, weight: torch.Tensor, name: str):
     if x.dim() < 1:
         raise LramError("%s must be [..., width]" % name)
+    if not (x.is_cuda and x.is_contiguous()):
+        _dev(x, name)
     width = x.shape[-1]
-    rows = x.numel() // width if width else 0
-    if weight.dtype not in (x.dtype, torch.float32):
+    if weight.dtype is not x.dtype and weight.dtype is not torch.float32:
         raise LramError("weight must be float32 or of %s's type" % name)
-    return rows, width, _type(x, name), _type(weight, "weight")
+    return x.numel() // width if width else 0, width, _type(x, name), _type(weight, "weight")
 
 
 def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, eps: float = 1e-5,
@@ -98,15 +113,21 @@ def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor
     dimension, and the rows' statistics (fp32 [...]) for the backward."""
     lib = _library()
     rows, width, dt, wt = _norm_args(x, weight, "x")
+    wp = _ptr(weight, "weight", weight.dtype, (width,), x)
+    bp = _ptr(bias, "bias", weight.dtype, (width,), x)
+    rp = hp = None
+    h = x
+    if residual is not None:
+        rp = _ptr(residual, "residual", x.dtype, x.shape, x)
+        h = torch.empty_like(x)
+        hp = h.data_ptr()
     y = torch.empty_like(x)
-    h = x if residual is None else torch.empty_like(x)
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
-    _check(lib.lram_layer_norm_forward(
-        _dev(x, "x"), None if residual is None else _dev(residual, "residual", x.dtype, x.shape, like=x),
-        _dev(weight, "weight", shape=(width,), like=x), _dev(bias, "bias", weight.dtype, (width,), like=x), dt, wt, rows,
-        width, float(eps), None if residual is None else h.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-        _stream(x)))
+    rc = lib.lram_layer_norm_forward(x.data_ptr(), rp, wp, bp, dt, wt, rows, width, eps, hp, y.data_ptr(),
+                                     mean.data_ptr(), rstd.data_ptr(), _stream(x.device))
+    if rc:
+        _check(rc)
     return y, h, mean, rstd
 
 
@@ -119,19 +140,25 @@ def layer_norm_backward(h: torch.Tensor, weight: torch.Tensor, mean: torch.Tenso
     lib = _library()
     rows, width, dt, wt = _norm_args(h, weight, "h")
     f32, lead = torch.float32, h.shape[:-1]
+    wp = _ptr(weight, "weight", weight.dtype, (width,), h)
+    mp, sp = _ptr(mean, "mean", f32, lead, h), _ptr(rstd, "rstd", f32, lead, h)
+    yp = _ptr(grad_y, "grad_y", h.dtype, h.shape, h)
+    gp = None if grad_h is None else _ptr(grad_h, "grad_h", h.dtype, h.shape, h)
     gx = torch.empty_like(h)
-    gw = torch.empty_like(weight) if want_grad_weight else None
-    gb = torch.empty_like(weight) if want_grad_weight else None
-    n = ctypes.c_size_t(0)
-    if want_grad_weight and workspace is None:
-        _check(lib.lram_layer_norm_backward_workspace_bytes(rows, width, dt, ctypes.byref(n)))
-    ws, ws_bytes, _keep = _scratch(n.value, workspace, h)
-    _check(lib.lram_layer_norm_backward(
-        _dev(h, "h"), _dev(weight, "weight", shape=(width,), like=h), _dev(mean, "mean", f32, lead, like=h),
-        _dev(rstd, "rstd", f32, lead, like=h), _dev(grad_y, "grad_y", h.dtype, h.shape, like=h),
-        None if grad_h is None else _dev(grad_h, "grad_h", h.dtype, h.shape, like=h), dt, wt, rows, width,
-        gx.data_ptr(), None if gw is None else gw.data_ptr(), None if gb is None else gb.data_ptr(), ws, ws_bytes,
-        _stream(h)))
+    gw = gb = gwp = gbp = ws = keep = None
+    ws_bytes = 0
+    if want_grad_weight:
+        gw, gb = torch.empty_like(weight), torch.empty_like(weight)
+        gwp, gbp = gw.data_ptr(), gb.data_ptr()
+        n = ctypes.c_size_t(0)
+        if workspace is None:
+            _check(lib.lram_layer_norm_backward_workspace_bytes(rows, width, dt, ctypes.byref(n)))
+        ws, ws_bytes, keep = _scratch(n.value, workspace, h)
+    rc = lib.lram_layer_norm_backward(h.data_ptr(), wp, mp, sp, yp, gp, dt, wt, rows, width, gx.data_ptr(), gwp, gbp,
+                                      ws, ws_bytes, _stream(h.device))
+    del keep
+    if rc:
+        _check(rc)
     return gx, gw, gb
 
 
@@ -235,48 +262,55 @@ class AttentionSaved(NamedTuple):
     residue: Optional[torch.Tensor]
 
 
-def _heads(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None):
-    """(pointer, row stride, head stride) of a [rows, heads, head_dim] tensor whose last dimension is dense."""
+def _heads(t: torch.Tensor, name: str, like: torch.Tensor):
+    """(address, row stride, head stride) of a [rows, heads, head_dim] tensor whose last dimension is dense."""
+    shape = t.shape
+    if len(shape) != 3:
+        raise LramError("%s must be [rows, heads, head_dim]" % name)
     if not t.is_cuda:
         raise LramError("%s must be a GPU tensor" % name)
-    if t.dim() != 3:
-        raise LramError("%s must be [rows, heads, head_dim]" % name)
-    if like is not None and (t.device != like.device or t.dtype != like.dtype or t.shape[2] != like.shape[2]):
+    if t is not like and (t.dtype is not like.dtype or t.device != like.device or shape[2] != like.shape[2]):
         raise LramError("%s must have q's device, type and head_dim" % name)
-    if t.stride(2) != 1 and t.numel():
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1 and t.numel():
         raise LramError("%s must be dense along head_dim" % name)
     # a dimension of size 0 or 1 has no stride to speak of
-    row = t.stride(0) if t.shape[0] > 1 else max(t.shape[1] * t.shape[2], t.shape[2])
-    return t.data_ptr(), row, t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    return (t.data_ptr(), row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2])
 
 
 def _describe(q, k, v, seqs: Packed, causal, scale, rel: Optional[RelativeBias]):
-    qp, q_row, q_head = _heads(q, "q")
-    kp, k_row, k_head = _heads(k, "k", q)
-    vp, v_row, v_head = _heads(v, "v", q)
+    a = _Attention()
+    a.q, a.q_row, a.q_head = _heads(q, "q", q)
+    a.k, a.k_row, a.k_head = _heads(k, "k", q)
+    a.v, a.v_row, a.v_head = _heads(v, "v", q)
     if k.shape != v.shape:
         raise LramError("k and v must have the same shape")
-    batch = seqs.start_q.numel() - 1
+    a.tq, heads, dim = q.shape
+    a.tk, a.kv_heads, _ = k.shape
+    a.heads, a.head_dim = heads, dim
+    batch = a.batch = seqs.start_q.numel() - 1
     if batch < 0:
         raise LramError("start_q must be [batch + 1]")
     i32 = torch.int32
-    a = _Attention(
-        dtype=_type(q, "q"), heads=q.shape[1], kv_heads=k.shape[1], head_dim=q.shape[2], batch=batch,
-        causal=int(bool(causal)), scale=1.0 / math.sqrt(max(q.shape[2], 1)) if scale is None else float(scale),
-        tq=q.shape[0], tk=k.shape[0], max_q=int(seqs.max_q), max_k=int(seqs.max_k), q=qp, k=kp, v=vp, q_row=q_row,
-        q_head=q_head, k_row=k_row, k_head=k_head, v_row=v_row, v_head=v_head,
-        start_q=_dev(seqs.start_q, "start_q", i32, (batch + 1,), like=q),
-        start_k=_dev(seqs.start_k, "start_k", i32, (batch + 1,), like=q),
-        used_k=None if seqs.used_k is None else _dev(seqs.used_k, "used_k", i32, (batch,), like=q))
+    a.dtype = _type(q, "q")
+    a.causal = 1 if causal else 0
+    a.scale = 1.0 / math.sqrt(max(dim, 1)) if scale is None else scale
+    a.max_q, a.max_k = seqs.max_q, seqs.max_k
+    a.start_q = _ptr(seqs.start_q, "start_q", i32, (batch + 1,), q)
+    a.start_k = _ptr(seqs.start_k, "start_k", i32, (batch + 1,), q)
+    if seqs.used_k is not None:
+        a.used_k = _ptr(seqs.used_k, "used_k", i32, (batch,), q)
     if rel is not None:
-        if rel.weight.dim() != 2 or rel.bucket.dim() != 1 or rel.bucket.numel() % 2 != 1:
+        w, bucket = rel
+        if w.dim() != 2 or bucket.dim() != 1 or bucket.numel() % 2 != 1:
             raise LramError("a relative bias has weight [heads, buckets] and bucket [2 reach + 1]")
-        if rel.weight.dtype not in (q.dtype, torch.float32):
+        if w.dtype is not q.dtype and w.dtype is not torch.float32:
             raise LramError("the relative bias's weight must be float32 or of q's type")
-        a.rel_weight = _dev(rel.weight, "rel.weight", shape=(q.shape[1], rel.weight.shape[1]), like=q)
-        a.rel_bucket = _dev(rel.bucket, "rel.bucket", i32, like=q)
-        a.wdtype = _type(rel.weight, "rel.weight")
-        a.rel_buckets, a.rel_reach = rel.weight.shape[1], rel.bucket.numel() // 2
+        buckets, n = w.shape[1], bucket.shape[0]
+        a.rel_weight = _ptr(w, "rel.weight", w.dtype, (heads, buckets), q)
+        a.rel_bucket = _ptr(bucket, "rel.bucket", i32, (n,), q)
+        a.wdtype = _type(w, "rel.weight")
+        a.rel_buckets, a.rel_reach = buckets, n // 2
     return a
 
 
@@ -290,17 +324,22 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: P
     lib = _library()
     a = _describe(q, k, v, seqs, causal, scale, rel)
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    saved = None
+    saved = lse = residue = None
     if save:
         saved = AttentionSaved(torch.empty(q.shape[:2], dtype=torch.float32, device=q.device),
-                               torch.empty_like(out) if q.dtype == torch.bfloat16 else None)
+                               torch.empty_like(out) if q.dtype is torch.bfloat16 else None)
+        lse = saved.lse.data_ptr()
+        residue = None if saved.residue is None else saved.residue.data_ptr()
     n = ctypes.c_size_t(0)
     if workspace is None:
-        _check(lib.lram_attention_forward_workspace_bytes(ctypes.byref(a), ctypes.byref(n)))
-    ws, ws_bytes, _keep = _scratch(n.value, workspace, q)
-    _check(lib.lram_attention_forward(
-        ctypes.byref(a), out.data_ptr(), saved.lse.data_ptr() if save else None,
-        saved.residue.data_ptr() if save and saved.residue is not None else None, ws, ws_bytes, _stream(q)))
+        rc = lib.lram_attention_forward_workspace_bytes(a, n)
+        if rc:
+            _check(rc)
+    ws, ws_bytes, keep = _scratch(n.value, workspace, q)
+    rc = lib.lram_attention_forward(a, out.data_ptr(), lse, residue, ws, ws_bytes, _stream(q.device))
+    del keep
+    if rc:
+        _check(rc)
     return out, saved
 
 
@@ -312,20 +351,22 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: 
     arguments); grad_rel, of the bias's weight, is None without one.  Rows of k and v that no query may see get zeros."""
     lib = _library()
     a = _describe(q, k, v, seqs, causal, scale, rel)
-    gq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    op, gp = _ptr(out, "out", q.dtype, q.shape, q), _ptr(grad_out, "grad_out", q.dtype, q.shape, q)
+    lp = _ptr(saved.lse, "saved.lse", torch.float32, q.shape[:2], q)
+    rp = None if saved.residue is None else _ptr(saved.residue, "saved.residue", q.dtype, q.shape, q)
+    gq = torch.empty_like(out)
     gk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
-    gv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    gv = torch.empty_like(gk)
     grel = None if rel is None else torch.empty_like(rel.weight)
     n = ctypes.c_size_t(0)
     if workspace is None:
-        _check(lib.lram_attention_backward_workspace_bytes(ctypes.byref(a), ctypes.byref(n)))
-    ws, ws_bytes, _keep = _scratch(n.value, workspace, q)
-    _check(lib.lram_attention_backward(
-        ctypes.byref(a), _dev(out, "out", q.dtype, q.shape, like=q),
-        None if saved.residue is None else _dev(saved.residue, "saved.residue", q.dtype, q.shape, like=q),
-        _dev(saved.lse, "saved.lse", torch.float32, q.shape[:2], like=q),
-        _dev(grad_out, "grad_out", q.dtype, q.shape, like=q), gq.data_ptr(), gk.data_ptr(), gv.data_ptr(),
-        None if grel is None else grel.data_ptr(), ws, ws_bytes, _stream(q)))
+        _check(lib.lram_attention_backward_workspace_bytes(a, n))
+    ws, ws_bytes, keep = _scratch(n.value, workspace, q)
+    rc = lib.lram_attention_backward(a, op, rp, lp, gp, gq.data_ptr(), gk.data_ptr(), gv.data_ptr(),
+                                     None if grel is None else grel.data_ptr(), ws, ws_bytes, _stream(q.device))
+    del keep
+    if rc:
+        _check(rc)
     return gq, gk, gv, grel
 
 
