@@ -88,7 +88,7 @@ typedef struct {
   const int32_t* used_k;      /* [batch] (device), nullable */
   const void* rel_weight;     /* [heads][rel_buckets], nullable */
   const int32_t* rel_bucket;  /* [2 rel_reach + 1] (device), each in [0, rel_buckets) */
-  int32_t rel_buckets;        /* 1 ... 1024 */
+  int32_t rel_buckets;        /* 1 ... 256 */
   int32_t rel_reach;          /* >= 0, heads / kv_heads (2 rel_reach + 193) <= 4096 */
 } lram_attention;
 

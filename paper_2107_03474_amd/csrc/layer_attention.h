@@ -83,21 +83,31 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b) {
 
 // Which sequence a tile belongs to, without knowing the lengths on the host: sequence b's tiles of `tile` units (scale
 // units per row) take the slots from start[b] scale / tile + b on, which leaves each at least as many as it needs and
-// ends before rows scale / tile + batch + 1.  Found by bisection; a slot past its sequence's last tile is empty.
+// ends before rows scale / tile + batch + 1; a slot past its sequence's last tile is empty.  Found by a wave that looks
+// at 64 places at once: a workgroup of a short sequence would wait longer for a bisection's loads than it works.
 __device__ __forceinline__ int64_t first_slot(const int32_t* start, int64_t rows, int b, int scale, int tile) {
   return (b ? clamp64(start[b], 0, rows) : 0) * scale / tile + b;
 }
 __device__ __forceinline__ int slot_sequence(const int32_t* start, int64_t rows, int batch, int scale, int tile,
                                              int64_t slot) {
-  int lo = 0, hi = batch;  // the last b with first_slot(b) <= slot
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (first_slot(start, rows, mid, scale, tile) <= slot)
-      lo = mid;
-    else
-      hi = mid - 1;
+  int lo = 0, n = batch + 1;  // the last b of lo ... lo + n - 1 with first_slot(b) <= slot
+  while (n > 1) {
+    const int step = (n + WAVE - 1) / WAVE, b = lo + (int)(threadIdx.x % WAVE) * step;
+    const bool at = b < lo + n && first_slot(start, rows, b, scale, tile) <= slot;
+    const int past = (__popcll(__builtin_amdgcn_ballot_w64(at)) - 1) * step;  // the first place always holds
+    lo += past;
+    n = min(step, n - past);
   }
   return lo;
+}
+
+// The grid's order: tiles of falling length (causal), but every second stretch of as many workgroups as there are compute
+// units turned round, so that workgroups that share one, a grid's length apart, are a long and a short one.  idx of n
+// tiles, each with `heads` workgroups.
+constexpr int UNITS = 256;
+__device__ __forceinline__ int in_turn(int idx, int n, int heads) {
+  const int stretch = max(1, UNITS / heads), first = idx / stretch * stretch;
+  return idx / stretch % 2 ? first + min(stretch, n - first) - 1 - (idx - first) : idx;
 }
 
 // Workgroups go round the 8 dies in turn, and neighbours in the grid are different heads: with 8 key heads, or a divisor or
@@ -329,8 +339,9 @@ template <int M>
 __device__ __forceinline__ bool find_work(const Args& a, Work* w) {
   const unsigned n = a.heads / a.group;
   w->head = heads_of(a, blockIdx.x % n);
-  w->split = blockIdx.x / n % a.splits;
-  const int slot = w->slot = a.slots - 1 - (int)(blockIdx.x / n / a.splits);  // long causal rows first
+  const int tile = in_turn(blockIdx.x / n, a.slots * a.splits, n);
+  w->split = tile % a.splits;
+  const int slot = w->slot = a.slots - 1 - tile / a.splits;  // long causal rows first
   const int b = slot_sequence(a.start_q, a.tq, a.batch, a.group, M, slot);
   w->s = sequence(a, b);
   const int64_t row0 = (slot - first_slot(a.start_q, a.tq, b, a.group, M)) * M;
@@ -376,7 +387,7 @@ int check_attention(const lram_attention& a, bool pointers) {
   if (a.heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 1) > (int64_t(1) << 24)) return LRAM_EINVAL;
   if (a.rel_weight) {
     if (a.wdtype != LRAM_F32 && !(a.wdtype == LRAM_BF16 && a.dtype == LRAM_BF16)) return LRAM_EDTYPE;
-    if (!a.rel_bucket || a.rel_buckets < 1 || a.rel_buckets > 1024 || a.rel_reach < 0 || a.rel_reach > 4096 ||
+    if (!a.rel_bucket || a.rel_buckets < 1 || a.rel_buckets > 256 || a.rel_reach < 0 || a.rel_reach > 4096 ||
         G * (2 * (a.rel_reach + BIAS_PAD) + 1) > 4096)
       return LRAM_EINVAL;
     if (off_align(a.rel_weight, elem_size(a.wdtype)) || off_align(a.rel_bucket, 4)) return LRAM_EINVAL;

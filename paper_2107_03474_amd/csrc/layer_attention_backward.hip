@@ -12,7 +12,7 @@
 // The bias's gradient: k_attention_dq adds up the diagonals of its 32 x 32 blocks of ds.  Rows are lanes and keys registers, so
 // a sum that moves on by one lane with every key collects a diagonal in a lane (diagonals); 8 keys' sums then go to the
 // wave's own table in LDS (one instruction, no two lanes in an entry: the order is fixed).  Blocks past reach go into a
-// register.  A workgroup leaves one row of sums by distance, and k_relative_grad adds the rows and gathers the buckets.
+// register.  A workgroup leaves its sums by bucket, and k_relative_grad adds up the workgroups'.
 
 #include "layer_attention.h"
 
@@ -27,7 +27,8 @@ struct Grads {
   const void *out, *residue, *grad_out;
   const float* lse;
   void *gq, *gk, *gv, *grel;
-  float *delta, *rel, *part;  // workspace: [tq heads], [slots][heads][2 reach + 1], [pieces][tk][kv_heads][2][D]
+  // workspace: [tq heads], [slots][heads][buckets], [pieces][tk][kv_heads][2][D] or [splits][tq][heads][D] (dq first)
+  float *delta, *rel, *part;
 };
 
 // Eight keys of 32 rows (a row to a lane, key 4 h + e in argument e) summed along the diagonals: lane p < 39 of the result
@@ -59,10 +60,11 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   extern __shared__ __attribute__((aligned(256))) char smem[];
   Lds lds = (Lds)smem;
   Work w;
-  if (!find_work<M>(a, &w)) {
+  const bool found = find_work<M>(a, &w);
+  float* const rel_row = o.rel + (((int64_t)w.slot * a.splits + w.split) * a.heads + w.head.first) * a.buckets;
+  if (!found) {
     if constexpr (BIAS)  // an empty slot's sums are zero
-      for (int t = threadIdx.x; t < 2 * a.reach + 1; t += THREADS)
-        o.rel[((int64_t)w.slot * a.heads + w.head.first) * (2 * a.reach + 1) + t] = 0;
+      for (int t = threadIdx.x; t < a.buckets; t += THREADS) rel_row[t] = 0;
     return;
   }
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
@@ -105,8 +107,12 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   float* const table = (float*)(smem + 4 * BYTES);
   float* const sums = table + width;         // [WAVES][width]
   float* const mine = sums + wave * width;
+  int* const of = (int*)(sums + WAVES * width);  // buckets
   if constexpr (BIAS) {
-    fill_bias(a, w.head.first, 1, table);
+    for (int t = threadIdx.x; t < width; t += THREADS) {
+      of[t] = bucket_of(a, t - a.reach - BIAS_PAD);
+      table[t] = rel_weight(a, w.head.first, of[t]) * LOG2E;
+    }
     for (int t = threadIdx.x; t < WAVES * width; t += THREADS) sums[t] = 0;
     bias = table + a.reach + BIAS_PAD - (r.i + off);
     __syncthreads();
@@ -196,7 +202,8 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
     }
   }
   if (r.valid) {
-    T* p = (T*)o.gq + at * D + 4 * h;
+    T* const p = (T*)o.gq + at * D + 4 * h;
+    float* const part = o.part + ((int64_t)w.split * a.tq * a.heads + at) * D + 4 * h;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -204,7 +211,10 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
         f32x4 x;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = acc[b][4 * u + e] * a.scale;
-        store4<T>(p + 32 * b + 8 * u, x);
+        if (a.splits > 1)
+          *(f32x4*)(part + 32 * b + 8 * u) = x;
+        else
+          store4<T>(p + 32 * b + 8 * u, x);
       }
   }
   if constexpr (BIAS) {
@@ -223,24 +233,34 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       far[WAVES + wave] = above;
     }
     __syncthreads();
-    const int n = 2 * a.reach + 1, ends = a.reach == 0 ? width : BIAS_PAD + 1;
-    float* const row = o.rel + ((int64_t)w.slot * a.heads + head) * n;
-    for (int t = 1 + threadIdx.x; t < n - 1; t += THREADS) row[t] = sums[BIAS_PAD + t];
-    if (wave < 2 && wave < n) {  // reach 0: one entry in all
-      float x = l < WAVES ? far[wave * WAVES + l] + (n == 1 ? far[WAVES + l] : 0.0f) : 0.0f;
-      for (int e = l; e < ends; e += WAVE) x += sums[(wave ? width - ends : 0) + e];
+    if (threadIdx.x < 2) {  // the far blocks' sums into the last entry of their side
+      float x = sums[threadIdx.x ? width - 1 : 0];
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) x += far[threadIdx.x * WAVES + v];
+      sums[threadIdx.x ? width - 1 : 0] = x;
+    }
+    __syncthreads();
+    for (int k = wave; k < a.buckets; k += WAVES) {
+      float x = 0;
+      for (int e = l; e < width; e += WAVE) x += of[e] == k ? sums[e] : 0.0f;
       x = wave_sum(x);
-      if (l == 0) row[wave ? n - 1 : 0] = x;
+      if (l == 0) rel_row[k] = x;
     }
   }
 }
 
-// 16 bytes a lane from the lane's address straight into LDS at dst + 16 lane (see dma16).
-__device__ __forceinline__ void dma16_from(const void* src, Lds dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-               :
-               : "s"((uint32_t)(uintptr_t)dst), "v"(src)
-               : "memory");
+// The pieces' dq added up, in their order.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void k_attention_dq_join(const float* part, int64_t n, int splits, T* gq) {
+  const int64_t at = ((int64_t)blockIdx.x * THREADS + threadIdx.x) * 4;
+  if (at >= n) return;
+  f32x4 x = *(const f32x4*)(part + at);
+  for (int p = 1; p < splits; ++p) {
+    const f32x4 y = *(const f32x4*)(part + p * n + at);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += y[e];
+  }
+  store4<T>(gq + at, x);
 }
 
 // k_attention_dkv: a wave's 32 keys stay in registers, and so do their values while a row of them takes 128 bytes; longer
@@ -258,190 +278,182 @@ constexpr int dkv_bytes() {
 }
 template <typename T, int D>
 constexpr int dkv_waves() { return dkv_bytes<T, D>() > 72 * 1024 ? 1 : 2; }  // a SIMD
-// What it keeps of a row: delta, lse, lse less the bias below and above reach, and where distance 0 to key 0 stands in the
-// bias table.
-enum { DELTA, LSE, BELOW, ABOVE, BASE, STATS };
+// What it keeps of a query: delta, lse, and lse less the bias below and above reach.
+enum { DELTA, LSE, BELOW, ABOVE, STATS };
 
-// The key tile of a workgroup and its piece of the packed rows.
+// The key tile of a workgroup and its piece of the rows: row r is query r % nq of the group's head r / nq, and the tile meets
+// the queries from `seen` on of every head.
 struct KeyWork {
   Seq s;
-  int j0, rows, begin, end;  // begin >= end: no row of the piece meets a key of the tile
+  int j0, seen;
+  int64_t lo, hi;
 };
-// Packed rows from first_row on see the key (causal).
-__device__ __forceinline__ int first_row(const Args& a, const Seq& s, int key) {
-  return a.causal ? max(key - (s.nk - s.nq), 0) * a.ratio : 0;
-}
 __device__ __forceinline__ bool key_work(const Args& a, int slot, int piece, KeyWork* w) {
   const int b = slot_sequence(a.start_k, a.tk, a.batch, 1, DKV_KEYS, slot);
   w->s = sequence(a, b);
   const int64_t from = (slot - first_slot(a.start_k, a.tk, b, 1, DKV_KEYS)) * DKV_KEYS;
   if (from >= w->s.cap) return false;
   w->j0 = (int)from;
-  w->rows = w->s.nq * a.ratio;
-  w->begin = w->j0 < w->s.nk ? first_row(a, w->s, w->j0) : w->rows;
-  w->end = w->rows;
-  const int64_t lo = (int64_t)piece * a.piece, hi = lo + a.piece;
-  if (w->begin < lo) w->begin = (int)(lo < w->rows ? lo : w->rows);
-  if (piece < a.splits - 1 && hi < w->end) w->end = (int)hi;
+  w->seen = w->j0 >= w->s.nk ? w->s.nq : a.causal ? max(w->j0 - (w->s.nk - w->s.nq), 0) : 0;
+  const int64_t rows = (int64_t)w->s.nq * a.ratio;
+  w->lo = min((int64_t)piece * a.piece, rows);
+  w->hi = piece < a.splits - 1 ? min(w->lo + a.piece, rows) : rows;
   return true;
+}
+// The rows of a piece, a stretch of queries of one head at a time; begin >= end: none left.
+struct Stretch {
+  int head, begin, end;
+};
+__device__ __forceinline__ Stretch stretch_from(const KeyWork& w, int64_t row) {
+  Stretch t{0, 0, 0};
+  if (w.s.nq == 0 || w.seen >= w.s.nq || row >= w.hi) return t;
+  t.head = (int)(row / w.s.nq);
+  t.begin = max((int)(row - (int64_t)t.head * w.s.nq), w.seen);
+  t.end = (int)min(w.hi - (int64_t)t.head * w.s.nq, (int64_t)w.s.nq);
+  if (t.begin < t.end) return t;
+  // the piece ends before the first query that sees the tile
+  return Stretch{0, 0, 0};
 }
 
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(Args a, Grads o) {
   using Ti = Tile<T, D>;
   using F = typename Frag<T>::type;
-  constexpr int TROWS = tile_rows<T, D>(), BYTES = TROWS * Ti::ROW, LOADS = TROWS * Ti::CH / 64 / WAVES;
+  constexpr int TROWS = tile_rows<T, D>(), BYTES = TROWS * Ti::ROW;
   constexpr bool VLDS = values_in_lds<T, D>();
   extern __shared__ __attribute__((aligned(256))) char smem[];
   Lds lds = (Lds)smem;
-  const int hk = blockIdx.x % a.kv_heads, piece = blockIdx.x / a.kv_heads % a.splits;
-  const int slot = blockIdx.x / a.kv_heads / a.splits;  // the first keys, which most rows see, first
+  const int hk = blockIdx.x % a.kv_heads;
+  const int tile = in_turn(blockIdx.x / a.kv_heads, a.slots * a.splits, a.kv_heads);
+  const int piece = tile % a.splits, slot = tile / a.splits;  // the first keys, which most rows see, first
   KeyWork w;
   if (!key_work(a, slot, piece, &w)) return;
-  if (a.splits > 1 && w.begin >= w.end) return;  // k_attention_dkv_join leaves it out
   const Seq& s = w.s;
+  Stretch t = stretch_from(w, w.lo);
+  const bool any = t.begin < t.end;
+  if (a.splits > 1 && !any) return;  // k_attention_dkv_join leaves it out
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
-  const int G = a.ratio, off = s.nk - s.nq, rows = w.rows;
+  const int off = s.nk - s.nq;
   const int jw = w.j0 + 32 * wave, j = jw + (l & 31);
   const bool valid = j < s.nk;
-  const int seen_from = first_row(a, s, j), wave_from = first_row(a, s, jw), wave_all = first_row(a, s, jw + 31);
+  // the wave's keys are seen by queries from `some` on, and all of them by those from `all` on
+  const int some = a.causal ? jw - off : 0, all = a.causal ? jw + 31 - off : 0;
   F k[D / 16], v[VLDS ? 1 : D / 16];
   const Lds vt = lds + 4 * BYTES;
-  if (VLDS && w.begin < w.end)
+  if (VLDS && any)
     load_rows<T, D, DKV_KEYS, WAVES>((const T*)a.v + s.k0 * a.v_row + hk * a.v_head, a.v_row, w.j0, s.nk, vt, wave);
   {
     const T* kp = (const T*)a.k + (s.k0 + j) * a.k_row + hk * a.k_head + 8 * h;
     const T* vp = (const T*)a.v + (s.k0 + j) * a.v_row + hk * a.v_head + 8 * h;
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) {
+    for (int e = 0; e < D / 16; ++e) {
       F z = {};
-      k[t] = valid ? *(const F*)(kp + 16 * t) : z;
-      if constexpr (!VLDS) v[t] = valid ? *(const F*)(vp + 16 * t) : z;
+      k[e] = valid ? *(const F*)(kp + 16 * e) : z;
+      if constexpr (!VLDS) v[e] = valid ? *(const F*)(vp + 16 * e) : z;
     }
   }
+  const int64_t g_row = (int64_t)a.heads * D;
+  const auto load = [&](int head, int i, int end, int buf) {
+    const int hq = hk * a.ratio + head;
+    load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, i, end,
+                                  lds + buf * 2 * BYTES, wave);
+    load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, i, end,
+                                  lds + buf * 2 * BYTES + BYTES, wave);
+  };
   // beside the tiles: [2][STATS][TROWS], then the bias table
   float* const stats = (float*)(smem + dkv_bytes<T, D>());
   float* const table = stats + 2 * STATS * TROWS;
   const int width = bias_width(a);
-  if constexpr (BIAS) {
-    fill_bias(a, hk * G, G, table);
-    __syncthreads();
-  }
-  uint32_t ra = Ti::row_base(l & 31), ca = Ti::col_base();
-  f32x16 dk[D / 32], dv[D / 32];
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) dk[t][e] = dv[t][e] = 0;
-
-  const T* const qh = (const T*)a.q + s.q0 * a.q_row + (int64_t)hk * G * a.q_head;
-  const T* const gh = (const T*)o.grad_out + (s.q0 * a.heads + hk * G) * D;
-  const float* const lse_h = o.lse + s.q0 * a.heads + hk * G;
-  const float* const delta_h = o.delta + s.q0 * a.heads + hk * G;
-  const int inv = 65536 / G + 1;  // x / G = x inv >> 16 for x < 128, G <= 64
-  // packed row t of a tile from row r0 on, i0 = r0 / G: (query, head of the group); past the last row its last one
-  const auto split_row = [&](int r0, int i0, int t, int* i, int* g) {
-    t = min(t, rows - 1 - r0);
-    const int x = r0 - i0 * G + t, di = x * inv >> 16;
-    *i = i0 + di;
-    *g = x - di * G;
-  };
-  const auto load = [&](int r0, int buf) {
-    const int i0 = r0 / G;
-#pragma unroll
-    for (int n = 0; n < LOADS; ++n) {
-      const int c = (wave * LOADS + n) * 64, p = c + l, r = p / Ti::CH;
-      const int ch = (p % Ti::CH) ^ Ti::swizzle(r);
-      int i, g;
-      split_row(r0, i0, r, &i, &g);
-      const Lds to = lds + buf * 2 * BYTES + c * 16;
-      dma16_from(qh + (int64_t)i * a.q_row + (int64_t)g * a.q_head + ch * Ti::PER, to);
-      dma16_from(gh + ((int64_t)i * a.heads + g) * D + ch * Ti::PER, to + BYTES);
-    }
-  };
-  // A tile's statistics, a row to a thread of the first wave: loaded with the tile before, written when it is done.
-  // A row past the piece's last one gets lse = inf, and with it p = 0.
+  // A tile's statistics, a query to a lane of the first wave: loaded with the tile before, written when that is done.  A
+  // query past the end gets lse = inf, and with it p = 0.
+  const bool keeper = wave == 0 && l < TROWS;
   float st_lse = 0, st_delta = 0;
-  const auto load_stats = [&](int r0) {
-    int i, g;
-    split_row(r0, r0 / G, l, &i, &g);
-    st_lse = r0 + l < w.end ? lse_h[(int64_t)i * a.heads + g] : INFINITY;
-    st_delta = delta_h[(int64_t)i * a.heads + g];
+  const auto load_stats = [&](int head, int i, int end) {
+    const int64_t at = (s.q0 + i + l) * a.heads + hk * a.ratio + head;
+    st_lse = i + l < end ? o.lse[at] : INFINITY;
+    st_delta = i + l < end ? o.delta[at] : 0.0f;
   };
-  const auto put_stats = [&](int r0, int buf) {
+  const auto put_stats = [&](int head, int buf) {
     float* to = stats + buf * STATS * TROWS + l;
     to[DELTA * TROWS] = st_delta;
     to[LSE * TROWS] = st_lse;
     if constexpr (BIAS) {
-      int i, g;
-      split_row(r0, r0 / G, l, &i, &g);
-      to[BELOW * TROWS] = st_lse - table[g * width];
-      to[ABOVE * TROWS] = st_lse - table[g * width + width - 1];
-      ((int*)to)[BASE * TROWS] = g * width + a.reach + BIAS_PAD - (i + off);
+      to[BELOW * TROWS] = st_lse - table[head * width];
+      to[ABOVE * TROWS] = st_lse - table[head * width + width - 1];
     }
   };
-  const bool keeper = wave == 0 && l < TROWS;
-  if (w.begin < w.end) {
-    load(w.begin, 0);
-    if (keeper) {
-      load_stats(w.begin);
-      put_stats(w.begin, 0);
-    }
+  if (any) {
+    load(t.head, t.begin, t.end, 0);
+    if (keeper) load_stats(t.head, t.begin, t.end);
   }
+  if constexpr (BIAS) {
+    fill_bias(a, hk * a.ratio, a.ratio, table);
+    __syncthreads();
+  }
+  if (any && keeper) put_stats(t.head, 0);
+  uint32_t ra = Ti::row_base(l & 31), ca = Ti::col_base();
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dk[b][e] = dv[b][e] = 0;
   int buf = 0;
-  for (int r0 = w.begin; r0 < w.end; r0 += TROWS, buf ^= 1) {
+  while (t.begin < t.end) {
     loads_done();
     __syncthreads();
-    const bool more = r0 + TROWS < w.end;
+    Stretch next = t;  // the tile after this one
+    next.begin += TROWS;
+    if (next.begin >= t.end) next = stretch_from(w, (int64_t)(t.head + 1) * s.nq);
+    const bool more = next.begin < next.end;
     if (more) {
-      load(r0 + TROWS, buf ^ 1);
-      if (keeper) load_stats(r0 + TROWS);
+      load(next.head, next.begin, next.end, buf ^ 1);
+      if (keeper) load_stats(next.head, next.begin, next.end);
     }
     asm volatile("" : "+v"(ra), "+v"(ca));  // the addresses are formed at their use: kept, they would not fit the registers
     const Lds qt = lds + buf * 2 * BYTES, gt = qt + BYTES;
     const float* const st = stats + buf * STATS * TROWS + 4 * h;
 #pragma unroll
     for (int rb = 0; rb < TROWS / 32; ++rb) {
-      // rows that none of the wave's keys meets
-      if (jw >= s.nk || r0 + 32 * rb + 31 < wave_from || r0 + 32 * rb >= w.end) continue;
-      int use = LSE;  // past reach one value of a row's bias serves the whole block, and is in the row's statistic
+      const int i = t.begin + 32 * rb;
+      if (jw >= s.nk || i + 31 < some || i >= t.end) continue;  // none of the queries meets the wave's keys
+      int use = LSE;  // past reach one value of the bias serves the whole block, and is in the query's statistic
       if constexpr (BIAS) {
-        const int i_first = (r0 + 32 * rb) / G, i_last = (min(r0 + 32 * rb + 32, rows) - 1) / G;
-        if (jw + 31 - (i_first + off) <= -a.reach) use = BELOW;
-        if (jw - (i_last + off) >= a.reach) use = ABOVE;
+        if (jw + 31 - (i + off) <= -a.reach) use = BELOW;
+        if (jw - (i + 31 + off) >= a.reach) use = ABOVE;
       }
-      const bool near = BIAS && use == LSE;
       f32x16 p, ds;
 #pragma unroll
       for (int e = 0; e < 16; ++e) p[e] = ds[e] = 0;
 #pragma unroll
-      for (int t = 0; t < D / 16; ++t) p = mma(Ti::row_frag(qt, ra, t, 32 * rb), k[t], p);
+      for (int x = 0; x < D / 16; ++x) p = mma(Ti::row_frag(qt, ra, x, 32 * rb), k[x], p);
 #pragma unroll
-      for (int t = 0; t < D / 16; ++t) {
+      for (int x = 0; x < D / 16; ++x) {
         if constexpr (VLDS)
-          ds = mma(Ti::row_frag(gt, ra, t, 32 * rb), Ti::row_frag(vt, ra, t, 32 * wave), ds);
+          ds = mma(Ti::row_frag(gt, ra, x, 32 * rb), Ti::row_frag(vt, ra, x, 32 * wave), ds);
         else
-          ds = mma(Ti::row_frag(gt, ra, t, 32 * rb), v[t], ds);
+          ds = mma(Ti::row_frag(gt, ra, x, 32 * rb), v[x], ds);
+      }
+      float unit = a.c;
+      if constexpr (BIAS) {
+        if (use == LSE) {  // entry of distance j - (i + 31) - off, the block's queries from there downwards
+          const float* at = table + t.head * width + a.reach + BIAS_PAD + j - (i + 31 + off) - 4 * h;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e] = fmaf(p[e], a.c, at[31 - 8 * (e >> 2) - (e & 3)]);
+          unit = 1;
+        }
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const f32x4 lse = *(const f32x4*)(st + use * TROWS + 32 * rb + 8 * u);
-        if (near) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int at = ((const int*)st)[BASE * TROWS + 32 * rb + 8 * u + e] + j;
-            p[4 * u + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * u + e], a.c, table[at]) - lse[e]);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[4 * u + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * u + e], a.c, -lse[e]));
-        }
         const f32x4 delta = *(const f32x4*)(st + DELTA * TROWS + 32 * rb + 8 * u);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ds[4 * u + e] = p[4 * u + e] * (ds[4 * u + e] - delta[e]);
+        for (int e = 0; e < 4; ++e) {
+          p[4 * u + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * u + e], unit, -lse[e]));
+          ds[4 * u + e] = p[4 * u + e] * (ds[4 * u + e] - delta[e]);
+        }
       }
-      if (r0 + 32 * rb < wave_all) {
-        const int need = seen_from - (r0 + 32 * rb) - 4 * h;
+      if (i < all) {
+        const int need = j - off - i - 4 * h;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const bool sees = 8 * (e >> 2) + (e & 3) >= need;
@@ -459,45 +471,47 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
         }
         const auto fx = to_frag<T>(x), fy = to_frag<T>(y);
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) dv[t] = mma(Ti::col_frag(gt, ca, t, 2 * rb + c), fx, dv[t]);
+        for (int b = 0; b < D / 32; ++b) dv[b] = mma(Ti::col_frag(gt, ca, b, 2 * rb + c), fx, dv[b]);
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) dk[t] = mma(Ti::col_frag(qt, ca, t, 2 * rb + c), fy, dk[t]);
+        for (int b = 0; b < D / 32; ++b) dk[b] = mma(Ti::col_frag(qt, ca, b, 2 * rb + c), fy, dk[b]);
       }
     }
-    if (more && keeper) put_stats(r0 + TROWS, buf ^ 1);
+    if (more && keeper) put_stats(next.head, buf ^ 1);
+    t = next;
+    buf ^= 1;
   }
   if (a.splits > 1) {
     if (j >= s.nk) return;
     float* const to = o.part + (((int64_t)piece * a.tk + s.k0 + j) * a.kv_heads + hk) * 2 * D + 4 * h;
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+    for (int b = 0; b < D / 32; ++b)
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         f32x4 x, y;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[e] = dk[t][4 * u + e] * a.scale;
-          y[e] = dv[t][4 * u + e];
+          x[e] = dk[b][4 * u + e] * a.scale;
+          y[e] = dv[b][4 * u + e];
         }
-        *(f32x4*)(to + 32 * t + 8 * u) = x;
-        *(f32x4*)(to + D + 32 * t + 8 * u) = y;
+        *(f32x4*)(to + 32 * b + 8 * u) = x;
+        *(f32x4*)(to + D + 32 * b + 8 * u) = y;
       }
     return;
   }
   if (j >= s.cap) return;
   const int64_t at = ((s.k0 + j) * a.kv_heads + hk) * D + 4 * h;
 #pragma unroll
-  for (int t = 0; t < D / 32; ++t)
+  for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       f32x4 x, y;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {  // rows of a cache past the sequence's keys: zeros
-        x[e] = valid ? dk[t][4 * u + e] * a.scale : 0.0f;
-        y[e] = valid ? dv[t][4 * u + e] : 0.0f;
+        x[e] = valid ? dk[b][4 * u + e] * a.scale : 0.0f;
+        y[e] = valid ? dv[b][4 * u + e] : 0.0f;
       }
-      store4<T>((T*)o.gk + at + 32 * t + 8 * u, x);
-      store4<T>((T*)o.gv + at + 32 * t + 8 * u, y);
+      store4<T>((T*)o.gk + at + 32 * b + 8 * u, x);
+      store4<T>((T*)o.gv + at + 32 * b + 8 * u, y);
     }
 }
 
@@ -507,14 +521,12 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
   const int hk = blockIdx.x % a.kv_heads, slot = blockIdx.x / a.kv_heads;
   KeyWork w;
   if (!key_work(a, slot, 0, &w)) return;
-  int used[2] = {a.splits, 0};  // pieces with rows for the tile: one range
+  unsigned used = 0;  // pieces with rows that meet the tile
   for (int p = 0; p < a.splits; ++p) {
     KeyWork x;
     key_work(a, slot, p, &x);
-    if (x.begin < x.end) {
-      used[0] = min(used[0], p);
-      used[1] = p + 1;
-    }
+    const Stretch t = stretch_from(x, x.lo);
+    used |= (unsigned)(t.begin < t.end) << p;
   }
   const int keys = min(DKV_KEYS, w.s.cap - w.j0);
   for (int t = threadIdx.x; t < keys * (2 * D / 4); t += THREADS) {
@@ -522,7 +534,8 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
     const int64_t at = (w.s.k0 + j) * a.kv_heads + hk;
     f32x4 x = {0, 0, 0, 0};
     if (j < w.s.nk)
-      for (int p = used[0]; p < used[1]; ++p) {
+      for (unsigned left = used; left; left &= left - 1) {
+        const int p = __ffs(left) - 1;
         const f32x4 y = *(const f32x4*)(o.part + ((int64_t)p * a.tk * a.kv_heads + at) * 2 * D + d);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] += y[e];
@@ -531,42 +544,46 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
   }
 }
 
-// A head's sums by distance over all slots, and its buckets' from them; a workgroup to a head.
+// The workgroups' sums [n][heads][buckets] added up; a workgroup to a head, 32 threads to a bucket.
 constexpr int REL_THREADS = 1024;
 template <typename W>
-__global__ __launch_bounds__(REL_THREADS) void k_relative_grad(Args a, const float* rel, W* grad) {
-  constexpr int COLS = 128, PARTS = REL_THREADS / COLS;
-  extern __shared__ float sum[];  // [n], then [PARTS][COLS]
-  const int n = 2 * a.reach + 1, head = blockIdx.x;
-  float* const part = sum + n;
-  const int c = threadIdx.x % COLS, p = threadIdx.x / COLS;
-  for (int d0 = 0; d0 < n; d0 += COLS) {
+__global__ __launch_bounds__(REL_THREADS) void k_relative_grad(const float* rel, int n, int heads, int buckets, W* grad) {
+  constexpr int COLS = 32, PARTS = REL_THREADS / COLS;
+  __shared__ float part[PARTS][COLS + 1];
+  const int head = blockIdx.x, c = threadIdx.x % COLS, p = threadIdx.x / COLS;
+  for (int k0 = 0; k0 < buckets; k0 += COLS) {
     float x = 0;
-    if (d0 + c < n)
-#pragma unroll 8
-      for (int s = p; s < a.slots; s += PARTS) x += rel[((int64_t)s * a.heads + head) * n + d0 + c];
-    part[p * COLS + c] = x;
+    if (k0 + c < buckets)
+#pragma unroll 4
+      for (int s = p; s < n; s += PARTS) x += rel[((int64_t)s * heads + head) * buckets + k0 + c];
+    part[p][c] = x;
     __syncthreads();
-    if (p == 0 && d0 + c < n) {
+    if (p == 0 && k0 + c < buckets) {
 #pragma unroll
-      for (int t = 1; t < PARTS; ++t) x += part[t * COLS + c];
-      sum[d0 + c] = x;
+      for (int t = 1; t < PARTS; ++t) x += part[t][c];
+      grad[(int64_t)head * buckets + k0 + c] = (W)x;
     }
     __syncthreads();
   }
-  const int wave = threadIdx.x / WAVE, l = threadIdx.x % WAVE;
-  for (int k = wave; k < a.buckets; k += REL_THREADS / WAVE) {
-    float x = 0;
-    for (int d = l; d < n; d += WAVE) x += bucket_of(a, d - a.reach) == k ? sum[d] : 0.0f;
-    x = wave_sum(x);
-    if (l == 0) grad[(int64_t)head * a.buckets + k] = (W)x;
-  }
 }
 
-// How the two kernels divide the work.  Packed rows come in pieces where the key tiles are few against the chip (about
-// four workgroups a CU are wanted), none shorter than 1,024 rows.
+// How the two kernels divide the work: keys (dq) and rows (dk, dv) come in pieces where the tiles are few against the chip
+// (about four workgroups a CU are wanted), none shorter than 1,024 (128 in fp32, whose products take sixteen times as
+// long).
+constexpr int MAX_PIECES = 16;
+struct Pieces {
+  int n, size;
+};
+Pieces pieces_of(int64_t tiles, int64_t length, int dtype) {
+  const int64_t shortest = dtype == LRAM_F32 ? 128 : 1024;
+  const int64_t wanted = tiles > 0 ? 1024 / tiles : 1;
+  const int64_t n = std::max<int64_t>(1, std::min<int64_t>({wanted, (length + shortest - 1) / shortest, MAX_PIECES}));
+  const int64_t size = std::max<int64_t>(64, ((length + n - 1) / n + 63) / 64 * 64);
+  return {(int)std::max<int64_t>(1, std::min(n, (length + size - 1) / size)), (int)std::min<int64_t>(size, 1 << 30)};
+}
 struct Plan {
-  int group, row_slots, key_slots, pieces, piece;
+  int group, row_slots, key_slots;
+  Pieces keys, rows;
   size_t delta, rel, part;  // floats of workspace
 };
 Plan plan_of(const lram_attention& a) {
@@ -575,15 +592,17 @@ Plan plan_of(const lram_attention& a) {
   p.group = a.rel_weight ? 1 : (int)G;
   p.row_slots = (int)(a.tq * p.group / (WAVES * ROWS) + a.batch + 1);
   p.key_slots = (int)(a.tk / DKV_KEYS + a.batch + 1);
-  const int64_t tiles = std::min<int64_t>((int64_t)a.batch * ((a.max_k + DKV_KEYS - 1) / DKV_KEYS), p.key_slots);
-  const int64_t rows = a.max_q * G;
-  int64_t pieces = tiles > 0 ? 1024 / (tiles * a.kv_heads) : 1;
-  pieces = std::max<int64_t>(1, std::min<int64_t>({pieces, (rows + 1023) / 1024, 16}));
-  p.piece = (int)std::min<int64_t>((rows / pieces + 64) / 64 * 64, 1 << 30);
-  p.pieces = (int)std::max<int64_t>(1, std::min(pieces, (rows + p.piece - 1) / p.piece));
+  const auto tiles = [&](int64_t longest, int64_t slots) {
+    return std::min<int64_t>((int64_t)a.batch * ((longest + 127) / 128), slots);
+  };
+  p.keys = pieces_of(tiles(a.max_q * p.group, p.row_slots) * (a.heads / p.group), a.max_k, a.dtype);
+  p.rows = pieces_of(tiles(a.max_k, p.key_slots) * a.kv_heads, a.max_q * G, a.dtype);
   p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
-  p.rel = a.rel_weight ? ((size_t)p.row_slots * a.heads * (2 * a.rel_reach + 1) + 3) / 4 * 4 : 0;
-  p.part = p.pieces > 1 ? (size_t)p.pieces * a.tk * a.kv_heads * 2 * a.head_dim : 0;
+  p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
+  // dq's pieces are joined before those of dk and dv are written
+  const size_t dq = p.keys.n > 1 ? (size_t)p.keys.n * a.tq * a.heads * a.head_dim : 0;
+  const size_t dkv = p.rows.n > 1 ? (size_t)p.rows.n * a.tk * a.kv_heads * 2 * a.head_dim : 0;
+  p.part = std::max(dq, dkv);
   return p;
 }
 
@@ -598,14 +617,22 @@ int go(Args x, const Grads& g, const lram_attention& d, const Plan& p, hipStream
   if (x.tq) {
     x.group = p.group;
     x.slots = p.row_slots;
-    if (int rc = launch(k_attention_dq<T, D, BIAS>, (int64_t)(x.heads / x.group) * x.slots,
-                        (size_t)4 * KEYS * Tile<T, D>::ROW + width * (1 + WAVES)))
+    x.splits = p.keys.n;
+    x.piece = p.keys.size;
+    if (int rc = launch(k_attention_dq<T, D, BIAS>, (int64_t)(x.heads / x.group) * x.slots * x.splits,
+                        (size_t)4 * KEYS * Tile<T, D>::ROW + width * (2 + WAVES)))
       return rc;
+    if (x.splits > 1) {
+      const int64_t n = x.tq * x.heads * D;
+      hipLaunchKernelGGL(k_attention_dq_join<T>, dim3((unsigned)((n / 4 + THREADS - 1) / THREADS)), dim3(THREADS), 0, s,
+                         (const float*)g.part, n, x.splits, (T*)g.gq);
+      if (int rc = layer_launched()) return rc;
+    }
   }
   if (x.tk) {
     x.slots = p.key_slots;
-    x.splits = p.pieces;
-    x.piece = p.piece;
+    x.splits = p.rows.n;
+    x.piece = p.rows.size;
     if (int rc = launch(k_attention_dkv<T, D, BIAS>, (int64_t)x.kv_heads * x.slots * x.splits,
                         dkv_bytes<T, D>() + 2 * STATS * tile_rows<T, D>() * 4 + width * x.ratio))
       return rc;
@@ -613,12 +640,10 @@ int go(Args x, const Grads& g, const lram_attention& d, const Plan& p, hipStream
       if (int rc = launch(k_attention_dkv_join<T, D>, (int64_t)x.kv_heads * x.slots, 0)) return rc;
   }
   if constexpr (BIAS) {
-    x.slots = x.tq ? p.row_slots : 0;
-    const size_t bytes = (size_t)(2 * x.reach + 1 + REL_THREADS) * 4;
     const auto finish = [&](auto w) {
       using W = decltype(w);
-      hipLaunchKernelGGL(k_relative_grad<W>, dim3(x.heads), dim3(REL_THREADS), bytes, s, x, (const float*)g.rel,
-                         (W*)g.grel);
+      hipLaunchKernelGGL(k_relative_grad<W>, dim3(x.heads), dim3(REL_THREADS), 0, s, (const float*)g.rel,
+                         x.tq ? p.row_slots * p.keys.n : 0, x.heads, x.buckets, (W*)g.grel);
       return layer_launched();
     };
     return d.wdtype == LRAM_BF16 ? finish(bf16()) : finish(float());

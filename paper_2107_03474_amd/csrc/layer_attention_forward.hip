@@ -39,12 +39,12 @@ struct Running {
 };
 
 // N blocks of 32 keys from key j0 on, at `kt` and `vt` in LDS.  lim: the last key that the lane's row sees; masked: some row
-// of the wave does not see every key of the tile.  bias: the lane's row of the bias table at distance -(i + off) (or
-// null); bias_far: whether one value of it, `far`, serves the whole tile.
+// of the wave does not see every key of the tile.  near: the bias differs from pair to pair, and `bias` is the lane's
+// row of its table at distance -(i + off); else one value of it, `far`, serves the whole tile.
 template <typename T, int D, int N, bool BIAS>
 __device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::type (&q)[D / 16], Lds kt, Lds vt,
-                                       uint32_t ka, uint32_t va, float c, int j0, int lim, bool masked, const float* bias, bool bias_far,
-                                       float far) {
+                                       uint32_t ka, uint32_t va, float c, int j0, int lim, bool masked,
+                                       const float* bias, bool near, float far) {
   using Ti = Tile<T, D>;
   const int h = threadIdx.x >> 5 & 1;
   f32x16 s[N];
@@ -56,18 +56,16 @@ __device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::t
   for (int k = 0; k < D / 16; ++k)
 #pragma unroll
     for (int b = 0; b < N; ++b) s[b] = mma(Ti::row_frag(kt, ka, k, 32 * b), q[k], s[b]);
+  float unit = c;  // z = unit s + far
   if constexpr (BIAS) {
-    if (bias_far) {
-#pragma unroll
-      for (int b = 0; b < N; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], c, far);
-    } else {
+    if (near) {
       const float* at = bias + j0 + 4 * h;
 #pragma unroll
       for (int b = 0; b < N; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], c, at[32 * b + 8 * (r >> 2) + (r & 3)]);
+      unit = 1;
+      far = 0;
     }
   }
   if (masked) {
@@ -82,8 +80,7 @@ __device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::t
   for (int b = 0; b < N; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
-  top = max_halves(top);
-  if constexpr (!BIAS) top *= c;
+  top = fmaf(max_halves(top), unit, far);
   if (__builtin_amdgcn_ballot_w64(top > st.m + GROWTH)) {
     const float m = fmaxf(st.m, top);
     const float a = __builtin_amdgcn_exp2f(st.m - (m == -INFINITY ? 0.0f : m));
@@ -94,13 +91,13 @@ __device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::t
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[b][r] *= a;
   }
-  const float m = st.m == -INFINITY ? 0.0f : st.m;
+  const float less = far - (st.m == -INFINITY ? 0.0f : st.m);
   float l = 0;
 #pragma unroll
   for (int b = 0; b < N; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[b][r] = __builtin_amdgcn_exp2f(BIAS ? s[b][r] - m : fmaf(s[b][r], c, -m));
+      s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], unit, less));
       l += s[b][r];
     }
   st.l += l;
@@ -195,7 +192,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       far = near_far[above];
     }
     attend<T, D, KEYS / 32, BIAS>(st, q, lds + buf * 2 * BYTES, lds + buf * 2 * BYTES + BYTES, ka, va, a.c, j0, lim,
-                                  masked, bias, whole, far);
+                                  masked, bias, !whole, far);
   }
   if (!r.valid) return;
   const float sum = add_halves(st.l), inv = sum == 0 ? 0.0f : 1.0f / sum;
@@ -278,7 +275,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
       far = near_far[above];
     }
     attend<T, D, N / 32, BIAS>(st, q, lds + buf * 2 * BYTES, lds + buf * 2 * BYTES + BYTES, ka, va, a.c, j0, lim,
-                               masked, bias, whole, far);
+                               masked, bias, !whole, far);
   }
   // join the waves: maxima and sums, then the scaled accumulators, through LDS
   constexpr int PITCH = D * 4 + 16;
@@ -362,7 +359,7 @@ struct Plan {
 };
 
 // Few rows: a sequence's packed rows fit one wave.  Pieces of the keys: as many as give the chip about four
-// workgroups a CU, none shorter than 1,024 keys.
+// workgroups a CU, none shorter than 1,024 keys (128 where fp32 products, a sixteenth of the rate, make them long).
 Plan plan_of(const lram_attention& a) {
   Plan p;
   const int64_t G = a.heads / a.kv_heads;
@@ -374,7 +371,8 @@ Plan plan_of(const lram_attention& a) {
   const int64_t work = heads * a.batch * std::max<int64_t>(1, (a.max_q * p.group + tile - 1) / tile);
   const int64_t real = std::min<int64_t>(work, heads * p.slots);
   int64_t splits = real > 0 ? (p.few ? 1024 : 512) / real : 1;
-  splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + 1023) / 1024});
+  const int64_t shortest = a.dtype == LRAM_F32 && !p.few ? 128 : 1024;
+  splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + shortest - 1) / shortest});
   if (splits < 1) splits = 1;
   p.piece = (int)std::min<int64_t>(((a.max_k + splits - 1) / splits + 127) / 128 * 128, INT32_MAX / 2);
   if (p.piece < 128) p.piece = 128;
