@@ -104,8 +104,9 @@ __device__ __forceinline__ int slot_sequence(const int32_t* start, int64_t rows,
 // The grid's order: tiles of falling length (causal), but every second stretch of as many workgroups as there are compute
 // units turned round, so that workgroups that share one, a grid's length apart, are a long and a short one.  idx of n
 // tiles, each with `heads` workgroups.
-constexpr int UNITS = 256;
+constexpr int UNITS = 256, TURN_MOST = 3;
 __device__ __forceinline__ int in_turn(int idx, int n, int heads) {
+  if ((int64_t)n * heads > TURN_MOST * UNITS) return idx;  // units that run dry take the next one by themselves
   const int stretch = max(1, UNITS / heads), first = idx / stretch * stretch;
   return idx / stretch % 2 ? first + min(stretch, n - first) - 1 - (idx - first) : idx;
 }
@@ -250,6 +251,13 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t src, Lds dst, uint3
                : "s"((uint32_t)(uintptr_t)dst), "v"(offset), "s"(src)
                : "memory");
 }
+// The same of 4 bytes a lane, to dst + 4 lane.
+__device__ __forceinline__ void dma4(__amdgpu_buffer_rsrc_t src, Lds dst, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :
+               : "s"((uint32_t)(uintptr_t)dst), "v"(offset), "s"(src)
+               : "memory");
+}
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 }
@@ -366,9 +374,46 @@ __device__ __forceinline__ void store4(T* p, f32x4 x) {
   *(V*)p = __builtin_convertvector(x, V);
 }
 
+// Tiles in LDS at once: the one in use and the one on its way.  (Three or four of the smaller ones cost workgroups a CU:
+// 32 x 256 tokens, 8 heads of 64, bf16, bias, us with 2 / 3 / 4: forward 20.5 / 22.4 / 25.9, dq 36 / 55 / 56, dk and dv
+// 24 / 24 / 33.)
+constexpr int STAGES = 2;
+template <typename T, int D>
+constexpr int ring_bytes() { return STAGES * 2 * KEYS * Tile<T, D>::ROW; }
 // Waves per SIMD: two; one where LDS holds one workgroup a CU.
 template <typename T, int D>
-constexpr int waves_per_simd() { return 4 * KEYS * Tile<T, D>::ROW > 80 * 1024 ? 1 : 2; }
+constexpr int waves_per_simd() { return ring_bytes<T, D>() > 80 * 1024 ? 1 : 2; }
+
+// The tiles of KEYS keys and values of a work item, passing through LDS; all waves go along together.
+template <typename T, int D>
+struct KeyRing {
+  static constexpr int BYTES = KEYS * Tile<T, D>::ROW;
+  const T *k, *v;
+  int64_t k_row, v_row;
+  Lds lds;
+  int wave, nk, end, place;
+
+  __device__ __forceinline__ KeyRing(const Args& a, const Work& w, Lds lds_, int wave_)
+      : k((const T*)a.k + w.s.k0 * a.k_row + w.head.kv * a.k_head),
+        v((const T*)a.v + w.s.k0 * a.v_row + w.head.kv * a.v_head),
+        k_row(a.k_row), v_row(a.v_row), lds(lds_), wave(wave_), nk(w.s.nk), end(w.kend), place(0) {
+    load(w.kbeg, 0);
+  }
+  __device__ __forceinline__ void load(int j0, int to) {
+    if (j0 >= end) return;
+    load_rows<T, D, KEYS, WAVES>(k, k_row, j0, nk, lds + to * 2 * BYTES, wave);
+    load_rows<T, D, KEYS, WAVES>(v, v_row, j0, nk, lds + to * 2 * BYTES + BYTES, wave);
+  }
+  // The tile from key j0 on, the next in line: keys here, values BYTES on.
+  __device__ __forceinline__ Lds next(int j0) {
+    loads_done();
+    __syncthreads();  // the tile is whole, and every wave has left the other place
+    const Lds tile = lds + place * 2 * BYTES;
+    place ^= 1;
+    load(j0 + KEYS, place);
+    return tile;
+  }
+};
 
 // ---------------------------------------------------------------------------
 // Host side.

@@ -56,9 +56,8 @@ template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention_dq(Args a, Grads o) {
   using Ti = Tile<T, D>;
   using F = typename Frag<T>::type;
-  constexpr int M = WAVES * ROWS, BYTES = KEYS * Ti::ROW;
+  constexpr int M = WAVES * ROWS;
   extern __shared__ __attribute__((aligned(256))) char smem[];
-  Lds lds = (Lds)smem;
   Work w;
   const bool found = find_work<M>(a, &w);
   float* const rel_row = o.rel + (((int64_t)w.slot * a.splits + w.split) * a.heads + w.head.first) * a.buckets;
@@ -67,6 +66,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       for (int t = threadIdx.x; t < a.buckets; t += THREADS) rel_row[t] = 0;
     return;
   }
+  KeyRing<T, D> ring(a, w, (Lds)smem, __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
   const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, first + (l & 31));
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const float* bias = nullptr;
   float far_bias[2] = {0, 0}, far_sum[2] = {0, 0};
   const int width = bias_width(a);
-  float* const table = (float*)(smem + 4 * BYTES);
+  float* const table = (float*)(smem + ring_bytes<T, D>());
   float* const sums = table + width;         // [WAVES][width]
   float* const mine = sums + wave * width;
   int* const of = (int*)(sums + WAVES * width);  // buckets
@@ -125,19 +125,8 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[b][e] = 0;
-  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.head.kv * a.k_head;
-  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.head.kv * a.v_head;
-  auto load = [&](int j0, int buf) {
-    load_rows<T, D, KEYS, WAVES>(kh, a.k_row, j0, w.s.nk, lds + buf * 2 * BYTES, wave);
-    load_rows<T, D, KEYS, WAVES>(vh, a.v_row, j0, w.s.nk, lds + buf * 2 * BYTES + BYTES, wave);
-  };
-  if (w.kbeg < w.kend) load(w.kbeg, 0);
-  int buf = 0;
-  for (int j0 = w.kbeg; j0 < w.kend; j0 += KEYS, buf ^= 1) {
-    loads_done();
-    __syncthreads();
-    if (j0 + KEYS < w.kend) load(j0 + KEYS, buf ^ 1);
-    const Lds kt = lds + buf * 2 * BYTES, vt = kt + BYTES;
+  for (int j0 = w.kbeg; j0 < w.kend; j0 += KEYS) {
+    const Lds kt = ring.next(j0), vt = kt + ring.BYTES;
 #pragma unroll
     for (int b = 0; b < KEYS / 32; ++b) {
       const int j = j0 + 32 * b;
@@ -274,12 +263,13 @@ constexpr int tile_rows() { return values_in_lds<T, D>() ? 32 : 64; }  // packed
 constexpr int DKV_KEYS = WAVES * 32;
 template <typename T, int D>
 constexpr int dkv_bytes() {
-  return 4 * tile_rows<T, D>() * Tile<T, D>::ROW + (values_in_lds<T, D>() ? DKV_KEYS * Tile<T, D>::ROW : 0);
+  return STAGES * 2 * tile_rows<T, D>() * Tile<T, D>::ROW +
+         (values_in_lds<T, D>() ? DKV_KEYS * Tile<T, D>::ROW : 0);
 }
 template <typename T, int D>
 constexpr int dkv_waves() { return dkv_bytes<T, D>() > 72 * 1024 ? 1 : 2; }  // a SIMD
-// What it keeps of a query: delta, lse, and lse less the bias below and above reach.
-enum { DELTA, LSE, BELOW, ABOVE, STATS };
+// What it keeps of a tile's queries beside them: lse and delta.
+enum { LSE, DELTA, STATS };
 
 // The key tile of a workgroup and its piece of the rows: row r is query r % nq of the group's head r / nq, and the tile meets
 // the queries from `seen` on of every head.
@@ -288,17 +278,19 @@ struct KeyWork {
   int j0, seen;
   int64_t lo, hi;
 };
-__device__ __forceinline__ bool key_work(const Args& a, int slot, int piece, KeyWork* w) {
+__device__ __forceinline__ bool key_work(const Args& a, int slot, KeyWork* w) {
   const int b = slot_sequence(a.start_k, a.tk, a.batch, 1, DKV_KEYS, slot);
   w->s = sequence(a, b);
   const int64_t from = (slot - first_slot(a.start_k, a.tk, b, 1, DKV_KEYS)) * DKV_KEYS;
   if (from >= w->s.cap) return false;
   w->j0 = (int)from;
   w->seen = w->j0 >= w->s.nk ? w->s.nq : a.causal ? max(w->j0 - (w->s.nk - w->s.nq), 0) : 0;
+  return true;
+}
+__device__ __forceinline__ void take_piece(const Args& a, int piece, KeyWork* w) {
   const int64_t rows = (int64_t)w->s.nq * a.ratio;
   w->lo = min((int64_t)piece * a.piece, rows);
   w->hi = piece < a.splits - 1 ? min(w->lo + a.piece, rows) : rows;
-  return true;
 }
 // The rows of a piece, a stretch of queries of one head at a time; begin >= end: none left.
 struct Stretch {
@@ -327,7 +319,8 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   const int tile = in_turn(blockIdx.x / a.kv_heads, a.slots * a.splits, a.kv_heads);
   const int piece = tile % a.splits, slot = tile / a.splits;  // the first keys, which most rows see, first
   KeyWork w;
-  if (!key_work(a, slot, piece, &w)) return;
+  if (!key_work(a, slot, &w)) return;
+  take_piece(a, piece, &w);
   const Seq& s = w.s;
   Stretch t = stretch_from(w, w.lo);
   const bool any = t.begin < t.end;
@@ -339,7 +332,7 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   // the wave's keys are seen by queries from `some` on, and all of them by those from `all` on
   const int some = a.causal ? jw - off : 0, all = a.causal ? jw + 31 - off : 0;
   F k[D / 16], v[VLDS ? 1 : D / 16];
-  const Lds vt = lds + 4 * BYTES;
+  const Lds vt = lds + STAGES * 2 * BYTES;
   if (VLDS && any)
     load_rows<T, D, DKV_KEYS, WAVES>((const T*)a.v + s.k0 * a.v_row + hk * a.v_head, a.v_row, w.j0, s.nk, vt, wave);
   {
@@ -352,74 +345,66 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
       if constexpr (!VLDS) v[e] = valid ? *(const F*)(vp + 16 * e) : z;
     }
   }
+  // The tiles of queries and their grad_out, passing through LDS: `next` is the next to load, into place `place`.
   const int64_t g_row = (int64_t)a.heads * D;
-  const auto load = [&](int head, int i, int end, int buf) {
-    const int hq = hk * a.ratio + head;
-    load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, i, end,
-                                  lds + buf * 2 * BYTES, wave);
-    load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, i, end,
-                                  lds + buf * 2 * BYTES + BYTES, wave);
-  };
-  // beside the tiles: [2][STATS][TROWS], then the bias table
-  float* const stats = (float*)(smem + dkv_bytes<T, D>());
-  float* const table = stats + 2 * STATS * TROWS;
+  // beside the tiles: [STAGES][STATS][TROWS], then the bias table
+  const Lds stats = lds + dkv_bytes<T, D>();
+  float* const table = (float*)(smem + dkv_bytes<T, D>()) + STAGES * STATS * TROWS;
   const int width = bias_width(a);
-  // A tile's statistics, a query to a lane of the first wave: loaded with the tile before, written when that is done.  A
-  // query past the end gets lse = inf, and with it p = 0.
-  const bool keeper = wave == 0 && l < TROWS;
-  float st_lse = 0, st_delta = 0;
-  const auto load_stats = [&](int head, int i, int end) {
-    const int64_t at = (s.q0 + i + l) * a.heads + hk * a.ratio + head;
-    st_lse = i + l < end ? o.lse[at] : INFINITY;
-    st_delta = i + l < end ? o.delta[at] : 0.0f;
+  Stretch next = t;
+  int place = 0;
+  const auto after = [&](Stretch x) {  // the tile after x
+    const int head = x.head;
+    x.begin += TROWS;
+    return x.begin < x.end ? x : stretch_from(w, (int64_t)(head + 1) * s.nq);
   };
-  const auto put_stats = [&](int head, int buf) {
-    float* to = stats + buf * STATS * TROWS + l;
-    to[DELTA * TROWS] = st_delta;
-    to[LSE * TROWS] = st_lse;
-    if constexpr (BIAS) {
-      to[BELOW * TROWS] = st_lse - table[head * width];
-      to[ABOVE * TROWS] = st_lse - table[head * width + width - 1];
+  const auto load = [&] {
+    const int hq = hk * a.ratio + next.head;
+    const Lds to = lds + place * 2 * BYTES;
+    load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, next.begin, next.end, to, wave);
+    load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, next.begin, next.end,
+                                  to + BYTES, wave);
+    if (wave < STATS && l < TROWS) {  // past the end: zeros, as in the tiles, and with them p dO = ds = 0
+      const float* const from = (wave == LSE ? o.lse : o.delta) + (s.q0 + next.begin) * a.heads + hq;
+      const int rows = min(next.end - next.begin, TROWS);
+      dma4(resource(from, (uint32_t)((rows - 1) * a.heads + 1) * 4), stats + (place * STATS + wave) * TROWS * 4,
+           (uint32_t)(l * a.heads) * 4);
     }
+    place ^= 1;
+    next = after(next);
   };
-  if (any) {
-    load(t.head, t.begin, t.end, 0);
-    if (keeper) load_stats(t.head, t.begin, t.end);
-  }
+  if (any) load();
   if constexpr (BIAS) {
     fill_bias(a, hk * a.ratio, a.ratio, table);
     __syncthreads();
   }
-  if (any && keeper) put_stats(t.head, 0);
   uint32_t ra = Ti::row_base(l & 31), ca = Ti::col_base();
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dk[b][e] = dv[b][e] = 0;
-  int buf = 0;
   while (t.begin < t.end) {
     loads_done();
     __syncthreads();
-    Stretch next = t;  // the tile after this one
-    next.begin += TROWS;
-    if (next.begin >= t.end) next = stretch_from(w, (int64_t)(t.head + 1) * s.nq);
-    const bool more = next.begin < next.end;
-    if (more) {
-      load(next.head, next.begin, next.end, buf ^ 1);
-      if (keeper) load_stats(next.head, next.begin, next.end);
-    }
+    const int in_use = place ^ 1;
+    if (next.begin < next.end)
+      load();
+    else
+      place ^= 1;
     asm volatile("" : "+v"(ra), "+v"(ca));  // the addresses are formed at their use: kept, they would not fit the registers
-    const Lds qt = lds + buf * 2 * BYTES, gt = qt + BYTES;
-    const float* const st = stats + buf * STATS * TROWS + 4 * h;
+    const Lds qt = lds + in_use * 2 * BYTES, gt = qt + BYTES;
+    const Lds st = stats + (in_use * STATS * TROWS + 4 * h) * 4;
 #pragma unroll
     for (int rb = 0; rb < TROWS / 32; ++rb) {
       const int i = t.begin + 32 * rb;
       if (jw >= s.nk || i + 31 < some || i >= t.end) continue;  // none of the queries meets the wave's keys
-      int use = LSE;  // past reach one value of the bias serves the whole block, and is in the query's statistic
+      bool near = false;  // past reach one value of the bias serves the whole block
+      float far = 0;
       if constexpr (BIAS) {
-        if (jw + 31 - (i + off) <= -a.reach) use = BELOW;
-        if (jw - (i + 31 + off) >= a.reach) use = ABOVE;
+        const bool below = jw + 31 - (i + off) <= -a.reach, above = jw - (i + 31 + off) >= a.reach;
+        near = !below && !above;
+        far = near ? 0.0f : table[t.head * width + (above ? width - 1 : 0)];
       }
       f32x16 p, ds;
 #pragma unroll
@@ -435,20 +420,22 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
       }
       float unit = a.c;
       if constexpr (BIAS) {
-        if (use == LSE) {  // entry of distance j - (i + 31) - off, the block's queries from there downwards
-          const float* at = table + t.head * width + a.reach + BIAS_PAD + j - (i + 31 + off) - 4 * h;
+        if (near) {  // entry of distance j - (i + 31) - off, the block's queries from there downwards
+          const float* from = table + t.head * width + a.reach + BIAS_PAD + j - (i + 31 + off) - 4 * h;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) p[e] = fmaf(p[e], a.c, at[31 - 8 * (e >> 2) - (e & 3)]);
+          for (int e = 0; e < 16; ++e) p[e] = fmaf(p[e], a.c, from[31 - 8 * (e >> 2) - (e & 3)]);
           unit = 1;
         }
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const f32x4 lse = *(const f32x4*)(st + use * TROWS + 32 * rb + 8 * u);
-        const f32x4 delta = *(const f32x4*)(st + DELTA * TROWS + 32 * rb + 8 * u);
+        const f32x4 lse =
+            *(const __attribute__((address_space(3))) f32x4*)(st + (LSE * TROWS + 32 * rb + 8 * u) * 4);
+        const f32x4 delta =
+            *(const __attribute__((address_space(3))) f32x4*)(st + (DELTA * TROWS + 32 * rb + 8 * u) * 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[4 * u + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * u + e], unit, -lse[e]));
+          p[4 * u + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * u + e], unit, BIAS ? far - lse[e] : -lse[e]));
           ds[4 * u + e] = p[4 * u + e] * (ds[4 * u + e] - delta[e]);
         }
       }
@@ -476,9 +463,7 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
         for (int b = 0; b < D / 32; ++b) dk[b] = mma(Ti::col_frag(qt, ca, b, 2 * rb + c), fy, dk[b]);
       }
     }
-    if (more && keeper) put_stats(next.head, buf ^ 1);
-    t = next;
-    buf ^= 1;
+    t = after(t);
   }
   if (a.splits > 1) {
     if (j >= s.nk) return;
@@ -515,31 +500,33 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
     }
 }
 
-// The pieces of a key tile's gradients added up, in their order; a workgroup to a tile and key head.
+// The pieces of a key tile's gradients added up, in their order; JOIN_PARTS workgroups to a tile and key head.
+constexpr int JOIN_PARTS = 8;
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o) {
-  const int hk = blockIdx.x % a.kv_heads, slot = blockIdx.x / a.kv_heads;
+  const int hk = blockIdx.x % a.kv_heads, part = blockIdx.x / a.kv_heads % JOIN_PARTS;
   KeyWork w;
-  if (!key_work(a, slot, 0, &w)) return;
+  if (!key_work(a, blockIdx.x / a.kv_heads / JOIN_PARTS, &w)) return;
   unsigned used = 0;  // pieces with rows that meet the tile
   for (int p = 0; p < a.splits; ++p) {
-    KeyWork x;
-    key_work(a, slot, p, &x);
-    const Stretch t = stretch_from(x, x.lo);
+    take_piece(a, p, &w);
+    const Stretch t = stretch_from(w, w.lo);
     used |= (unsigned)(t.begin < t.end) << p;
   }
-  const int keys = min(DKV_KEYS, w.s.cap - w.j0);
-  for (int t = threadIdx.x; t < keys * (2 * D / 4); t += THREADS) {
-    const int j = w.j0 + t / (2 * D / 4), d = t % (2 * D / 4) * 4;
+  constexpr int KEYS_EACH = DKV_KEYS / JOIN_PARTS, VECS = 2 * D / 4;
+  for (int t = threadIdx.x; t < KEYS_EACH * VECS; t += THREADS) {
+    const int j = w.j0 + part * KEYS_EACH + t / VECS, d = t % VECS * 4;
+    if (j >= w.s.cap) return;
     const int64_t at = (w.s.k0 + j) * a.kv_heads + hk;
     f32x4 x = {0, 0, 0, 0};
-    if (j < w.s.nk)
-      for (unsigned left = used; left; left &= left - 1) {
-        const int p = __ffs(left) - 1;
-        const f32x4 y = *(const f32x4*)(o.part + ((int64_t)p * a.tk * a.kv_heads + at) * 2 * D + d);
+#pragma unroll 4
+    for (int p = 0; p < a.splits; ++p) {
+      f32x4 y = {0, 0, 0, 0};
+      if (j < w.s.nk && (used >> p & 1))
+        y = *(const f32x4*)(o.part + ((int64_t)p * a.tk * a.kv_heads + at) * 2 * D + d);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += y[e];
-      }
+      for (int e = 0; e < 4; ++e) x[e] += y[e];
+    }
     store4<T>((d < D ? (T*)o.gk + d : (T*)o.gv + d - D) + at * D, x);
   }
 }
@@ -620,7 +607,7 @@ int go(Args x, const Grads& g, const lram_attention& d, const Plan& p, hipStream
     x.splits = p.keys.n;
     x.piece = p.keys.size;
     if (int rc = launch(k_attention_dq<T, D, BIAS>, (int64_t)(x.heads / x.group) * x.slots * x.splits,
-                        (size_t)4 * KEYS * Tile<T, D>::ROW + width * (2 + WAVES)))
+                        ring_bytes<T, D>() + width * (2 + WAVES)))
       return rc;
     if (x.splits > 1) {
       const int64_t n = x.tq * x.heads * D;
@@ -634,10 +621,10 @@ int go(Args x, const Grads& g, const lram_attention& d, const Plan& p, hipStream
     x.splits = p.rows.n;
     x.piece = p.rows.size;
     if (int rc = launch(k_attention_dkv<T, D, BIAS>, (int64_t)x.kv_heads * x.slots * x.splits,
-                        dkv_bytes<T, D>() + 2 * STATS * tile_rows<T, D>() * 4 + width * x.ratio))
+                        dkv_bytes<T, D>() + STAGES * STATS * tile_rows<T, D>() * 4 + width * x.ratio))
       return rc;
     if (x.splits > 1)
-      if (int rc = launch(k_attention_dkv_join<T, D>, (int64_t)x.kv_heads * x.slots, 0)) return rc;
+      if (int rc = launch(k_attention_dkv_join<T, D>, (int64_t)x.kv_heads * x.slots * JOIN_PARTS, 0)) return rc;
   }
   if constexpr (BIAS) {
     const auto finish = [&](auto w) {

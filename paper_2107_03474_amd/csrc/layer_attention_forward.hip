@@ -140,11 +140,11 @@ __device__ __forceinline__ void put_lse(const Args& a, const Out& o, int split, 
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention(Args a, Out o) {
   using Ti = Tile<T, D>;
-  constexpr int M = WAVES * ROWS, BYTES = KEYS * Ti::ROW;
+  constexpr int M = WAVES * ROWS;
   extern __shared__ __attribute__((aligned(256))) char smem[];
-  Lds lds = (Lds)smem;
   Work w;
   if (!find_work<M>(a, &w)) return;
+  KeyRing<T, D> ring(a, w, (Lds)smem, __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE;
   const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, first + (l & 31));
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const float* bias = nullptr;
   float near_far[2] = {0, 0};
   if constexpr (BIAS) {
-    float* table = (float*)(smem + 4 * BYTES);
+    float* table = (float*)(smem + ring_bytes<T, D>());
     fill_bias(a, w.head.first, G, table);
     bias = table + r.g * bias_width(a) + a.reach + BIAS_PAD - (r.i + off);
     __syncthreads();
@@ -170,18 +170,8 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const uint32_t ka = Ti::row_base(l & 31), va = Ti::col_base();
   Running<D> st;
   st.clear();
-  const T* kh = (const T*)a.k + w.s.k0 * a.k_row + w.head.kv * a.k_head;
-  const T* vh = (const T*)a.v + w.s.k0 * a.v_row + w.head.kv * a.v_head;
-  auto load = [&](int j0, int buf) {
-    load_rows<T, D, KEYS, WAVES>(kh, a.k_row, j0, w.s.nk, lds + buf * 2 * BYTES, wave);
-    load_rows<T, D, KEYS, WAVES>(vh, a.v_row, j0, w.s.nk, lds + buf * 2 * BYTES + BYTES, wave);
-  };
-  if (w.kbeg < w.kend) load(w.kbeg, 0);
-  int buf = 0;
-  for (int j0 = w.kbeg; j0 < w.kend; j0 += KEYS, buf ^= 1) {
-    loads_done();
-    __syncthreads();  // this tile is whole, and every wave has left the other buffer
-    if (j0 + KEYS < w.kend) load(j0 + KEYS, buf ^ 1);
+  for (int j0 = w.kbeg; j0 < w.kend; j0 += KEYS) {
+    const Lds tile = ring.next(j0);
     if (j0 > lim_last) continue;
     const bool masked = j0 + KEYS - 1 > lim_first;
     bool whole = false;
@@ -191,7 +181,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       whole = below || above;
       far = near_far[above];
     }
-    attend<T, D, KEYS / 32, BIAS>(st, q, lds + buf * 2 * BYTES, lds + buf * 2 * BYTES + BYTES, ka, va, a.c, j0, lim,
+    attend<T, D, KEYS / 32, BIAS>(st, q, tile, tile + ring.BYTES, ka, va, a.c, j0, lim,
                                   masked, bias, !whole, far);
   }
   if (!r.valid) return;
@@ -398,7 +388,7 @@ int go(Args x, const Out& o, const Plan& p, hipStream_t s) {
     rc = launch(k_attention_few<T, D, BIAS>,
                 std::max<size_t>(few_bytes<T, D>(), WAVES * ROWS * (D * 4 + 16 + 8)) + table);
   else
-    rc = launch(k_attention<T, D, BIAS>, (size_t)4 * KEYS * Tile<T, D>::ROW + table);
+    rc = launch(k_attention<T, D, BIAS>, ring_bytes<T, D>() + table);
   if (rc || x.splits == 1) return rc;
   const int64_t threads = x.tq * x.heads * (D / 4);
   hipLaunchKernelGGL((k_attention_join<T, D>), dim3((unsigned)((threads + THREADS - 1) / THREADS)), dim3(THREADS), 0, s,
