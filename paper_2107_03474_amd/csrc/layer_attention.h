@@ -81,15 +81,41 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b) {
   return s;
 }
 
-// Which sequence a tile belongs to, without knowing the lengths on the host: sequence b's tiles of `tile` units (scale
-// units per row) take the slots from start[b] scale / tile + b on, which leaves each at least as many as it needs and
-// ends before rows scale / tile + batch + 1; a slot past its sequence's last tile is empty.  Found by a wave that looks
-// at 64 places at once: a workgroup of a short sequence would wait longer for a bisection's loads than it works.
+// Which sequence and which of its tiles a slot of the grid is, without knowing the lengths on the host.  A tile holds `tile`
+// units, of which a row of `start` has `scale`.  The grid has rows scale / tile + batch + 1 slots, at least as many as
+// there are tiles; those left over are empty.
+//
+// Up to 63 sequences, a lane for each (and one for the rows past the last): the longest sequences first, ties by their
+// order, so that the workgroups that start last are short (8 packed texts of 1 to 4,321, 16/4 heads of 128, us in the
+// batch's order and this one: forward 127 / F1, dq 158 / F2, dk and dv 259 / F3).  More sequences: sequence b takes
+// the slots from start[b] scale / tile + b on, which leaves each as many as it needs, and is found by a wave that looks at
+// 64 places at once.
+struct Place {
+  int b;
+  int64_t tile;  // past the sequence's last one: an empty slot
+};
 __device__ __forceinline__ int64_t first_slot(const int32_t* start, int64_t rows, int b, int scale, int tile) {
   return (b ? clamp64(start[b], 0, rows) : 0) * scale / tile + b;
 }
-__device__ __forceinline__ int slot_sequence(const int32_t* start, int64_t rows, int batch, int scale, int tile,
-                                             int64_t slot) {
+__device__ __forceinline__ Place place_of(const int32_t* start, int64_t rows, int batch, int scale, int tile, int slot) {
+  if (batch < WAVE) {
+    const int lane = threadIdx.x % WAVE;
+    int mine = 0;
+    if (lane <= batch) {
+      const int64_t from = lane ? clamp64(start[lane], 0, rows) : 0;
+      const int64_t to = lane < batch ? clamp64(start[lane + 1], from, rows) : rows;
+      mine = (int)(((to - from) * scale + tile - 1) / tile);
+    }
+    int first = 0;
+    for (int b = 0; b <= batch; ++b) {
+      const int other = __builtin_amdgcn_readlane(mine, b);
+      first += other > mine || (other == mine && b < lane) ? other : 0;
+    }
+    const uint64_t at = __builtin_amdgcn_ballot_w64(lane <= batch && first <= slot && slot - first < mine);
+    if (!at) return {0, INT64_MAX / 2 / tile};
+    const int b = __ffsll((unsigned long long)at) - 1;
+    return {b, slot - __builtin_amdgcn_readlane(first, b)};
+  }
   int lo = 0, n = batch + 1;  // the last b of lo ... lo + n - 1 with first_slot(b) <= slot
   while (n > 1) {
     const int step = (n + WAVE - 1) / WAVE, b = lo + (int)(threadIdx.x % WAVE) * step;
@@ -98,7 +124,7 @@ __device__ __forceinline__ int slot_sequence(const int32_t* start, int64_t rows,
     lo += past;
     n = min(step, n - past);
   }
-  return lo;
+  return {lo, slot - first_slot(start, rows, lo, scale, tile)};
 }
 
 // The grid's order: tiles of falling length (causal), but every second stretch of as many workgroups as there are compute
@@ -349,11 +375,13 @@ __device__ __forceinline__ bool find_work(const Args& a, Work* w) {
   w->head = heads_of(a, blockIdx.x % n);
   const int tile = in_turn(blockIdx.x / n, a.slots * a.splits, n);
   w->split = tile % a.splits;
-  const int slot = w->slot = a.slots - 1 - tile / a.splits;  // long causal rows first
-  const int b = slot_sequence(a.start_q, a.tq, a.batch, a.group, M, slot);
-  w->s = sequence(a, b);
-  const int64_t row0 = (slot - first_slot(a.start_q, a.tq, b, a.group, M)) * M;
-  if (row0 >= (int64_t)w->s.nq * a.group) return false;
+  w->slot = tile / a.splits;
+  const Place at = place_of(a.start_q, a.tq, a.batch, a.group, M, w->slot);
+  w->s = sequence(a, at.b);
+  // a sequence's last rows, which see most keys (causal), first
+  const int64_t tiles = ((int64_t)w->s.nq * a.group + M - 1) / M;
+  if (at.tile >= tiles) return false;
+  const int64_t row0 = (tiles - 1 - at.tile) * M;
   w->row0 = (int)row0;
   const int rows = w->s.nq * a.group;
   const int last = (w->row0 + M < rows ? w->row0 + M : rows) - 1;

@@ -20,7 +20,7 @@ namespace {
 
 // The value of the lane before, going round the wave.
 __device__ __forceinline__ float next_lane(float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x13c, 0xf, 0xf, false));
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x13c, 0xf, 0xf, true));
 }
 
 struct Grads {
@@ -279,9 +279,9 @@ struct KeyWork {
   int64_t lo, hi;
 };
 __device__ __forceinline__ bool key_work(const Args& a, int slot, KeyWork* w) {
-  const int b = slot_sequence(a.start_k, a.tk, a.batch, 1, DKV_KEYS, slot);
-  w->s = sequence(a, b);
-  const int64_t from = (slot - first_slot(a.start_k, a.tk, b, 1, DKV_KEYS)) * DKV_KEYS;
+  const Place at = place_of(a.start_k, a.tk, a.batch, 1, DKV_KEYS, slot);
+  w->s = sequence(a, at.b);
+  const int64_t from = at.tile * DKV_KEYS;
   if (from >= w->s.cap) return false;
   w->j0 = (int)from;
   w->seen = w->j0 >= w->s.nk ? w->s.nq : a.causal ? max(w->j0 - (w->s.nk - w->s.nq), 0) : 0;
@@ -555,15 +555,16 @@ __global__ __launch_bounds__(REL_THREADS) void k_relative_grad(const float* rel,
 }
 
 // How the two kernels divide the work: keys (dq) and rows (dk, dv) come in pieces where the tiles are few against the chip
-// (about four workgroups a CU are wanted), none shorter than 1,024 (128 in fp32, whose products take sixteen times as
-// long).
+// (about 1,024 workgroups are wanted, and 1,536 for the rows in bf16), none shorter than 1,024 (128 in fp32, whose
+// products take sixteen times as long).  dk and dv with the join, 8 packed texts of 1 to 4,321, 16/4 heads of 128, us for
+// 1,024 / 1,536 / 2,048 / 3,072: 306 / 282 / 292 / 313.
 constexpr int MAX_PIECES = 16;
 struct Pieces {
   int n, size;
 };
-Pieces pieces_of(int64_t tiles, int64_t length, int dtype) {
+Pieces pieces_of(int64_t tiles, int64_t length, int dtype, int64_t groups) {
   const int64_t shortest = dtype == LRAM_F32 ? 128 : 1024;
-  const int64_t wanted = tiles > 0 ? 1024 / tiles : 1;
+  const int64_t wanted = tiles > 0 ? groups / tiles : 1;
   const int64_t n = std::max<int64_t>(1, std::min<int64_t>({wanted, (length + shortest - 1) / shortest, MAX_PIECES}));
   const int64_t size = std::max<int64_t>(64, ((length + n - 1) / n + 63) / 64 * 64);
   return {(int)std::max<int64_t>(1, std::min(n, (length + size - 1) / size)), (int)std::min<int64_t>(size, 1 << 30)};
@@ -582,8 +583,8 @@ Plan plan_of(const lram_attention& a) {
   const auto tiles = [&](int64_t longest, int64_t slots) {
     return std::min<int64_t>((int64_t)a.batch * ((longest + 127) / 128), slots);
   };
-  p.keys = pieces_of(tiles(a.max_q * p.group, p.row_slots) * (a.heads / p.group), a.max_k, a.dtype);
-  p.rows = pieces_of(tiles(a.max_k, p.key_slots) * a.kv_heads, a.max_q * G, a.dtype);
+  p.keys = pieces_of(tiles(a.max_q * p.group, p.row_slots) * (a.heads / p.group), a.max_k, a.dtype, 1024);
+  p.rows = pieces_of(tiles(a.max_k, p.key_slots) * a.kv_heads, a.max_q * G, a.dtype, a.dtype == LRAM_F32 ? 1024 : 1536);
   p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written

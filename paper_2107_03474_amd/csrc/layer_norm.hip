@@ -257,12 +257,23 @@ Shape shape_of(int64_t width, int dtype) {
   return {16 * WAVE, chunks <= 32 * WAVE ? 2 : 4};
 }
 
+// The backward pass holds three rows and the weights' sums, so its rows take more threads with a chunk each (16,384 rows of
+// 8,192 bf16 with grad_sum: 256 threads with four chunks each 526 us, 1,024 with one 222 us).
+Shape backward_shape_of(int64_t width, int dtype) {
+  const int64_t chunks = (width + CHUNK_BYTES / (int)elem_size(dtype) - 1) / (CHUNK_BYTES / (int)elem_size(dtype));
+  if (chunks <= 2 * WAVE) return {WAVE, chunks <= WAVE ? 1 : 2};
+  for (int G : {4 * WAVE, 8 * WAVE, 16 * WAVE})
+    if (chunks <= G) return {G, 1};
+  return {16 * WAVE, chunks <= 32 * WAVE ? 2 : 4};
+}
+
 // Workgroups of the backward pass: enough to keep HBM busy, and few against the rows, since each leaves a partial row
-// of its own for the second kernel.
+// of its own for the second kernel (us of both kernels with half, as many and twice as many: 8,192 x 512 bf16 13.9 / 12.8 /
+// 17.8, 5,003 x 1,021 fp32 21.7 / 20.4 / 24.0, 16,384 x 8,192 bf16 382 / 230 / 236).
 int64_t groups_of(int64_t rows, const Shape& sh) {
   const int64_t teams = sh.G == WAVE ? NORM_WAVES : 1;
   const int64_t all = (rows + teams - 1) / teams;
-  const int64_t most = sh.G > 4 * WAVE ? 512 : 1024;
+  const int64_t most = sh.G > 4 * WAVE ? 4096 * WAVE / sh.G : 1024;
   return all < most ? all : most;
 }
 
@@ -272,7 +283,7 @@ int by_shape(const Shape& sh, F f) {
   if (sh.G == g && sh.NC == n) return f(std::integral_constant<int, g>(), std::integral_constant<int, n>());
   LRAM_SHAPE(64, 1) LRAM_SHAPE(64, 2) LRAM_SHAPE(64, 4)
   LRAM_SHAPE(256, 1) LRAM_SHAPE(256, 2) LRAM_SHAPE(256, 4)
-  LRAM_SHAPE(1024, 2) LRAM_SHAPE(1024, 4)
+  LRAM_SHAPE(512, 1) LRAM_SHAPE(1024, 1) LRAM_SHAPE(1024, 2) LRAM_SHAPE(1024, 4)
 #undef LRAM_SHAPE
   return LRAM_EINVAL;
 }
@@ -340,7 +351,7 @@ int lram_layer_norm_forward(const void* x, const void* residual, const void* wei
 int lram_layer_norm_backward_workspace_bytes(int64_t rows, int64_t width, int dtype, size_t* bytes) {
   if (!bytes) return LRAM_EINVAL;
   if (int rc = check_norm(dtype, LRAM_F32, rows, width)) return rc;
-  const int64_t n = groups_of(rows, shape_of(width, dtype));
+  const int64_t n = groups_of(rows, backward_shape_of(width, dtype));
   *bytes = n > 1 ? (size_t)n * 2 * width * 4 : 0;
   return LRAM_OK;
 }
@@ -358,7 +369,7 @@ int lram_layer_norm_backward(const void* h, const void* weight, const float* mea
       off_align(mean, 4) || off_align(rstd, 4) || off_align(weight, elem_size(wdtype)) ||
       off_align(grad_weight, elem_size(wdtype)) || off_align(grad_bias, elem_size(wdtype)))
     return LRAM_EINVAL;
-  const Shape sh = shape_of(width, dtype);
+  const Shape sh = backward_shape_of(width, dtype);
   const int64_t groups = groups_of(rows, sh);
   const bool two = grad_weight && groups > 1;
   if (two && (!workspace || off_align(workspace, 16) || ws_bytes < (size_t)groups * 2 * width * 4))
