@@ -271,12 +271,14 @@ constexpr int dkv_waves() { return dkv_bytes<T, D>() > 72 * 1024 ? 1 : 2; }  // 
 // What it keeps of a tile's queries beside them: lse and delta.
 enum { LSE, DELTA, STATS };
 
-// The key tile of a workgroup and its piece of the rows: row r is query r % nq of the group's head r / nq, and the tile meets
-// the queries from `seen` on of every head.
+// The key tile of a workgroup and its piece of the queries, lo to hi (lo >= hi: none meets the tile).  It walks from the last
+// queries to the first, and over the heads of its group at each: the workgroups of a sequence that run side by side read
+// the same rows at the same time, whatever the first query is that sees their keys, and share them in their L2 (2 x 8,192
+// causal tokens, 32/8 heads of 128: head by head from the first query on 64 % of the reads missed it, M1).
 struct KeyWork {
   Seq s;
-  int j0, seen;
-  int64_t lo, hi;
+  int j0, seen;  // queries from `seen` on see a key of the tile
+  int lo, hi;
 };
 __device__ __forceinline__ bool key_work(const Args& a, int slot, KeyWork* w) {
   const Place at = place_of(a.start_k, a.tk, a.batch, 1, DKV_KEYS, slot);
@@ -288,23 +290,9 @@ __device__ __forceinline__ bool key_work(const Args& a, int slot, KeyWork* w) {
   return true;
 }
 __device__ __forceinline__ void take_piece(const Args& a, int piece, KeyWork* w) {
-  const int64_t rows = (int64_t)w->s.nq * a.ratio;
-  w->lo = min((int64_t)piece * a.piece, rows);
-  w->hi = piece < a.splits - 1 ? min(w->lo + a.piece, rows) : rows;
-}
-// The rows of a piece, a stretch of queries of one head at a time; begin >= end: none left.
-struct Stretch {
-  int head, begin, end;
-};
-__device__ __forceinline__ Stretch stretch_from(const KeyWork& w, int64_t row) {
-  Stretch t{0, 0, 0};
-  if (w.s.nq == 0 || w.seen >= w.s.nq || row >= w.hi) return t;
-  t.head = (int)(row / w.s.nq);
-  t.begin = max((int)(row - (int64_t)t.head * w.s.nq), w.seen);
-  t.end = (int)min(w.hi - (int64_t)t.head * w.s.nq, (int64_t)w.s.nq);
-  if (t.begin < t.end) return t;
-  // the piece ends before the first query that sees the tile
-  return Stretch{0, 0, 0};
+  const int64_t lo = (int64_t)piece * a.piece;
+  w->hi = piece < a.splits - 1 ? (int)min(lo + a.piece, (int64_t)w->s.nq) : w->s.nq;
+  w->lo = (int)min((int64_t)max(w->seen, (int)min(lo, (int64_t)w->s.nq)), (int64_t)w->hi);
 }
 
 template <typename T, int D, bool BIAS>
@@ -322,8 +310,7 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   if (!key_work(a, slot, &w)) return;
   take_piece(a, piece, &w);
   const Seq& s = w.s;
-  Stretch t = stretch_from(w, w.lo);
-  const bool any = t.begin < t.end;
+  const bool any = w.lo < w.hi;
   if (a.splits > 1 && !any) return;  // k_attention_dkv_join leaves it out
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
   const int off = s.nk - s.nq;
@@ -345,33 +332,31 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
       if constexpr (!VLDS) v[e] = valid ? *(const F*)(vp + 16 * e) : z;
     }
   }
-  // The tiles of queries and their grad_out, passing through LDS: `next` is the next to load, into place `place`.
-  const int64_t g_row = (int64_t)a.heads * D;
+  // The tiles of queries and their grad_out pass through LDS; queries i0 ... of head g, the next to load (into place
+  // `place`) and the one in use.
   // beside the tiles: [STAGES][STATS][TROWS], then the bias table
   const Lds stats = lds + dkv_bytes<T, D>();
   float* const table = (float*)(smem + dkv_bytes<T, D>()) + STAGES * STATS * TROWS;
   const int width = bias_width(a);
-  Stretch next = t;
-  int place = 0;
-  const auto after = [&](Stretch x) {  // the tile after x
-    const int head = x.head;
-    x.begin += TROWS;
-    return x.begin < x.end ? x : stretch_from(w, (int64_t)(head + 1) * s.nq);
-  };
+  const int64_t g_row = (int64_t)a.heads * D;
+  const int top = (w.hi - 1) / TROWS * TROWS;
+  int place = 0, next_i = top, next_g = 0;
   const auto load = [&] {
-    const int hq = hk * a.ratio + next.head;
+    const int hq = hk * a.ratio + next_g;
     const Lds to = lds + place * 2 * BYTES;
-    load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, next.begin, next.end, to, wave);
-    load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, next.begin, next.end,
-                                  to + BYTES, wave);
+    load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, next_i, w.hi, to, wave);
+    load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, next_i, w.hi, to + BYTES, wave);
     if (wave < STATS && l < TROWS) {  // past the end: zeros, as in the tiles, and with them p dO = ds = 0
-      const float* const from = (wave == LSE ? o.lse : o.delta) + (s.q0 + next.begin) * a.heads + hq;
-      const int rows = min(next.end - next.begin, TROWS);
+      const float* const from = (wave == LSE ? o.lse : o.delta) + (s.q0 + next_i) * a.heads + hq;
+      const int rows = min(w.hi - next_i, TROWS);
       dma4(resource(from, (uint32_t)((rows - 1) * a.heads + 1) * 4), stats + (place * STATS + wave) * TROWS * 4,
            (uint32_t)(l * a.heads) * 4);
     }
     place ^= 1;
-    next = after(next);
+    if (++next_g == a.ratio) {
+      next_g = 0;
+      next_i -= TROWS;
+    }
   };
   if (any) load();
   if constexpr (BIAS) {
@@ -384,11 +369,12 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dk[b][e] = dv[b][e] = 0;
-  while (t.begin < t.end) {
+  int i0 = top, g = 0;
+  while (any && i0 + TROWS > w.lo) {
     loads_done();
     __syncthreads();
     const int in_use = place ^ 1;
-    if (next.begin < next.end)
+    if (next_i + TROWS > w.lo)
       load();
     else
       place ^= 1;
@@ -397,14 +383,14 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
     const Lds st = stats + (in_use * STATS * TROWS + 4 * h) * 4;
 #pragma unroll
     for (int rb = 0; rb < TROWS / 32; ++rb) {
-      const int i = t.begin + 32 * rb;
-      if (jw >= s.nk || i + 31 < some || i >= t.end) continue;  // none of the queries meets the wave's keys
+      const int i = i0 + 32 * rb;
+      if (jw >= s.nk || i + 31 < some || i >= w.hi) continue;  // none of the queries meets the wave's keys
       bool near = false;  // past reach one value of the bias serves the whole block
       float far = 0;
       if constexpr (BIAS) {
         const bool below = jw + 31 - (i + off) <= -a.reach, above = jw - (i + 31 + off) >= a.reach;
         near = !below && !above;
-        far = near ? 0.0f : table[t.head * width + (above ? width - 1 : 0)];
+        far = near ? 0.0f : table[g * width + (above ? width - 1 : 0)];
       }
       f32x16 p, ds;
 #pragma unroll
@@ -421,7 +407,7 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
       float unit = a.c;
       if constexpr (BIAS) {
         if (near) {  // entry of distance j - (i + 31) - off, the block's queries from there downwards
-          const float* from = table + t.head * width + a.reach + BIAS_PAD + j - (i + 31 + off) - 4 * h;
+          const float* from = table + g * width + a.reach + BIAS_PAD + j - (i + 31 + off) - 4 * h;
 #pragma unroll
           for (int e = 0; e < 16; ++e) p[e] = fmaf(p[e], a.c, from[31 - 8 * (e >> 2) - (e & 3)]);
           unit = 1;
@@ -463,7 +449,10 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
         for (int b = 0; b < D / 32; ++b) dk[b] = mma(Ti::col_frag(qt, ca, b, 2 * rb + c), fy, dk[b]);
       }
     }
-    t = after(t);
+    if (++g == a.ratio) {
+      g = 0;
+      i0 -= TROWS;
+    }
   }
   if (a.splits > 1) {
     if (j >= s.nk) return;
@@ -510,8 +499,7 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
   unsigned used = 0;  // pieces with rows that meet the tile
   for (int p = 0; p < a.splits; ++p) {
     take_piece(a, p, &w);
-    const Stretch t = stretch_from(w, w.lo);
-    used |= (unsigned)(t.begin < t.end) << p;
+    used |= (unsigned)(w.lo < w.hi) << p;
   }
   constexpr int KEYS_EACH = DKV_KEYS / JOIN_PARTS, VECS = 2 * D / 4;
   for (int t = threadIdx.x; t < KEYS_EACH * VECS; t += THREADS) {
@@ -562,10 +550,12 @@ constexpr int MAX_PIECES = 16;
 struct Pieces {
   int n, size;
 };
-Pieces pieces_of(int64_t tiles, int64_t length, int dtype, int64_t groups) {
+// rows: units of work that one of `length` stands for.
+Pieces pieces_of(int64_t tiles, int64_t length, int rows, int dtype, int64_t groups) {
   const int64_t shortest = dtype == LRAM_F32 ? 128 : 1024;
   const int64_t wanted = tiles > 0 ? groups / tiles : 1;
-  const int64_t n = std::max<int64_t>(1, std::min<int64_t>({wanted, (length + shortest - 1) / shortest, MAX_PIECES}));
+  const int64_t n = std::max<int64_t>(
+      1, std::min<int64_t>({wanted, (length * rows + shortest - 1) / shortest, (length + 63) / 64, MAX_PIECES}));
   const int64_t size = std::max<int64_t>(64, ((length + n - 1) / n + 63) / 64 * 64);
   return {(int)std::max<int64_t>(1, std::min(n, (length + size - 1) / size)), (int)std::min<int64_t>(size, 1 << 30)};
 }
@@ -583,8 +573,8 @@ Plan plan_of(const lram_attention& a) {
   const auto tiles = [&](int64_t longest, int64_t slots) {
     return std::min<int64_t>((int64_t)a.batch * ((longest + 127) / 128), slots);
   };
-  p.keys = pieces_of(tiles(a.max_q * p.group, p.row_slots) * (a.heads / p.group), a.max_k, a.dtype, 1024);
-  p.rows = pieces_of(tiles(a.max_k, p.key_slots) * a.kv_heads, a.max_q * G, a.dtype, a.dtype == LRAM_F32 ? 1024 : 1536);
+  p.keys = pieces_of(tiles(a.max_q * p.group, p.row_slots) * (a.heads / p.group), a.max_k, 1, a.dtype, 1024);
+  p.rows = pieces_of(tiles(a.max_k, p.key_slots) * a.kv_heads, a.max_q, (int)G, a.dtype, a.dtype == LRAM_F32 ? 1024 : 1536);
   p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written
