@@ -443,6 +443,46 @@ struct KeyRing {
   }
 };
 
+// The same with the keys one tile ahead of the values.
+template <typename T, int D>
+struct KeyAhead {
+  static constexpr int BYTES = KEYS * Tile<T, D>::ROW;
+  const T *k, *v;
+  int64_t k_row, v_row;
+  Lds lds;
+  int wave, nk, end, place;  // of the values in use, and of the next keys to be loaded
+
+  __device__ __forceinline__ KeyAhead(const Args& a, const Work& w, Lds lds_, int wave_)
+      : k((const T*)a.k + w.s.k0 * a.k_row + w.head.kv * a.k_head),
+        v((const T*)a.v + w.s.k0 * a.v_row + w.head.kv * a.v_head),
+        k_row(a.k_row), v_row(a.v_row), lds(lds_), wave(wave_), nk(w.s.nk), end(w.kend), place(1) {
+    load_k(w.kbeg, 0);
+    load_v(w.kbeg, 0);
+    load_k(w.kbeg + KEYS, 1);
+  }
+  __device__ __forceinline__ void load_k(int j0, int to) {
+    if (j0 < end) load_rows<T, D, KEYS, WAVES>(k, k_row, j0, nk, lds + to * BYTES, wave);
+  }
+  __device__ __forceinline__ void load_v(int j0, int to) {
+    if (j0 < end) load_rows<T, D, KEYS, WAVES>(v, v_row, j0, nk, lds + (2 + to) * BYTES, wave);
+  }
+  __device__ __forceinline__ Lds first() {
+    loads_done();
+    __syncthreads();
+    return lds;
+  }
+  // The tile from key j0 on becomes the one in use.
+  __device__ __forceinline__ void next(int j0) {
+    loads_done();
+    __syncthreads();  // its values and the next one's keys are whole; every wave has left the other places
+    place ^= 1;
+    load_k(j0 + 2 * KEYS, place);
+    load_v(j0 + KEYS, place ^ 1);
+  }
+  __device__ __forceinline__ Lds keys() const { return lds + (place ^ 1) * BYTES; }  // of the tile after it
+  __device__ __forceinline__ Lds values() const { return lds + (2 + place) * BYTES; }
+};
+
 // ---------------------------------------------------------------------------
 // Host side.
 

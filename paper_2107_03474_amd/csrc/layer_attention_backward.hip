@@ -35,21 +35,18 @@ struct Grads {
 // holds the sum over lane c's key k with c + 7 - k = p.
 __device__ __forceinline__ float diagonals(float k0, float k1, float k2, float k3) {
   const float keys[4] = {k0, k1, k2, k3};
-  float half[2] = {0, 0};  // keys 0..3 and 4..7: the lower and the upper half's lanes, each with zeros beside them
+  float part[8];  // a key each: its rows in the lower half's lanes, zeros beside them
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, keys[e]), 0, false, false);
     const unsigned lower = r[0], upper = r[1];
-    if (e) {
-      half[0] = next_lane(half[0]);
-      half[1] = next_lane(half[1]);
-    }
-    half[0] += __builtin_bit_cast(float, lower);
-    half[1] += __builtin_bit_cast(float, upper);
+    part[e] = __builtin_bit_cast(float, lower);
+    part[4 + e] = __builtin_bit_cast(float, upper);
   }
+  float sum = part[0];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) half[0] = next_lane(half[0]);
-  return half[0] + half[1];
+  for (int k = 1; k < 8; ++k) sum = next_lane(sum) + part[k];
+  return sum;
 }
 
 template <typename T, int D, bool BIAS>
@@ -171,12 +168,13 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
         } else {
           // entry of distance (j + 8 u) - (first + off), and lane p holds the distance 7 - p more
           float* const t = mine + a.reach + BIAS_PAD + j - (first + off) + 7 - l;
+          float sum[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const float sum = diagonals(s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]);
-            if (l < 39)
-              __hip_atomic_fetch_add(t + 8 * u, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-          }
+          for (int u = 0; u < 4; ++u) sum[u] = diagonals(s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]);
+          if (l < 39)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              __hip_atomic_fetch_add(t + 8 * u, sum[u], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         }
       }
 #pragma unroll

@@ -38,48 +38,67 @@ struct Running {
   }
 };
 
-// N blocks of 32 keys from key j0 on, at `kt` and `vt` in LDS.  lim: the last key that the lane's row sees; masked: some row
-// of the wave does not see every key of the tile.  near: the bias differs from pair to pair, and `bias` is the lane's
-// row of its table at distance -(i + off); else one value of it, `far`, serves the whole tile.
-template <typename T, int D, int N, bool BIAS>
-__device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::type (&q)[D / 16], Lds kt, Lds vt,
-                                       uint32_t ka, uint32_t va, float c, int j0, int lim, bool masked,
-                                       const float* bias, bool near, float far) {
-  using Ti = Tile<T, D>;
+// Scores of 32 keys (a block of rows of the tile at kt) with the wave's 32 rows.
+template <typename T, int D>
+__device__ __forceinline__ f32x16 scores(const typename Frag<T>::type (&q)[D / 16], Lds kt, uint32_t ka, int first_key) {
+  f32x16 s;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = 0;
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) s = mma(Tile<T, D>::row_frag(kt, ka, k, first_key), q[k], s);
+  return s;
+}
+
+// Asks the compiler to spread a step's matrix instructions over its vector instructions and LDS reads: a block's products
+// with the keys, each followed by six vector instructions of the weights, then those with the values.  (8,192 causal
+// tokens, 16/8 heads of 64, bias: 191 -> 183 us; with heads of 128 the compiler's own order is the faster: 555 us, 585 with
+// this one.)
+template <typename T, int D>
+__device__ __forceinline__ void interleave() {
+  if constexpr (sizeof(T) == 2 && D <= 64) {
+    constexpr int MFMA = 0x8, VALU = 0x2, DS_READ = 0x100;
+    __builtin_amdgcn_sched_group_barrier(DS_READ, 2, 0);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(VALU, 6, 0);
+      __builtin_amdgcn_sched_group_barrier(DS_READ, 1, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      __builtin_amdgcn_sched_group_barrier(DS_READ, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(VALU, 1, 0);
+    }
+  }
+}
+
+// What a wave adds to scores of the 32 keys from j on: z = unit s + far after it.  near: the bias differs from pair to pair, and
+// `bias` is the lane's row of its table at distance -(i + off); else one value of it, `far`, serves the block.
+// masked: some row of the wave does not see every key; lim: the last key that the lane's row sees.
+template <bool BIAS>
+__device__ __forceinline__ void prepare(f32x16& s, float c, int j, const float* bias, bool near, bool masked, int lim) {
   const int h = threadIdx.x >> 5 & 1;
-  f32x16 s[N];
-#pragma unroll
-  for (int b = 0; b < N; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[b][r] = 0;
-#pragma unroll
-  for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-    for (int b = 0; b < N; ++b) s[b] = mma(Ti::row_frag(kt, ka, k, 32 * b), q[k], s[b]);
-  float unit = c;  // z = unit s + far
   if constexpr (BIAS) {
     if (near) {
-      const float* at = bias + j0 + 4 * h;
+      const float* at = bias + j + 4 * h;
 #pragma unroll
-      for (int b = 0; b < N; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] = fmaf(s[b][r], c, at[32 * b + 8 * (r >> 2) + (r & 3)]);
-      unit = 1;
-      far = 0;
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], c, at[8 * (r >> 2) + (r & 3)]);
     }
   }
   if (masked) {
-    const int last = lim - j0 - 4 * h;
+    const int last = lim - j - 4 * h;
 #pragma unroll
-    for (int b = 0; b < N; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r >> 2) + (r & 3) <= last ? s[b][r] : -INFINITY;
+    for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) <= last ? s[r] : -INFINITY;
   }
-  float top = s[0][0];
+}
+
+// The running maximum after a block's scores; the sums are rescaled if it grew by more than GROWTH in some row.
+template <int D>
+__device__ __forceinline__ void grow(Running<D>& st, const f32x16& s, float unit, float far) {
+  float top = s[0];
 #pragma unroll
-  for (int b = 0; b < N; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
   top = fmaf(max_halves(top), unit, far);
   if (__builtin_amdgcn_ballot_w64(top > st.m + GROWTH)) {
     const float m = fmaxf(st.m, top);
@@ -91,24 +110,33 @@ __device__ __forceinline__ void attend(Running<D>& st, const typename Frag<T>::t
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[b][r] *= a;
   }
+}
+
+// The weights of a block, in place of its scores.
+template <int D>
+__device__ __forceinline__ void weigh(Running<D>& st, f32x16& s, float unit, float far) {
   const float less = far - (st.m == -INFINITY ? 0.0f : st.m);
   float l = 0;
 #pragma unroll
-  for (int b = 0; b < N; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], unit, less));
-      l += s[b][r];
-    }
+  for (int r = 0; r < 16; ++r) {
+    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit, less));
+    l += s[r];
+  }
   st.l += l;
+}
+
+// The block's weights times its values, rows first_key ... of the tile at vt (a multiple of 32).
+template <typename T, int D>
+__device__ __forceinline__ void collect(Running<D>& st, const f32x16& s, Lds vt, uint32_t va, int first_key) {
 #pragma unroll
-  for (int k = 0; k < 2 * N; ++k) {
+  for (int k = 0; k < 2; ++k) {
     f32x8 p;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = s[k / 2][8 * (k % 2) + e];
+    for (int e = 0; e < 8; ++e) p[e] = s[8 * k + e];
     const auto f = to_frag<T>(p);
 #pragma unroll
-    for (int b = 0; b < D / 32; ++b) st.o[b] = mma(Ti::col_frag(vt, va, b, k), f, st.o[b]);
+    for (int b = 0; b < D / 32; ++b)
+      st.o[b] = mma(Tile<T, D>::col_frag(vt, va, b, first_key / 16 + k), f, st.o[b]);
   }
 }
 
@@ -144,7 +172,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   extern __shared__ __attribute__((aligned(256))) char smem[];
   Work w;
   if (!find_work<M>(a, &w)) return;
-  KeyRing<T, D> ring(a, w, (Lds)smem, __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE));
+  KeyAhead<T, D> ring(a, w, (Lds)smem, __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE;
   const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, first + (l & 31));
@@ -170,19 +198,45 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const uint32_t ka = Ti::row_base(l & 31), va = Ti::col_base();
   Running<D> st;
   st.clear();
-  for (int j0 = w.kbeg; j0 < w.kend; j0 += KEYS) {
-    const Lds tile = ring.next(j0);
-    if (j0 > lim_last) continue;
-    const bool masked = j0 + KEYS - 1 > lim_first;
-    bool whole = false;
-    float far = 0;
-    if constexpr (BIAS) {
-      const bool below = j0 + KEYS - 1 - (i_first + off) <= -a.reach, above = j0 - (i_last + off) >= a.reach;
-      whole = below || above;
-      far = near_far[above];
+  // The scores of a tile are formed one tile ahead, between the weights of this one: the matrix cores and the vector
+  // units work at the same time.
+  f32x16 s[KEYS / 32], next[KEYS / 32];
+  const auto tile = [&](int j0, Lds kt, Lds vt, auto more) {
+#pragma unroll
+    for (int b = 0; b < KEYS / 32; ++b) {
+      const int j = j0 + 32 * b;
+      bool near = false;
+      float far = 0;
+      if constexpr (BIAS) {
+        const bool below = j + 31 - (i_first + off) <= -a.reach, above = j - (i_last + off) >= a.reach;
+        near = !below && !above;
+        far = near ? 0.0f : near_far[above];
+      }
+      const float unit = near ? 1.0f : a.c;
+      prepare<BIAS>(s[b], a.c, j, bias, near, j + 31 > lim_first, lim);
+      grow(st, s[b], unit, far);
+      if constexpr (decltype(more)::value) next[b] = scores<T, D>(q, kt, ka, 32 * b);
+      weigh(st, s[b], unit, far);
+      collect<T, D>(st, s[b], vt, va, 32 * b);
+      interleave<T, D>();
     }
-    attend<T, D, KEYS / 32, BIAS>(st, q, tile, tile + ring.BYTES, ka, va, a.c, j0, lim,
-                                  masked, bias, !whole, far);
+    if constexpr (decltype(more)::value)
+#pragma unroll
+      for (int b = 0; b < KEYS / 32; ++b) s[b] = next[b];
+  };
+  if (w.kbeg < w.kend) {
+    const Lds kt = ring.first();
+#pragma unroll
+    for (int b = 0; b < KEYS / 32; ++b) s[b] = scores<T, D>(q, kt, ka, 32 * b);
+  }
+  int j0 = w.kbeg;
+  for (; j0 + KEYS < w.kend; j0 += KEYS) {
+    ring.next(j0);
+    if (j0 <= lim_last) tile(j0, ring.keys(), ring.values(), std::true_type());
+  }
+  if (j0 < w.kend) {
+    ring.next(j0);
+    if (j0 <= lim_last) tile(j0, ring.keys(), ring.values(), std::false_type());
   }
   if (!r.valid) return;
   const float sum = add_halves(st.l), inv = sum == 0 ? 0.0f : 1.0f / sum;
@@ -256,16 +310,19 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
     } else {
       loads_left<0>();
     }
-    const bool masked = j0 + N - 1 > lim_first;
-    bool whole = false;
+    bool near = false;
     float far = 0;
     if constexpr (BIAS) {
       const bool below = j0 + N - 1 - (i_first + off) <= -a.reach, above = j0 - (i_last + off) >= a.reach;
-      whole = below || above;
-      far = near_far[above];
+      near = !below && !above;
+      far = near ? 0.0f : near_far[above];
     }
-    attend<T, D, N / 32, BIAS>(st, q, lds + buf * 2 * BYTES, lds + buf * 2 * BYTES + BYTES, ka, va, a.c, j0, lim,
-                               masked, bias, !whole, far);
+    const float unit = near ? 1.0f : a.c;
+    f32x16 s = scores<T, D>(q, lds + buf * 2 * BYTES, ka, 0);
+    prepare<BIAS>(s, a.c, j0, bias, near, j0 + N - 1 > lim_first, lim);
+    grow(st, s, unit, far);
+    weigh(st, s, unit, far);
+    collect<T, D>(st, s, lds + buf * 2 * BYTES + BYTES, va, 0);
   }
   // join the waves: maxima and sums, then the scaled accumulators, through LDS
   constexpr int PITCH = D * 4 + 16;
