@@ -79,7 +79,7 @@ typedef struct {
   int32_t batch;              /* sequences, at least 0 */
   int32_t causal;             /* 0 or 1 */
   float scale;                /* finite, > 0 */
-  int64_t tq, tk;             /* rows of q, of k and v; tq heads / kv_heads <= 2^30, tk < 2^31 */
+  int64_t tq, tk;             /* rows of q, of k and v; tq heads / kv_heads <= 2^30, tk <= 2^30 */
   int64_t max_q, max_k;
   const void *q, *k, *v;      /* [tq][heads][head_dim], [tk][kv_heads][head_dim] with the strides below */
   int64_t q_row, q_head, k_row, k_head, v_row, v_head; /* in elements: multiples of 16 bytes, rows at least head_dim

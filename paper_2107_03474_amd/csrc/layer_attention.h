@@ -70,61 +70,75 @@ __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { 
 
 // Sequence b; b = batch is the rows past the last sequence, which see nothing.  The first sequence starts at row 0.
 __device__ __forceinline__ Seq sequence(const Args& a, int b) {
+  const int next = b < a.batch ? b + 1 : b;
+  const int64_t q0 = a.start_q[b], q1 = a.start_q[next], k0 = a.start_k[b], k1 = a.start_k[next];
+  const int64_t used = a.used_k && b < a.batch ? a.used_k[b] : INT32_MAX;
   Seq s;
-  s.q0 = b ? clamp64(a.start_q[b], 0, a.tq) : 0;
-  const int64_t q1 = b < a.batch ? clamp64(a.start_q[b + 1], s.q0, a.tq) : a.tq;
-  s.k0 = b ? clamp64(a.start_k[b], 0, a.tk) : 0;
-  const int64_t k1 = b < a.batch ? clamp64(a.start_k[b + 1], s.k0, a.tk) : a.tk;
-  s.nq = (int32_t)(q1 - s.q0);
-  s.cap = (int32_t)(k1 - s.k0);
-  s.nk = b < a.batch ? (a.used_k ? (int32_t)clamp64(a.used_k[b], 0, s.cap) : s.cap) : 0;
+  s.q0 = b ? clamp64(q0, 0, a.tq) : 0;
+  s.k0 = b ? clamp64(k0, 0, a.tk) : 0;
+  s.nq = (int32_t)((b < a.batch ? clamp64(q1, s.q0, a.tq) : a.tq) - s.q0);
+  s.cap = (int32_t)((b < a.batch ? clamp64(k1, s.k0, a.tk) : a.tk) - s.k0);
+  s.nk = b < a.batch ? (int32_t)clamp64(used, 0, s.cap) : 0;
   return s;
 }
 
-// Which sequence and which of its tiles a slot of the grid is, without knowing the lengths on the host.  A tile holds `tile`
-// units, of which a row of `start` has `scale`.  The grid has rows scale / tile + batch + 1 slots, at least as many as
-// there are tiles; those left over are empty.
+// Which sequence and which of its tiles a slot of the grid is, without knowing the lengths on the host.  Tiles hold `tile`
+// packed rows, `scale` to a query (BY_KEYS: rows of k and v, 1 to a row).  The grid has rows scale / tile + batch + 1 slots, at
+// least as many as there are tiles; those left over are empty.
 //
-// Up to 63 sequences, a lane for each (and one for the rows past the last): the longest sequences first, ties by their
-// order, so that the workgroups that start last are short (8 packed texts of 1 to 4,321, 16/4 heads of 128, us in the
-// batch's order and this one: forward 127 / F1, dq 158 / F2, dk and dv 259 / F3).  More sequences: sequence b takes
-// the slots from start[b] scale / tile + b on, which leaves each as many as it needs, and is found by a wave that looks at
-// 64 places at once.
+// Up to 63 sequences, a lane for each (and one for the rows past the last), all of whose places are read at once: the
+// longest sequences come first, ties in their order, so that the workgroups that start last are short.  More sequences:
+// sequence b takes the slots from start[b] scale / tile + b on, which leaves each as many as it needs, and is found by a
+// wave that looks at 64 places at once.
 struct Place {
-  int b;
+  Seq s;
   int64_t tile;  // past the sequence's last one: an empty slot
 };
 __device__ __forceinline__ int64_t first_slot(const int32_t* start, int64_t rows, int b, int scale, int tile) {
   return (b ? clamp64(start[b], 0, rows) : 0) * scale / tile + b;
 }
-__device__ __forceinline__ Place place_of(const int32_t* start, int64_t rows, int batch, int scale, int tile, int slot) {
+__device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+template <bool BY_KEYS>
+__device__ __forceinline__ Place place_of(const Args& a, int scale, int tile, int slot) {
+  const int lane = threadIdx.x % WAVE, batch = a.batch;
   if (batch < WAVE) {
-    const int lane = threadIdx.x % WAVE;
-    int mine = 0;
-    if (lane <= batch) {
-      const int64_t from = lane ? clamp64(start[lane], 0, rows) : 0;
-      const int64_t to = lane < batch ? clamp64(start[lane + 1], from, rows) : rows;
-      mine = (int)(((to - from) * scale + tile - 1) / tile);
-    }
-    int first = 0;
-    for (int b = 0; b <= batch; ++b) {
-      const int other = __builtin_amdgcn_readlane(mine, b);
-      first += other > mine || (other == mine && b < lane) ? other : 0;
+    const Seq s = sequence(a, lane <= batch ? lane : batch);
+    const int mine = lane > batch ? 0 : (int)(((int64_t)(BY_KEYS ? s.cap : s.nq) * scale + tile - 1) / tile);
+    const int one = of_lane(mine, 0);
+    int first;  // slot of the sequence's first tile
+    if (__builtin_amdgcn_ballot_w64(lane < batch && mine != one) == 0 && of_lane(mine, batch) <= one) {
+      first = lane * one;
+    } else {
+      first = 0;
+      for (int b = 0; b <= batch; ++b) {
+        const int other = of_lane(mine, b);
+        first += other > mine || (other == mine && b < lane) ? other : 0;
+      }
     }
     const uint64_t at = __builtin_amdgcn_ballot_w64(lane <= batch && first <= slot && slot - first < mine);
-    if (!at) return {0, INT64_MAX / 2 / tile};
+    Place p{};
+    p.tile = INT32_MAX;
+    if (!at) return p;
     const int b = __ffsll((unsigned long long)at) - 1;
-    return {b, slot - __builtin_amdgcn_readlane(first, b)};
+    p.s.q0 = of_lane((int)s.q0, b);  // the starts are 32-bit
+    p.s.k0 = of_lane((int)s.k0, b);
+    p.s.nq = of_lane(s.nq, b);
+    p.s.nk = of_lane(s.nk, b);
+    p.s.cap = of_lane(s.cap, b);
+    p.tile = slot - of_lane(first, b);
+    return p;
   }
+  const int32_t* const start = BY_KEYS ? a.start_k : a.start_q;
+  const int64_t rows = BY_KEYS ? a.tk : a.tq;
   int lo = 0, n = batch + 1;  // the last b of lo ... lo + n - 1 with first_slot(b) <= slot
   while (n > 1) {
-    const int step = (n + WAVE - 1) / WAVE, b = lo + (int)(threadIdx.x % WAVE) * step;
+    const int step = (n + WAVE - 1) / WAVE, b = lo + lane * step;
     const bool at = b < lo + n && first_slot(start, rows, b, scale, tile) <= slot;
     const int past = (__popcll(__builtin_amdgcn_ballot_w64(at)) - 1) * step;  // the first place always holds
     lo += past;
     n = min(step, n - past);
   }
-  return {lo, slot - first_slot(start, rows, lo, scale, tile)};
+  return {sequence(a, lo), slot - first_slot(start, rows, lo, scale, tile)};
 }
 
 // The grid's order: tiles of falling length (causal), but every second stretch of as many workgroups as there are compute
@@ -376,8 +390,8 @@ __device__ __forceinline__ bool find_work(const Args& a, Work* w) {
   const int tile = in_turn(blockIdx.x / n, a.slots * a.splits, n);
   w->split = tile % a.splits;
   w->slot = tile / a.splits;
-  const Place at = place_of(a.start_q, a.tq, a.batch, a.group, M, w->slot);
-  w->s = sequence(a, at.b);
+  const Place at = place_of<false>(a, a.group, M, w->slot);
+  w->s = at.s;
   // a sequence's last rows, which see most keys (causal), first
   const int64_t tiles = ((int64_t)w->s.nq * a.group + M - 1) / M;
   if (at.tile >= tiles) return false;
@@ -494,7 +508,7 @@ int check_attention(const lram_attention& a, bool pointers) {
   const int64_t G = a.heads / a.kv_heads;
   if (a.batch < 0 || a.batch > 1 << 24 || (a.causal & ~1) || !(a.scale > 0) || !(a.scale < INFINITY))
     return LRAM_EINVAL;
-  if (a.tq < 0 || a.tk < 0 || a.tk > INT32_MAX || a.tq > (1 << 30) / G || a.max_q < 0 || a.max_k < 0)
+  if (a.tq < 0 || a.tk < 0 || a.tk > 1 << 30 || a.tq > (1 << 30) / G || a.max_q < 0 || a.max_k < 0)
     return LRAM_EINVAL;
   // work items of every kernel (at most 64 pieces of tiles of 32 rows) stay below 2^31 workgroups of 256 threads
   if (a.heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 1) > (int64_t(1) << 24)) return LRAM_EINVAL;
@@ -513,7 +527,7 @@ int check_attention(const lram_attention& a, bool pointers) {
   if (!pointers) return LRAM_OK;
   if (a.tq && (!a.q || off_align(a.q, 16))) return LRAM_EINVAL;
   if (a.tk && (!a.k || !a.v || off_align(a.k, 16) || off_align(a.v, 16))) return LRAM_EINVAL;
-  if (a.batch && (!a.start_q || !a.start_k)) return LRAM_EINVAL;
+  if (!a.start_q || !a.start_k) return LRAM_EINVAL;
   if (off_align(a.start_q, 4) || off_align(a.start_k, 4) || off_align(a.used_k, 4)) return LRAM_EINVAL;
   return LRAM_OK;
 }

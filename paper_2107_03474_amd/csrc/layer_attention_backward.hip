@@ -55,6 +55,11 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   using F = typename Frag<T>::type;
   constexpr int M = WAVES * ROWS;
   extern __shared__ __attribute__((aligned(256))) char smem[];
+  constexpr int IDS = 2;  // of a thread, asked for while the work is looked up
+  int ids[IDS];
+  if constexpr (BIAS)
+#pragma unroll
+    for (int t = 0; t < IDS; ++t) ids[t] = bucket_of(a, (int)(t * THREADS + threadIdx.x) - a.reach - BIAS_PAD);
   Work w;
   const bool found = find_work<M>(a, &w);
   float* const rel_row = o.rel + (((int64_t)w.slot * a.splits + w.split) * a.heads + w.head.first) * a.buckets;
@@ -106,9 +111,10 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   float* const mine = sums + wave * width;
   int* const of = (int*)(sums + WAVES * width);  // buckets
   if constexpr (BIAS) {
-    for (int t = threadIdx.x; t < width; t += THREADS) {
-      of[t] = bucket_of(a, t - a.reach - BIAS_PAD);
-      table[t] = rel_weight(a, w.head.first, of[t]) * LOG2E;
+    for (int n = 0, t = threadIdx.x; t < width; ++n, t += THREADS) {
+      const int id = n == 0 ? ids[0] : n == 1 ? ids[1] : bucket_of(a, t - a.reach - BIAS_PAD);
+      of[t] = id;
+      table[t] = rel_weight(a, w.head.first, id) * LOG2E;
     }
     for (int t = threadIdx.x; t < WAVES * width; t += THREADS) sums[t] = 0;
     bias = table + a.reach + BIAS_PAD - (r.i + off);
@@ -227,11 +233,22 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       sums[threadIdx.x ? width - 1 : 0] = x;
     }
     __syncthreads();
-    for (int k = wave; k < a.buckets; k += WAVES) {
-      float x = 0;
-      for (int e = l; e < width; e += WAVE) x += of[e] == k ? sums[e] : 0.0f;
-      x = wave_sum(x);
-      if (l == 0) rel_row[k] = x;
+    for (int e0 = 0; e0 < width; e0 += 8 * WAVE) {
+      int b[8];
+      float y[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int e = e0 + t * WAVE + l;
+        b[t] = of[min(e, width - 1)];
+        y[t] = e < width ? sums[e] : 0.0f;
+      }
+      for (int k = wave; k < a.buckets; k += WAVES) {
+        float x = 0;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) x += b[t] == k ? y[t] : 0.0f;
+        x = wave_sum(x);
+        if (l == 0) rel_row[k] = e0 ? rel_row[k] + x : x;
+      }
     }
   }
 }
@@ -279,8 +296,8 @@ struct KeyWork {
   int lo, hi;
 };
 __device__ __forceinline__ bool key_work(const Args& a, int slot, KeyWork* w) {
-  const Place at = place_of(a.start_k, a.tk, a.batch, 1, DKV_KEYS, slot);
-  w->s = sequence(a, at.b);
+  const Place at = place_of<true>(a, 1, DKV_KEYS, slot);
+  w->s = at.s;
   const int64_t from = at.tile * DKV_KEYS;
   if (from >= w->s.cap) return false;
   w->j0 = (int)from;
