@@ -10,7 +10,7 @@
 // would be added up in memory by atomics, in an order that varies.  p and ds are rounded to the operands' type.
 //
 // The bias's gradient: k_attention_dq adds up the diagonals of its 32 x 32 blocks of ds.  Rows are lanes and keys registers, so
-// a sum that moves on by one lane with every key collects a diagonal in a lane (diagonals); 8 keys' sums then go to the
+// a sum that moves on by one lane with every key collects a diagonal in a lane (diagonals); a block's sums then go to the
 // wave's own table in LDS (one instruction, no two lanes in an entry: the order is fixed).  Blocks past reach go into a
 // register.  A workgroup leaves its sums by bucket, and k_relative_grad adds up the workgroups'.
 
@@ -31,21 +31,23 @@ struct Grads {
   float *delta, *rel, *part;
 };
 
-// Eight keys of 32 rows (a row to a lane, key 4 h + e in argument e) summed along the diagonals: lane p < 39 of the result
-// holds the sum over lane c's key k with c + 7 - k = p.
-__device__ __forceinline__ float diagonals(float k0, float k1, float k2, float k3) {
-  const float keys[4] = {k0, k1, k2, k3};
-  float part[8];  // a key each: its rows in the lower half's lanes, zeros beside them
+// A block of 32 keys x 32 rows (a row to a lane) summed along its diagonals: lane p < 63 of the result holds the sum over
+// lane c's key k with c + 31 - k = p.
+__device__ __forceinline__ float diagonals(const f32x16& s) {
+  float sum = 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, keys[e]), 0, false, false);
-    const unsigned lower = r[0], upper = r[1];
-    part[e] = __builtin_bit_cast(float, lower);
-    part[4 + e] = __builtin_bit_cast(float, upper);
+  for (int u = 0; u < 4; ++u) {
+    float part[8];  // keys 8 u ..., one each: its rows in the lower half's lanes, zeros beside them
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, (float)s[4 * u + e]), 0, false, false);
+      const unsigned lower = r[0], upper = r[1];
+      part[e] = __builtin_bit_cast(float, lower);
+      part[4 + e] = __builtin_bit_cast(float, upper);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum = u + k ? next_lane(sum) + part[k] : part[k];
   }
-  float sum = part[0];
-#pragma unroll
-  for (int k = 1; k < 8; ++k) sum = next_lane(sum) + part[k];
   return sum;
 }
 
@@ -172,15 +174,12 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
           far_sum[0] += above ? 0.0f : sum;
           far_sum[1] += above ? sum : 0.0f;
         } else {
-          // entry of distance (j + 8 u) - (first + off), and lane p holds the distance 7 - p more
-          float* const t = mine + a.reach + BIAS_PAD + j - (first + off) + 7 - l;
-          float sum[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) sum[u] = diagonals(s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]);
-          if (l < 39)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-              __hip_atomic_fetch_add(t + 8 * u, sum[u], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          // lane p holds the sum at distance j - (first + off) + 31 - p.  (One such instruction to a block and not one to
+          // 8 keys: LDS takes 100 cycles and more for it; dq of 32 x 256 tokens, 8 heads of 64: 32 and D1 us.)
+          const float sum = diagonals(s);
+          if (l < 63)
+            __hip_atomic_fetch_add(mine + a.reach + BIAS_PAD + j - (first + off) + 31 - l, sum, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_WORKGROUP);
         }
       }
 #pragma unroll
