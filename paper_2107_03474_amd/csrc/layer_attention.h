@@ -546,6 +546,14 @@ Args args_of(const lram_attention& a) {
   return x;
 }
 
+// Whether the expected lengths make a batch of like sequences, whose tiles run in rounds over the chip: then as many pieces
+// as fill one round (two workgroups a CU) are best, where the pieces of ragged ones, which even out, may be twice as
+// many.
+constexpr int64_t ROUND = 512;
+bool alike(const lram_attention& a) {
+  return a.batch * (double)a.max_q <= 1.25 * (double)a.tq && a.max_k <= 2 * a.max_q;
+}
+
 // More than 64 KB of a workgroup's LDS has to be asked for, once for a kernel and a device.
 int allow_lds(const void* kernel, size_t bytes) {
   if (bytes <= 64 * 1024) return LRAM_OK;

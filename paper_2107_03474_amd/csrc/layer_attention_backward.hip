@@ -556,18 +556,19 @@ __global__ __launch_bounds__(REL_THREADS) void k_relative_grad(const float* rel,
   }
 }
 
-// How the two kernels divide the work: keys (dq) and rows (dk, dv) come in pieces where the tiles are few against the chip
-// (about 1,024 workgroups are wanted, and 1,536 for the rows in bf16), none shorter than 1,024 (128 in fp32, whose
-// products take sixteen times as long).  dk and dv with the join, 8 packed texts of 1 to 4,321, 16/4 heads of 128, us for
-// 1,024 / 1,536 / 2,048 / 3,072: 306 / 282 / 292 / 313.
+// How the two kernels divide the work: keys (dq) and queries (dk, dv) come in pieces where the tiles are few against the
+// chip, none shorter than 1,024 rows (128 in fp32, whose products take sixteen times as long).  dq: a round of workgroups,
+// two where sequences differ in bf16.  dk and dv: causal tiles meet half of the pieces, so n of them make (n + 1) / 2
+// workgroups a tile.  us with the join, 2 x 2,048 causal tokens, 16/8 heads of 128: dq of one round / two 76 / 108, dk and
+// dv in 2 / 3 (a round) / 4 pieces 120 / 115 / 153; 8 packed texts of 1 to 4,321, 16/4 heads of 128, dk and dv for 768 /
+// 1,024 / 1,536 / 2,048 workgroups 407 / 343 / 319 / 325.
 constexpr int MAX_PIECES = 16;
 struct Pieces {
   int n, size;
 };
 // rows: units of work that one of `length` stands for.
-Pieces pieces_of(int64_t tiles, int64_t length, int rows, int dtype, int64_t groups) {
+Pieces pieces_of(int64_t wanted, int64_t length, int rows, int dtype) {
   const int64_t shortest = dtype == LRAM_F32 ? 128 : 1024;
-  const int64_t wanted = tiles > 0 ? groups / tiles : 1;
   const int64_t n = std::max<int64_t>(
       1, std::min<int64_t>({wanted, (length * rows + shortest - 1) / shortest, (length + 63) / 64, MAX_PIECES}));
   const int64_t size = std::max<int64_t>(64, ((length + n - 1) / n + 63) / 64 * 64);
@@ -584,11 +585,18 @@ Plan plan_of(const lram_attention& a) {
   p.group = a.rel_weight ? 1 : (int)G;
   p.row_slots = (int)(a.tq * p.group / (WAVES * ROWS) + a.batch + 1);
   p.key_slots = (int)(a.tk / DKV_KEYS + a.batch + 1);
-  const auto tiles = [&](int64_t longest, int64_t slots) {
-    return std::min<int64_t>((int64_t)a.batch * ((longest + 127) / 128), slots);
+  const auto tiles = [&](int64_t longest, int64_t slots, int64_t heads) {
+    return std::max<int64_t>(1, std::min<int64_t>((int64_t)a.batch * ((longest + 127) / 128), slots) * heads);
   };
-  p.keys = pieces_of(tiles(a.max_q * p.group, p.row_slots) * (a.heads / p.group), a.max_k, 1, a.dtype, 1024);
-  p.rows = pieces_of(tiles(a.max_k, p.key_slots) * a.kv_heads, a.max_q, (int)G, a.dtype, a.dtype == LRAM_F32 ? 1024 : 1536);
+  const bool even = a.dtype == LRAM_F32 || alike(a);
+  const int64_t row_tiles = tiles(a.max_q * p.group, p.row_slots, a.heads / p.group);
+  const int64_t key_tiles = tiles(a.max_k, p.key_slots, a.kv_heads);
+  p.keys = pieces_of((even ? ROUND : 2 * ROUND) / row_tiles, a.max_k, 1, a.dtype);
+  p.rows = pieces_of(a.dtype == LRAM_F32 ? ROUND / key_tiles
+                     : !even             ? 3 * ROUND / key_tiles
+                     : a.causal          ? 2 * ROUND / key_tiles - 1
+                                         : ROUND / key_tiles,
+                     a.max_q, (int)G, a.dtype);
   p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written

@@ -406,11 +406,11 @@ struct Plan {
 };
 
 // Few rows: a sequence's packed rows fit one wave.  Pieces of the keys, where row tiles are few against the chip: as many
-// as make 512 workgroups (1,024 of k_attention in bf16, whose pieces of a ragged batch even out), none shorter than 1,024
-// keys (128 where fp32 products, a sixteenth of the rate, make them long).  us, with the join, for 256 / 512 / 1,024 / 2,048
-// workgroups: 32 tokens over caches of 256 to 8,192, 32/8 heads of 128: 122 / 122 / 144 / 139; for 512 / 1,024 / 1,536
-// / 2,048: 4 x 100 queries over 12,345, 300, 8,000 and 101 keys 103 / 84 / 83 / 86; five texts of 1 to 1,000 in fp32, 8/4
-// heads of 64: 43 / 50 / 57 / 57.
+// as make a round of workgroups (two rounds of k_attention where sequences differ in bf16), none shorter than 1,024 keys
+// (128 where fp32 products, a sixteenth of the rate, make them long).  us, with the join: 32 tokens over caches of 256 to
+// 8,192, 32/8 heads of 128, half a round / one / two / four 122 / 122 / 144 / 139; 4 x 100 queries over 12,345, 300, 8,000
+// and 101 keys, one / two / three / four 103 / 84 / 83 / 86; 2 x 2,048 causal tokens, 16/8 heads of 128, one / two 62 /
+// 88; five texts of 1 to 1,000 in fp32, 8/4 heads of 64, one / two / four 43 / 50 / 57.
 Plan plan_of(const lram_attention& a) {
   Plan p;
   const int64_t G = a.heads / a.kv_heads;
@@ -421,7 +421,7 @@ Plan plan_of(const lram_attention& a) {
   const int64_t heads = a.heads / p.group;
   const int64_t work = heads * a.batch * std::max<int64_t>(1, (a.max_q * p.group + tile - 1) / tile);
   const int64_t real = std::min<int64_t>(work, heads * p.slots);
-  int64_t splits = real > 0 ? (p.few || a.dtype == LRAM_F32 ? 512 : 1024) / real : 1;
+  int64_t splits = real > 0 ? (p.few || a.dtype == LRAM_F32 || alike(a) ? ROUND : 2 * ROUND) / real : 1;
   const int64_t shortest = a.dtype == LRAM_F32 && !p.few ? 128 : 1024;
   splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + shortest - 1) / shortest});
   if (splits < 1) splits = 1;
