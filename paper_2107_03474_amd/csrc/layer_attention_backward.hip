@@ -12,7 +12,7 @@
 // The bias's gradient: k_attention_dq adds up the diagonals of its 32 x 32 blocks of ds.  Rows are lanes and keys registers, so
 // a sum that moves on by one lane with every key collects a diagonal in a lane (diagonals); a block's sums then go to the
 // wave's own table in LDS (one instruction, no two lanes in an entry: the order is fixed).  Blocks past reach go into a
-// register.  A workgroup leaves its sums by bucket, and k_relative_grad adds up the workgroups'.
+// register.  A workgroup leaves its sums by bucket, and relative_grad adds up the workgroups'.
 
 #include "layer_attention.h"
 
@@ -29,6 +29,7 @@ struct Grads {
   void *gq, *gk, *gv, *grel;
   // workspace: [tq heads], [slots][heads][buckets], [pieces][tk][kv_heads][2][D] or [splits][tq][heads][D] (dq first)
   float *delta, *rel, *part;
+  int rel_rows;
 };
 
 // A block of 32 keys x 32 rows (a row to a lane) summed along its diagonals: lane p < 63 of the result holds the sum over
@@ -282,6 +283,31 @@ constexpr int dkv_bytes() {
 }
 template <typename T, int D>
 constexpr int dkv_waves() { return dkv_bytes<T, D>() > 72 * 1024 ? 1 : 2; }  // a SIMD
+// The bias's gradient from k_attention_dq's sums [rel_rows][heads][buckets], by the workgroup of a head at the end of the
+// grid of k_attention_dkv (a kernel of its own cost 4 us): 8 threads to a bucket, each a fixed set of the rows.
+__device__ __forceinline__ void relative_grad(const Args& a, const Grads& o, int head, float* lds) {
+  constexpr int COLS = 32, PARTS = THREADS / COLS;
+  const int c = threadIdx.x % COLS, p = threadIdx.x / COLS;
+  for (int k0 = 0; k0 < a.buckets; k0 += COLS) {
+    float x = 0;
+    if (k0 + c < a.buckets)
+#pragma unroll 8
+      for (int s = p; s < o.rel_rows; s += PARTS) x += o.rel[((int64_t)s * a.heads + head) * a.buckets + k0 + c];
+    lds[p * COLS + c] = x;
+    __syncthreads();
+    if (p == 0 && k0 + c < a.buckets) {
+#pragma unroll
+      for (int t = 1; t < PARTS; ++t) x += lds[t * COLS + c];
+      const int64_t at = (int64_t)head * a.buckets + k0 + c;
+      if (a.rel_bf16)
+        ((bf16*)o.grel)[at] = (bf16)x;
+      else
+        ((float*)o.grel)[at] = x;
+    }
+    __syncthreads();
+  }
+}
+
 // What it keeps of a tile's queries beside them: lse and delta.
 enum { LSE, DELTA, STATS };
 
@@ -317,6 +343,13 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   constexpr bool VLDS = values_in_lds<T, D>();
   extern __shared__ __attribute__((aligned(256))) char smem[];
   Lds lds = (Lds)smem;
+  if constexpr (BIAS) {
+    const int tiles = a.kv_heads * a.slots * a.splits;
+    if ((int)blockIdx.x >= tiles) {
+      relative_grad(a, o, blockIdx.x - tiles, (float*)smem);
+      return;
+    }
+  }
   const int hk = blockIdx.x % a.kv_heads;
   const int tile = in_turn(blockIdx.x / a.kv_heads, a.slots * a.splits, a.kv_heads);
   const int piece = tile % a.splits, slot = tile / a.splits;  // the first keys, which most rows see, first
@@ -533,29 +566,6 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
   }
 }
 
-// The workgroups' sums [n][heads][buckets] added up; a workgroup to a head, 32 threads to a bucket.
-constexpr int REL_THREADS = 1024;
-template <typename W>
-__global__ __launch_bounds__(REL_THREADS) void k_relative_grad(const float* rel, int n, int heads, int buckets, W* grad) {
-  constexpr int COLS = 32, PARTS = REL_THREADS / COLS;
-  __shared__ float part[PARTS][COLS + 1];
-  const int head = blockIdx.x, c = threadIdx.x % COLS, p = threadIdx.x / COLS;
-  for (int k0 = 0; k0 < buckets; k0 += COLS) {
-    float x = 0;
-    if (k0 + c < buckets)
-#pragma unroll 4
-      for (int s = p; s < n; s += PARTS) x += rel[((int64_t)s * heads + head) * buckets + k0 + c];
-    part[p][c] = x;
-    __syncthreads();
-    if (p == 0 && k0 + c < buckets) {
-#pragma unroll
-      for (int t = 1; t < PARTS; ++t) x += part[t][c];
-      grad[(int64_t)head * buckets + k0 + c] = (W)x;
-    }
-    __syncthreads();
-  }
-}
-
 // How the two kernels divide the work: keys (dq) and queries (dk, dv) come in pieces where the tiles are few against the
 // chip, none shorter than 1,024 rows (128 in fp32, whose products take sixteen times as long).  dq: a round of workgroups,
 // two where sequences differ in bf16.  dk and dv: causal tiles meet half of the pieces, so n of them make (n + 1) / 2
@@ -607,7 +617,7 @@ Plan plan_of(const lram_attention& a) {
 }
 
 template <typename T, int D, bool BIAS>
-int go(Args x, const Grads& g, const lram_attention& d, const Plan& p, hipStream_t s) {
+int go(Args x, const Grads& g, const Plan& p, hipStream_t s) {
   const size_t width = BIAS ? (size_t)(2 * (x.reach + BIAS_PAD) + 1) * 4 : 0;
   const auto launch = [&](auto kernel, int64_t grid, size_t bytes) {
     if (int rc = allow_lds((const void*)kernel, bytes)) return rc;
@@ -629,24 +639,15 @@ int go(Args x, const Grads& g, const lram_attention& d, const Plan& p, hipStream
       if (int rc = layer_launched()) return rc;
     }
   }
-  if (x.tk) {
-    x.slots = p.key_slots;
+  if (x.tk || BIAS) {
+    x.slots = x.tk ? p.key_slots : 0;
     x.splits = p.rows.n;
     x.piece = p.rows.size;
-    if (int rc = launch(k_attention_dkv<T, D, BIAS>, (int64_t)x.kv_heads * x.slots * x.splits,
+    if (int rc = launch(k_attention_dkv<T, D, BIAS>, (int64_t)x.kv_heads * x.slots * x.splits + (BIAS ? x.heads : 0),
                         dkv_bytes<T, D>() + STAGES * STATS * tile_rows<T, D>() * 4 + width * x.ratio))
       return rc;
-    if (x.splits > 1)
-      if (int rc = launch(k_attention_dkv_join<T, D>, (int64_t)x.kv_heads * x.slots * JOIN_PARTS, 0)) return rc;
-  }
-  if constexpr (BIAS) {
-    const auto finish = [&](auto w) {
-      using W = decltype(w);
-      hipLaunchKernelGGL(k_relative_grad<W>, dim3(x.heads), dim3(REL_THREADS), 0, s, (const float*)g.rel,
-                         x.tq ? p.row_slots * p.keys.n : 0, x.heads, x.buckets, (W*)g.grel);
-      return layer_launched();
-    };
-    return d.wdtype == LRAM_BF16 ? finish(bf16()) : finish(float());
+    if (x.tk && x.splits > 1)
+      return launch(k_attention_dkv_join<T, D>, (int64_t)x.kv_heads * x.slots * JOIN_PARTS, 0);
   }
   return LRAM_OK;
 }
@@ -683,9 +684,9 @@ int lram_attention_backward(const lram_attention* a, const void* out, const void
   x.splits = 1;
   float* const ws = (float*)workspace;
   const Grads g{out, residue, grad_out, lse, grad_q, grad_k, grad_v, grad_rel, ws, ws + p.delta,
-                ws + p.delta + p.rel};
+                ws + p.delta + p.rel, a->tq ? p.row_slots * p.keys.n : 0};
   return by_kind(*a, [&](auto t, auto d, auto bias) {
-    return go<decltype(t), decltype(d)::value, decltype(bias)::value>(x, g, *a, p, (hipStream_t)stream);
+    return go<decltype(t), decltype(d)::value, decltype(bias)::value>(x, g, p, (hipStream_t)stream);
   });
 }
 
