@@ -177,6 +177,10 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, first + (l & 31));
   const int head = w.head.first + r.g;
+  if (a.splits > 1 && w.kbeg >= w.kend) {  // a piece without keys: the join leaves it out
+    if (r.valid && l < 32) put_lse(a, o, w.split, (w.s.q0 + r.i) * a.heads + head, -INFINITY);
+    return;
+  }
   typename Frag<T>::type q[D / 16];
   load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
   // last key of the lane's row, and of the wave's first and last rows
@@ -272,6 +276,10 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
   const int G = a.group, off = w.s.nk - w.s.nq, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, w.row0 + (l & 31));
   const int head = w.head.first + r.g;
+  if (a.splits > 1 && w.kbeg >= w.kend) {
+    if (r.valid && threadIdx.x < 32) put_lse(a, o, w.split, (w.s.q0 + r.i) * a.heads + head, -INFINITY);
+    return;
+  }
   typename Frag<T>::type q[D / 16];
   load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
   const int lim = a.causal && r.valid ? min(r.i + off, w.s.nk - 1) : w.s.nk - 1;
