@@ -7,7 +7,8 @@
 // Two kernels, each forming p again, so that every sum has one owner and one order: k_attention_dq keeps 128 packed
 // rows and walks over the keys (scores transposed, as in the forward pass), k_attention_dkv keeps 128 keys and walks over
 // the packed rows, the G heads of its group among them.  Seven products instead of the five of a single kernel, whose dq
-// would be added up in memory by atomics, in an order that varies.  p and ds are rounded to the operands' type.
+// would be added up in memory by atomics, in an order that varies.  p and ds are rounded to the operands' type, the matrix
+// cores' own, half a unit of which is what q, k, v and the results carry anyway; sums and delta stay in fp32.
 //
 // The bias's gradient: k_attention_dq adds up the diagonals of its 32 x 32 blocks of ds.  Rows are lanes and keys registers, so
 // a sum that moves on by one lane with every key collects a diagonal in a lane (diagonals); a block's sums then go to the
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
           far_sum[1] += above ? sum : 0.0f;
         } else {
           // lane p holds the sum at distance j - (first + off) + 31 - p.  (One such instruction to a block and not one to
-          // 8 keys: LDS takes 100 cycles and more for it; dq of 32 x 256 tokens, 8 heads of 64: 32 and D1 us.)
+          // 8 keys: LDS takes 100 cycles and more for it; dq of 32 x 256 tokens, 8 heads of 64: 32 and 27 us.)
           const float sum = diagonals(s);
           if (l < 63)
             __hip_atomic_fetch_add(mine + a.reach + BIAS_PAD + j - (first + off) + 31 - l, sum, __ATOMIC_RELAXED,
@@ -314,7 +315,8 @@ enum { LSE, DELTA, STATS };
 // The key tile of a workgroup and its piece of the queries, lo to hi (lo >= hi: none meets the tile).  It walks from the last
 // queries to the first, and over the heads of its group at each: the workgroups of a sequence that run side by side read
 // the same rows at the same time, whatever the first query is that sees their keys, and share them in their L2 (2 x 8,192
-// causal tokens, 32/8 heads of 128: head by head from the first query on 64 % of the reads missed it, M1).
+// causal tokens, 32/8 heads of 128: head by head from the first query on 64 % of the reads missed it, 8.8 GB of them; in
+// step 12 %, 1.6 GB).
 struct KeyWork {
   Seq s;
   int j0, seen;  // queries from `seen` on see a key of the tile
@@ -576,11 +578,11 @@ constexpr int MAX_PIECES = 16;
 struct Pieces {
   int n, size;
 };
-// rows: units of work that one of `length` stands for.
-Pieces pieces_of(int64_t wanted, int64_t length, int rows, int dtype) {
+// rows: units of work that one of `length` stands for; tiles: of the grid.
+Pieces pieces_of(int64_t wanted, int64_t length, int rows, int dtype, int64_t tiles) {
   const int64_t shortest = dtype == LRAM_F32 ? 128 : 1024;
-  const int64_t n = std::max<int64_t>(
-      1, std::min<int64_t>({wanted, (length * rows + shortest - 1) / shortest, (length + 63) / 64, MAX_PIECES}));
+  int64_t n = std::min<int64_t>({wanted, (length * rows + shortest - 1) / shortest, (length + 63) / 64, MAX_PIECES});
+  if (n < 1 || !few_enough(tiles)) n = 1;
   const int64_t size = std::max<int64_t>(64, ((length + n - 1) / n + 63) / 64 * 64);
   return {(int)std::max<int64_t>(1, std::min(n, (length + size - 1) / size)), (int)std::min<int64_t>(size, 1 << 30)};
 }
@@ -601,12 +603,12 @@ Plan plan_of(const lram_attention& a) {
   const bool even = a.dtype == LRAM_F32 || alike(a);
   const int64_t row_tiles = tiles(a.max_q * p.group, p.row_slots, a.heads / p.group);
   const int64_t key_tiles = tiles(a.max_k, p.key_slots, a.kv_heads);
-  p.keys = pieces_of((even ? ROUND : 2 * ROUND) / row_tiles, a.max_k, 1, a.dtype);
+  p.keys = pieces_of((even ? ROUND : 2 * ROUND) / row_tiles, a.max_k, 1, a.dtype, (int64_t)p.row_slots * (a.heads / p.group));
   p.rows = pieces_of(a.dtype == LRAM_F32 ? ROUND / key_tiles
                      : !even             ? 3 * ROUND / key_tiles
                      : a.causal          ? 2 * ROUND / key_tiles - 1
                                          : ROUND / key_tiles,
-                     a.max_q, (int)G, a.dtype);
+                     a.max_q, (int)G, a.dtype, (int64_t)p.key_slots * a.kv_heads);
   p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written

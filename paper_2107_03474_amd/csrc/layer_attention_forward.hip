@@ -4,7 +4,8 @@
 // k_attention: prompts.  A workgroup holds 128 packed rows, 32 to a wave, whose queries stay in registers; keys and values
 // pass through LDS in tiles of 64, the next tile's loads in flight while one is used.  One pass: running maximum m and
 // sum l a row, accumulators rescaled only when the maximum grows by more than 2^8 (the weights stay exact in that
-// range, and the branch is rarely taken).
+// range, and the branch is rarely taken).  A tile's scores are formed while the one before it is weighed.  Weights go into
+// the product with the values rounded to the values' type, the matrix cores' own; their sum is of the unrounded ones.
 // k_attention_few: a few queries over many keys.  The four waves of a workgroup share the same 32 rows and take key
 // tiles in turn, each through LDS of its own without barriers, and join their sums at the end.
 // Where rows are few against the chip the keys are divided into pieces (either kernel) that k_attention_join joins.
@@ -432,7 +433,7 @@ Plan plan_of(const lram_attention& a) {
   int64_t splits = real > 0 ? (p.few || a.dtype == LRAM_F32 || alike(a) ? ROUND : 2 * ROUND) / real : 1;
   const int64_t shortest = a.dtype == LRAM_F32 && !p.few ? 128 : 1024;
   splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + shortest - 1) / shortest});
-  if (splits < 1) splits = 1;
+  if (splits < 1 || !few_enough(heads * p.slots)) splits = 1;
   p.piece = (int)std::min<int64_t>(((a.max_k + splits - 1) / splits + 127) / 128 * 128, INT32_MAX / 2);
   if (p.piece < 128) p.piece = 128;
   p.splits = (int)std::min<int64_t>(splits, std::max<int64_t>(1, (a.max_k + p.piece - 1) / p.piece));

@@ -202,6 +202,30 @@ def test_whatever_the_starts_hold_stays_inside():
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [62, 63, 64, 65, 300])
+def test_many_sequences(n, dtype):
+    """A lane to a sequence below 64, a search from there on; empty ones among them, first and last."""
+    lengths = [(37 * i) % 150 if i % 5 and i < n - 2 else 0 for i in range(n)]
+    _case(lengths, lengths, 4, 2, 32, dtype, True)
+    lengths = [0 if i == 7 else 1 + (53 * i) % 40 for i in range(n)]
+    _case(lengths, [1 + (29 * i) % 90 for i in range(n)], 2, 2, 64, dtype, True, rel=(8, 12, True))
+    _case([1] * n, [(71 * i) % 130 for i in range(n)], 8, 2, 64, dtype, True, train=False, capacity=130)
+
+
+def test_whatever_many_starts_hold_stays_inside():
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    q, k, v, do = (_randn(g, (300, 2, 64), BF16) for _ in range(4))
+    rel = lram.RelativeBias(torch.ones((2, 4), dtype=BF16, device=DEV), torch.zeros(5, dtype=torch.int32, device=DEV))
+    up = torch.arange(71, dtype=torch.int32, device=DEV) * 4
+    for start in (up.flip(0).contiguous(), up * 1000, up - 140, (up * 37) % 301):
+        seqs = lram.Packed(start, start, 100, 100, None)
+        out, saved = lram.attention_forward(q, k, v, seqs, True, rel=rel, save=True)
+        lram.attention_backward(q, k, v, seqs, out, saved, do, True, rel=rel)
+        torch.cuda.synchronize()
+
+
 def test_a_sequence_that_is_not_finite_stays_alone():
     g = torch.Generator(device=DEV)
     g.manual_seed(1)
