@@ -4,10 +4,11 @@
 //     g = dy w;   dx = rs (g - mean g - n mean(g n)) + dh,  n = (h - mu) rs;  dw = sum dy n,  db = sum dy
 //
 // Bound by HBM: a row is read once and stays in registers between its statistics and its result (mean first, then
-// the squared distances from it: no cancellation).  A row belongs to a group of threads, one wave while 32 elements a lane
-// hold it, else a workgroup; a thread owns the same columns of every row, so that in the backward pass the
-// weights' gradients add up in its registers over the rows that the group takes, and only one partial row per
-// workgroup goes through memory to the second kernel.
+// the squared distances from it: no cancellation).  A row belongs to a wave or a workgroup; a thread owns the same columns of
+// every row, so that in the backward pass the weights' gradients add up in its registers over the rows that the group
+// takes, and only one partial row per workgroup goes through memory to the second kernel.
+
+#include <algorithm>
 
 #include "layer_common.h"
 
@@ -245,15 +246,20 @@ __global__ __launch_bounds__(FIN_COLS* FIN_ROWS) void k_norm_finish(const float*
   }
 }
 
-// Threads of a row and chunks of a thread: a wave up to four chunks a lane, then workgroups.
+// Threads of a row and chunks of a thread: a thread to a chunk, which is the shortest way through a row, but waves take
+// rows of up to four chunks a lane where there are many (us of a thread to a chunk / waves: 64 rows x 2,048 bf16 3.2 / 5.4,
+// 1,024 x 2,048 4.8 / 6.4, 2,048 x 1,024 6.1 / 5.2, 5,003 x 500 fp32 11.4 / 7.2, 8,192 x 2,048 bf16 22.5 / 23.2; of one chunk
+// / four to 256 threads: 16,384 x 8,192 bf16 192 / 200, 64 x 8,192 4.2 / 5.8).
+constexpr int64_t FEW_ROWS = 1024;
 struct Shape {
   int G, NC;
 };
-Shape shape_of(int64_t width, int dtype) {
+Shape shape_of(int64_t rows, int64_t width, int dtype) {
   const int64_t chunks = (width + CHUNK_BYTES / (int)elem_size(dtype) - 1) / (CHUNK_BYTES / (int)elem_size(dtype));
-  for (int G : {WAVE, 4 * WAVE})
-    for (int NC : {1, 2, 4})
-      if (chunks <= (int64_t)G * NC) return {G, NC};
+  for (int NC : {1, 2, 4})
+    if ((NC == 1 || rows > FEW_ROWS) && chunks <= WAVE * NC) return {WAVE, NC};
+  for (int G : {4 * WAVE, 8 * WAVE, 16 * WAVE})
+    if (chunks <= G) return {G, 1};
   return {16 * WAVE, chunks <= 32 * WAVE ? 2 : 4};
 }
 
@@ -282,8 +288,7 @@ int by_shape(const Shape& sh, F f) {
 #define LRAM_SHAPE(g, n) \
   if (sh.G == g && sh.NC == n) return f(std::integral_constant<int, g>(), std::integral_constant<int, n>());
   LRAM_SHAPE(64, 1) LRAM_SHAPE(64, 2) LRAM_SHAPE(64, 4)
-  LRAM_SHAPE(256, 1) LRAM_SHAPE(256, 2) LRAM_SHAPE(256, 4)
-  LRAM_SHAPE(512, 1) LRAM_SHAPE(1024, 1) LRAM_SHAPE(1024, 2) LRAM_SHAPE(1024, 4)
+  LRAM_SHAPE(256, 1) LRAM_SHAPE(512, 1) LRAM_SHAPE(1024, 1) LRAM_SHAPE(1024, 2) LRAM_SHAPE(1024, 4)
 #undef LRAM_SHAPE
   return LRAM_EINVAL;
 }
@@ -330,18 +335,24 @@ int lram_layer_norm_forward(const void* x, const void* residual, const void* wei
   if (off_align(x, 16) || off_align(residual, 16) || off_align(sum, 16) || off_align(y, 16) || off_align(mean, 4) ||
       off_align(rstd, 4) || off_align(weight, elem_size(wdtype)) || off_align(bias, elem_size(wdtype)))
     return LRAM_EINVAL;
-  const Shape sh = shape_of(width, dtype);
+  const Shape sh = shape_of(rows, width, dtype);
   return by_types(dtype, wdtype, [&](auto t, auto v) {
     using T = decltype(t);
     using W = decltype(v);
     return by_shape(sh, [&](auto g, auto n) {
       constexpr int G = decltype(g)::value, NC = decltype(n)::value;
-      const unsigned grid = (unsigned)(G == WAVE ? (rows + NORM_WAVES - 1) / NORM_WAVES : rows);
+      constexpr int64_t EACH = G == WAVE ? NORM_WAVES : 1;  // rows of a workgroup
+      constexpr int64_t MOST = ((int64_t(1) << 32) / threads_of(G) - 1) * EACH;  // of a launch: less than 2^32 threads
       const auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads_of(G)), 0, (hipStream_t)stream, (const T*)x,
-                           (const T*)residual, (const W*)weight, (const W*)bias, rows, (int)width, (float)eps, (T*)sum,
-                           (T*)y, mean, rstd);
-        return layer_launched();
+        for (int64_t row = 0; row < rows; row += MOST) {
+          const int64_t n = std::min(rows - row, MOST), at = row * width;
+          hipLaunchKernelGGL(kernel, dim3((unsigned)((n + EACH - 1) / EACH)), dim3(threads_of(G)), 0, (hipStream_t)stream,
+                             (const T*)x + at, residual ? (const T*)residual + at : nullptr, (const W*)weight,
+                             (const W*)bias, n, (int)width, (float)eps, sum ? (T*)sum + at : nullptr, (T*)y + at,
+                             mean ? mean + row : nullptr, rstd ? rstd + row : nullptr);
+          if (int rc = layer_launched()) return rc;
+        }
+        return (int)LRAM_OK;
       };
       return residual ? go(k_norm_forward<T, W, G, NC, true>) : go(k_norm_forward<T, W, G, NC, false>);
     });

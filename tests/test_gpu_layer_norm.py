@@ -52,6 +52,23 @@ def test_many_rows_share_a_workgroup():
     _check(*_inputs(5001, 8192, BF16, F32))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [1024, 1025])
+def test_waves_and_workgroups_share_a_width(rows, dtype):
+    for width in (260, 900, 1021, 2001):
+        _check(*_inputs(rows, width, dtype, dtype, width))
+
+
+def test_without_gradients():
+    x, r, dy, dh, w, b = _inputs(30, 96, BF16, F32)
+    w.requires_grad_()
+    with torch.no_grad():
+        y, h = lram.layer_norm(x, w, b, residual=r)
+        assert not y.requires_grad and torch.equal(lram.layer_norm(x, w, b), lram.layer_norm_forward(x, w, b)[0])
+    y2, h2 = lram.layer_norm(x, w, b, residual=r)
+    assert y2.requires_grad and torch.equal(y, y2) and torch.equal(h, h2)
+
+
 def test_constant_rows_and_large_means():
     x, r, dy, dh, w, b = _inputs(40, 320, F32, F32, 3, mean=1000.0)  # variance far below the squared mean
     _check(x, None, dy, None, w, b)
