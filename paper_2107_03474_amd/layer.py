@@ -93,6 +93,11 @@ def _scratch(nbytes: int, workspace: Optional[torch.Tensor], like: torch.Tensor)
     return _dev(workspace, "workspace", like=like), workspace.numel() * workspace.element_size(), workspace
 
 
+def _records(*inputs: Optional[torch.Tensor]) -> bool:
+    """Whether autograd follows a call with these inputs."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)
+
+
 # ---------------------------------------------------------------------------
 # Layer norm.
 
@@ -191,7 +196,11 @@ class LayerNorm(torch.autograd.Function):
 def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, eps: float = 1e-5,
                residual: Optional[torch.Tensor] = None):
     """The layer norm of x, differentiable; with a residual (y, h): the norm of h = x + residual, and h."""
-    y, h = LayerNorm.apply(x, residual, weight, bias, float(eps))
+    if not _records(x, residual, weight, bias):
+        y, h, _, _ = layer_norm_forward(x.contiguous(), weight.contiguous(), bias.contiguous(), float(eps),
+                                        None if residual is None else residual.contiguous())
+    else:
+        y, h = LayerNorm.apply(x, residual, weight, bias, float(eps))
     return y if residual is None else (y, h)
 
 
@@ -395,5 +404,8 @@ class Attention(torch.autograd.Function):
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Packed, causal: bool = False,
               scale: Optional[float] = None, rel: Optional[RelativeBias] = None) -> torch.Tensor:
     """``attention_forward``'s result, differentiable in q, k, v and the bias's weight."""
+    if not _records(q, k, v, None if rel is None else rel.weight):
+        rel = None if rel is None else RelativeBias(rel.weight.contiguous(), rel.bucket)
+        return attention_forward(q, k, v, seqs, causal, scale, rel)[0]  # nothing to be kept for a backward
     return Attention.apply(q, k, v, None if rel is None else rel.weight, None if rel is None else rel.bucket, seqs,
                            bool(causal), scale)

@@ -288,6 +288,16 @@ def test_autograd():
     ref.assert_close("dw", w.grad, want["dw"])
 
 
+def test_without_gradients():
+    q, k, v, seqs, bias, do, got = _case([60, 5], [60, 5], 4, 2, 64, BF16, True, rel=(16, 40, True))
+    rel = lram.RelativeBias(bias.weight.requires_grad_(), bias.bucket)
+    with torch.no_grad():
+        out = lram.attention(q, k, v, seqs, True, rel=rel)
+    assert not out.requires_grad and torch.equal(out, got["out"])
+    out = lram.attention(q, k, v, seqs, True, rel=rel)
+    assert out.requires_grad and torch.equal(out, got["out"])
+
+
 def test_gradients_by_differences():
     """Directional differences of the kernel's own forward, in fp32, against its gradients: the forward's bounded errors
     over the step, and the third-order term taken from the 64-bit form's differences at the same step."""
