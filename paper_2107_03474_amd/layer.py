@@ -127,7 +127,7 @@ def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor
         h = torch.empty_like(x)
         hp = h.data_ptr()
     y = torch.empty_like(x)
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
     rstd = torch.empty_like(mean)
     rc = lib.lram_layer_norm_forward(x.data_ptr(), rp, wp, bp, dt, wt, rows, width, eps, hp, y.data_ptr(),
                                      mean.data_ptr(), rstd.data_ptr(), _stream(x.device))
@@ -332,10 +332,10 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: P
     ``attention_backward``."""
     lib = _library()
     a = _describe(q, k, v, seqs, causal, scale, rel)
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    out = q.new_empty(q.shape)
     saved = lse = residue = None
     if save:
-        saved = AttentionSaved(torch.empty(q.shape[:2], dtype=torch.float32, device=q.device),
+        saved = AttentionSaved(q.new_empty(q.shape[:2], dtype=torch.float32),
                                torch.empty_like(out) if q.dtype is torch.bfloat16 else None)
         lse = saved.lse.data_ptr()
         residue = None if saved.residue is None else saved.residue.data_ptr()
@@ -364,7 +364,7 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: 
     lp = _ptr(saved.lse, "saved.lse", torch.float32, q.shape[:2], q)
     rp = None if saved.residue is None else _ptr(saved.residue, "saved.residue", q.dtype, q.shape, q)
     gq = torch.empty_like(out)
-    gk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    gk = k.new_empty(k.shape)
     gv = torch.empty_like(gk)
     grel = None if rel is None else torch.empty_like(rel.weight)
     n = ctypes.c_size_t(0)
