@@ -336,7 +336,7 @@ __device__ __forceinline__ int bucket_of(const Args& a, int d) {
 }
 __device__ __forceinline__ void fill_bias(const Args& a, int first_head, int heads, float* table) {
   const int n = bias_width(a);
-  for (int i = threadIdx.x; i < heads * n; i += THREADS)
+  for (int i = threadIdx.x; i < heads * n; i += blockDim.x)
     table[i] = rel_weight(a, first_head + i / n, bucket_of(a, i % n - a.reach - BIAS_PAD)) * LOG2E;
 }
 
@@ -460,10 +460,10 @@ struct KeyRing {
   }
 };
 
-// The same with the keys one tile ahead of the values.
-template <typename T, int D>
+// The same with the keys one tile ahead of the values, and a tile to each of the workgroup's teams.
+template <typename T, int D, int TEAMS>
 struct KeyAhead {
-  static constexpr int BYTES = KEYS * Tile<T, D>::ROW;
+  static constexpr int STEP = TEAMS * KEYS, BYTES = STEP * Tile<T, D>::ROW;
   const T *k, *v;
   int64_t k_row, v_row;
   Lds lds;
@@ -475,26 +475,26 @@ struct KeyAhead {
         k_row(a.k_row), v_row(a.v_row), lds(lds_), wave(wave_), nk(w.s.nk), end(w.kend), place(1) {
     load_k(w.kbeg, 0);
     load_v(w.kbeg, 0);
-    load_k(w.kbeg + KEYS, 1);
+    load_k(w.kbeg + STEP, 1);
   }
   __device__ __forceinline__ void load_k(int j0, int to) {
-    if (j0 < end) load_rows<T, D, KEYS, WAVES>(k, k_row, j0, nk, lds + to * BYTES, wave);
+    if (j0 < end) load_rows<T, D, STEP, TEAMS * WAVES>(k, k_row, j0, nk, lds + to * BYTES, wave);
   }
   __device__ __forceinline__ void load_v(int j0, int to) {
-    if (j0 < end) load_rows<T, D, KEYS, WAVES>(v, v_row, j0, nk, lds + (2 + to) * BYTES, wave);
+    if (j0 < end) load_rows<T, D, STEP, TEAMS * WAVES>(v, v_row, j0, nk, lds + (2 + to) * BYTES, wave);
   }
   __device__ __forceinline__ Lds first() {
     loads_done();
     __syncthreads();
     return lds;
   }
-  // The tile from key j0 on becomes the one in use.
+  // The tiles from key j0 on become those in use.
   __device__ __forceinline__ void next(int j0) {
     loads_done();
     __syncthreads();  // its values and the next one's keys are whole; every wave has left the other places
     place ^= 1;
-    load_k(j0 + 2 * KEYS, place);
-    load_v(j0 + KEYS, place ^ 1);
+    load_k(j0 + 2 * STEP, place);
+    load_v(j0 + STEP, place ^ 1);
   }
   __device__ __forceinline__ Lds keys() const { return lds + (place ^ 1) * BYTES; }  // of the tile after it
   __device__ __forceinline__ Lds values() const { return lds + (2 + place) * BYTES; }

@@ -166,20 +166,26 @@ __device__ __forceinline__ void put_lse(const Args& a, const Out& o, int split, 
     o.lse[at] = lse;
 }
 
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention(Args a, Out o) {
+// TEAMS: of four waves each, which share the rows and take the tiles of keys in turn; the second joins its sums to the
+// first's at the end (plan_of: when).
+template <typename T, int D, int TEAMS>
+constexpr int prompt_bytes() { return TEAMS * ring_bytes<T, D>(); }
+template <typename T, int D, bool BIAS, int TEAMS>
+__global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_attention(Args a, Out o) {
   using Ti = Tile<T, D>;
   constexpr int M = WAVES * ROWS;
   extern __shared__ __attribute__((aligned(256))) char smem[];
   Work w;
   if (!find_work<M>(a, &w)) return;
-  KeyAhead<T, D> ring(a, w, (Lds)smem, __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE));
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE;
+  using Ring = KeyAhead<T, D, TEAMS>;
+  Ring ring(a, w, (Lds)smem, __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) % WAVES, l = threadIdx.x % WAVE;
+  const int team = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
   const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, first + (l & 31));
   const int head = w.head.first + r.g;
   if (a.splits > 1 && w.kbeg >= w.kend) {  // a piece without keys: the join leaves it out
-    if (r.valid && l < 32) put_lse(a, o, w.split, (w.s.q0 + r.i) * a.heads + head, -INFINITY);
+    if (r.valid && l < 32 && !team) put_lse(a, o, w.split, (w.s.q0 + r.i) * a.heads + head, -INFINITY);
     return;
   }
   typename Frag<T>::type q[D / 16];
@@ -192,7 +198,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const float* bias = nullptr;
   float near_far[2] = {0, 0};
   if constexpr (BIAS) {
-    float* table = (float*)(smem + ring_bytes<T, D>());
+    float* table = (float*)(smem + prompt_bytes<T, D, TEAMS>());
     fill_bias(a, w.head.first, G, table);
     bias = table + r.g * bias_width(a) + a.reach + BIAS_PAD - (r.i + off);
     __syncthreads();
@@ -229,22 +235,45 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
 #pragma unroll
       for (int b = 0; b < KEYS / 32; ++b) s[b] = next[b];
   };
+  const int mine = team * KEYS, at_lds = mine * Ti::ROW;  // the team's tile of a step
   if (w.kbeg < w.kend) {
-    const Lds kt = ring.first();
+    const Lds kt = ring.first() + at_lds;
 #pragma unroll
     for (int b = 0; b < KEYS / 32; ++b) s[b] = scores<T, D>(q, kt, ka, 32 * b);
   }
   int j0 = w.kbeg;
-  for (; j0 + KEYS < w.kend; j0 += KEYS) {
+  for (; j0 + Ring::STEP < w.kend; j0 += Ring::STEP) {
     ring.next(j0);
-    if (j0 <= lim_last) tile(j0, ring.keys(), ring.values(), std::true_type());
+    if (j0 + mine <= lim_last) tile(j0 + mine, ring.keys() + at_lds, ring.values() + at_lds, std::true_type());
   }
   if (j0 < w.kend) {
     ring.next(j0);
-    if (j0 <= lim_last) tile(j0, ring.keys(), ring.values(), std::false_type());
+    if (j0 + mine <= lim_last) tile(j0 + mine, ring.keys() + at_lds, ring.values() + at_lds, std::false_type());
+  }
+  float sum = add_halves(st.l);
+  if constexpr (TEAMS == 2) {  // the second team's sums join the first one's, through the LDS that held the tiles
+    constexpr int SUMS = D / 2;  // accumulators of a lane
+    static_assert((SUMS + 2) * THREADS * 4 <= prompt_bytes<T, D, TEAMS>(), "they fit");
+    float* const to = (float*)smem + threadIdx.x % THREADS;
+    __syncthreads();
+    if (team) {
+      to[0] = st.m;
+      to[THREADS] = sum;
+#pragma unroll
+      for (int e = 0; e < SUMS; ++e) to[(2 + e) * THREADS] = st.o[e / 16][e % 16];
+    }
+    __syncthreads();
+    if (team) return;
+    const float other = to[0], m = fmaxf(st.m, other), m0 = m == -INFINITY ? 0.0f : m;
+    const float f = __builtin_amdgcn_exp2f(st.m - m0), g = __builtin_amdgcn_exp2f(other - m0);
+    sum = sum * f + to[THREADS] * g;
+    st.m = m;
+#pragma unroll
+    for (int e = 0; e < SUMS; ++e)
+      st.o[e / 16][e % 16] = fmaf(to[(2 + e) * THREADS], g, st.o[e / 16][e % 16] * f);
   }
   if (!r.valid) return;
-  const float sum = add_halves(st.l), inv = sum == 0 ? 0.0f : 1.0f / sum;
+  const float inv = sum == 0 ? 0.0f : 1.0f / sum;
   const int64_t at = (w.s.q0 + r.i) * a.heads + head;
   if (l < 32) put_lse(a, o, w.split, at, sum == 0 ? -INFINITY : st.m + __builtin_amdgcn_logf(sum));
 #pragma unroll
@@ -411,6 +440,7 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(Args a, Out o) {
 
 struct Plan {
   bool few;
+  bool teams;  // two of them
   int group, slots, splits, piece;
 };
 
@@ -420,6 +450,12 @@ struct Plan {
 // 8,192, 32/8 heads of 128, half a round / one / two / four 122 / 122 / 144 / 139; 4 x 100 queries over 12,345, 300, 8,000
 // and 101 keys, one / two / three / four 103 / 84 / 83 / 86; 2 x 2,048 causal tokens, 16/8 heads of 128, one / two 62 /
 // 88; five texts of 1 to 1,000 in fp32, 8/4 heads of 64, one / two / four 43 / 50 / 57.
+// Two teams where k_attention's tiles leave a compute unit one workgroup, or causal ones of many lengths not much more, and
+// the longest walk is what counts; a round is then a workgroup a unit.  us without / with (bf16): causal, 16/8 heads of 64
+// and bias, 1,024 tokens 24 / 19, 2,176 45 / 34, 2,560 52 / 39, 3,500 71 / 67, 4,097 84 / 84; 8/8 heads of 64, 4,097 72 / 50,
+// 6,000 104 / 71; 16/4 heads of 128, 2,048 44 / 40; both directions, 8/8 heads of 64, 4,096 64 / 55, 4,224 89 / 97; 24 x 256 13 / 18,
+// 32 x 64 5.6 / 6.3; pieces of prompts over caches of 101 to 12,345, 32/8 heads of 128, 78 / 83; 8 heads of 64 in fp32, 2,048
+// tokens, 63 / 93.
 Plan plan_of(const lram_attention& a) {
   Plan p;
   const int64_t G = a.heads / a.kv_heads;
@@ -430,7 +466,10 @@ Plan plan_of(const lram_attention& a) {
   const int64_t heads = a.heads / p.group;
   const int64_t work = heads * a.batch * std::max<int64_t>(1, (a.max_q * p.group + tile - 1) / tile);
   const int64_t real = std::min<int64_t>(work, heads * p.slots);
-  int64_t splits = real > 0 ? (p.few || a.dtype == LRAM_F32 || alike(a) ? ROUND : 2 * ROUND) / real : 1;
+  const bool even = p.few || a.dtype == LRAM_F32 || alike(a);
+  p.teams = !p.few && a.dtype == LRAM_BF16 && even && a.max_k > 256 &&
+            real <= (a.causal && a.max_k > 1024 ? 3 * UNITS / 2 : UNITS);
+  int64_t splits = real > 0 ? (p.teams ? UNITS : even ? ROUND : 2 * ROUND) / real : 1;
   const int64_t shortest = a.dtype == LRAM_F32 && !p.few ? 128 : 1024;
   splits = std::min<int64_t>({splits, MAX_SPLITS, (a.max_k + shortest - 1) / shortest});
   if (splits < 1 || !few_enough(heads * p.slots)) splits = 1;
@@ -448,17 +487,23 @@ template <typename T, int D, bool BIAS>
 int go(Args x, const Out& o, const Plan& p, hipStream_t s) {
   const unsigned grid = (unsigned)(x.heads / x.group) * x.slots * x.splits;
   const size_t table = BIAS ? (size_t)x.group * (2 * (x.reach + BIAS_PAD) + 1) * 4 : 0;
-  const auto launch = [&](auto kernel, size_t bytes) {
+  const auto launch = [&](auto kernel, size_t bytes, int threads) {
     if (int rc = allow_lds((const void*)kernel, bytes)) return rc;
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(THREADS), bytes, s, x, o);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), bytes, s, x, o);
     return layer_launched();
   };
-  int rc;
+  const auto prompt = [&](auto teams) {
+    constexpr int TEAMS = decltype(teams)::value;
+    return launch(k_attention<T, D, BIAS, TEAMS>, prompt_bytes<T, D, TEAMS>() + table, TEAMS * THREADS);
+  };
+  int rc = LRAM_OK;
+  if constexpr (sizeof(T) == 2)
+    if (p.teams) rc = prompt(std::integral_constant<int, 2>());
   if (p.few)
     rc = launch(k_attention_few<T, D, BIAS>,
-                std::max<size_t>(few_bytes<T, D>(), WAVES * ROWS * (D * 4 + 16 + 8)) + table);
-  else
-    rc = launch(k_attention<T, D, BIAS>, ring_bytes<T, D>() + table);
+                std::max<size_t>(few_bytes<T, D>(), WAVES * ROWS * (D * 4 + 16 + 8)) + table, THREADS);
+  else if (!p.teams)
+    rc = prompt(std::integral_constant<int, 1>());
   if (rc || x.splits == 1) return rc;
   const int64_t threads = x.tq * x.heads * (D / 4);
   hipLaunchKernelGGL((k_attention_join<T, D>), dim3((unsigned)((threads + THREADS - 1) / THREADS)), dim3(THREADS), 0, s,

@@ -143,6 +143,16 @@ def test_divided_rows(d, dtype):
     _case([2500], [130], 1, 1, d, dtype, False, layout="separate", rel=(16, 30, True))
 
 
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_few_tiles_of_long_rows(causal, d):
+    """Tiles of keys shared out among the waves of a workgroup: odd and even numbers of them, ends inside them."""
+    for n in (257, 300, 384, 449, 1030, 1100):
+        _case([n], [n], 4, 2, d, BF16, causal, rel=(32, 128, True) if n % 2 else None)
+    _case([400, 390], [470, 130], 2, 2, d, BF16, causal, layout="separate")
+    _case([600], [2500], 2, 1, d, BF16, causal, train=False, layout="separate", rel=(16, 64, True))
+
+
 def test_hints_do_not_change_results():
     lengths = [150, 1, 290]
     for hints in ((0, 0), (1, 1), (1, 290), (290, 1), (10 ** 9, 10 ** 9)):
