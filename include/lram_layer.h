@@ -89,7 +89,8 @@ typedef struct {
   const void* rel_weight;     /* [heads][rel_buckets], nullable */
   const int32_t* rel_bucket;  /* [2 rel_reach + 1] (device), each in [0, rel_buckets) */
   int32_t rel_buckets;        /* 1 ... 256 */
-  int32_t rel_reach;          /* >= 0, heads / kv_heads (2 rel_reach + 193) <= 4096 */
+  int32_t rel_reach;          /* >= 0, heads / kv_heads (2 rel_reach + 193) <= 4096; in fp32 with head_dim 128
+                                 2 rel_reach + 193 <= 1365 */
 } lram_attention;
 
 /*

@@ -429,10 +429,11 @@ constexpr int ring_bytes() { return STAGES * 2 * KEYS * Tile<T, D>::ROW; }
 template <typename T, int D>
 constexpr int waves_per_simd() { return ring_bytes<T, D>() > 80 * 1024 ? 1 : 2; }
 
-// The tiles of KEYS keys and values of a work item, passing through LDS; all waves go along together.
-template <typename T, int D>
+// The tiles of KEYS keys and values of a work item, one to each of the workgroup's teams, passing through LDS; all waves go
+// along together.
+template <typename T, int D, int TEAMS>
 struct KeyRing {
-  static constexpr int BYTES = KEYS * Tile<T, D>::ROW;
+  static constexpr int STEP = TEAMS * KEYS, BYTES = STEP * Tile<T, D>::ROW;
   const T *k, *v;
   int64_t k_row, v_row;
   Lds lds;
@@ -446,21 +447,21 @@ struct KeyRing {
   }
   __device__ __forceinline__ void load(int j0, int to) {
     if (j0 >= end) return;
-    load_rows<T, D, KEYS, WAVES>(k, k_row, j0, nk, lds + to * 2 * BYTES, wave);
-    load_rows<T, D, KEYS, WAVES>(v, v_row, j0, nk, lds + to * 2 * BYTES + BYTES, wave);
+    load_rows<T, D, STEP, TEAMS * WAVES>(k, k_row, j0, nk, lds + to * 2 * BYTES, wave);
+    load_rows<T, D, STEP, TEAMS * WAVES>(v, v_row, j0, nk, lds + to * 2 * BYTES + BYTES, wave);
   }
-  // The tile from key j0 on, the next in line: keys here, values BYTES on.
+  // The tiles from key j0 on, the next in line: keys here, values BYTES on.
   __device__ __forceinline__ Lds next(int j0) {
     loads_done();
-    __syncthreads();  // the tile is whole, and every wave has left the other place
+    __syncthreads();  // the tiles are whole, and every wave has left the other place
     const Lds tile = lds + place * 2 * BYTES;
     place ^= 1;
-    load(j0 + KEYS, place);
+    load(j0 + STEP, place);
     return tile;
   }
 };
 
-// The same with the keys one tile ahead of the values, and a tile to each of the workgroup's teams.
+// The same with the keys a step ahead of the values.
 template <typename T, int D, int TEAMS>
 struct KeyAhead {
   static constexpr int STEP = TEAMS * KEYS, BYTES = STEP * Tile<T, D>::ROW;
@@ -507,6 +508,13 @@ constexpr int64_t MOST_GROUPS = int64_t(1) << 24;
 // Whether a grid of so many tiles may have 64 pieces of each; the joins, 256 threads to 8 or more rows, then fit too.
 bool few_enough(int64_t tiles) { return tiles < MOST_GROUPS / 64; }
 
+// LDS of a workgroup of k_attention_dq: tiles, the bias, sums of it for every wave, buckets.
+constexpr int64_t LDS_BYTES = 160 * 1024;
+int64_t dq_lds(const lram_attention& a, int teams) {
+  const int64_t tiles = (int64_t)STAGES * 2 * KEYS * a.head_dim * (int64_t)elem_size(a.dtype);
+  return teams * tiles + (a.rel_weight ? (2 + teams * WAVES) * (2 * ((int64_t)a.rel_reach + BIAS_PAD) + 1) * 4 : 0);
+}
+
 int check_attention(const lram_attention& a, bool pointers) {
   if (a.dtype != LRAM_F32 && a.dtype != LRAM_BF16) return LRAM_EDTYPE;
   if (a.head_dim != 32 && a.head_dim != 64 && a.head_dim != 128) return LRAM_EDTYPE;
@@ -523,7 +531,7 @@ int check_attention(const lram_attention& a, bool pointers) {
   if (a.rel_weight) {
     if (a.wdtype != LRAM_F32 && !(a.wdtype == LRAM_BF16 && a.dtype == LRAM_BF16)) return LRAM_EDTYPE;
     if (!a.rel_bucket || a.rel_buckets < 1 || a.rel_buckets > 256 || a.rel_reach < 0 || a.rel_reach > 4096 ||
-        G * (2 * (a.rel_reach + BIAS_PAD) + 1) > 4096)
+        G * (2 * (a.rel_reach + BIAS_PAD) + 1) > 4096 || dq_lds(a, 1) > LDS_BYTES)
       return LRAM_EINVAL;
     if (off_align(a.rel_weight, elem_size(a.wdtype)) || off_align(a.rel_bucket, 4)) return LRAM_EINVAL;
   }

@@ -53,27 +53,30 @@ __device__ __forceinline__ float diagonals(const f32x16& s) {
   return sum;
 }
 
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention_dq(Args a, Grads o) {
+// TEAMS: as in k_attention.
+template <typename T, int D, bool BIAS, int TEAMS>
+__global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_attention_dq(Args a, Grads o) {
   using Ti = Tile<T, D>;
   using F = typename Frag<T>::type;
-  constexpr int M = WAVES * ROWS;
+  constexpr int M = WAVES * ROWS, ALL = TEAMS * THREADS, TABLES = TEAMS * WAVES;
   extern __shared__ __attribute__((aligned(256))) char smem[];
   constexpr int IDS = 2;  // of a thread, asked for while the work is looked up
   int ids[IDS];
   if constexpr (BIAS)
 #pragma unroll
-    for (int t = 0; t < IDS; ++t) ids[t] = bucket_of(a, (int)(t * THREADS + threadIdx.x) - a.reach - BIAS_PAD);
+    for (int t = 0; t < IDS; ++t) ids[t] = bucket_of(a, (int)(t * ALL + threadIdx.x) - a.reach - BIAS_PAD);
   Work w;
   const bool found = find_work<M>(a, &w);
   float* const rel_row = o.rel + (((int64_t)w.slot * a.splits + w.split) * a.heads + w.head.first) * a.buckets;
   if (!found) {
     if constexpr (BIAS)  // an empty slot's sums are zero
-      for (int t = threadIdx.x; t < a.buckets; t += THREADS) rel_row[t] = 0;
+      for (int t = threadIdx.x; t < a.buckets; t += ALL) rel_row[t] = 0;
     return;
   }
-  KeyRing<T, D> ring(a, w, (Lds)smem, __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE));
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
+  using Ring = KeyRing<T, D, TEAMS>;
+  const int place = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
+  Ring ring(a, w, (Lds)smem, place);
+  const int wave = place % WAVES, team = place / WAVES;
   const int G = a.group, off = w.s.nk - w.s.nq, first = w.row0 + wave * ROWS, rows = w.s.nq * G;
   const Row r = row_of(a, w.s, first + (l & 31));
   const int head = w.head.first + r.g;
@@ -99,7 +102,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
     delta = add_halves(delta);
     if (r.valid) {
       lse = o.lse[at];
-      if (l < 32) o.delta[at] = delta;
+      if (l < 32 && !team) o.delta[at] = delta;
     }
   }
   const int lim = a.causal && r.valid ? min(r.i + off, w.s.nk - 1) : w.s.nk - 1;
@@ -110,17 +113,17 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   const float* bias = nullptr;
   float far_bias[2] = {0, 0}, far_sum[2] = {0, 0};
   const int width = bias_width(a);
-  float* const table = (float*)(smem + ring_bytes<T, D>());
-  float* const sums = table + width;         // [WAVES][width]
-  float* const mine = sums + wave * width;
-  int* const of = (int*)(sums + WAVES * width);  // buckets
+  float* const table = (float*)(smem + TEAMS * ring_bytes<T, D>());
+  float* const sums = table + width;              // [TABLES][width]
+  float* const mine = sums + place * width;
+  int* const of = (int*)(sums + TABLES * width);  // buckets
   if constexpr (BIAS) {
-    for (int n = 0, t = threadIdx.x; t < width; ++n, t += THREADS) {
+    for (int n = 0, t = threadIdx.x; t < width; ++n, t += ALL) {
       const int id = n == 0 ? ids[0] : n == 1 ? ids[1] : bucket_of(a, t - a.reach - BIAS_PAD);
       of[t] = id;
       table[t] = rel_weight(a, w.head.first, id) * LOG2E;
     }
-    for (int t = threadIdx.x; t < WAVES * width; t += THREADS) sums[t] = 0;
+    for (int t = threadIdx.x; t < TABLES * width; t += ALL) sums[t] = 0;
     bias = table + a.reach + BIAS_PAD - (r.i + off);
     __syncthreads();
     far_bias[0] = table[0];
@@ -132,11 +135,11 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[b][e] = 0;
-  for (int j0 = w.kbeg; j0 < w.kend; j0 += KEYS) {
-    const Lds kt = ring.next(j0), vt = kt + ring.BYTES;
+  for (int j0 = w.kbeg; j0 < w.kend; j0 += Ring::STEP) {
+    const Lds kt = ring.next(j0) + team * KEYS * Ti::ROW, vt = kt + Ring::BYTES;
 #pragma unroll
     for (int b = 0; b < KEYS / 32; ++b) {
-      const int j = j0 + 32 * b;
+      const int j = j0 + team * KEYS + 32 * b;
       if (j > lim_last) continue;
       f32x16 s, dp;
 #pragma unroll
@@ -195,7 +198,18 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
       }
     }
   }
-  if (r.valid) {
+  if constexpr (TEAMS == 2) {  // the second team's sums join the first one's, through the LDS that held the tiles
+    float* const to = (float*)smem + threadIdx.x % THREADS;
+    __syncthreads();
+    if (team)
+#pragma unroll
+      for (int e = 0; e < D / 2; ++e) to[e * THREADS] = acc[e / 16][e % 16];
+    __syncthreads();
+    if (!team)
+#pragma unroll
+      for (int e = 0; e < D / 2; ++e) acc[e / 16][e % 16] += to[e * THREADS];
+  }
+  if (r.valid && !team) {
     T* const p = (T*)o.gq + at * D + 4 * h;
     float* const part = o.part + ((int64_t)w.split * a.tq * a.heads + at) * D + 4 * h;
 #pragma unroll
@@ -214,23 +228,23 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
   if constexpr (BIAS) {
     // the waves' tables added up, then the entries past reach, with the far blocks' sums, into the last one's
     __syncthreads();
-    for (int t = threadIdx.x; t < width; t += THREADS) {
+    for (int t = threadIdx.x; t < width; t += ALL) {
       float x = 0;
 #pragma unroll
-      for (int v = 0; v < WAVES; ++v) x += sums[v * width + t];
+      for (int v = 0; v < TABLES; ++v) x += sums[v * width + t];
       sums[t] = x;
     }
-    float* const far = (float*)smem;  // [2][WAVES]; the tiles are done with
+    float* const far = (float*)smem;  // [2][TABLES]; the tiles are done with
     const float below = wave_sum(far_sum[0]), above = wave_sum(far_sum[1]);
     if (l == 0) {
-      far[wave] = below;
-      far[WAVES + wave] = above;
+      far[place] = below;
+      far[TABLES + place] = above;
     }
     __syncthreads();
     if (threadIdx.x < 2) {  // the far blocks' sums into the last entry of their side
       float x = sums[threadIdx.x ? width - 1 : 0];
 #pragma unroll
-      for (int v = 0; v < WAVES; ++v) x += far[threadIdx.x * WAVES + v];
+      for (int v = 0; v < TABLES; ++v) x += far[threadIdx.x * TABLES + v];
       sums[threadIdx.x ? width - 1 : 0] = x;
     }
     __syncthreads();
@@ -243,7 +257,7 @@ __global__ __launch_bounds__(THREADS, (waves_per_simd<T, D>())) void k_attention
         b[t] = of[min(e, width - 1)];
         y[t] = e < width ? sums[e] : 0.0f;
       }
-      for (int k = wave; k < a.buckets; k += WAVES) {
+      for (int k = place; k < a.buckets; k += TABLES) {
         float x = 0;
 #pragma unroll
         for (int t = 0; t < 8; ++t) x += b[t] == k ? y[t] : 0.0f;
@@ -574,6 +588,9 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
 // workgroups a tile.  us with the join, 2 x 2,048 causal tokens, 16/8 heads of 128: dq of one round / two 76 / 108, dk and
 // dv in 2 / 3 (a round) / 4 pieces 120 / 115 / 153; 8 packed texts of 1 to 4,321, 16/4 heads of 128, dk and dv for 768 /
 // 1,024 / 1,536 / 2,048 workgroups 407 / 343 / 319 / 325.
+// k_attention_dq with two teams, as in the forward pass, us without / with: causal, 16/8 heads of 64 and bias, 300 tokens 17.4 /
+// 16.1, 1,024 33 / 26, 2,304 60 / 45, 4,097 107 / 110; 8/8 heads of 64, 512 13.5 / 14.2, 6,000 107 / 85; 16/4 heads of 128, 2,600
+// 80 / 68, 4,096 140 / 146; both directions, 8/8 heads of 64, 4,096 71 / 66, 4,224 108 / 118.
 constexpr int MAX_PIECES = 16;
 struct Pieces {
   int n, size;
@@ -581,13 +598,15 @@ struct Pieces {
 // rows: units of work that one of `length` stands for; tiles: of the grid.
 Pieces pieces_of(int64_t wanted, int64_t length, int rows, int dtype, int64_t tiles) {
   const int64_t shortest = dtype == LRAM_F32 ? 128 : 1024;
-  int64_t n = std::min<int64_t>({wanted, (length * rows + shortest - 1) / shortest, (length + 63) / 64, MAX_PIECES});
+  const int64_t step = dtype == LRAM_F32 ? KEYS : 2 * KEYS;  // whole steps of two teams
+  int64_t n = std::min<int64_t>({wanted, (length * rows + shortest - 1) / shortest, (length + step - 1) / step, MAX_PIECES});
   if (n < 1 || !few_enough(tiles)) n = 1;
-  const int64_t size = std::max<int64_t>(64, ((length + n - 1) / n + 63) / 64 * 64);
+  const int64_t size = std::max<int64_t>(step, ((length + n - 1) / n + step - 1) / step * step);
   return {(int)std::max<int64_t>(1, std::min(n, (length + size - 1) / size)), (int)std::min<int64_t>(size, 1 << 30)};
 }
 struct Plan {
   int group, row_slots, key_slots;
+  bool teams;  // two of them in k_attention_dq
   Pieces keys, rows;
   size_t delta, rel, part;  // floats of workspace
 };
@@ -603,7 +622,9 @@ Plan plan_of(const lram_attention& a) {
   const bool even = a.dtype == LRAM_F32 || alike(a);
   const int64_t row_tiles = tiles(a.max_q * p.group, p.row_slots, a.heads / p.group);
   const int64_t key_tiles = tiles(a.max_k, p.key_slots, a.kv_heads);
-  p.keys = pieces_of((even ? ROUND : 2 * ROUND) / row_tiles, a.max_k, 1, a.dtype, (int64_t)p.row_slots * (a.heads / p.group));
+  p.teams = a.dtype == LRAM_BF16 && even && a.max_k > (a.rel_weight ? 256 : 512) && dq_lds(a, 2) <= LDS_BYTES &&
+            row_tiles <= (a.causal && a.max_k > 1024 ? 3 * UNITS / 2 : UNITS);
+  p.keys = pieces_of((p.teams ? UNITS : even ? ROUND : 2 * ROUND) / row_tiles, a.max_k, 1, a.dtype, (int64_t)p.row_slots * (a.heads / p.group));
   p.rows = pieces_of(a.dtype == LRAM_F32 ? ROUND / key_tiles
                      : !even             ? 3 * ROUND / key_tiles
                      : a.causal          ? 2 * ROUND / key_tiles - 1
@@ -621,9 +642,9 @@ Plan plan_of(const lram_attention& a) {
 template <typename T, int D, bool BIAS>
 int go(Args x, const Grads& g, const Plan& p, hipStream_t s) {
   const size_t width = BIAS ? (size_t)(2 * (x.reach + BIAS_PAD) + 1) * 4 : 0;
-  const auto launch = [&](auto kernel, int64_t grid, size_t bytes) {
+  const auto launch = [&](auto kernel, int64_t grid, size_t bytes, int threads = THREADS) {
     if (int rc = allow_lds((const void*)kernel, bytes)) return rc;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(THREADS), bytes, s, x, g);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), bytes, s, x, g);
     return layer_launched();
   };
   if (x.tq) {
@@ -631,9 +652,16 @@ int go(Args x, const Grads& g, const Plan& p, hipStream_t s) {
     x.slots = p.row_slots;
     x.splits = p.keys.n;
     x.piece = p.keys.size;
-    if (int rc = launch(k_attention_dq<T, D, BIAS>, (int64_t)(x.heads / x.group) * x.slots * x.splits,
-                        ring_bytes<T, D>() + width * (2 + WAVES)))
-      return rc;
+    const auto dq = [&](auto teams) {
+      constexpr int TEAMS = decltype(teams)::value;
+      return launch(k_attention_dq<T, D, BIAS, TEAMS>, (int64_t)(x.heads / x.group) * x.slots * x.splits,
+                    TEAMS * ring_bytes<T, D>() + width * (2 + TEAMS * WAVES), TEAMS * THREADS);
+    };
+    int rc = LRAM_OK;
+    if constexpr (sizeof(T) == 2)
+      if (p.teams) rc = dq(std::integral_constant<int, 2>());
+    if (!p.teams) rc = dq(std::integral_constant<int, 1>());
+    if (rc) return rc;
     if (x.splits > 1) {
       const int64_t n = x.tq * x.heads * D;
       hipLaunchKernelGGL(k_attention_dq_join<T>, dim3((unsigned)((n / 4 + THREADS - 1) / THREADS)), dim3(THREADS), 0, s,

@@ -111,6 +111,12 @@ def test_bias_of_a_large_group_and_reach():
     _case([3], [300], 8, 1, 64, BF16, True, rel=(32, 128, False))
 
 
+@pytest.mark.parametrize("d,dtype,reach", [(128, BF16, 1951), (128, F32, 586), (64, F32, 1951), (128, BF16, 313),
+                                           (128, BF16, 314)])
+def test_the_longest_reach(d, dtype, reach):
+    _case([500], [500], 2, 2, d, dtype, True, rel=(64, reach, True))
+
+
 @pytest.mark.parametrize("layout", ["heads", "separate"])
 def test_layouts(layout):
     _case([90, 33], [90, 33], 4, 2, 64, BF16, True, layout=layout)

@@ -119,6 +119,20 @@ def test_attention_refuses(lib):
     assert _attention_fwd(lib, tq=0, q=None, out=None) == 0  # empty: nothing to do
 
 
+@pytest.mark.parametrize("dtype,d,heads,reach", [(1, 128, 4, 1951), (0, 64, 4, 1951), (0, 128, 4, 586), (1, 64, 8, 927),
+                                                 (1, 64, 256, 0)])
+def test_the_longest_reach(lib, dtype, d, heads, reach):
+    """What the header allows, and one more."""
+    n = ctypes.c_size_t(0)
+    for extra, rc in ((0, 0), (1, EINVAL)):
+        a = _describe(**dict(BIAS, dtype=dtype, wdtype=dtype, head_dim=d, heads=heads, kv_heads=4, rel_reach=reach + extra,
+                             q_row=heads * d, k_row=4 * d, v_row=4 * d))
+        if heads == 256:  # 64 heads of a group leave no room for a table
+            rc = EINVAL
+        assert lib.lram_attention_forward_workspace_bytes(ctypes.byref(a), ctypes.byref(n)) == rc
+        assert lib.lram_attention_backward_workspace_bytes(ctypes.byref(a), ctypes.byref(n)) == rc
+
+
 @pytest.mark.parametrize("buckets,reach,both", [(32, 128, True), (32, 128, False), (8, 4, True), (16, 1000, False),
                                                 (2, 1, True), (1, 1, False), (3, 40, False), (4, 3, True)])
 def test_buckets_follow_their_definition(buckets, reach, both):
