@@ -53,8 +53,9 @@ struct Args {
   int32_t causal, buckets, reach;
   int32_t rel_bf16;
   int32_t slots;   // row (or key) tiles of all sequences, some of them empty
-  int32_t splits;  // pieces of the keys
-  int32_t piece;   // keys of a piece
+  int32_t splits;  // pieces of the keys (dk, dv: of the rows)
+  int32_t piece;   // keys (queries) of a piece
+  int32_t parts;   // dk, dv: so many pieces share a piece's queries, by their heads
   float c;         // scale log2 e
   float scale;
 };
@@ -557,6 +558,7 @@ Args args_of(const lram_attention& a) {
   x.tq = a.tq, x.tk = a.tk;
   x.heads = a.heads, x.kv_heads = a.kv_heads, x.ratio = x.group = a.heads / a.kv_heads, x.batch = a.batch;
   x.causal = a.causal, x.buckets = a.rel_buckets, x.reach = a.rel_reach, x.rel_bf16 = a.wdtype == LRAM_BF16;
+  x.parts = 1;
   x.scale = a.scale;
   x.c = a.scale * LOG2E;
   return x;

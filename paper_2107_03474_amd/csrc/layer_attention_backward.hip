@@ -346,8 +346,9 @@ __device__ __forceinline__ bool key_work(const Args& a, int slot, KeyWork* w) {
   return true;
 }
 __device__ __forceinline__ void take_piece(const Args& a, int piece, KeyWork* w) {
-  const int64_t lo = (int64_t)piece * a.piece;
-  w->hi = piece < a.splits - 1 ? (int)min(lo + a.piece, (int64_t)w->s.nq) : w->s.nq;
+  const int range = piece / a.parts, last = a.splits / a.parts - 1;
+  const int64_t lo = (int64_t)range * a.piece;
+  w->hi = range < last ? (int)min(lo + a.piece, (int64_t)w->s.nq) : w->s.nq;
   w->lo = (int)min((int64_t)max(w->seen, (int)min(lo, (int64_t)w->s.nq)), (int64_t)w->hi);
 }
 
@@ -403,7 +404,8 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   const int width = bias_width(a);
   const int64_t g_row = (int64_t)a.heads * D;
   const int top = (w.hi - 1) / TROWS * TROWS;
-  int place = 0, next_i = top, next_g = 0;
+  const int g_first = a.ratio / a.parts * (piece % a.parts), g_end = g_first + a.ratio / a.parts;
+  int place = 0, next_i = top, next_g = g_first;
   const auto load = [&] {
     const int hq = hk * a.ratio + next_g;
     const Lds to = lds + place * 2 * BYTES;
@@ -416,8 +418,8 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
            (uint32_t)(l * a.heads) * 4);
     }
     place ^= 1;
-    if (++next_g == a.ratio) {
-      next_g = 0;
+    if (++next_g == g_end) {
+      next_g = g_first;
       next_i -= TROWS;
     }
   };
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dk[b][e] = dv[b][e] = 0;
-  int i0 = top, g = 0;
+  int i0 = top, g = g_first;
   while (any && i0 + TROWS > w.lo) {
     loads_done();
     __syncthreads();
@@ -512,8 +514,8 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
         for (int b = 0; b < D / 32; ++b) dk[b] = mma(Ti::col_frag(qt, ca, b, 2 * rb + c), fy, dk[b]);
       }
     }
-    if (++g == a.ratio) {
-      g = 0;
+    if (++g == g_end) {
+      g = g_first;
       i0 -= TROWS;
     }
   }
@@ -588,21 +590,32 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
 // workgroups a tile.  us with the join, 2 x 2,048 causal tokens, 16/8 heads of 128: dq of one round / two 76 / 108, dk and
 // dv in 2 / 3 (a round) / 4 pieces 120 / 115 / 153; 8 packed texts of 1 to 4,321, 16/4 heads of 128, dk and dv for 768 /
 // 1,024 / 1,536 / 2,048 workgroups 407 / 343 / 319 / 325.
+// In fp32, dk and dv for 512 / 1,024 / 2,048 workgroups: 2,048 causal tokens, 8 heads of 64, 108 / 146 / 139; 2,000, 8 heads of 128,
+// 322 / 265 / 265; texts of 1 to 500, 64/8 heads of 128, 599 / 470 / 401; of 1 to 1,000, 8/4 heads of 64, 85 / 83 / 81.
 // k_attention_dq with two teams, as in the forward pass, us without / with: causal, 16/8 heads of 64 and bias, 300 tokens 17.4 /
 // 16.1, 1,024 33 / 26, 2,304 60 / 45, 4,097 107 / 110; 8/8 heads of 64, 512 13.5 / 14.2, 6,000 107 / 85; 16/4 heads of 128, 2,600
 // 80 / 68, 4,096 140 / 146; both directions, 8/8 heads of 64, 4,096 71 / 66, 4,224 108 / 118.
 constexpr int MAX_PIECES = 16;
 struct Pieces {
-  int n, size;
+  int n, size, parts;
 };
-// rows: units of work that one of `length` stands for; tiles: of the grid.
+// rows: units of work that one of `length` stands for, heads that pieces can share out (parts); tiles: of the grid.
 Pieces pieces_of(int64_t wanted, int64_t length, int rows, int dtype, int64_t tiles) {
   const int64_t shortest = dtype == LRAM_F32 ? 128 : 1024;
   const int64_t step = dtype == LRAM_F32 ? KEYS : 2 * KEYS;  // whole steps of two teams
-  int64_t n = std::min<int64_t>({wanted, (length * rows + shortest - 1) / shortest, (length + step - 1) / step, MAX_PIECES});
-  if (n < 1 || !few_enough(tiles)) n = 1;
+  const auto at_least = [&](int64_t work) {
+    return few_enough(tiles) ? std::min<int64_t>({wanted, (length * rows + work - 1) / work, MAX_PIECES}) : 1;
+  };
+  int64_t n = std::max<int64_t>(1, std::min(at_least(shortest), (length + step - 1) / step));
   const int64_t size = std::max<int64_t>(step, ((length + n - 1) / n + step - 1) / step * step);
-  return {(int)std::max<int64_t>(1, std::min(n, (length + size - 1) / size)), (int)std::min<int64_t>(size, 1 << 30)};
+  n = std::max<int64_t>(1, std::min(n, (length + size - 1) / size));
+  // queries that cannot be divided any further are, by their heads (in fp32 down to 64 rows; 8/1 heads of 128 and 200 queries:
+  // dk and dv 156 -> 58 us)
+  const int64_t most = at_least(dtype == LRAM_F32 ? KEYS : shortest);
+  int parts = 1;
+  for (int p = 2; p <= rows; ++p)
+    if (rows % p == 0 && n * p <= most) parts = p;
+  return {(int)n * parts, (int)std::min<int64_t>(size, 1 << 30), parts};
 }
 struct Plan {
   int group, row_slots, key_slots;
@@ -624,12 +637,13 @@ Plan plan_of(const lram_attention& a) {
   const int64_t key_tiles = tiles(a.max_k, p.key_slots, a.kv_heads);
   p.teams = a.dtype == LRAM_BF16 && even && a.max_k > (a.rel_weight ? 256 : 512) && dq_lds(a, 2) <= LDS_BYTES &&
             row_tiles <= (a.causal && a.max_k > 1024 ? 3 * UNITS / 2 : UNITS);
-  p.keys = pieces_of((p.teams ? UNITS : even ? ROUND : 2 * ROUND) / row_tiles, a.max_k, 1, a.dtype, (int64_t)p.row_slots * (a.heads / p.group));
-  p.rows = pieces_of(a.dtype == LRAM_F32 ? ROUND / key_tiles
-                     : !even             ? 3 * ROUND / key_tiles
-                     : a.causal          ? 2 * ROUND / key_tiles - 1
-                                         : ROUND / key_tiles,
-                     a.max_q, (int)G, a.dtype, (int64_t)p.key_slots * a.kv_heads);
+  p.keys = pieces_of((p.teams ? UNITS : even ? ROUND : 2 * ROUND) / row_tiles, a.max_k, 1, a.dtype,
+                     (int64_t)p.row_slots * (a.heads / p.group));
+  const int64_t wanted = a.dtype == LRAM_F32 ? (!alike(a) ? 4 : a.head_dim == 128 ? 2 : 1) * ROUND / key_tiles
+                         : !even             ? 3 * ROUND / key_tiles
+                         : a.causal          ? 2 * ROUND / key_tiles - 1
+                                             : ROUND / key_tiles;
+  p.rows = pieces_of(wanted, a.max_q, (int)G, a.dtype, (int64_t)p.key_slots * a.kv_heads);
   p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written
@@ -673,6 +687,7 @@ int go(Args x, const Grads& g, const Plan& p, hipStream_t s) {
     x.slots = x.tk ? p.key_slots : 0;
     x.splits = p.rows.n;
     x.piece = p.rows.size;
+    x.parts = p.rows.parts;
     if (int rc = launch(k_attention_dkv<T, D, BIAS>, (int64_t)x.kv_heads * x.slots * x.splits + (BIAS ? x.heads : 0),
                         dkv_bytes<T, D>() + STAGES * STATS * tile_rows<T, D>() * 4 + width * x.ratio))
       return rc;

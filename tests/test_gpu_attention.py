@@ -149,6 +149,16 @@ def test_divided_rows(d, dtype):
     _case([2500], [130], 1, 1, d, dtype, False, layout="separate", rel=(16, 30, True))
 
 
+@pytest.mark.parametrize("group", [2, 5, 6, 8])
+def test_rows_divided_by_heads(group):
+    """Few queries of many heads on a key head: pieces of the rows are sets of heads."""
+    for n in ([200], [64, 65], [300, 310, 290], [1]):
+        _case(n, n, group, 1, 64, F32, True, rel=(16, 40, True))
+        _case(n, n, 2 * group, 2, 32, F32, False)
+    _case([5], [700], group, 1, 128, F32, True, layout="separate")
+    _case([130], [70], group, 1, 128, BF16, False, layout="separate")
+
+
 @pytest.mark.parametrize("d", [32, 64, 128])
 @pytest.mark.parametrize("causal", [False, True])
 def test_few_tiles_of_long_rows(causal, d):
