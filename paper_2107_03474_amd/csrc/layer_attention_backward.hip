@@ -291,13 +291,13 @@ constexpr bool values_in_lds() { return Tile<T, D>::ROW >= 256; }
 template <typename T, int D>
 constexpr int tile_rows() { return values_in_lds<T, D>() ? 32 : 64; }  // packed rows
 constexpr int DKV_KEYS = WAVES * 32;
-template <typename T, int D>
+template <typename T, int D, int TEAMS>
 constexpr int dkv_bytes() {
-  return STAGES * 2 * tile_rows<T, D>() * Tile<T, D>::ROW +
+  return TEAMS * STAGES * 2 * tile_rows<T, D>() * Tile<T, D>::ROW +
          (values_in_lds<T, D>() ? DKV_KEYS * Tile<T, D>::ROW : 0);
 }
 template <typename T, int D>
-constexpr int dkv_waves() { return dkv_bytes<T, D>() > 72 * 1024 ? 1 : 2; }  // a SIMD
+constexpr int dkv_waves() { return dkv_bytes<T, D, 1>() > 72 * 1024 ? 1 : 2; }  // a SIMD
 // The bias's gradient from k_attention_dq's sums [rel_rows][heads][buckets], by the workgroup of a head at the end of the
 // grid of k_attention_dkv (a kernel of its own cost 4 us): 8 threads to a bucket, each a fixed set of the rows.
 __device__ __forceinline__ void relative_grad(const Args& a, const Grads& o, int head, float* lds) {
@@ -352,8 +352,9 @@ __device__ __forceinline__ void take_piece(const Args& a, int piece, KeyWork* w)
   w->lo = (int)min((int64_t)max(w->seen, (int)min(lo, (int64_t)w->s.nq)), (int64_t)w->hi);
 }
 
-template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(Args a, Grads o) {
+// TEAMS: of four waves each, which share the keys and take the tiles of queries in turn.
+template <typename T, int D, bool BIAS, int TEAMS>
+__global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attention_dkv(Args a, Grads o) {
   using Ti = Tile<T, D>;
   using F = typename Frag<T>::type;
   constexpr int TROWS = tile_rows<T, D>(), BYTES = TROWS * Ti::ROW;
@@ -363,6 +364,7 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   if constexpr (BIAS) {
     const int tiles = a.kv_heads * a.slots * a.splits;
     if ((int)blockIdx.x >= tiles) {
+      if (threadIdx.x >= THREADS) return;
       relative_grad(a, o, blockIdx.x - tiles, (float*)smem);
       return;
     }
@@ -376,16 +378,18 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   const Seq& s = w.s;
   const bool any = w.lo < w.hi;
   if (a.splits > 1 && !any) return;  // k_attention_dkv_join leaves it out
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
+  const int at_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), l = threadIdx.x % WAVE, h = l >> 5;
+  const int wave = at_wave % WAVES, team = at_wave / WAVES;
   const int off = s.nk - s.nq;
   const int jw = w.j0 + 32 * wave, j = jw + (l & 31);
   const bool valid = j < s.nk;
   // the wave's keys are seen by queries from `some` on, and all of them by those from `all` on
   const int some = a.causal ? jw - off : 0, all = a.causal ? jw + 31 - off : 0;
   F k[D / 16], v[VLDS ? 1 : D / 16];
-  const Lds vt = lds + STAGES * 2 * BYTES;
+  const Lds vt = lds + TEAMS * STAGES * 2 * BYTES;
   if (VLDS && any)
-    load_rows<T, D, DKV_KEYS, WAVES>((const T*)a.v + s.k0 * a.v_row + hk * a.v_head, a.v_row, w.j0, s.nk, vt, wave);
+    load_rows<T, D, DKV_KEYS, TEAMS * WAVES>((const T*)a.v + s.k0 * a.v_row + hk * a.v_head, a.v_row, w.j0, s.nk, vt,
+                                             at_wave);
   {
     const T* kp = (const T*)a.k + (s.k0 + j) * a.k_row + hk * a.k_head + 8 * h;
     const T* vp = (const T*)a.v + (s.k0 + j) * a.v_row + hk * a.v_head + 8 * h;
@@ -398,9 +402,10 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   }
   // The tiles of queries and their grad_out pass through LDS; queries i0 ... of head g, the next to load (into place
   // `place`) and the one in use.
-  // beside the tiles: [STAGES][STATS][TROWS], then the bias table
-  const Lds stats = lds + dkv_bytes<T, D>();
-  float* const table = (float*)(smem + dkv_bytes<T, D>()) + STAGES * STATS * TROWS;
+  // beside the tiles: [TEAMS][STAGES][STATS][TROWS], then the bias table
+  const Lds tiles_at = lds + team * STAGES * 2 * BYTES;
+  const Lds stats = lds + dkv_bytes<T, D, TEAMS>() + team * STAGES * STATS * TROWS * 4;
+  float* const table = (float*)(smem + dkv_bytes<T, D, TEAMS>()) + TEAMS * STAGES * STATS * TROWS;
   const int width = bias_width(a);
   const int64_t g_row = (int64_t)a.heads * D;
   const int top = (w.hi - 1) / TROWS * TROWS;
@@ -408,7 +413,7 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   int place = 0, next_i = top, next_g = g_first;
   const auto load = [&] {
     const int hq = hk * a.ratio + next_g;
-    const Lds to = lds + place * 2 * BYTES;
+    const Lds to = tiles_at + place * 2 * BYTES;
     load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, next_i, w.hi, to, wave);
     load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, next_i, w.hi, to + BYTES, wave);
     if (wave < STATS && l < TROWS) {  // past the end: zeros, as in the tiles, and with them p dO = ds = 0
@@ -418,12 +423,20 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
            (uint32_t)(l * a.heads) * 4);
     }
     place ^= 1;
-    if (++next_g == g_end) {
-      next_g = g_first;
-      next_i -= TROWS;
-    }
   };
-  if (any) load();
+  const auto advance = [&](int steps, int& i, int& g) {
+#pragma unroll
+    for (int t = 0; t < TEAMS; ++t)
+      if (t < steps && ++g == g_end) {
+        g = g_first;
+        i -= TROWS;
+      }
+  };
+  // tiles of all heads that the piece meets, from the last queries on
+  int left = any ? (top / TROWS - w.lo / TROWS + 1) * (g_end - g_first) : 0;
+  advance(team, next_i, next_g);
+  int i0 = next_i, g = next_g;
+  if (team < left) load();
   if constexpr (BIAS) {
     fill_bias(a, hk * a.ratio, a.ratio, table);
     __syncthreads();
@@ -434,17 +447,18 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dk[b][e] = dv[b][e] = 0;
-  int i0 = top, g = g_first;
-  while (any && i0 + TROWS > w.lo) {
+  for (; left > 0; left -= TEAMS) {
     loads_done();
     __syncthreads();
+    if (team >= left) break;  // the last step of an odd number: nothing to wait for but the end
     const int in_use = place ^ 1;
-    if (next_i + TROWS > w.lo)
+    advance(TEAMS, next_i, next_g);
+    if (team + TEAMS < left)
       load();
     else
       place ^= 1;
     asm volatile("" : "+v"(ra), "+v"(ca));  // the addresses are formed at their use: kept, they would not fit the registers
-    const Lds qt = lds + in_use * 2 * BYTES, gt = qt + BYTES;
+    const Lds qt = tiles_at + in_use * 2 * BYTES, gt = qt + BYTES;
     const Lds st = stats + (in_use * STATS * TROWS + 4 * h) * 4;
 #pragma unroll
     for (int rb = 0; rb < TROWS / 32; ++rb) {
@@ -514,10 +528,24 @@ __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void k_attention_dkv(
         for (int b = 0; b < D / 32; ++b) dk[b] = mma(Ti::col_frag(qt, ca, b, 2 * rb + c), fy, dk[b]);
       }
     }
-    if (++g == g_end) {
-      g = g_first;
-      i0 -= TROWS;
+    advance(TEAMS, i0, g);
+  }
+  if constexpr (TEAMS == 2) {  // the second team's sums join the first one's, through the LDS that held the tiles
+    static_assert(D / 2 * THREADS * 4 <= dkv_bytes<T, D, TEAMS>(), "they fit");
+    float* const to = (float*)smem + threadIdx.x % THREADS;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      f32x16(&sum)[D / 32] = k ? dv : dk;
+      __syncthreads();
+      if (team)
+#pragma unroll
+        for (int e = 0; e < D / 2; ++e) to[e * THREADS] = sum[e / 16][e % 16];
+      __syncthreads();
+      if (!team)
+#pragma unroll
+        for (int e = 0; e < D / 2; ++e) sum[e / 16][e % 16] += to[e * THREADS];
     }
+    if (team) return;
   }
   if (a.splits > 1) {
     if (j >= s.nk) return;
@@ -595,6 +623,9 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
 // k_attention_dq with two teams, as in the forward pass, us without / with: causal, 16/8 heads of 64 and bias, 300 tokens 17.4 /
 // 16.1, 1,024 33 / 26, 2,304 60 / 45, 4,097 107 / 110; 8/8 heads of 64, 512 13.5 / 14.2, 6,000 107 / 85; 16/4 heads of 128, 2,600
 // 80 / 68, 4,096 140 / 146; both directions, 8/8 heads of 64, 4,096 71 / 66, 4,224 108 / 118.
+// k_attention_dkv with two teams, where its workgroups leave each a compute unit of its own (UNITS) and the rows are no shorter
+// than 256, us without / with, the join included: causal, 16/8 heads of 64 and bias, 256 tokens 20.7 / 17.0, 1,024 40 / 32, 2,048 (320
+// workgroups) 50 / 60; 16/4 heads of 128, 512 52 / 41, 2,048 (288) 74 / 89; 8/8 heads of 64, 2,048 35 / 30; 32 x 256 (512) 22.6 / 29.6.
 constexpr int MAX_PIECES = 16;
 struct Pieces {
   int n, size, parts;
@@ -619,7 +650,7 @@ Pieces pieces_of(int64_t wanted, int64_t length, int rows, int dtype, int64_t ti
 }
 struct Plan {
   int group, row_slots, key_slots;
-  bool teams;  // two of them in k_attention_dq
+  bool teams, key_teams;  // two of them in k_attention_dq, in k_attention_dkv
   Pieces keys, rows;
   size_t delta, rel, part;  // floats of workspace
 };
@@ -644,6 +675,8 @@ Plan plan_of(const lram_attention& a) {
                          : a.causal          ? 2 * ROUND / key_tiles - 1
                                              : ROUND / key_tiles;
   p.rows = pieces_of(wanted, a.max_q, (int)G, a.dtype, (int64_t)p.key_slots * a.kv_heads);
+  const int64_t busy = a.causal ? key_tiles * (p.rows.n + 1) / 2 : key_tiles * p.rows.n;
+  p.key_teams = a.dtype == LRAM_BF16 && a.max_q * G >= 256 && busy <= UNITS;
   p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written
@@ -688,9 +721,18 @@ int go(Args x, const Grads& g, const Plan& p, hipStream_t s) {
     x.splits = p.rows.n;
     x.piece = p.rows.size;
     x.parts = p.rows.parts;
-    if (int rc = launch(k_attention_dkv<T, D, BIAS>, (int64_t)x.kv_heads * x.slots * x.splits + (BIAS ? x.heads : 0),
-                        dkv_bytes<T, D>() + STAGES * STATS * tile_rows<T, D>() * 4 + width * x.ratio))
-      return rc;
+    const auto dkv = [&](auto teams) {
+      constexpr int TEAMS = decltype(teams)::value;
+      return launch(k_attention_dkv<T, D, BIAS, TEAMS>,
+                    (int64_t)x.kv_heads * x.slots * x.splits + (BIAS ? x.heads : 0),
+                    dkv_bytes<T, D, TEAMS>() + TEAMS * STAGES * STATS * tile_rows<T, D>() * 4 + width * x.ratio,
+                    TEAMS * THREADS);
+    };
+    int rc = LRAM_OK;
+    if constexpr (sizeof(T) == 2)
+      if (p.key_teams) rc = dkv(std::integral_constant<int, 2>());
+    if (!p.key_teams) rc = dkv(std::integral_constant<int, 1>());
+    if (rc) return rc;
     if (x.tk && x.splits > 1)
       return launch(k_attention_dkv_join<T, D>, (int64_t)x.kv_heads * x.slots * JOIN_PARTS, 0);
   }
