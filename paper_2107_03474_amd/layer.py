@@ -90,6 +90,7 @@ def _scratch(nbytes: int, workspace: Optional[torch.Tensor], like: torch.Tensor)
         if not nbytes:
             return None, 0, None
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+        return workspace.data_ptr(), nbytes, workspace
     return _dev(workspace, "workspace", like=like), workspace.numel() * workspace.element_size(), workspace
 
 
