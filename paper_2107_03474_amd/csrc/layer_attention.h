@@ -564,6 +564,13 @@ Args args_of(const lram_attention& a) {
   return x;
 }
 
+// The call with the expected lengths no longer than the tensors, so that no product of them overflows.
+lram_attention bounded(lram_attention a) {
+  a.max_q = std::min(a.max_q, a.tq);
+  a.max_k = std::min(a.max_k, a.tk);
+  return a;
+}
+
 // Whether the expected lengths make a batch of like sequences, whose tiles run in rounds over the chip: then as many pieces
 // as fill one round (two workgroups a CU) are best, where the pieces of ragged ones, which even out, may be twice as
 // many.

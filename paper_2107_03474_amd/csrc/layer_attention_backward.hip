@@ -654,7 +654,8 @@ struct Plan {
   Pieces keys, rows;
   size_t delta, rel, part;  // floats of workspace
 };
-Plan plan_of(const lram_attention& a) {
+Plan plan_of(const lram_attention& call) {
+  const lram_attention a = bounded(call);
   Plan p;
   const int64_t G = a.heads / a.kv_heads;
   p.group = a.rel_weight ? 1 : (int)G;

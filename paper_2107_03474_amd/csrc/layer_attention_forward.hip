@@ -456,7 +456,8 @@ struct Plan {
 // 6,000 104 / 71; 16/4 heads of 128, 2,048 44 / 40; both directions, 8/8 heads of 64, 4,096 64 / 55, 4,224 89 / 97; 24 x 256 13 / 18,
 // 32 x 64 5.6 / 6.3; pieces of prompts over caches of 101 to 12,345, 32/8 heads of 128, 78 / 83; 8 heads of 64 in fp32, 2,048
 // tokens, 63 / 93.
-Plan plan_of(const lram_attention& a) {
+Plan plan_of(const lram_attention& call) {
+  const lram_attention a = bounded(call);
   Plan p;
   const int64_t G = a.heads / a.kv_heads;
   p.few = a.max_q * G <= ROWS;

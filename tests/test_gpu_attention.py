@@ -171,7 +171,7 @@ def test_few_tiles_of_long_rows(causal, d):
 
 def test_hints_do_not_change_results():
     lengths = [150, 1, 290]
-    for hints in ((0, 0), (1, 1), (1, 290), (290, 1), (10 ** 9, 10 ** 9)):
+    for hints in ((0, 0), (1, 1), (1, 290), (290, 1), (10 ** 9, 10 ** 9), ((1 << 63) - 1,) * 2):
         _case(lengths, lengths, 4, 2, 64, BF16, True, hints=hints, rel=(32, 128, True))
         _case(lengths, lengths, 2, 1, 128, BF16, False, hints=hints)
 

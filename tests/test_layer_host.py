@@ -119,6 +119,16 @@ def test_attention_refuses(lib):
     assert _attention_fwd(lib, tq=0, q=None, out=None) == 0  # empty: nothing to do
 
 
+def test_expected_lengths_past_the_tensors(lib):
+    """The workspace of any expectation is that of the tensors' whole lengths at most."""
+    n, want = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    for size in (lib.lram_attention_forward_workspace_bytes, lib.lram_attention_backward_workspace_bytes):
+        assert size(ctypes.byref(_describe(max_q=300, max_k=300)), ctypes.byref(want)) == 0
+        for longest in (301, 1 << 31, 1 << 40, (1 << 63) - 1):
+            assert size(ctypes.byref(_describe(max_q=longest, max_k=longest)), ctypes.byref(n)) == 0
+            assert n.value == want.value
+
+
 @pytest.mark.parametrize("dtype,d,heads,reach", [(1, 128, 4, 1951), (0, 64, 4, 1951), (0, 128, 4, 586), (1, 64, 8, 927),
                                                  (1, 64, 256, 0)])
 def test_the_longest_reach(lib, dtype, d, heads, reach):
