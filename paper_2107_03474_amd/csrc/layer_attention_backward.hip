@@ -626,6 +626,8 @@ __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a, Grads o)
 // k_attention_dkv with two teams, where its workgroups leave each a compute unit of its own (UNITS) and the rows are no shorter
 // than 256, us without / with, the join included: causal, 16/8 heads of 64 and bias, 256 tokens 20.7 / 17.0, 1,024 40 / 32, 2,048 (320
 // workgroups) 50 / 60; 16/4 heads of 128, 512 52 / 41, 2,048 (288) 74 / 89; 8/8 heads of 64, 2,048 35 / 30; 32 x 256 (512) 22.6 / 29.6.
+// They also take the place of two pieces where sequences differ: six texts of 20 to 3,000, 32/8 heads of 128, 433 / 353, 8 heads of
+// 64 with bias 133 / 109; three of 200 to 6,000, 24/8 heads of 128, 707 / 603; eight of 1 to 3,321, 8 heads of 64, 75 / 78.
 constexpr int MAX_PIECES = 16;
 struct Pieces {
   int n, size, parts;
@@ -675,9 +677,14 @@ Plan plan_of(const lram_attention& call) {
                          : !even             ? 3 * ROUND / key_tiles
                          : a.causal          ? 2 * ROUND / key_tiles - 1
                                              : ROUND / key_tiles;
-  p.rows = pieces_of(wanted, a.max_q, (int)G, a.dtype, (int64_t)p.key_slots * a.kv_heads);
+  const auto rows_of = [&](int64_t n) {
+    return pieces_of(n, a.max_q, (int)G, a.dtype, (int64_t)p.key_slots * a.kv_heads);
+  };
+  p.rows = rows_of(wanted);
   const int64_t busy = a.causal ? key_tiles * (p.rows.n + 1) / 2 : key_tiles * p.rows.n;
-  p.key_teams = a.dtype == LRAM_BF16 && a.max_q * G >= 256 && busy <= UNITS;
+  const bool halves = !even && p.rows.n == 2;
+  if (halves) p.rows = rows_of(1);
+  p.key_teams = a.dtype == LRAM_BF16 && a.max_q * G >= 256 && (halves || busy <= UNITS);
   p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written

@@ -149,6 +149,13 @@ def test_divided_rows(d, dtype):
     _case([2500], [130], 1, 1, d, dtype, False, layout="separate", rel=(16, 30, True))
 
 
+def test_long_texts_among_short_ones():
+    """Tiles enough for the chip, of sequences that differ much."""
+    lengths = [2200, 3, 700, 0, 1100, 64]
+    _case(lengths, lengths, 12, 12, 64, BF16, True, rel=(32, 128, True))
+    _case(lengths, lengths, 16, 8, 128, BF16, False)
+
+
 @pytest.mark.parametrize("group", [2, 5, 6, 8])
 def test_rows_divided_by_heads(group):
     """Few queries of many heads on a key head: pieces of the rows are sets of heads."""
