@@ -105,9 +105,12 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
       if (l < 32 && !team) o.delta[at] = delta;
     }
   }
-  const int lim = a.causal && r.valid ? min(r.i + off, w.s.nk - 1) : w.s.nk - 1;
+  // last key of the lane's row, and of the wave's first and last rows.  With a bias, rows past the last query see none:
+  // their weight is 2^bias, which passes fp32's range from a bias of 89 on, and inf times their zeros would be NaN.
+  const bool part = BIAS && first + ROWS > rows;
+  const int lim = BIAS && !r.valid ? -1 : a.causal && r.valid ? min(r.i + off, w.s.nk - 1) : w.s.nk - 1;
   const int i_first = first / G, i_last = (min(first + ROWS, rows) - 1) / G;
-  const int lim_first = a.causal ? min(i_first + off, w.s.nk - 1) : w.s.nk - 1;
+  const int lim_first = part ? -1 : a.causal ? min(i_first + off, w.s.nk - 1) : w.s.nk - 1;
   const int lim_last = first >= rows ? -1 : (a.causal ? min(i_last + off, w.s.nk - 1) : w.s.nk - 1);
   // with a bias G = 1: the lane's row is query i of one head
   const float* bias = nullptr;
@@ -416,7 +419,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
     const Lds to = tiles_at + place * 2 * BYTES;
     load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, next_i, w.hi, to, wave);
     load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, next_i, w.hi, to + BYTES, wave);
-    if (wave < STATS && l < TROWS) {  // past the end: zeros, as in the tiles, and with them p dO = ds = 0
+    if (wave < STATS && l < TROWS) {  // past the end: zeros, as in the tiles
       const float* const from = (wave == LSE ? o.lse : o.delta) + (s.q0 + next_i) * a.heads + hq;
       const int rows = min(w.hi - next_i, TROWS);
       dma4(resource(from, (uint32_t)((rows - 1) * a.heads + 1) * 4), stats + (place * STATS + wave) * TROWS * 4,
@@ -504,11 +507,16 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
           ds[4 * u + e] = p[4 * u + e] * (ds[4 * u + e] - delta[e]);
         }
       }
-      if (i < all) {
-        const int need = j - off - i - 4 * h;
+      // Rows past the last query: p = 1 and with zeros beside it p dO = ds = 0, but p = 2^bias with one, and no number from a
+      // bias of 89 on.
+      const bool part = BIAS && i + 32 > w.hi;
+      if (i < all || part) {
+        const int need = i < all ? j - off - i - 4 * h : -4 * h, end = w.hi - i - 4 * h;
+        const unsigned many = max(end - need, 0);  // rows from `need` on, up to the last
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const bool sees = 8 * (e >> 2) + (e & 3) >= need;
+          const int row = 8 * (e >> 2) + (e & 3);
+          const bool sees = BIAS ? (unsigned)(row - need) < many : row >= need;
           p[e] = sees ? p[e] : 0.0f;
           ds[e] = sees ? ds[e] : 0.0f;
         }
