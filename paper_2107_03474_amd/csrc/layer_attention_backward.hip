@@ -28,8 +28,9 @@ struct Grads {
   const void *out, *residue, *grad_out;
   const float* lse;
   void *gq, *gk, *gv, *grel;
-  // workspace: [tq heads], [slots][heads][buckets], [pieces][tk][kv_heads][2][D] or [splits][tq][heads][D] (dq first)
-  float *delta, *rel, *part;
+  // workspace: row_lse and delta [tq heads], [slots][heads][buckets], [pieces][tk][kv_heads][2][D] or
+  // [splits][tq][heads][D] (dq first)
+  float *row_lse, *delta, *rel, *part;
   int rel_rows;
 };
 
@@ -101,8 +102,13 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
     }
     delta = add_halves(delta);
     if (r.valid) {
+      // a row that meets no key, each of its weights -inf among the reasons: 2^(-inf - inf) = 0 is the p of all its pairs
       lse = o.lse[at];
-      if (l < 32 && !team) o.delta[at] = delta;
+      lse = lse == -INFINITY ? INFINITY : lse;
+      if (l < 32 && !team) {
+        o.row_lse[at] = lse;
+        o.delta[at] = delta;
+      }
     }
   }
   // last key of the lane's row, and of the wave's first and last rows.  With a bias, rows past the last query see none:
@@ -420,7 +426,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
     load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, next_i, w.hi, to, wave);
     load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, next_i, w.hi, to + BYTES, wave);
     if (wave < STATS && l < TROWS) {  // past the end: zeros, as in the tiles
-      const float* const from = (wave == LSE ? o.lse : o.delta) + (s.q0 + next_i) * a.heads + hq;
+      const float* const from = (wave == LSE ? o.row_lse : o.delta) + (s.q0 + next_i) * a.heads + hq;
       const int rows = min(w.hi - next_i, TROWS);
       dma4(resource(from, (uint32_t)((rows - 1) * a.heads + 1) * 4), stats + (place * STATS + wave) * TROWS * 4,
            (uint32_t)(l * a.heads) * 4);
@@ -662,7 +668,7 @@ struct Plan {
   int group, row_slots, key_slots;
   bool teams, key_teams;  // two of them in k_attention_dq, in k_attention_dkv
   Pieces keys, rows;
-  size_t delta, rel, part;  // floats of workspace
+  size_t stats, rel, part;  // floats of workspace; stats: of row_lse and of delta each
 };
 Plan plan_of(const lram_attention& call) {
   const lram_attention a = bounded(call);
@@ -693,7 +699,7 @@ Plan plan_of(const lram_attention& call) {
   const bool halves = !even && p.rows.n == 2;
   if (halves) p.rows = rows_of(1);
   p.key_teams = a.dtype == LRAM_BF16 && a.max_q * G >= 256 && (halves || busy <= UNITS);
-  p.delta = ((size_t)a.tq * a.heads + 3) / 4 * 4;
+  p.stats = ((size_t)a.tq * a.heads + 3) / 4 * 4;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written
   const size_t dq = p.keys.n > 1 ? (size_t)p.keys.n * a.tq * a.heads * a.head_dim : 0;
@@ -763,7 +769,7 @@ int lram_attention_backward_workspace_bytes(const lram_attention* a, size_t* byt
   if (!a || !bytes) return LRAM_EINVAL;
   if (int rc = check_attention(*a, false)) return rc;
   const Plan p = plan_of(*a);
-  *bytes = (p.delta + p.rel + p.part) * 4;
+  *bytes = (2 * p.stats + p.rel + p.part) * 4;
   return LRAM_OK;
 }
 
@@ -781,13 +787,13 @@ int lram_attention_backward(const lram_attention* a, const void* out, const void
     return LRAM_EINVAL;
   if (residue && a->dtype != LRAM_BF16) return LRAM_EDTYPE;
   const Plan p = plan_of(*a);
-  const size_t need = (p.delta + p.rel + p.part) * 4;
+  const size_t need = (2 * p.stats + p.rel + p.part) * 4;
   if (need && (!workspace || off_align(workspace, 16) || ws_bytes < need)) return LRAM_EWORKSPACE;
   Args x = args_of(*a);
   x.splits = 1;
   float* const ws = (float*)workspace;
-  const Grads g{out, residue, grad_out, lse, grad_q, grad_k, grad_v, grad_rel, ws, ws + p.delta,
-                ws + p.delta + p.rel, a->tq ? p.row_slots * p.keys.n : 0};
+  const Grads g{out, residue, grad_out, lse, grad_q, grad_k, grad_v, grad_rel, ws, ws + p.stats,
+                ws + 2 * p.stats, ws + 2 * p.stats + p.rel, a->tq ? p.row_slots * p.keys.n : 0};
   return by_kind(*a, [&](auto t, auto d, auto bias) {
     return go<decltype(t), decltype(d)::value, decltype(bias)::value>(x, g, p, (hipStream_t)stream);
   });

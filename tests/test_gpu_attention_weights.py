@@ -1,5 +1,7 @@
 """Attention whose relative position bias has weights far from zero, against the 64-bit form and its derived bounds
 (layer_reference.py)."""
+import math
+
 import pytest
 import torch
 
@@ -54,3 +56,47 @@ def test_a_shift_of_every_weight(lengths, shift, reach, causal, dtype):
     want = ref.attention(q, k, v, lengths, lengths, _starts(lengths), _starts(lengths), causal, 0.125, w, bucket, do)
     for n, t in got.items():
         ref.assert_close(n, t, want[n])
+
+
+def _by_autograd(q, k, v, do, lengths, causal, w, bucket):
+    """Values in 64 bits from the definition; a query whose keys all have weight -inf meets none."""
+    reach = bucket.numel() // 2
+    leaves = [t.double().requires_grad_() for t in (q, k, v, w)]
+    q64, k64, v64, w64 = leaves
+    group, outs = q.shape[1] // k.shape[1], []
+    for n, s in zip(lengths, _starts(lengths)):
+        i = torch.arange(n, device=DEV)
+        far = i[None] - i[:, None]
+        z = q64[s:s + n].transpose(0, 1) @ k64[s:s + n].transpose(0, 1).repeat_interleave(group, 0).transpose(1, 2) * 0.125
+        bias = w64[:, bucket.long()[far.clamp(-reach, reach) + reach]]
+        seen = (bias != -math.inf) & (far <= 0 if causal else torch.ones_like(far, dtype=torch.bool))
+        z = torch.where(seen, z + torch.where(seen, bias, 0.0), -1e300)
+        p = torch.softmax(z, 2) * seen.any(2, keepdim=True)
+        outs.append((p @ v64[s:s + n].transpose(0, 1).repeat_interleave(group, 0)).transpose(0, 1))
+    out = torch.cat(outs)
+    out.backward(do.double())
+    return dict(out=out.detach(), dq=q64.grad, dk=k64.grad, dv=v64.grad, dw=w64.grad)
+
+
+@BOTH_TYPES
+@BOTH_WAYS
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("reach", [3, 128])
+def test_weights_of_minus_infinity_hide_keys(lengths, reach, causal, dtype):
+    """Head 0: no key at all; head 1: not a query's own key, so that a text's first query (causal) meets none; head 2:
+    no key past reach.  The bounds are those of weights of -300, whose keys weigh nothing either."""
+    q, k, v, do = _inputs(lengths, 4, 2, 64, dtype, 7)
+    bucket = lram.relative_buckets(8, reach)
+    w = torch.randn((4, 8), generator=torch.Generator().manual_seed(8)).to(DEV).to(dtype)
+    w[0] = w[1, 0] = w[2, bucket[0]] = w[2, bucket[-1]] = -math.inf
+    got = _run(q, k, v, do, lengths, causal, w, bucket)
+    value = _by_autograd(q, k, v, do, lengths, causal, w, bucket)
+    like = ref.attention(q, k, v, lengths, lengths, _starts(lengths), _starts(lengths), causal, 0.125,
+                         w.clamp(min=-300.0), bucket, do)
+    for n in value:
+        ref.assert_close(n, got[n], (value[n], like[n][1]))
+    assert not got["out"][:, 0].any() and not got["dq"][:, 0].any() and not got["dw"][0].any()
+    assert (got["lse"][:, 0] == -math.inf).all()
+    if causal:
+        first = _starts(lengths)
+        assert not got["out"][first, 1].any() and not got["dq"][first, 1].any()
