@@ -28,9 +28,9 @@ struct Grads {
   const void *out, *residue, *grad_out;
   const float* lse;
   void *gq, *gk, *gv, *grel;
-  // workspace: row_lse and delta [tq heads], [slots][heads][buckets], [pieces][tk][kv_heads][2][D] or
+  // workspace: row_lse, delta and (with a bias) share [tq heads], [slots][heads][buckets], [pieces][tk][kv_heads][2][D] or
   // [splits][tq][heads][D] (dq first)
-  float *row_lse, *delta, *rel, *part;
+  float *row_lse, *delta, *share, *rel, *part;
   int rel_rows;
 };
 
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
   F q[D / 16], g[D / 16];
   load_query<T, D>(a, (const T*)a.q, a.q_row, a.q_head, w.s, head, r, q);
   load_query<T, D>(a, (const T*)o.grad_out, (int64_t)a.heads * D, D, w.s, head, r, g);
-  float delta = 0, lse = 0;
+  float delta = 0, lse = 0, share = 1;  // share: what p lacks beside 2^(z - lse) (parts_of)
   {
     F x[D / 16];
     load_query<T, D>(a, (const T*)o.out, (int64_t)a.heads * D, D, w.s, head, r, x);
@@ -105,10 +105,17 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
       // a row that meets no key, each of its weights -inf among the reasons: 2^(-inf - inf) = 0 is the p of all its pairs
       lse = o.lse[at];
       lse = lse == -INFINITY ? INFINITY : lse;
+      if constexpr (BIAS) {
+        const LseParts part = parts_of(lse);
+        lse = part.top;
+        share = __builtin_amdgcn_exp2f(-part.rest);
+      }
       if (l < 32 && !team) {
         o.row_lse[at] = lse;
         o.delta[at] = delta;
+        if constexpr (BIAS) o.share[at] = share;
       }
+      if constexpr (BIAS) delta *= share;
     }
   }
   // last key of the lane's row, and of the wave's first and last rows.  With a bias, rows past the last query see none:
@@ -120,7 +127,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
   const int lim_last = first >= rows ? -1 : (a.causal ? min(i_last + off, w.s.nk - 1) : w.s.nk - 1);
   // with a bias G = 1: the lane's row is query i of one head
   const float* bias = nullptr;
-  float far_bias[2] = {0, 0}, far_sum[2] = {0, 0};
+  float far_bias[2] = {0, 0}, far_unit[2] = {a.c, a.c}, far_sum[2] = {0, 0};
   const int width = bias_width(a);
   float* const table = (float*)(smem + TEAMS * ring_bytes<T, D>());
   float* const sums = table + width;              // [TABLES][width]
@@ -130,13 +137,15 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
     for (int n = 0, t = threadIdx.x; t < width; ++n, t += ALL) {
       const int id = n == 0 ? ids[0] : n == 1 ? ids[1] : bucket_of(a, t - a.reach - BIAS_PAD);
       of[t] = id;
-      table[t] = rel_weight(a, w.head.first, id) * LOG2E;
+      table[t] = in_log2(rel_weight(a, w.head.first, id));
     }
     for (int t = threadIdx.x; t < TABLES * width; t += ALL) sums[t] = 0;
     bias = table + a.reach + BIAS_PAD - (r.i + off);
     __syncthreads();
     far_bias[0] = table[0];
     far_bias[1] = table[width - 1];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) far_unit[side] = unit_beside(far_bias[side], a.c);
   }
   const uint32_t ka = Ti::row_base(l & 31), ca = Ti::col_base();
   f32x16 acc[D / 32];
@@ -165,8 +174,9 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
         far = far_bias[above];
       }
       if (whole) {
+        const float unit = BIAS ? far_unit[above] : a.c;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.c, far - lse));
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], unit, far - lse));
       } else {
         const float* t = bias + j + 4 * h;
 #pragma unroll
@@ -174,7 +184,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
           s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.c, t[8 * (e >> 2) + (e & 3)]) - lse);
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] *= dp[e] - delta;
+      for (int e = 0; e < 16; ++e) s[e] *= BIAS ? fmaf(dp[e], share, -delta) : dp[e] - delta;
       if (j + 31 > lim_first) {
         const int last = lim - j - 4 * h;
 #pragma unroll
@@ -332,8 +342,10 @@ __device__ __forceinline__ void relative_grad(const Args& a, const Grads& o, int
   }
 }
 
-// What it keeps of a tile's queries beside them: lse and delta.
-enum { LSE, DELTA, STATS };
+// What it keeps of a tile's queries beside them: lse, delta and, with a bias, share.
+enum { LSE, DELTA, SHARE };
+template <bool BIAS>
+constexpr int stats_of() { return BIAS ? 3 : 2; }
 
 // The key tile of a workgroup and its piece of the queries, lo to hi (lo >= hi: none meets the tile).  It walks from the last
 // queries to the first, and over the heads of its group at each: the workgroups of a sequence that run side by side read
@@ -368,6 +380,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
   using F = typename Frag<T>::type;
   constexpr int TROWS = tile_rows<T, D>(), BYTES = TROWS * Ti::ROW;
   constexpr bool VLDS = values_in_lds<T, D>();
+  constexpr int STATS = stats_of<BIAS>();
   extern __shared__ __attribute__((aligned(256))) char smem[];
   Lds lds = (Lds)smem;
   if constexpr (BIAS) {
@@ -426,7 +439,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
     load_rows<T, D, TROWS, WAVES>((const T*)a.q + s.q0 * a.q_row + hq * a.q_head, a.q_row, next_i, w.hi, to, wave);
     load_rows<T, D, TROWS, WAVES>((const T*)o.grad_out + s.q0 * g_row + hq * D, g_row, next_i, w.hi, to + BYTES, wave);
     if (wave < STATS && l < TROWS) {  // past the end: zeros, as in the tiles
-      const float* const from = (wave == LSE ? o.row_lse : o.delta) + (s.q0 + next_i) * a.heads + hq;
+      const float* const from = (wave == LSE ? o.row_lse : wave == DELTA ? o.delta : o.share) + (s.q0 + next_i) * a.heads + hq;
       const int rows = min(w.hi - next_i, TROWS);
       dma4(resource(from, (uint32_t)((rows - 1) * a.heads + 1) * 4), stats + (place * STATS + wave) * TROWS * 4,
            (uint32_t)(l * a.heads) * 4);
@@ -446,9 +459,13 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
   advance(team, next_i, next_g);
   int i0 = next_i, g = next_g;
   if (team < left) load();
+  bool vast = false;  // some weight is: rows have a share
   if constexpr (BIAS) {
-    fill_bias(a, hk * a.ratio, a.ratio, table);
+    char* const flags = (char*)(table + a.ratio * width);  // a wave's each
+    const bool mine = __builtin_amdgcn_ballot_w64(fill_bias(a, hk * a.ratio, a.ratio, table)) != 0;
+    if (l == 0) flags[at_wave] = mine;
     __syncthreads();
+    vast = __builtin_amdgcn_ballot_w64(l < TEAMS * WAVES && flags[l & (TEAMS * WAVES - 1)]) != 0;
   }
   uint32_t ra = Ti::row_base(l & 31), ca = Ti::col_base();
   f32x16 dk[D / 32], dv[D / 32];
@@ -492,7 +509,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
         else
           ds = mma(Ti::row_frag(gt, ra, x, 32 * rb), v[x], ds);
       }
-      float unit = a.c;
+      float unit = BIAS && vast ? unit_beside(far, a.c) : a.c;
       if constexpr (BIAS) {
         if (near) {  // entry of distance j - (i + 31) - off, the block's queries from there downwards
           const float* from = table + g * width + a.reach + BIAS_PAD + j - (i + 31 + off) - 4 * h;
@@ -516,7 +533,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
       // Rows past the last query: p = 1 and with zeros beside it p dO = ds = 0, but p = 2^bias with one, and no number from a
       // bias of 89 on.
       const bool part = BIAS && i + 32 > w.hi;
-      if (i < all || part) {
+      if (i < all || part || vast) {
         const int need = i < all ? j - off - i - 4 * h : -4 * h, end = w.hi - i - 4 * h;
         const unsigned many = max(end - need, 0);  // rows from `need` on, up to the last
 #pragma unroll
@@ -525,6 +542,18 @@ __global__ __launch_bounds__(TEAMS* THREADS, (dkv_waves<T, D>())) void k_attenti
           const bool sees = BIAS ? (unsigned)(row - need) < many : row >= need;
           p[e] = sees ? p[e] : 0.0f;
           ds[e] = sees ? ds[e] : 0.0f;
+        }
+        if (BIAS && vast) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const f32x4 share =
+                *(const __attribute__((address_space(3))) f32x4*)(st + (SHARE * TROWS + 32 * rb + 8 * u) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              p[4 * u + e] *= share[e];
+              ds[4 * u + e] *= share[e];
+            }
+          }
         }
       }
 #pragma unroll
@@ -668,7 +697,8 @@ struct Plan {
   int group, row_slots, key_slots;
   bool teams, key_teams;  // two of them in k_attention_dq, in k_attention_dkv
   Pieces keys, rows;
-  size_t stats, rel, part;  // floats of workspace; stats: of row_lse and of delta each
+  size_t stats, rel, part;  // floats of workspace; stats: of row_lse, of delta and of share each
+  int kinds;                // how many of those there are
 };
 Plan plan_of(const lram_attention& call) {
   const lram_attention a = bounded(call);
@@ -700,6 +730,7 @@ Plan plan_of(const lram_attention& call) {
   if (halves) p.rows = rows_of(1);
   p.key_teams = a.dtype == LRAM_BF16 && a.max_q * G >= 256 && (halves || busy <= UNITS);
   p.stats = ((size_t)a.tq * a.heads + 3) / 4 * 4;
+  p.kinds = a.rel_weight ? 3 : 2;
   p.rel = a.rel_weight ? ((size_t)p.row_slots * p.keys.n * a.heads * a.rel_buckets + 3) / 4 * 4 : 0;
   // dq's pieces are joined before those of dk and dv are written
   const size_t dq = p.keys.n > 1 ? (size_t)p.keys.n * a.tq * a.heads * a.head_dim : 0;
@@ -747,7 +778,8 @@ int go(Args x, const Grads& g, const Plan& p, hipStream_t s) {
       constexpr int TEAMS = decltype(teams)::value;
       return launch(k_attention_dkv<T, D, BIAS, TEAMS>,
                     (int64_t)x.kv_heads * x.slots * x.splits + (BIAS ? x.heads : 0),
-                    dkv_bytes<T, D, TEAMS>() + TEAMS * STAGES * STATS * tile_rows<T, D>() * 4 + width * x.ratio,
+                    dkv_bytes<T, D, TEAMS>() + TEAMS * STAGES * stats_of<BIAS>() * tile_rows<T, D>() * 4 +
+                        (BIAS ? width * x.ratio + TEAMS * WAVES : 0),
                     TEAMS * THREADS);
     };
     int rc = LRAM_OK;
@@ -769,7 +801,7 @@ int lram_attention_backward_workspace_bytes(const lram_attention* a, size_t* byt
   if (!a || !bytes) return LRAM_EINVAL;
   if (int rc = check_attention(*a, false)) return rc;
   const Plan p = plan_of(*a);
-  *bytes = (2 * p.stats + p.rel + p.part) * 4;
+  *bytes = (p.kinds * p.stats + p.rel + p.part) * 4;
   return LRAM_OK;
 }
 
@@ -787,13 +819,13 @@ int lram_attention_backward(const lram_attention* a, const void* out, const void
     return LRAM_EINVAL;
   if (residue && a->dtype != LRAM_BF16) return LRAM_EDTYPE;
   const Plan p = plan_of(*a);
-  const size_t need = (2 * p.stats + p.rel + p.part) * 4;
+  const size_t need = (p.kinds * p.stats + p.rel + p.part) * 4;
   if (need && (!workspace || off_align(workspace, 16) || ws_bytes < need)) return LRAM_EWORKSPACE;
   Args x = args_of(*a);
   x.splits = 1;
   float* const ws = (float*)workspace;
   const Grads g{out, residue, grad_out, lse, grad_q, grad_k, grad_v, grad_rel, ws, ws + p.stats,
-                ws + 2 * p.stats, ws + 2 * p.stats + p.rel, a->tq ? p.row_slots * p.keys.n : 0};
+                ws + 2 * p.stats, ws + p.kinds * p.stats, ws + p.kinds * p.stats + p.rel, a->tq ? p.row_slots * p.keys.n : 0};
   return by_kind(*a, [&](auto t, auto d, auto bias) {
     return go<decltype(t), decltype(d)::value, decltype(bias)::value>(x, g, p, (hipStream_t)stream);
   });

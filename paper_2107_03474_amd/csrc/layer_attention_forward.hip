@@ -196,7 +196,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
   const int lim_first = a.causal ? min(i_first + off, w.s.nk - 1) : w.s.nk - 1;
   const int lim_last = first >= rows ? -1 : (a.causal ? min(i_last + off, w.s.nk - 1) : w.s.nk - 1);
   const float* bias = nullptr;
-  float near_far[2] = {0, 0};
+  float near_far[2] = {0, 0}, far_unit[2] = {a.c, a.c};
   if constexpr (BIAS) {
     float* table = (float*)(smem + prompt_bytes<T, D, TEAMS>());
     fill_bias(a, w.head.first, G, table);
@@ -205,6 +205,8 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
     const float* mine = table + (r.valid ? r.g : 0) * bias_width(a);
     near_far[0] = mine[0];
     near_far[1] = mine[bias_width(a) - 1];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) far_unit[side] = unit_beside(near_far[side], a.c);
   }
   const uint32_t ka = Ti::row_base(l & 31), va = Ti::col_base();
   Running<D> st;
@@ -216,14 +218,15 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
 #pragma unroll
     for (int b = 0; b < KEYS / 32; ++b) {
       const int j = j0 + 32 * b;
-      bool near = false;
+      bool near = false, above = false;
       float far = 0;
       if constexpr (BIAS) {
-        const bool below = j + 31 - (i_first + off) <= -a.reach, above = j - (i_last + off) >= a.reach;
+        const bool below = j + 31 - (i_first + off) <= -a.reach;
+        above = j - (i_last + off) >= a.reach;
         near = !below && !above;
         far = near ? 0.0f : near_far[above];
       }
-      const float unit = near ? 1.0f : a.c;
+      const float unit = near ? 1.0f : BIAS ? far_unit[above] : a.c;
       prepare<BIAS>(s[b], a.c, j, bias, near, j + 31 > lim_first, lim);
       grow(st, s[b], unit, far);
       if constexpr (decltype(more)::value) next[b] = scores<T, D>(q, kt, ka, 32 * b);
@@ -275,7 +278,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
   if (!r.valid) return;
   const float inv = sum == 0 ? 0.0f : 1.0f / sum;
   const int64_t at = (w.s.q0 + r.i) * a.heads + head;
-  if (l < 32) put_lse(a, o, w.split, at, sum == 0 ? -INFINITY : st.m + __builtin_amdgcn_logf(sum));
+  if (l < 32) put_lse(a, o, w.split, at, lse_of(st.m, sum));
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
   const int i_first = w.row0 / G, i_last = (min(w.row0 + ROWS, rows) - 1) / G;
   const int lim_first = a.causal ? min(i_first + off, w.s.nk - 1) : w.s.nk - 1;
   const float* bias = nullptr;
-  float near_far[2] = {0, 0};
+  float near_far[2] = {0, 0}, far_unit[2] = {a.c, a.c};
   if constexpr (BIAS) {
     float* table = (float*)(smem + few_bytes<T, D>());
     fill_bias(a, w.head.first, G, table);
@@ -325,6 +328,8 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
     const float* mine = table + (r.valid ? r.g : 0) * bias_width(a);
     near_far[0] = mine[0];
     near_far[1] = mine[bias_width(a) - 1];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) far_unit[side] = unit_beside(near_far[side], a.c);
   }
   const uint32_t ka = Ti::row_base(l & 31), va = Ti::col_base();
   Running<D> st;
@@ -348,14 +353,15 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
     } else {
       loads_left<0>();
     }
-    bool near = false;
+    bool near = false, above = false;
     float far = 0;
     if constexpr (BIAS) {
-      const bool below = j0 + N - 1 - (i_first + off) <= -a.reach, above = j0 - (i_last + off) >= a.reach;
+      const bool below = j0 + N - 1 - (i_first + off) <= -a.reach;
+      above = j0 - (i_last + off) >= a.reach;
       near = !below && !above;
       far = near ? 0.0f : near_far[above];
     }
-    const float unit = near ? 1.0f : a.c;
+    const float unit = near ? 1.0f : BIAS ? far_unit[above] : a.c;
     f32x16 s = scores<T, D>(q, lds + buf * 2 * BYTES, ka, 0);
     prepare<BIAS>(s, a.c, j0, bias, near, j0 + N - 1 > lim_first, lim);
     grow(st, s, unit, far);
@@ -382,7 +388,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
     sum += ml[(WAVES + v) * ROWS + (l & 31)] * __builtin_amdgcn_exp2f(ml[v * ROWS + (l & 31)] - m0);
   const float f = sum == 0 ? 0.0f : __builtin_amdgcn_exp2f(st.m - m0) / sum;
   const int64_t at = (w.s.q0 + r.i) * a.heads + head;
-  if (wave == 0 && l < 32 && r.valid) put_lse(a, o, w.split, at, sum == 0 ? -INFINITY : m + __builtin_amdgcn_logf(sum));
+  if (wave == 0 && l < 32 && r.valid) put_lse(a, o, w.split, at, lse_of(m, sum));
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -417,14 +423,15 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(Args a, Out o) {
   const int d = threadIdx.x % PER * 4;
   if (at >= n) return;
   float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, o.part_lse[s * n + at]);
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, parts_of(o.part_lse[s * n + at]).top);
   const float m0 = m == -INFINITY ? 0.0f : m;
   float sum = 0;
   f32x4 x = {0, 0, 0, 0};
   for (int s = 0; s < a.splits; ++s) {
     const float lse = o.part_lse[s * n + at];
     if (lse == -INFINITY) continue;  // a piece without keys
-    const float f = __builtin_amdgcn_exp2f(lse - m0);
+    const LseParts part = parts_of(lse);
+    const float f = __builtin_amdgcn_exp2f(part.top - m0 + part.rest);
     sum += f;
     const f32x4 y = *(const f32x4*)(o.part + (s * n + at) * D + d);
 #pragma unroll
@@ -435,7 +442,7 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(Args a, Out o) {
   for (int e = 0; e < 4; ++e) x[e] *= inv;
   a.splits = 1;
   put<T, D>(a, o, 0, at, d, x);
-  if (d == 0) put_lse(a, o, 0, at, sum == 0 ? -INFINITY : m + __builtin_amdgcn_logf(sum));
+  if (d == 0) put_lse(a, o, 0, at, lse_of(m, sum));
 }
 
 struct Plan {

@@ -243,7 +243,8 @@ def pack(queries: Sequence[int], keys: Optional[Sequence[int]] = None, capacity:
 class RelativeBias(NamedTuple):
     """Learned bias of a query-key pair by head and bucket of their distance: weight [heads, buckets] (q's type or
     fp32), bucket [2 reach + 1] int32 (``relative_buckets``): the bucket of key minus query = -reach ... reach, the ends
-    aligned; longer distances take the last one's."""
+    aligned; longer distances take the last one's.  A weight of -inf hides its keys; finite ones from 1.2e7 on in
+    magnitude, the type's lowest value among them, count alike, and no score matters beside them."""
     weight: torch.Tensor
     bucket: torch.Tensor
 
