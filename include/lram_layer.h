@@ -68,8 +68,8 @@ int lram_layer_norm_backward(const void* h, const void* weight, const float* mea
  *
  * The lengths stay on the device: nothing waits for them, and a captured call may be replayed over others.  max_q and
  * max_k are the longest nq and nk expected, from which the host chooses how to divide the work; lengths beyond them
- * cost time, not results.  start_q[0] and start_k[0] are taken as 0; rows of q past the last sequence give zeros, and
- * whatever the device arrays hold, no row outside the tensors is addressed.  A value that is not finite can reach
+ * cost time, not results.  Rows of q before the first sequence and past the last one give zeros, and whatever the device
+ * arrays hold, no row outside the tensors is addressed.  A value that is not finite can reach
  * every query of its own sequence (a product with weight 0 is formed in a tile), never another sequence's, and keys
  * at and past nk are not read into any result.
  */

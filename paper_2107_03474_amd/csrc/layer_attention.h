@@ -52,7 +52,7 @@ struct Args {
   int32_t group;  // of them, those packed in a tile: ratio or 1
   int32_t causal, buckets, reach;
   int32_t rel_bf16;
-  int32_t slots;   // row (or key) tiles of all sequences, some of them empty
+  int32_t slots;   // row (or key) tiles of all stretches (sequence), some of them empty
   int32_t splits;  // pieces of the keys (dk, dv: of the rows)
   int32_t piece;   // keys (queries) of a piece
   int32_t parts;   // dk, dv: so many pieces share a piece's queries, by their heads
@@ -69,72 +69,76 @@ struct Seq {
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
-// Sequence b; b = batch is the rows past the last sequence, which see nothing.  The first sequence starts at row 0.
-__device__ __forceinline__ Seq sequence(const Args& a, int b) {
-  const int next = b < a.batch ? b + 1 : b;
-  const int64_t q0 = a.start_q[b], q1 = a.start_q[next], k0 = a.start_k[b], k1 = a.start_k[next];
-  const int64_t used = a.used_k && b < a.batch ? a.used_k[b] : INT32_MAX;
+// The tensors' rows come in batch + 2 stretches: those before the first sequence (0), the sequences (1 ... batch) and those
+// past the last one (batch + 1).  The first and the last see nothing.
+__device__ __forceinline__ Seq sequence(const Args& a, int e) {
+  const int from = e ? e - 1 : 0, to = e <= a.batch ? e : a.batch;  // starts
+  const bool real = from < to;
+  const int64_t q0 = a.start_q[from], q1 = a.start_q[to], k0 = a.start_k[from], k1 = a.start_k[to];
+  const int64_t used = a.used_k && real ? a.used_k[from] : INT32_MAX;
   Seq s;
-  s.q0 = b ? clamp64(q0, 0, a.tq) : 0;
-  s.k0 = b ? clamp64(k0, 0, a.tk) : 0;
-  s.nq = (int32_t)((b < a.batch ? clamp64(q1, s.q0, a.tq) : a.tq) - s.q0);
-  s.cap = (int32_t)((b < a.batch ? clamp64(k1, s.k0, a.tk) : a.tk) - s.k0);
-  s.nk = b < a.batch ? (int32_t)clamp64(used, 0, s.cap) : 0;
+  s.q0 = e ? clamp64(q0, 0, a.tq) : 0;
+  s.k0 = e ? clamp64(k0, 0, a.tk) : 0;
+  s.nq = (int32_t)((e <= a.batch ? clamp64(q1, s.q0, a.tq) : a.tq) - s.q0);
+  s.cap = (int32_t)((e <= a.batch ? clamp64(k1, s.k0, a.tk) : a.tk) - s.k0);
+  s.nk = real ? (int32_t)clamp64(used, 0, s.cap) : 0;
   return s;
 }
 
-// Which sequence and which of its tiles a slot of the grid is, without knowing the lengths on the host.  Tiles hold `tile`
-// packed rows, `scale` to a query (BY_KEYS: rows of k and v, 1 to a row).  The grid has rows scale / tile + batch + 1 slots, at
-// least as many as there are tiles; those left over are empty.
+// Which stretch and which of its tiles a slot of the grid is, without knowing the lengths on the host.  Tiles hold `tile`
+// packed rows, `scale` to a query (BY_KEYS: rows of k and v, 1 to a row).  The grid has slots_of slots, at least as many as
+// there are tiles; those left over are empty.
 //
-// Up to 63 sequences, a lane for each (and one for the rows past the last), all of whose places are read at once: the
-// longest sequences come first, ties in their order, so that the workgroups that start last are short.  More sequences:
-// sequence b takes the slots from start[b] scale / tile + b on, which leaves each as many as it needs, and is found by a
-// wave that looks at 64 places at once.
+// Up to 62 sequences, a lane for each stretch, all of whose places are read at once: the longest come first, ties in their
+// order, so that the workgroups that start last are short.  More sequences: stretch e, which begins at row r, takes the
+// slots from r scale / tile + e on, which leaves each as many as it needs, and is found by a wave that looks at 64 places
+// at once.
+inline int slots_of(int64_t rows, int64_t scale, int tile, int batch) { return (int)(rows * scale / tile + batch + 2); }
 struct Place {
   Seq s;
-  int64_t tile;  // past the sequence's last one: an empty slot
+  int64_t tile;  // past the stretch's last one: an empty slot
 };
-__device__ __forceinline__ int64_t first_slot(const int32_t* start, int64_t rows, int b, int scale, int tile) {
-  return (b ? clamp64(start[b], 0, rows) : 0) * scale / tile + b;
+__device__ __forceinline__ int64_t first_slot(const int32_t* start, int64_t rows, int e, int scale, int tile) {
+  return (e ? clamp64(start[e - 1], 0, rows) : 0) * scale / tile + e;
 }
 __device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 template <bool BY_KEYS>
 __device__ __forceinline__ Place place_of(const Args& a, int scale, int tile, int slot) {
-  const int lane = threadIdx.x % WAVE, batch = a.batch;
-  if (batch < WAVE) {
-    const Seq s = sequence(a, lane <= batch ? lane : batch);
-    const int mine = lane > batch ? 0 : (int)(((int64_t)(BY_KEYS ? s.cap : s.nq) * scale + tile - 1) / tile);
-    const int one = of_lane(mine, 0);
-    int first;  // slot of the sequence's first tile
-    if (__builtin_amdgcn_ballot_w64(lane < batch && mine != one) == 0 && of_lane(mine, batch) <= one) {
-      first = lane * one;
+  const int lane = threadIdx.x % WAVE, last = a.batch + 1;
+  if (last < WAVE) {
+    const Seq s = sequence(a, lane <= last ? lane : last);
+    const int mine = lane > last ? 0 : (int)(((int64_t)(BY_KEYS ? s.cap : s.nq) * scale + tile - 1) / tile);
+    const int one = of_lane(mine, 1);
+    int first;  // slot of the stretch's first tile
+    if (__builtin_amdgcn_ballot_w64(lane && lane < last && mine != one) == 0 && of_lane(mine, 0) == 0 &&
+        of_lane(mine, last) <= one) {
+      first = (lane - 1) * one;  // like sequences from row 0 on
     } else {
       first = 0;
-      for (int b = 0; b <= batch; ++b) {
-        const int other = of_lane(mine, b);
-        first += other > mine || (other == mine && b < lane) ? other : 0;
+      for (int e = 0; e <= last; ++e) {
+        const int other = of_lane(mine, e);
+        first += other > mine || (other == mine && e < lane) ? other : 0;
       }
     }
-    const uint64_t at = __builtin_amdgcn_ballot_w64(lane <= batch && first <= slot && slot - first < mine);
+    const uint64_t at = __builtin_amdgcn_ballot_w64(lane <= last && first <= slot && slot - first < mine);
     Place p{};
     p.tile = INT32_MAX;
     if (!at) return p;
-    const int b = __ffsll((unsigned long long)at) - 1;
-    p.s.q0 = of_lane((int)s.q0, b);  // the starts are 32-bit
-    p.s.k0 = of_lane((int)s.k0, b);
-    p.s.nq = of_lane(s.nq, b);
-    p.s.nk = of_lane(s.nk, b);
-    p.s.cap = of_lane(s.cap, b);
-    p.tile = slot - of_lane(first, b);
+    const int e = __ffsll((unsigned long long)at) - 1;
+    p.s.q0 = of_lane((int)s.q0, e);  // the starts are 32-bit
+    p.s.k0 = of_lane((int)s.k0, e);
+    p.s.nq = of_lane(s.nq, e);
+    p.s.nk = of_lane(s.nk, e);
+    p.s.cap = of_lane(s.cap, e);
+    p.tile = slot - of_lane(first, e);
     return p;
   }
   const int32_t* const start = BY_KEYS ? a.start_k : a.start_q;
   const int64_t rows = BY_KEYS ? a.tk : a.tq;
-  int lo = 0, n = batch + 1;  // the last b of lo ... lo + n - 1 with first_slot(b) <= slot
+  int lo = 0, n = last + 1;  // the last e of lo ... lo + n - 1 with first_slot(e) <= slot
   while (n > 1) {
-    const int step = (n + WAVE - 1) / WAVE, b = lo + lane * step;
-    const bool at = b < lo + n && first_slot(start, rows, b, scale, tile) <= slot;
+    const int step = (n + WAVE - 1) / WAVE, e = lo + lane * step;
+    const bool at = e < lo + n && first_slot(start, rows, e, scale, tile) <= slot;
     // the first place holds; where the starts do not rise, none may, and the search stays inside them all the same
     const int past = max(__popcll(__builtin_amdgcn_ballot_w64(at)) - 1, 0) * step;
     lo += past;
@@ -560,7 +564,7 @@ int check_attention(const lram_attention& a, bool pointers) {
     return LRAM_EINVAL;
   // a grid holds less than 2^32 threads: tiles of 32 rows or more, a workgroup of 256 each; pieces are made where they
   // fit (few_enough)
-  if (a.heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 2) >= MOST_GROUPS) return LRAM_EINVAL;
+  if (a.heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 3) >= MOST_GROUPS) return LRAM_EINVAL;
   if (a.rel_weight) {
     if (a.wdtype != LRAM_F32 && !(a.wdtype == LRAM_BF16 && a.dtype == LRAM_BF16)) return LRAM_EDTYPE;
     if (!a.rel_bucket || a.rel_buckets < 1 || a.rel_buckets > 256 || a.rel_reach < 0 || a.rel_reach > 4096 ||

@@ -705,8 +705,8 @@ Plan plan_of(const lram_attention& call) {
   Plan p;
   const int64_t G = a.heads / a.kv_heads;
   p.group = a.rel_weight ? 1 : (int)G;
-  p.row_slots = (int)(a.tq * p.group / (WAVES * ROWS) + a.batch + 1);
-  p.key_slots = (int)(a.tk / DKV_KEYS + a.batch + 1);
+  p.row_slots = slots_of(a.tq, p.group, WAVES * ROWS, a.batch);
+  p.key_slots = slots_of(a.tk, 1, DKV_KEYS, a.batch);
   const auto tiles = [&](int64_t longest, int64_t slots, int64_t heads) {
     return std::max<int64_t>(1, std::min<int64_t>((int64_t)a.batch * ((longest + 127) / 128), slots) * heads);
   };

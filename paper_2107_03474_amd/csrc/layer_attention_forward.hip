@@ -470,7 +470,7 @@ Plan plan_of(const lram_attention& call) {
   p.few = a.max_q * G <= ROWS;
   const int tile = p.few ? ROWS : WAVES * ROWS;
   p.group = a.rel_weight && !p.few ? 1 : (int)G;
-  p.slots = (int)(a.tq * p.group / tile + a.batch + 1);
+  p.slots = slots_of(a.tq, p.group, tile, a.batch);
   const int64_t heads = a.heads / p.group;
   const int64_t work = heads * a.batch * std::max<int64_t>(1, (a.max_q * p.group + tile - 1) / tile);
   const int64_t real = std::min<int64_t>(work, heads * p.slots);

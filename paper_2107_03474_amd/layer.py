@@ -211,7 +211,8 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, eps: f
 class Packed(NamedTuple):
     """Where a batch's sequences lie (int32 device tensors): sequence b has the rows start_q[b] ... start_q[b + 1] - 1 of
     q and start_k[b] ... start_k[b + 1] - 1 of k and v, of the latter only the first used_k[b] where used_k is given (a
-    cache).  max_q and max_k: the longest expected; what exceeds them costs time, not results."""
+    cache).  Rows before the first sequence and past the last one belong to none.  max_q and max_k: the longest expected; what
+    exceeds them costs time, not results."""
     start_q: torch.Tensor
     start_k: torch.Tensor
     max_q: int
