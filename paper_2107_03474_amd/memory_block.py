@@ -18,26 +18,53 @@ from .memory_layer import MemorySubnetwork
 
 
 class KeyValueCache:
-    """Keys and values of ``batch`` sequences, ``capacity`` rows each; ``used`` [batch] int32 counts the rows in use.  The
-    caller keeps a sequence's length within the capacity."""
+    """Keys and values of ``batch`` sequences, ``capacity`` rows each; ``used`` [batch] int32 counts the rows in use."""
 
     def __init__(self, batch: int, capacity: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda"):
+        if batch < 0 or capacity < 0 or batch * capacity > 1 << 30:
+            raise ValueError("a cache holds batch * capacity rows, 2^30 at most")
         self.batch, self.capacity = batch, capacity
-        self.k = torch.empty((batch * capacity, kv_heads, head_dim), dtype=dtype, device=device)
-        self.v = torch.empty_like(self.k)
+        # one row more, which takes what belongs to no sequence
+        self._k = torch.empty((batch * capacity + 1, kv_heads, head_dim), dtype=dtype, device=device)
+        self._v = torch.empty_like(self._k)
+        self.k, self.v = self._k[:-1], self._v[:-1]
         self.used = torch.zeros(batch, dtype=torch.int32, device=device)
         self.start = torch.arange(batch + 1, dtype=torch.int32, device=device) * capacity
+        # of the rows before the first sequence, of each sequence and past the last one: the end of its place in the cache
+        self._end = torch.zeros(batch + 2, dtype=torch.int32, device=device)
+        self._end[1:-1] = self.start[1:]
+        self._base = torch.zeros_like(self._end)
+        self._longest = 0  # no sequence has more rows, as far as the plans' max_q can be trusted
 
     def append(self, k: torch.Tensor, v: torch.Tensor, seqs: Packed) -> Packed:
-        """Adds the rows of k and v (packed by seqs.start_q) to their sequences; the plan of attention over the cache."""
-        rows = k.shape[0]
-        more = seqs.start_q[1:] - seqs.start_q[:-1]
-        of = torch.repeat_interleave(torch.arange(self.batch, device=k.device), more.long(), output_size=rows)
-        at = (self.start[:-1] + self.used - seqs.start_q[:-1])[of] + torch.arange(rows, device=k.device)
-        self.k.index_copy_(0, at, k)
-        self.v.index_copy_(0, at, v)
+        """Adds the rows of k and v (packed by seqs.start_q; rows of no sequence are left out) to their sequences; the plan of
+        attention over the cache.  A sequence that would outgrow the capacity is refused, and nothing is added; the lengths
+        are on the device, so that this is found by seqs.max_q, and where that is too low, or in a captured call, the rows
+        past the capacity are left out."""
+        if k.shape != v.shape or k.shape[1:] != self.k.shape[1:]:
+            raise ValueError("k and v must be [rows, kv_heads, head_dim] of the cache")
+        if seqs.start_q.numel() != self.batch + 1:
+            raise ValueError("the plan must be of the cache's %d sequences" % self.batch)
+        start = seqs.start_q
+        more = start[1:] - start[:-1]
+        longest = self._longest + seqs.max_q
+        if longest > self.capacity and self.batch and not (k.is_cuda and torch.cuda.is_current_stream_capturing()):
+            longest = int((self.used + more).max())  # waits for the device, which few calls have to
+            if longest > self.capacity:
+                raise ValueError("a sequence has more rows than the cache's capacity of %d" % self.capacity)
+        self._longest = min(longest, self.capacity)
+        row = torch.arange(k.shape[0], dtype=torch.int32, device=k.device)
+        of = torch.searchsorted(start, row, right=True)
+        base = self._base[1:-1]
+        torch.add(self.start[:-1], self.used, out=base)
+        base -= start[:-1]
+        at = self._base[of] + row
+        at = torch.where(at < self._end[of], at, self.batch * self.capacity).long()
+        self._k.index_copy_(0, at, k)
+        self._v.index_copy_(0, at, v)
         self.used += more
-        return Packed(seqs.start_q, self.start, seqs.max_q, self.capacity, self.used)
+        self.used.clamp_(max=self.capacity)
+        return Packed(start, self.start, seqs.max_q, self.capacity, self.used)
 
 
 class MemoryBlock(torch.nn.Module):
