@@ -84,6 +84,13 @@ def _ptr(t: torch.Tensor, name: str, dtype: torch.dtype, shape, like: torch.Tens
     return t.data_ptr()
 
 
+def _moved(t: torch.Tensor):
+    """(address, copy) of a contiguous tensor that does not start on 16 bytes, as the kernels want it: later rows of an odd
+    width, among them the gradients that torch.cat hands on."""
+    t = t.clone()
+    return t.data_ptr(), t
+
+
 def _scratch(nbytes: int, workspace: Optional[torch.Tensor], like: torch.Tensor):
     """(pointer, bytes, tensor to keep until the launch) of a call's workspace."""
     if workspace is None:
@@ -121,16 +128,21 @@ def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor
     rows, width, dt, wt = _norm_args(x, weight, "x")
     wp = _ptr(weight, "weight", weight.dtype, (width,), x)
     bp = _ptr(bias, "bias", weight.dtype, (width,), x)
+    xp = x.data_ptr()
+    if xp & 15:
+        xp, x = _moved(x)
     rp = hp = None
     h = x
     if residual is not None:
         rp = _ptr(residual, "residual", x.dtype, x.shape, x)
+        if rp & 15:
+            rp, residual = _moved(residual)
         h = torch.empty_like(x)
         hp = h.data_ptr()
     y = torch.empty_like(x)
     mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
     rstd = torch.empty_like(mean)
-    rc = lib.lram_layer_norm_forward(x.data_ptr(), rp, wp, bp, dt, wt, rows, width, eps, hp, y.data_ptr(),
+    rc = lib.lram_layer_norm_forward(xp, rp, wp, bp, dt, wt, rows, width, eps, hp, y.data_ptr(),
                                      mean.data_ptr(), rstd.data_ptr(), _stream(x.device))
     if rc:
         _check(rc)
@@ -150,6 +162,13 @@ def layer_norm_backward(h: torch.Tensor, weight: torch.Tensor, mean: torch.Tenso
     mp, sp = _ptr(mean, "mean", f32, lead, h), _ptr(rstd, "rstd", f32, lead, h)
     yp = _ptr(grad_y, "grad_y", h.dtype, h.shape, h)
     gp = None if grad_h is None else _ptr(grad_h, "grad_h", h.dtype, h.shape, h)
+    hp = h.data_ptr()
+    if yp & 15:
+        yp, grad_y = _moved(grad_y)
+    if gp is not None and gp & 15:
+        gp, grad_h = _moved(grad_h)
+    if hp & 15:
+        hp, h = _moved(h)
     gx = torch.empty_like(h)
     gw = gb = gwp = gbp = ws = keep = None
     ws_bytes = 0
@@ -160,7 +179,7 @@ def layer_norm_backward(h: torch.Tensor, weight: torch.Tensor, mean: torch.Tenso
         if workspace is None:
             _check(lib.lram_layer_norm_backward_workspace_bytes(rows, width, dt, ctypes.byref(n)))
         ws, ws_bytes, keep = _scratch(n.value, workspace, h)
-    rc = lib.lram_layer_norm_backward(h.data_ptr(), wp, mp, sp, yp, gp, dt, wt, rows, width, gx.data_ptr(), gwp, gbp,
+    rc = lib.lram_layer_norm_backward(hp, wp, mp, sp, yp, gp, dt, wt, rows, width, gx.data_ptr(), gwp, gbp,
                                       ws, ws_bytes, _stream(h.device))
     del keep
     if rc:
@@ -363,7 +382,10 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: 
     arguments); grad_rel, of the bias's weight, is None without one.  Rows of k and v that no query may see get zeros."""
     lib = _library()
     a = _describe(q, k, v, seqs, causal, scale, rel)
-    op, gp = _ptr(out, "out", q.dtype, q.shape, q), _ptr(grad_out, "grad_out", q.dtype, q.shape, q)
+    op = _ptr(out, "out", q.dtype, q.shape, q)
+    gp = _ptr(grad_out, "grad_out", q.dtype, q.shape, q)
+    if gp & 15:
+        gp, grad_out = _moved(grad_out)
     lp = _ptr(saved.lse, "saved.lse", torch.float32, q.shape[:2], q)
     rp = None if saved.residue is None else _ptr(saved.residue, "saved.residue", q.dtype, q.shape, q)
     gq = torch.empty_like(out)
