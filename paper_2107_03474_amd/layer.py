@@ -12,6 +12,7 @@ import math
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import BF16, F32, LramError, _dev
 from . import load as _load_library
@@ -102,8 +103,10 @@ def _scratch(nbytes: int, workspace: Optional[torch.Tensor], like: torch.Tensor)
 
 
 def _records(*inputs: Optional[torch.Tensor]) -> bool:
-    """Whether autograd follows a call with these inputs."""
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)
+    """Whether autograd follows a call with these inputs (forward mode, which the wrappers refuse, among it: a tensor that
+    carries a tangent shows it only to them)."""
+    return (forward_ad._current_level >= 0 or
+            torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs))
 
 
 # ---------------------------------------------------------------------------
