@@ -19,6 +19,7 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 import torch  # noqa: F401  -- loads the HIP runtime liblram.so must share
+from torch.autograd.function import once_differentiable
 
 __all__ = ["neighbors", "forward", "backward", "backward_workspace_bytes", "lookup", "LramLookup",
            "library_path", "load", "LramError", "F32", "BF16", "SCATTER_ATOMIC", "SCATTER_SORTED",
@@ -376,6 +377,7 @@ class LramLookup(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         q, table, *saved = ctx.saved_tensors
         g32 = g.contiguous().to(torch.float32)
@@ -453,6 +455,7 @@ class ThetaLookup(torch.autograd.Function):
         return theta_forward(z, table, ctx.K)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         z, table = ctx.saved_tensors
         g32 = g.contiguous().to(torch.float32)

@@ -13,6 +13,7 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.function import once_differentiable
 
 from . import BF16, F32, LramError, _dev
 from . import load as _load_library
@@ -206,6 +207,7 @@ class LayerNorm(torch.autograd.Function):
         return y, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy, gh):
         h, weight, mean, rstd = ctx.saved_tensors
         if gy is None:
@@ -420,6 +422,7 @@ class Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         q, k, v, out, lse, residue, weight, bucket, start_q, start_k, used_k = ctx.saved_tensors
         max_q, max_k, causal, scale = ctx.rest

@@ -39,3 +39,12 @@ def test_forward_mode_is_refused(call, inputs):
         with pytest.raises(NotImplementedError):
             call(forward_ad.make_dual(x, torch.ones_like(x)), *rest)
         call(x, *rest)  # no tangent: nothing to refuse
+
+
+@pytest.mark.parametrize("call,inputs", CALLS, ids=NAMES)
+def test_second_derivatives_are_refused(call, inputs):
+    x, *rest = inputs()
+    x.requires_grad_()
+    first, = torch.autograd.grad(call(x, *rest).square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        first.sum().backward()
