@@ -125,9 +125,9 @@ def _norm_args(x: torch.Tensor, weight: torch.Tensor, name: str):
 
 
 def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, eps: float = 1e-5,
-                       residual: Optional[torch.Tensor] = None):
+                       residual: Optional[torch.Tensor] = None, save: bool = True):
     """(y, h, mean, rstd): h = x + residual in x's type (x itself without a residual), y its layer norm over the last
-    dimension, and the rows' statistics (fp32 [...]) for the backward."""
+    dimension, and the rows' statistics (fp32 [...]) for the backward, None without ``save``."""
     lib = _library()
     rows, width, dt, wt = _norm_args(x, weight, "x")
     wp = _ptr(weight, "weight", weight.dtype, (width,), x)
@@ -144,10 +144,13 @@ def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor
         h = torch.empty_like(x)
         hp = h.data_ptr()
     y = torch.empty_like(x)
-    mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
-    rstd = torch.empty_like(mean)
-    rc = lib.lram_layer_norm_forward(xp, rp, wp, bp, dt, wt, rows, width, eps, hp, y.data_ptr(),
-                                     mean.data_ptr(), rstd.data_ptr(), _stream(x.device))
+    mean = rstd = mp = sp = None
+    if save:
+        mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
+        rstd = torch.empty_like(mean)
+        mp, sp = mean.data_ptr(), rstd.data_ptr()
+    rc = lib.lram_layer_norm_forward(xp, rp, wp, bp, dt, wt, rows, width, eps, hp, y.data_ptr(), mp, sp,
+                                     _stream(x.device))
     if rc:
         _check(rc)
     return y, h, mean, rstd
@@ -223,7 +226,7 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, eps: f
     """The layer norm of x, differentiable; with a residual (y, h): the norm of h = x + residual, and h."""
     if not _records(x, residual, weight, bias):
         y, h, _, _ = layer_norm_forward(x.contiguous(), weight.contiguous(), bias.contiguous(), float(eps),
-                                        None if residual is None else residual.contiguous())
+                                        None if residual is None else residual.contiguous(), save=False)
     else:
         y, h = LayerNorm.apply(x, residual, weight, bias, float(eps))
     return y if residual is None else (y, h)

@@ -13,7 +13,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from .layer import Packed, RelativeBias, attention, attention_forward, layer_norm, layer_norm_forward, relative_buckets
+from .layer import Packed, RelativeBias, attention, attention_forward, layer_norm, relative_buckets
 from .memory_layer import MemorySubnetwork
 
 
@@ -108,6 +108,6 @@ class MemoryBlock(torch.nn.Module):
         q, k, v = self._heads(x)
         seqs = cache.append(k, v, seqs)
         a, _ = attention_forward(q, cache.k, cache.v, seqs, True, rel=RelativeBias(self.bias, self.bucket))
-        x, _, _, _ = layer_norm_forward(self.proj(a.flatten(1)), self.norm_w[0], self.norm_b[0], self.eps, residual=x)
-        x, _, _, _ = layer_norm_forward(self.memory(x).contiguous(), self.norm_w[1], self.norm_b[1], self.eps, residual=x)
+        x, _ = layer_norm(self.proj(a.flatten(1)), self.norm_w[0], self.norm_b[0], self.eps, residual=x)
+        x, _ = layer_norm(self.memory(x), self.norm_w[1], self.norm_b[1], self.eps, residual=x)
         return x
