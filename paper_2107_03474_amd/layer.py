@@ -152,6 +152,10 @@ def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor
     rc = lib.lram_layer_norm_forward(xp, rp, wp, bp, dt, wt, rows, width, eps, hp, y.data_ptr(), mp, sp,
                                      _stream(x.device))
     if rc:
+        if not 1 <= width <= 16384:
+            raise LramError("rows must have 1 to 16384 elements")
+        if not eps >= 0:
+            raise LramError("eps must not be negative")
         _check(rc)
     return y, h, mean, rstd
 
@@ -272,7 +276,8 @@ class RelativeBias(NamedTuple):
     """Learned bias of a query-key pair by head and bucket of their distance: weight [heads, buckets] (q's type or
     fp32), bucket [2 reach + 1] int32 (``relative_buckets``): the bucket of key minus query = -reach ... reach, the ends
     aligned; longer distances take the last one's.  A weight of -inf hides its keys; finite ones from 1.2e7 on in
-    magnitude, the type's lowest value among them, count alike, and no score matters beside them."""
+    magnitude, the type's lowest value among them, count alike, and no score matters beside them.  At most 256 buckets, and
+    heads / kv_heads (2 reach + 193) at most 4096 (in fp32 with head_dim 128: 2 reach + 193 at most 1365)."""
     weight: torch.Tensor
     bucket: torch.Tensor
 
@@ -317,6 +322,44 @@ def _heads(t: torch.Tensor, name: str, like: torch.Tensor):
     return (t.data_ptr(), row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2])
 
 
+HEAD_DIMS = (32, 64, 128)
+
+
+def bias_refusal(heads: int, kv_heads: int, head_dim: int, dtype: torch.dtype, buckets: int, reach: int) -> Optional[str]:
+    """Why a relative bias of this size is not offered (its distances have to fit the kernels' LDS), None if it is."""
+    if not 1 <= buckets <= 256:
+        return "a relative bias has 1 to 256 buckets"
+    if heads // kv_heads * (2 * reach + 193) > 4096:
+        return "heads / kv_heads (2 reach + 193) must be at most 4096 with a relative bias"
+    if dtype == torch.float32 and head_dim == 128 and 2 * reach + 193 > 1365:
+        return "2 reach + 193 must be at most 1365 with a relative bias, float32 and head_dim 128"
+    return None
+
+
+def _check_attention(rc: int, a: _Attention):
+    """Raises what the library refused, in the caller's terms where they can be told."""
+    why = None
+    if rc in (1, 3):  # argument, type
+        per = 8 if a.dtype == BF16 else 4
+        strides = (a.q_row, a.q_head, a.k_row, a.k_head, a.v_row, a.v_head)
+        if a.head_dim not in HEAD_DIMS:
+            why = "head_dim must be 32, 64 or 128"
+        elif a.kv_heads < 1 or a.heads < 1 or a.heads % a.kv_heads or a.heads > 64 * a.kv_heads:
+            why = "q's heads must be a multiple of k's, at most 64 times as many"
+        elif not 0 < a.scale < math.inf:
+            why = "scale must be positive and finite"
+        elif any(p is not None and p % 16 for p in (a.q, a.k, a.v)) or any(s % per for s in strides) or any(
+                not a.head_dim <= s <= 1 << 22 for s in strides[::2]):
+            why = ("q, k and v must start on 16 bytes, with strides of whole 16 bytes and rows at least head_dim and at most "
+                   "2^22 elements apart")
+        elif a.rel_weight:
+            why = bias_refusal(a.heads, a.kv_heads, a.head_dim, torch.float32 if a.dtype == F32 else torch.bfloat16,
+                               a.rel_buckets, a.rel_reach)
+    if why:
+        raise LramError(why)
+    _check(rc)
+
+
 def _describe(q, k, v, seqs: Packed, causal, scale, rel: Optional[RelativeBias]):
     a = _Attention()
     a.q, a.q_row, a.q_head = _heads(q, "q", q)
@@ -357,7 +400,8 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: P
                       scale: Optional[float] = None, rel: Optional[RelativeBias] = None, save: bool = False,
                       workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[AttentionSaved]]:
     """(out, saved): softmax(scale q k^T + bias) v of packed sequences, q [rows, heads, head_dim], k and v [rows, kv_heads,
-    head_dim] (any row and head strides; head_dim 32, 64 or 128; scale 1 / sqrt(head_dim) by default).  The ends of a
+    head_dim] (from 16 bytes on, with row and head strides of whole 16 bytes; head_dim 32, 64 or 128; scale 1 / sqrt(head_dim)
+    by default).  The ends of a
     sequence's queries and keys are aligned, and ``causal`` queries see no key past theirs.  saved (with ``save``): for
     ``attention_backward``."""
     lib = _library()
@@ -373,12 +417,12 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: P
     if workspace is None:
         rc = lib.lram_attention_forward_workspace_bytes(a, n)
         if rc:
-            _check(rc)
+            _check_attention(rc, a)
     ws, ws_bytes, keep = _scratch(n.value, workspace, q)
     rc = lib.lram_attention_forward(a, out.data_ptr(), lse, residue, ws, ws_bytes, _stream(q.device))
     del keep
     if rc:
-        _check(rc)
+        _check_attention(rc, a)
     return out, saved
 
 
@@ -402,13 +446,13 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: 
     grel = None if rel is None else torch.empty_like(rel.weight)
     n = ctypes.c_size_t(0)
     if workspace is None:
-        _check(lib.lram_attention_backward_workspace_bytes(a, n))
+        _check_attention(lib.lram_attention_backward_workspace_bytes(a, n), a)
     ws, ws_bytes, keep = _scratch(n.value, workspace, q)
     rc = lib.lram_attention_backward(a, op, rp, lp, gp, gq.data_ptr(), gk.data_ptr(), gv.data_ptr(),
                                      None if grel is None else grel.data_ptr(), ws, ws_bytes, _stream(q.device))
     del keep
     if rc:
-        _check(rc)
+        _check_attention(rc, a)
     return gq, gk, gv, grel
 
 

@@ -13,7 +13,8 @@ from typing import Optional, Sequence
 
 import torch
 
-from .layer import Packed, RelativeBias, attention, attention_forward, layer_norm, relative_buckets
+from .layer import (HEAD_DIMS, Packed, RelativeBias, attention, attention_forward, bias_refusal, layer_norm,
+                    relative_buckets)
 from .memory_layer import MemorySubnetwork
 
 
@@ -75,6 +76,11 @@ class MemoryBlock(torch.nn.Module):
         kv_heads = heads if kv_heads is None else kv_heads
         if w % heads or heads % kv_heads:
             raise ValueError("w must be a multiple of heads, and heads of kv_heads")
+        if w // heads not in HEAD_DIMS:
+            raise ValueError("w / heads must be 32, 64 or 128")
+        refusal = bias_refusal(heads, kv_heads, w // heads, dtype, buckets, reach)
+        if refusal:
+            raise ValueError(refusal)
         self.heads, self.kv_heads, self.head_dim, self.causal, self.eps = heads, kv_heads, w // heads, causal, eps
         new = dict(device=device, dtype=dtype)
         self.qkv = torch.nn.Linear(w, (heads + 2 * kv_heads) * self.head_dim, **new)
