@@ -562,8 +562,8 @@ int check_attention(const lram_attention& a, bool pointers) {
     return LRAM_EINVAL;
   if (a.tq < 0 || a.tk < 0 || a.tk > 1 << 30 || a.tq > (1 << 30) / G || a.max_q < 0 || a.max_k < 0)
     return LRAM_EINVAL;
-  // a grid holds less than 2^32 threads: tiles of 32 rows or more, a workgroup of 256 each; pieces are made where they
-  // fit (few_enough)
+  // a grid holds less than 2^32 threads: tiles of 32 rows with a workgroup of 256 each, of 128 rows with one of 512 at most;
+  // pieces are made where they fit (few_enough, tiles_of)
   if (a.heads * (std::max(a.tq * G, a.tk) / 32 + a.batch + 3) >= MOST_GROUPS) return LRAM_EINVAL;
   if (a.rel_weight) {
     if (a.wdtype != LRAM_F32 && !(a.wdtype == LRAM_BF16 && a.dtype == LRAM_BF16)) return LRAM_EDTYPE;
@@ -598,6 +598,12 @@ Args args_of(const lram_attention& a) {
   x.scale = a.scale;
   x.c = a.scale * LOG2E;
   return x;
+}
+
+// Tiles that a call of expected length `longest` has, of `slots` at most: `rows` in all (packed rows, keys) fill as many as
+// they do whatever the sequences' lengths, so that an expectation below them does not lead to pieces of many tiles.
+int64_t tiles_of(const lram_attention& a, int64_t longest, int64_t rows, int tile, int64_t slots) {
+  return std::min(std::max(a.batch * std::max<int64_t>(1, (longest + tile - 1) / tile), rows / tile), slots);
 }
 
 // The call with the expected lengths no longer than the tensors, so that no product of them overflows.

@@ -707,12 +707,13 @@ Plan plan_of(const lram_attention& call) {
   p.group = a.rel_weight ? 1 : (int)G;
   p.row_slots = slots_of(a.tq, p.group, WAVES * ROWS, a.batch);
   p.key_slots = slots_of(a.tk, 1, DKV_KEYS, a.batch);
-  const auto tiles = [&](int64_t longest, int64_t slots, int64_t heads) {
-    return std::max<int64_t>(1, std::min<int64_t>((int64_t)a.batch * ((longest + 127) / 128), slots) * heads);
-  };
   const bool even = a.dtype == LRAM_F32 || alike(a);
-  const int64_t row_tiles = tiles(a.max_q * p.group, p.row_slots, a.heads / p.group);
-  const int64_t key_tiles = tiles(a.max_k, p.key_slots, a.kv_heads);
+  const auto tiles = [&](int64_t longest, int64_t rows, int64_t slots, int64_t heads) {
+    return std::max<int64_t>(1, tiles_of(a, longest, rows, 128, slots) * heads);
+  };
+  const int64_t row_tiles = tiles(a.max_q * p.group, a.tq * p.group, p.row_slots, a.heads / p.group);
+  // of a cache, what its sequences have in use
+  const int64_t key_tiles = tiles(a.max_k, a.used_k ? 0 : a.tk, p.key_slots, a.kv_heads);
   p.teams = a.dtype == LRAM_BF16 && even && a.max_k > (a.rel_weight ? 256 : 512) && dq_lds(a, 2) <= LDS_BYTES &&
             row_tiles <= (a.causal && a.max_k > 1024 ? 3 * UNITS / 2 : UNITS);
   p.keys = pieces_of((p.teams ? UNITS : even ? ROUND : 2 * ROUND) / row_tiles, a.max_k, 1, a.dtype,

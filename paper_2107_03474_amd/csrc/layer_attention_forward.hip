@@ -472,8 +472,7 @@ Plan plan_of(const lram_attention& call) {
   p.group = a.rel_weight && !p.few ? 1 : (int)G;
   p.slots = slots_of(a.tq, p.group, tile, a.batch);
   const int64_t heads = a.heads / p.group;
-  const int64_t work = heads * a.batch * std::max<int64_t>(1, (a.max_q * p.group + tile - 1) / tile);
-  const int64_t real = std::min<int64_t>(work, heads * p.slots);
+  const int64_t real = heads * tiles_of(a, a.max_q * p.group, a.tq * p.group, tile, p.slots);
   const bool even = p.few || a.dtype == LRAM_F32 || alike(a);
   p.teams = !p.few && a.dtype == LRAM_BF16 && even && a.max_k > 256 &&
             real <= (a.causal && a.max_k > 1024 ? 3 * UNITS / 2 : UNITS);
