@@ -291,21 +291,25 @@ struct Tile {
 
 // 16 bytes a lane from memory straight into LDS at dst + 16 lane; a lane whose offset lies past the resource's end
 // gets zeros.  Written out so that the compiler does not wait for it at the next read of any tile: the kernels wait
-// themselves (loads_left), before the barrier or the reads that need it.  m0, the destination's register, holds nothing
-// else in these kernels.
+// themselves (loads_left), before the barrier or the reads that need it.  m0, the destination's register, is named as
+// written: the compiler keeps no values there (it says so, in a warning), but may share one setting of it among its own
+// instructions.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t src, Lds dst, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"((uint32_t)(uintptr_t)dst), "v"(offset), "s"(src)
-               : "memory");
+               : "memory", "m0");
 }
 // The same of 4 bytes a lane, to dst + 4 lane.
 __device__ __forceinline__ void dma4(__amdgpu_buffer_rsrc_t src, Lds dst, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
                :
                : "s"((uint32_t)(uintptr_t)dst), "v"(offset), "s"(src)
-               : "memory");
+               : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 }
