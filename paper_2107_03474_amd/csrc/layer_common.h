@@ -17,17 +17,6 @@ constexpr int WAVE = 64;
 
 using bf16 = __bf16;
 
-template <int DT>
-struct Elem;
-template <>
-struct Elem<LRAM_F32> {
-  using type = float;
-};
-template <>
-struct Elem<LRAM_BF16> {
-  using type = bf16;
-};
-
 // N consecutive elements, loaded and stored whole.  Rows of odd sizes start on any element: the type promises no
 // alignment beyond an element's (the memory system takes such vectors).
 template <typename T, int N>
