@@ -7,8 +7,10 @@
  * Conventions, beyond those of lram.h (streams, caller-owned memory, status codes, host checks before any launch,
  * nothing kept between calls):
  *   - dtype is that of the activations and their gradients, LRAM_F32 or LRAM_BF16; wdtype that of the learned weights and
- *     theirs: LRAM_F32, or LRAM_BF16 beside bf16 activations.  All sums, statistics and softmax terms are fp32; a result
- *     is rounded once, to nearest even.
+ *     theirs: LRAM_F32, or LRAM_BF16 beside bf16 activations.  Sums, statistics, maxima, lse and partial results are fp32; a
+ *     result is rounded once, to nearest even.  In bf16 the matrix cores take bf16 operands, so that the softmax's weights
+ *     and, backward, ds = p (dO.v - dO.out) are rounded to bf16 too before the products that use them (the weights' own
+ *     sum is of the unrounded ones); fp32 rounds nothing in between.
  *   - Every result is the same, bit for bit, on every call with the same inputs: no sum's order depends on timing.
  *   - Tensors are dense row-major unless a stride is given, and 16-byte aligned; fp32 per-row arrays, int32 arrays
  *     and learned weights need the alignment of an element.
@@ -39,7 +41,7 @@ int lram_layer_norm_forward(const void* x, const void* residual, const void* wei
                             int wdtype, int64_t rows, int64_t width, double eps, void* sum, void* y, float* mean,
                             float* rstd, void* stream);
 
-/* Device workspace of lram_layer_norm_backward (0 without weight gradients; host only). */
+/* Device workspace of an lram_layer_norm_backward that gives the weight gradients (host only); without them it needs none. */
 int lram_layer_norm_backward_workspace_bytes(int64_t rows, int64_t width, int dtype, size_t* bytes);
 
 /*
@@ -62,7 +64,7 @@ int lram_layer_norm_backward(const void* h, const void* weight, const float* mea
  * of queries and keys are aligned: a prompt, a piece of one, or one token over a cache):
  *     s_ij = scale q_i . k_j + rel_weight[h][rel_bucket[clamp(j - i - (nk - nq), -rel_reach, rel_reach) + rel_reach]]
  *     out_i = sum_j softmax_j(s_ij) v_j,   0 where a query meets no key
- * The bias (Sec. 3.2's model learns positions; here by bucketed distance) is nullable.  A weight of -inf hides its keys as
+ * The bias (Sec. 3.2's model learns positions; here by bucketed distance, as T5's does) is nullable.  A weight of -inf hides its keys as
  * `causal` does.  Finite weights of 1.16e7 (2^24 / log2 e) and more in magnitude, a type's lowest value among them, count
  * alike: no score matters beside them, so that a query that meets no other keys has the even average of theirs.
  *

@@ -248,8 +248,11 @@ __global__ __launch_bounds__(FIN_COLS* FIN_ROWS) void k_norm_finish(const float*
 
 // Threads of a row and chunks of a thread: a thread to a chunk, which is the shortest way through a row, but waves take
 // rows of up to four chunks a lane where there are many (us of a thread to a chunk / waves: 64 rows x 2,048 bf16 3.2 / 5.4,
-// 1,024 x 2,048 4.8 / 6.4, 2,048 x 1,024 6.1 / 5.2, 5,003 x 500 fp32 11.4 / 7.2, 8,192 x 2,048 bf16 22.5 / 23.2; of one chunk
-// / four to 256 threads: 16,384 x 8,192 bf16 192 / 200, 64 x 8,192 4.2 / 5.8).
+// 1,024 x 2,048 4.8 / 6.4, 2,048 x 1,024 6.1 / 5.2, 5,003 x 500 fp32 11.4 / 7.2; of one chunk / four to 256 threads:
+// 16,384 x 8,192 bf16 192 / 200, 64 x 8,192 4.2 / 5.8).  With more than two chunks a lane the two are close, and one rule
+// serves both types though bf16 leans the other way (with a residual: fp32 8,192 x 520 15.2 / 13.1, 40,000 x 520 77 / 61,
+// 8,192 x 1,024 23.8 / 24.2, 2,048 x 800 7.6 / 8.1; bf16 40,000 x 1,040 94 / 84, 8,192 x 2,048 23.8 / 24.1, 8,192 x 1,600
+// 19.9 / 23.0, 2,048 x 1,600 8.3 / 10.5).
 constexpr int64_t FEW_ROWS = 1024;
 struct Shape {
   int G, NC;

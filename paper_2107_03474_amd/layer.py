@@ -2,8 +2,9 @@
 attention over packed sequences, and the learned relative position bias inside it.
 
 As in the package's other calls, this module only marshals torch tensors and the current HIP stream into the C ABI
-(``include/lram_layer.h``); the work is done by the library's HIP kernels, and there is no fallback.  Gradients come in
-their inputs' types, rounded once from fp32.
+(``include/lram_layer.h``); the work is done by the library's HIP kernels, and there is no fallback.  Sums, statistics and
+partial results are fp32, and results and gradients come in their inputs' types, rounded once from it.  In bf16 attention's
+softmax weights and their gradient are rounded as well, where they enter a product of the matrix cores.
 """
 from __future__ import annotations
 
@@ -283,8 +284,9 @@ class RelativeBias(NamedTuple):
 
 
 def relative_buckets(buckets: int, reach: int, both: bool = True, device="cuda") -> torch.Tensor:
-    """Buckets of the distances -reach ... reach: half of a side's one distance each, the others growing as powers up to
-    reach; ``both``: half of the buckets for keys behind the query, else none (a key behind it counts as distance 0)."""
+    """Buckets of the distances -reach ... reach by T5's rule (Raffel et al., arXiv 1910.10683, Sec. 2.1): half of a side's
+    one distance each, the others growing as powers up to reach; ``both``: half of the buckets for keys behind the query,
+    else none (a key behind it counts as distance 0)."""
     side = buckets // 2 if both else buckets
     near = max(side // 2, 1)
     n = side - near
