@@ -66,7 +66,9 @@ int lram_layer_norm_backward(const void* h, const void* weight, const float* mea
  *     out_i = sum_j softmax_j(s_ij) v_j,   0 where a query meets no key
  * The bias (Sec. 3.2's model learns positions; here by bucketed distance, as T5's does) is nullable.  A weight of -inf hides its keys as
  * `causal` does.  Finite weights of 1.16e7 (2^24 / log2 e) and more in magnitude, a type's lowest value among them, count
- * alike: no score matters beside them, so that a query that meets no other keys has the even average of theirs.
+ * alike: no score matters beside them, so that a query that meets no other keys has the even average of theirs.  Scores
+ * themselves are meant to stay below that in magnitude: fp32 holds no digit of them behind the point from there on, and
+ * from 256 times it on results may be NaN.
  *
  * The lengths stay on the device: nothing waits for them, and a captured call may be replayed over others.  max_q and
  * max_k are the longest nq and nk expected, from which the host chooses how to divide the work; lengths beyond them
@@ -100,7 +102,7 @@ typedef struct {
 /*
  * lram_attention_forward -- out [tq][heads][head_dim] in dtype.
  *   lse      [tq][heads] fp32: nullable; log2 sum_j 2^(s_ij log2 e), -inf where a query meets no key (the base that the
- *            kernels work in); +-2^100 (1 + log2(n) / 32) where the n keys that count are those of weights that count alike
+ *            kernels work in); +-2^126 (1 + log2(n) / 32) where the n keys that count are those of weights that count alike
  *   residue  as out, nullable, bf16 only: out before its rounding minus out.  With it the backward's
  *            <grad_out, out> is that of the unrounded result.
  *   workspace: lram_attention_forward_workspace_bytes (0 unless the keys are divided because rows are few).

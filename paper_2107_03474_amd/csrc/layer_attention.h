@@ -334,29 +334,29 @@ __device__ __forceinline__ void load_rows(const T* head, int64_t stride, int row
 
 // Weights far past any score.  From 2^24 on (a weight of 1.2e7, times log2 e) fp32 holds no digit behind the point, so that
 // scores beside such a weight say nothing, and times log2 e the type's lowest value, a common mask, would be -inf, which
-// hides a key altogether.  Finite weights from there on all count as +-2^100: any score added to it leaves it as it is, and
-// a row that meets no other keys (or one that meets keys of +2^100) has the even average of those.  Its maximum is then
-// +-2^100 and its sum a count, which m + log2 l would lose: the row's lse is m (1 + log2 l / 32) instead, l <= 2^30.
-constexpr float FAR_WEIGHT = 0x1p24f, VAST = 0x1p100f, BARELY = 0x1p-100f;
+// hides a key altogether.  Finite weights from there on all count as +-2^126: a score added to it leaves it as it is, and
+// a row that meets no other keys (or one that meets keys of +2^126) has the even average of those.  Its maximum is then
+// +-2^126 and its sum a count, which m + log2 l would lose: the row's lse is m (1 + log2 l / 32) instead, l <= 2^30.
+constexpr float FAR_WEIGHT = 0x1p24f, VAST = 0x1p126f, BARELY = 0x1p-100f;
 __device__ __forceinline__ float in_log2(float weight) {
   const float t = weight * LOG2E;
   return fabsf(t) >= FAR_WEIGHT && fabsf(weight) < INFINITY ? copysignf(VAST, weight) : t;
 }
-__device__ __forceinline__ bool is_vast(float x) { return fabsf(x) >= 0.5f * VAST && fabsf(x) < INFINITY; }
+__device__ __forceinline__ bool is_vast(float x) { return fabsf(x) >= VAST && fabsf(x) < 2 * VAST; }
 // The scores' factor beside a bias that serves a whole block: next to nothing where the bias is vast, so that subtracting
 // the maximum does not bring them back (not 0, which would make the -inf of a key that is not seen NaN).
-__device__ __forceinline__ float unit_beside(float far, float c) { return is_vast(far) ? c * BARELY : c; }
-__device__ __forceinline__ float lse_of(float m, float sum) {
+__device__ __forceinline__ float unit_beside(float far, float c) { return is_vast(far) ? BARELY : c; }
+__device__ __forceinline__ float lse_of(float m, float sum, bool bias) {
   const float l = __builtin_amdgcn_logf(sum);
-  return sum == 0 ? -INFINITY : is_vast(m) ? fmaf(m, l * 0x1p-5f, m) : m + l;
+  return sum == 0 ? -INFINITY : bias && fabsf(m) == VAST ? fmaf(m, l * 0x1p-5f, m) : m + l;
 }
 // An lse as the two parts of log2 of a sum: the maximum where it is vast, and what is left beside it.
 struct LseParts {
   float top, rest;
 };
-__device__ __forceinline__ LseParts parts_of(float lse) {
-  if (!is_vast(lse)) return {lse, 0.0f};
-  return {copysignf(VAST, lse), fmaf(fabsf(lse), 0x1p-95f, -32.0f)};
+__device__ __forceinline__ LseParts parts_of(float lse, bool bias) {
+  if (!bias || !is_vast(lse)) return {lse, 0.0f};
+  return {copysignf(VAST, lse), fmaf(fabsf(lse), 32 / VAST, -32.0f)};
 }
 
 // The bias by distance of the group's heads, times log2 e, in LDS: [G][2 (reach + BIAS_PAD) + 1], constant past reach.

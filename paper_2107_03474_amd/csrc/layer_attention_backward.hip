@@ -106,7 +106,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
       lse = o.lse[at];
       lse = lse == -INFINITY ? INFINITY : lse;
       if constexpr (BIAS) {
-        const LseParts part = parts_of(lse);
+        const LseParts part = parts_of(lse, BIAS);
         lse = part.top;
         share = __builtin_amdgcn_exp2f(-part.rest);
       }

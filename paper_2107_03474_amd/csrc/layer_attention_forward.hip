@@ -278,7 +278,7 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
   if (!r.valid) return;
   const float inv = sum == 0 ? 0.0f : 1.0f / sum;
   const int64_t at = (w.s.q0 + r.i) * a.heads + head;
-  if (l < 32) put_lse(a, o, w.split, at, lse_of(st.m, sum));
+  if (l < 32) put_lse(a, o, w.split, at, lse_of(st.m, sum, BIAS));
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(THREADS, 1) void k_attention_few(Args a, Out o) {
     sum += ml[(WAVES + v) * ROWS + (l & 31)] * __builtin_amdgcn_exp2f(ml[v * ROWS + (l & 31)] - m0);
   const float f = sum == 0 ? 0.0f : __builtin_amdgcn_exp2f(st.m - m0) / sum;
   const int64_t at = (w.s.q0 + r.i) * a.heads + head;
-  if (wave == 0 && l < 32 && r.valid) put_lse(a, o, w.split, at, lse_of(m, sum));
+  if (wave == 0 && l < 32 && r.valid) put_lse(a, o, w.split, at, lse_of(m, sum, BIAS));
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -423,14 +423,14 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(Args a, Out o) {
   const int d = threadIdx.x % PER * 4;
   if (at >= n) return;
   float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, parts_of(o.part_lse[s * n + at]).top);
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, parts_of(o.part_lse[s * n + at], a.rel_weight).top);
   const float m0 = m == -INFINITY ? 0.0f : m;
   float sum = 0;
   f32x4 x = {0, 0, 0, 0};
   for (int s = 0; s < a.splits; ++s) {
     const float lse = o.part_lse[s * n + at];
     if (lse == -INFINITY) continue;  // a piece without keys
-    const LseParts part = parts_of(lse);
+    const LseParts part = parts_of(lse, a.rel_weight);
     const float f = __builtin_amdgcn_exp2f(part.top - m0 + part.rest);
     sum += f;
     const f32x4 y = *(const f32x4*)(o.part + (s * n + at) * D + d);
@@ -442,7 +442,7 @@ __global__ __launch_bounds__(THREADS) void k_attention_join(Args a, Out o) {
   for (int e = 0; e < 4; ++e) x[e] *= inv;
   a.splits = 1;
   put<T, D>(a, o, 0, at, d, x);
-  if (d == 0) put_lse(a, o, 0, at, lse_of(m, sum));
+  if (d == 0) put_lse(a, o, 0, at, lse_of(m, sum, a.rel_weight));
 }
 
 struct Plan {

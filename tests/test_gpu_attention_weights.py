@@ -206,3 +206,19 @@ def test_vast_weights_over_a_cache(nq, nk, dtype):
     ref.assert_close("out", out, (zero["out"][0], zero["out"][1] + more["out"]))
     ref.assert_close("dv", dv, (zero["dv"][0], zero["dv"][1] + 2 * 44 * ref.E * ref.attention(
         q * 0, k, v, nq, nk, _starts(nq), _starts(nk), False, 0.125, do=do.abs())["dv"][0]))
+
+
+@BOTH_TYPES
+@BOTH_WAYS
+def test_vast_weights_beside_scores_of_next_to_nothing(causal, dtype):
+    """A scale that makes every score 0: the mean of the values that are seen, in blocks with keys that are not, too."""
+    lengths = [33, 150]
+    q, k, v, do = _inputs(lengths, 4, 2, 64, dtype, 15)
+    w = torch.full((4, 8), torch.finfo(dtype).min, dtype=dtype, device=DEV)
+    rel, seqs = lram.RelativeBias(w, lram.relative_buckets(8, 3)), lram.pack(lengths)
+    out, saved = lram.attention_forward(q, k, v, seqs, causal, 1e-20, rel, save=True)
+    dq, dk, dv, dw = lram.attention_backward(q, k, v, seqs, out, saved, do, causal, 1e-20, rel)
+    want = _with_bounds(q, k, v, do, lengths, causal, w, rel.bucket)
+    for n, t in dict(out=out, dv=dv).items():
+        ref.assert_close(n, t, want[n])
+    assert all(torch.isfinite(t).all() for t in (dq, dk, dw))

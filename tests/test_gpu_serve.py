@@ -27,3 +27,46 @@ def test_padded_batches():
     with pytest.raises(ValueError, match="capacity"):
         block.serve(torch.randn((14, 128), device=DEV), lram.pack([13, 1]), plain)
     assert plain.used.tolist() == [20, 18]
+
+
+def test_a_captured_step_appends_as_an_eager_one():
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    eager, captured = (KeyValueCache(3, 16, 2, 32, torch.float32) for _ in range(2))
+    k, v = (torch.randn((7, 2, 32), generator=g, device=DEV) for _ in range(2))
+    q = torch.randn((7, 4, 32), generator=g, device=DEV)
+    seqs = lram.pack([2, 1, 3])  # and a row of no sequence
+    more = seqs._replace(start_q=seqs.start_q.clone())
+
+    def step(cache, seqs):
+        return lram.attention_forward(q, cache.k, cache.v, cache.append(k, v, seqs), True)[0]
+
+    for c in (eager, captured):
+        c.k.zero_()
+        c.v.zero_()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(captured, more)
+    torch.cuda.current_stream().wait_stream(s)
+    captured.used.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(captured, more)
+    for lengths in ([2, 1, 3], [1, 1, 1], [0, 6, 0], [2, 2, 2]):
+        other = lram.pack(lengths)
+        more.start_q.copy_(other.start_q)
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, generator=g, device=DEV))
+        want = step(eager, other)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(captured.used, eager.used)
+    for _ in range(4):  # past the capacity: left out, and nobody else's rows are met
+        before = captured.k.view(3, 16, 2, 32)[0].clone()
+        more.start_q.copy_(lram.pack([0, 6, 0]).start_q)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(captured.k.view(3, 16, 2, 32)[0], before)
+    assert captured.used.tolist() == [5, 16, 6]
