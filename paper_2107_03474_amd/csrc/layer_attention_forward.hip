@@ -224,7 +224,8 @@ __global__ __launch_bounds__(TEAMS* THREADS, (waves_per_simd<T, D>())) void k_at
         const bool below = j + 31 - (i_first + off) <= -a.reach;
         above = j - (i_last + off) >= a.reach;
         near = !below && !above;
-        far = near ? 0.0f : near_far[above];
+        // a block past the wave's last key meets no distance of its own, and that one's weight may hold anything
+        far = near || j > lim_last ? 0.0f : near_far[above];
       }
       const float unit = near ? 1.0f : BIAS ? far_unit[above] : a.c;
       prepare<BIAS>(s[b], a.c, j, bias, near, j + 31 > lim_first, lim);

@@ -222,3 +222,24 @@ def test_vast_weights_beside_scores_of_next_to_nothing(causal, dtype):
     for n, t in dict(out=out, dv=dv).items():
         ref.assert_close(n, t, want[n])
     assert all(torch.isfinite(t).all() for t in (dq, dk, dw))
+
+
+@BOTH_TYPES
+@pytest.mark.parametrize("nq,nk", [([1, 5], [20, 33]), ([40, 1], [45, 70]), ([130], [150])], ids=str)
+@pytest.mark.parametrize("reach", [2, 10])
+def test_weights_that_no_pair_meets(nq, nk, reach, dtype):
+    """Buckets of keys behind the query, in causal attention: whatever their weights hold, NaN among it, nothing changes."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(13)
+    q, do = (torch.randn((sum(nq), 4, 64), generator=g, device=DEV).to(dtype) for _ in range(2))
+    k, v = (torch.randn((sum(nk), 4, 64), generator=g, device=DEV).to(dtype) for _ in range(2))
+    bucket, seqs = lram.relative_buckets(8, reach), lram.pack(nq, nk)
+    got = []
+    for unmet in (0.0, math.nan, math.inf, -math.inf):
+        w = torch.randn((4, 8), generator=torch.Generator().manual_seed(14)).to(DEV).to(dtype)
+        w[:, 4:] = unmet
+        rel = lram.RelativeBias(w, bucket)
+        out, saved = lram.attention_forward(q, k, v, seqs, True, rel=rel, save=True)
+        got.append((out, saved.lse, *lram.attention_backward(q, k, v, seqs, out, saved, do, True, rel=rel)))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
