@@ -64,11 +64,11 @@ int lram_layer_norm_backward(const void* h, const void* weight, const float* mea
  * of queries and keys are aligned: a prompt, a piece of one, or one token over a cache):
  *     s_ij = scale q_i . k_j + rel_weight[h][rel_bucket[clamp(j - i - (nk - nq), -rel_reach, rel_reach) + rel_reach]]
  *     out_i = sum_j softmax_j(s_ij) v_j,   0 where a query meets no key
- * The bias (Sec. 3.2's model learns positions; here by bucketed distance, as T5's does) is nullable.  A weight of -inf hides its keys as
- * `causal` does.  Finite weights of 1.16e7 (2^24 / log2 e) and more in magnitude, a type's lowest value among them, count
- * alike: no score matters beside them, so that a query that meets no other keys has the even average of theirs.  Scores
- * themselves have to stay below that in magnitude: fp32 holds no digit of them behind the point from there on, so that
- * gradients mean nothing, and from 128 times it on results may be NaN.
+ * The bias (Sec. 3.2's model learns positions; here by bucketed distance, as T5's does) is nullable.  A weight of -inf
+ * hides its keys as `causal` does.  Finite weights of 1.16e7 (2^24 / log2 e) and more in magnitude, a type's lowest value
+ * among them, count alike: no score matters beside them, so that a query that meets no other keys has the even average of
+ * theirs.  Scores themselves have to stay below that in magnitude: fp32 holds no digit of them behind the point from there
+ * on, so that gradients mean nothing, and from 128 times it on results may be NaN.
  *
  * The lengths stay on the device: nothing waits for them, and a captured call may be replayed over others.  max_q and
  * max_k are the longest nq and nk expected, from which the host chooses how to divide the work; lengths beyond them
