@@ -550,4 +550,10 @@ class SparseAdam:
 from . import layer as _layer  # noqa: E402
 from .layer import *  # noqa: E402,F401,F403
 
-__all__ += _layer.__all__
+# Positions and the cache of a layer that serves.
+from . import positions as _positions  # noqa: E402
+from .positions import *  # noqa: E402,F401,F403
+from . import paged as _paged  # noqa: E402
+from .paged import *  # noqa: E402,F401,F403
+
+__all__ += _layer.__all__ + _positions.__all__ + _paged.__all__

@@ -21,7 +21,7 @@ DEPS = [LOOKUP] + sorted(glob.glob(os.path.join(CSRC, "lram_*.h"))) + [
 # the operators of the layer around it
 LAYER = sorted(glob.glob(os.path.join(CSRC, "layer_*.hip")))
 LAYER_DEPS = LAYER + sorted(glob.glob(os.path.join(CSRC, "layer_*.h"))) + [
-    os.path.join(ROOT, "include", "lram.h"), os.path.join(ROOT, "include", "lram_layer.h")]
+    os.path.join(ROOT, "include", n) for n in ("lram.h", "lram_layer.h", "lram_cache.h")]
 SOURCES = [LOOKUP] + LAYER
 
 HIPCC_FLAGS = [

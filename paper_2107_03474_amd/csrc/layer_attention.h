@@ -33,7 +33,6 @@ using bf16x4 = __bf16 __attribute__((ext_vector_type(4)));
 using s16x4 = short __attribute__((ext_vector_type(4)));
 using Lds = __attribute__((address_space(3))) char*;
 
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr int ROWS = 32;     // packed rows (or keys) of a wave
 constexpr int KEYS = 64;     // keys of a tile in LDS
 constexpr int WAVES = 4, THREADS = WAVES * WAVE;
@@ -332,16 +331,9 @@ __device__ __forceinline__ void load_rows(const T* head, int64_t stride, int row
   }
 }
 
-// Weights far past any score.  From 2^24 on (a weight of 1.2e7, times log2 e) fp32 holds no digit behind the point, so that
-// scores beside such a weight say nothing, and times log2 e the type's lowest value, a common mask, would be -inf, which
-// hides a key altogether.  Finite weights from there on all count as +-2^126: a score added to it leaves it as it is, and
-// a row that meets no other keys (or one that meets keys of +2^126) has the even average of those.  Its maximum is then
-// +-2^126 and its sum a count, which m + log2 l would lose: the row's lse is m (1 + log2 l / 32) instead, l <= 2^30.
-constexpr float FAR_WEIGHT = 0x1p24f, VAST = 0x1p126f, BARELY = 0x1p-100f;
-__device__ __forceinline__ float in_log2(float weight) {
-  const float t = weight * LOG2E;
-  return fabsf(t) >= FAR_WEIGHT && fabsf(weight) < INFINITY ? copysignf(VAST, weight) : t;
-}
+// in_log2 makes finite weights far past any score +-VAST; the lse of a row whose maximum that is is m (1 + log2 l / 32), since
+// m + log2 l would lose the count l <= 2^30.
+constexpr float BARELY = 0x1p-100f;
 __device__ __forceinline__ bool is_vast(float x) { return fabsf(x) >= VAST && fabsf(x) < 2 * VAST; }
 // The scores' factor beside a bias that serves a whole block: next to nothing where the bias is vast, so that subtracting
 // the maximum does not bring them back (not 0, which would make the -inf of a key that is not seen NaN).

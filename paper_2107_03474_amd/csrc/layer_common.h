@@ -53,6 +53,18 @@ __device__ __forceinline__ float wave_sum(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
+constexpr float LOG2E = 1.4426950408889634f;
+
+// A bias's weights far past any score.  From 2^24 on (a weight of 1.2e7, times log2 e) fp32 holds no digit behind the point,
+// so that scores beside such a weight say nothing, and times log2 e the type's lowest value, a common mask, would be -inf,
+// which hides a key altogether.  Finite weights from there on all count as +-2^126: a score added to it leaves it as it is,
+// and a row that meets no other keys (or one that meets keys of +2^126) has the even average of those.
+constexpr float FAR_WEIGHT = 0x1p24f, VAST = 0x1p126f;
+__device__ __forceinline__ float in_log2(float weight) {
+  const float t = weight * LOG2E;
+  return fabsf(t) >= FAR_WEIGHT && fabsf(weight) < INFINITY ? copysignf(VAST, weight) : t;
+}
+
 inline bool off_align(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 inline uintptr_t elem_size(int dtype) { return dtype == LRAM_BF16 ? 2 : 4; }
 

@@ -1,0 +1,525 @@
+// layer_paged_attention.hip -- part of liblram: attention of new tokens over the cache in pages, for gfx950.
+//
+// In units of log 2, z_ij = c q_i . k_j + t_h(p_j - p_i), c = scale log2 e; p_ij = 2^(z_ij - m_i) / l_i; out_i = sum_j p_ij v_j;
+// weight_j += sum p_ij.  The G = heads / kv_heads query heads of a key head and the sequence's tokens are columns of one
+// matrix (column n: token n / G, head n % G of the group), 16 to a product of the matrix cores.
+//
+// A single token meets every key once: bound by HBM.  A wave takes blocks of 16 F keys straight from HBM into the operands'
+// registers (the pages hold them in that order), forms S^T = K Q^T, moves the maximum only when it grows by more than 2^8,
+// and has in its results the second operand of O^T += V^T P^T.  No value crosses lanes but the maximum, and LDS is met once,
+// when the four waves of a workgroup join what they have.  Long caches are cut into pieces, joined by a second kernel.
+
+#include <type_traits>
+
+#include "layer_paged.h"
+
+namespace {
+
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+
+constexpr int ATTEND_WAVES = 4, ATTEND_THREADS = ATTEND_WAVES * WAVE;
+constexpr int BIAS_MOST = 4096;  // group (2 reach + 193): a group's table by distance 0 ... reach is half of it
+constexpr float GROW = 8;
+
+template <typename T>
+struct Operand;  // 16 bytes of elements
+template <>
+struct Operand<bf16> {
+  using type = bf16x8;
+};
+template <>
+struct Operand<float> {
+  using type = f32x4;
+};
+
+struct Attend {
+  Pool p;
+  const void* q;
+  void* out;
+  int64_t q_row, q_head;
+  float c;
+  const void* rel_weight;
+  const int32_t* rel_bucket;
+  int buckets, reach, rel_bf16;
+  int tiles, pieces, piece;  // workgroups along a sequence's columns, along its keys, and keys of one of these
+  float* part;               // [piece][row][head][dim]
+  float2* stat;              // [piece][row][head]: maximum and sum
+  float2* whole;             // [row][head]: maximum and 1 / sum (weighing)
+};
+
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
+// The maximum and the sum over the four lanes l, l + 16, l + 32, l + 48, the same in all of them.
+__device__ __forceinline__ float of_groups(float x, bool sum) {
+  const int a = __builtin_bit_cast(int, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  const float u = __builtin_bit_cast(float, (unsigned)r[0]), v = __builtin_bit_cast(float, (unsigned)r[1]);
+  const float y = sum ? u + v : fmaxf(u, v);
+  const int b = __builtin_bit_cast(int, y);
+  const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  const float w = __builtin_bit_cast(float, (unsigned)s[0]), z = __builtin_bit_cast(float, (unsigned)s[1]);
+  return sum ? w + z : fmaxf(w, z);
+}
+
+// The columns of a tile that a lane holds: its query's operand, position and place.
+template <typename T, int D>
+struct Column {
+  static constexpr int CH = D / (4 * PageTile<T>::E);
+  typename Operand<T>::type q[CH];
+  int position, head;  // head: of the group
+  int64_t row;         // -1: none
+
+  __device__ __forceinline__ void load(const Attend& a, const CacheSeq& s, int kv_head, int64_t n) {
+    const int lane = threadIdx.x % WAVE;
+    const int64_t i = n / a.p.group;
+    head = (int)(n - i * a.p.group);
+    row = i < s.nq ? s.q0 + i : -1;
+    position = i < s.nq ? s.at + (int)i : INT32_MIN;
+    const T* const x = (const T*)a.q + (row < 0 ? 0 : row * a.q_row + (kv_head * a.p.group + head) * a.q_head);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      q[c] = {};
+      if (row >= 0) q[c] = *(const typename Operand<T>::type*)(x + (4 * c + lane / 16) * PageTile<T>::E);
+    }
+  }
+};
+
+// The bias of a group's heads by distance, in LDS.
+__device__ __forceinline__ void load_bias(const Attend& a, int kv_head, float* bias) {
+  const int n = a.reach + 1;
+  for (int i = threadIdx.x; i < a.p.group * n; i += blockDim.x) {
+    const int h = i / n, far = i - h * n, bucket = a.rel_bucket[a.reach - far];
+    const int64_t at = (int64_t)(kv_head * a.p.group + h) * a.buckets + min(max(bucket, 0), a.buckets - 1);
+    bias[i] = in_log2(a.rel_bf16 ? (float)((const bf16*)a.rel_weight)[at] : ((const float*)a.rel_weight)[at]);
+  }
+}
+
+// Scores of a block of 16 F keys of which `left` are used: z[h][r] of key 16 h + 4 (lane / 16) + r, -inf where it is not met.
+template <typename T, int D, bool BIAS>
+__device__ __forceinline__ void scores(const Attend& a, const Column<T, D>& col,
+                                       const typename Operand<T>::type (&k)[PageTile<T>::F][Column<T, D>::CH],
+                                       const int4 (&at)[PageTile<T>::F], int left, const float* bias,
+                                       f32x4 (&z)[PageTile<T>::F]) {
+  const int g = threadIdx.x % WAVE / 16;
+#pragma unroll
+  for (int h = 0; h < PageTile<T>::F; ++h) {
+    f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < Column<T, D>::CH; ++c) s = mma(k[h][c], col.q[c], s);
+    const int p[4] = {at[h].x, at[h].y, at[h].z, at[h].w};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const bool met = p[r] <= col.position && h * 16 + 4 * g + r < left;
+      float x = s[r] * a.c;
+      if constexpr (BIAS) {
+        const uint32_t far = (uint32_t)col.position - (uint32_t)p[r];
+        x += bias[col.head * (a.reach + 1) + (int)min(met ? far : 0, (uint32_t)a.reach)];
+      }
+      z[h][r] = met ? x : -INFINITY;
+    }
+  }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void load_keys(const Pool& p, int64_t keys,
+                                          typename Operand<T>::type (&k)[PageTile<T>::F][Column<T, D>::CH],
+                                          int4 (&at)[PageTile<T>::F]) {
+  using Ti = PageTile<T>;
+  const int lane = threadIdx.x % WAVE;
+  const T* const x = (const T*)p.k + keys * D + lane * Ti::E;
+#pragma unroll
+  for (int h = 0; h < Ti::F; ++h) {
+#pragma unroll
+    for (int c = 0; c < Column<T, D>::CH; ++c)
+      k[h][c] = *(const typename Operand<T>::type*)(x + h * 16 * D + c * WAVE * Ti::E);
+    at[h] = *(const int4*)(p.position + keys + h * 16 + lane / 16 * 4);
+  }
+}
+
+template <typename T, int D, int CT, bool BIAS>
+__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_attention(Attend a) {
+  using Ti = PageTile<T>;
+  using Op = typename Operand<T>::type;
+  constexpr int E = Ti::E, F = Ti::F, KEYS = Ti::KEYS, DB = D / 16, COLS = 16 * CT;
+  __shared__ __align__(16) float joined[ATTEND_WAVES][16][D + 4];
+  __shared__ float2 stats[ATTEND_WAVES][COLS];
+  __shared__ float bias[BIAS ? BIAS_MOST / 2 : 1];
+  const Pool& p = a.p;
+  const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), g = lane / 16;
+  int64_t id = blockIdx.x;
+  const int head = (int)(id % p.kv_heads);
+  id /= p.kv_heads;
+  const int b = (int)(id % p.batch);
+  id /= p.batch;
+  const int tile0 = (int)(id % a.tiles), piece = (int)(id / a.tiles);
+  const CacheSeq s = cache_seq(p, b);
+  if (piece == 0 && tile0 == 0) {  // rows of no sequence
+    const int64_t n = (int64_t)p.group * D;
+    const auto clear = [&](int64_t from, int64_t to) {
+      for (int64_t i = from * n + threadIdx.x; i < to * n; i += ATTEND_THREADS) {
+        const int64_t row = i / n;
+        ((T*)a.out)[(row * p.heads + head * p.group) * D + i % n] = (T)0.0f;
+      }
+    };
+    if (b == 0) clear(0, clamp_row(p.start[0], p.rows));
+    if (b == p.batch - 1) clear(clamp_row(p.start[p.batch], p.rows), p.rows);
+  }
+  if (piece && (int64_t)piece * a.piece >= s.nk) return;
+  const bool alone = a.pieces == 1 || s.nk <= a.piece;  // no other piece has keys
+  if constexpr (BIAS) {
+    load_bias(a, head, bias);
+    __syncthreads();
+  }
+  for (int64_t tile = tile0; tile * COLS < (int64_t)s.nq * p.group; tile += a.tiles) {
+    Column<T, D> col[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) col[t].load(a, s, head, tile * COLS + t * 16 + lane % 16);
+    f32x4 o[DB][CT] = {};
+    float m[CT], l[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) m[t] = -INFINITY, l[t] = 0;
+    for (int64_t base = (int64_t)piece * a.piece; base < s.nk; base += (int64_t)a.pieces * a.piece) {
+      const int end = (int)min(base + a.piece, (int64_t)s.nk);
+      for (int slot = (int)base + wave * KEYS; slot < end; slot += ATTEND_WAVES * KEYS) {
+        const int page = __builtin_amdgcn_readfirstlane(page_of(p, b, slot));
+        if (page < 0) continue;
+        const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
+        const int left = s.nk - slot;
+        Op k[F][Column<T, D>::CH], v[DB];
+        int4 at[F];
+        load_keys<T, D>(p, keys, k, at);
+        const T* const x = (const T*)p.v + keys * D + lane * E;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) v[d] = *(const Op*)(x + d * WAVE * E);
+        if (left < KEYS) {  // what lies past the last key is never met, NaN or not
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+              if (e / 4 * 16 + 4 * g + e % 4 >= left) v[d][e] = 0;
+        }
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          f32x4 z[F];
+          scores<T, D, BIAS>(a, col[t], k, at, left, bias, z);
+          float top = z[0][0];
+#pragma unroll
+          for (int h = 0; h < F; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, z[h][r]);
+          top = of_groups(top, false);
+          if (__builtin_amdgcn_ballot_w64(top > m[t] + GROW)) {
+            const float now = fmaxf(m[t], top), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - now);
+            m[t] = now;
+            l[t] *= f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d][t] *= f;
+          }
+          const float top_used = m[t] == -INFINITY ? 0.0f : m[t];
+          Op w;
+#pragma unroll
+          for (int h = 0; h < F; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float e = __builtin_amdgcn_exp2f(z[h][r] - top_used);
+              l[t] += e;
+              w[h * 4 + r] = (T)e;
+            }
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[d][t] = mma(v[d], w, o[d][t]);
+        }
+      }
+    }
+    // the waves' parts, in their order
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      l[t] = of_groups(l[t], true);
+      if (g == 0) stats[wave][t * 16 + lane] = {m[t], l[t]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) top = fmaxf(top, stats[w][t * 16 + lane % 16].x);
+        const float f = m[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[t] - top);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) *(f32x4*)&joined[wave][lane % 16][d * 16 + 4 * g] = o[d][t] * f;
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < 16 * (D / 4); i += ATTEND_THREADS) {
+        const int n = i / (D / 4), d = i % (D / 4) * 4;
+        const int64_t at = tile * COLS + t * 16 + n, token = at / p.group;
+        if (token >= s.nq) continue;
+        const int64_t place = (s.q0 + token) * p.heads + head * p.group + (at - token * p.group);
+        float top = -INFINITY, sum = 0;
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) top = fmaxf(top, stats[w][t * 16 + n].x);
+        f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) {
+          const float2 st = stats[w][t * 16 + n];
+          sum += st.x == -INFINITY ? st.y : st.y * __builtin_amdgcn_exp2f(st.x - top);  // NaN stays
+          x += *(const f32x4*)&joined[w][n][d];
+        }
+        if (alone) {
+          const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+          const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+          store_n<T, 4>((T*)a.out + place * D + d, y);
+          if (a.whole && d == 0) a.whole[place] = {top, inv};
+        } else {
+          const int64_t to = (int64_t)piece * p.rows * p.heads + place;
+          *(f32x4*)(a.part + to * D + d) = x;
+          if (d == 0) a.stat[to] = {top, sum};
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// The pieces' parts of a query and head joined.
+template <typename T, int D>
+__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_join(Attend a, int rows_each) {
+  constexpr int LANES = D / 4, TEAMS = ATTEND_THREADS / LANES;
+  __shared__ float tops[ATTEND_WAVES];
+  __shared__ __align__(16) float parts[TEAMS][D];
+  __shared__ float sums[TEAMS];
+  const Pool& p = a.p;
+  const int h = (int)(blockIdx.x % p.heads), b = (int)(blockIdx.x / p.heads % p.batch);
+  const int first = (int)(blockIdx.x / p.heads / p.batch);
+  const CacheSeq s = cache_seq(p, b);
+  if (s.nk <= a.piece) return;
+  const int pieces = (int)min(((int64_t)s.nk + a.piece - 1) / a.piece, (int64_t)a.pieces);
+  const int team = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
+  const int64_t step = p.rows * p.heads;
+  for (int i = first; i < s.nq; i += rows_each) {
+    const int64_t place = (s.q0 + i) * p.heads + h;
+    float top = -INFINITY;
+    for (int n = threadIdx.x; n < pieces; n += ATTEND_THREADS) top = fmaxf(top, a.stat[n * step + place].x);
+#pragma unroll
+    for (int o = WAVE / 2; o; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
+    if (threadIdx.x % WAVE == 0) tops[threadIdx.x / WAVE] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    float sum = 0;
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int n = team; n < pieces; n += TEAMS) {
+      const float2 st = a.stat[n * step + place];
+      const f32x4 y = *(const f32x4*)(a.part + (n * step + place) * D + d);
+      const float f = st.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.x - top);
+      sum += st.x == -INFINITY ? st.y : st.y * f;
+      x += y * f;
+    }
+    *(f32x4*)&parts[team][d] = x;
+    if (d == 0) sums[team] = sum;
+    __syncthreads();
+    if (team == 0) {
+      for (int n = 1; n < TEAMS; ++n) {
+        x += *(const f32x4*)&parts[n][d];
+        sum += sums[n];
+      }
+      const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+      const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+      store_n<T, 4>((T*)a.out + place * D + d, y);
+      if (a.whole && d == 0) a.whole[place] = {top, inv};
+    }
+    __syncthreads();
+  }
+}
+
+// The weight that each key gathers: a wave keeps a block of keys and goes over the sequence's queries, in a fixed order.
+template <typename T, int D, bool BIAS>
+__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int blocks) {
+  using Ti = PageTile<T>;
+  using Op = typename Operand<T>::type;
+  constexpr int F = Ti::F, KEYS = Ti::KEYS;
+  __shared__ float bias[BIAS ? BIAS_MOST / 2 : 1];
+  const Pool& p = a.p;
+  const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int head = (int)(blockIdx.x % p.kv_heads), b = (int)(blockIdx.x / p.kv_heads % p.batch);
+  const int64_t first = blockIdx.x / p.kv_heads / p.batch;
+  const CacheSeq s = cache_seq(p, b);
+  if (s.nq == 0 || first * (ATTEND_WAVES * KEYS) >= s.nk) return;
+  if constexpr (BIAS) {
+    load_bias(a, head, bias);
+    __syncthreads();
+  }
+  for (int64_t slot = (first * ATTEND_WAVES + wave) * KEYS; slot < s.nk; slot += (int64_t)blocks * ATTEND_WAVES * KEYS) {
+    const int page = __builtin_amdgcn_readfirstlane(page_of(p, b, (int)slot));
+    if (page < 0) continue;
+    const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
+    const int left = s.nk - (int)slot;
+    Op k[F][Column<T, D>::CH];
+    int4 at[F];
+    load_keys<T, D>(p, keys, k, at);
+    f32x4 got[F] = {};
+    for (int64_t n = 0; n < (int64_t)s.nq * p.group; n += 16) {
+      Column<T, D> col;
+      col.load(a, s, head, n + lane % 16);
+      const float2 st = col.row < 0 ? float2{0, 0} : a.whole[col.row * p.heads + head * p.group + col.head];
+      f32x4 z[F];
+      scores<T, D, BIAS>(a, col, k, at, left, bias, z);
+#pragma unroll
+      for (int h = 0; h < F; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          got[h][r] += z[h][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(z[h][r] - st.x) * st.y;
+    }
+#pragma unroll
+    for (int h = 0; h < F; ++h) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int o = 1; o < 16; o *= 2) got[h][r] += __shfl_xor(got[h][r], o);
+      if (lane % 16 == 0) {
+        float* const w = p.weight + keys + h * 16 + lane / 16 * 4;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (h * 16 + lane / 16 * 4 + r < left) w[r] += got[h][r];
+      }
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_clear(T* out, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * ATTEND_THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * ATTEND_THREADS)
+    out[i] = (T)0.0f;
+}
+
+struct Plan {
+  int ct;
+  int64_t tiles, pieces, piece;
+  size_t part, stat, whole;  // bytes
+};
+
+constexpr int64_t PIECE_STEP = 128, PIECE_LEAST = 512, GROUPS_WANTED = 2048;
+constexpr int64_t MOST_GROUPS = ((int64_t)1 << 32) / ATTEND_THREADS - 1;
+
+int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+Plan plan_of(const lram_paged& p, bool weigh) {
+  Plan x{};
+  const int64_t G = p.heads / p.kv_heads, lists = std::max<int64_t>(1, (int64_t)p.batch * p.kv_heads);
+  // a plan that understates the rows is found out by how many there are
+  const int64_t tokens = std::max({std::min(p.max_q, p.rows), over(p.rows, std::max(p.batch, 1)), (int64_t)1});
+  const int64_t keys = std::max<int64_t>(1, std::min(p.max_k, p.width * p.page));
+  x.ct = tokens * G > 16 ? 4 : 1;
+  x.tiles = std::max<int64_t>(1, std::min(over(tokens * G, 16 * x.ct), MOST_GROUPS / lists));
+  const int64_t wanted = std::min(over(GROUPS_WANTED, lists * x.tiles), MOST_GROUPS / (lists * x.tiles));
+  x.piece = over(over(keys, std::max<int64_t>(1, wanted)), PIECE_STEP) * PIECE_STEP;
+  x.piece = std::max(x.piece, PIECE_LEAST);
+  x.pieces = over(keys, x.piece);
+  const size_t places = (size_t)p.rows * p.heads;
+  if (x.pieces > 1) {
+    x.part = (size_t)x.pieces * places * p.head_dim * sizeof(float);
+    x.stat = (size_t)x.pieces * places * sizeof(float2);
+  }
+  if (weigh) x.whole = places * sizeof(float2);
+  return x;
+}
+
+int check_queries(const lram_paged& p, const lram_paged_queries& a) {
+  if (int rc = check_pool(p, true)) return rc;
+  const int64_t G = p.heads / p.kv_heads;
+  if (!(a.scale > 0) || !(a.scale < INFINITY) || (a.weigh & ~1) || (a.weigh && p.pages && !p.weight)) return LRAM_EINVAL;
+  if (bad_strides(a.q_row, a.q_head, p.heads, p.head_dim, p.dtype)) return LRAM_EINVAL;
+  if ((int64_t)p.batch * p.heads > MOST_GROUPS) return LRAM_EINVAL;
+  if (a.rel_weight) {
+    if (a.wdtype != LRAM_F32 && !(a.wdtype == LRAM_BF16 && p.dtype == LRAM_BF16)) return LRAM_EDTYPE;
+    if (!a.rel_bucket || a.rel_buckets < 1 || a.rel_buckets > 256 || a.rel_reach < 0 || a.rel_reach > BIAS_MOST ||
+        G * (2 * (int64_t)a.rel_reach + 193) > BIAS_MOST)
+      return LRAM_EINVAL;
+    if (off_align(a.rel_weight, elem_size(a.wdtype)) || off_align(a.rel_bucket, 4)) return LRAM_EINVAL;
+  }
+  return LRAM_OK;
+}
+
+template <typename F>
+int by_form(int dtype, int dim, F f) {
+  const auto of = [&](auto t) {
+    return dim == 128 ? f(t, std::integral_constant<int, 128>())
+           : dim == 64 ? f(t, std::integral_constant<int, 64>())
+                       : f(t, std::integral_constant<int, 32>());
+  };
+  return dtype == LRAM_BF16 ? of(bf16()) : of(float());
+}
+
+}  // namespace
+
+extern "C" {
+
+int lram_paged_attention_workspace_bytes(const lram_paged* p, const lram_paged_queries* q, size_t* bytes) {
+  if (!p || !q || !bytes) return LRAM_EINVAL;
+  if (int rc = check_queries(*p, *q)) return rc;
+  const Plan x = plan_of(*p, q->weigh);
+  *bytes = x.part + x.stat + x.whole;
+  return LRAM_OK;
+}
+
+int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void* out, void* workspace, size_t ws_bytes,
+                         void* stream) {
+  if (!p || !q) return LRAM_EINVAL;
+  if (int rc = check_queries(*p, *q)) return rc;
+  if (p->rows == 0) return LRAM_OK;
+  if (!q->q || !out || off_align(q->q, 16) || off_align(out, 16)) return LRAM_EINVAL;
+  const Plan x = plan_of(*p, q->weigh);
+  const size_t need = x.part + x.stat + x.whole;
+  if (need && (!workspace || off_align(workspace, 16) || ws_bytes < need)) return LRAM_EWORKSPACE;
+  Attend a{};
+  a.p = pool_of(*p);
+  a.q = q->q, a.out = out, a.q_row = q->q_row, a.q_head = q->q_head;
+  a.c = q->scale * LOG2E;
+  a.rel_weight = q->rel_weight, a.rel_bucket = q->rel_bucket, a.buckets = q->rel_buckets, a.reach = q->rel_reach;
+  a.rel_bf16 = q->wdtype == LRAM_BF16;
+  a.tiles = (int)x.tiles, a.pieces = (int)x.pieces, a.piece = (int)x.piece;
+  char* const ws = (char*)workspace;
+  if (x.part) a.part = (float*)ws, a.stat = (float2*)(ws + x.part);
+  if (x.whole) a.whole = (float2*)(ws + x.part + x.stat);
+  if (p->batch == 0) {
+    const int64_t n = p->rows * p->heads * p->head_dim;
+    const dim3 grid((unsigned)std::min<int64_t>(over(n, ATTEND_THREADS), 4096));
+    if (p->dtype == LRAM_BF16)
+      hipLaunchKernelGGL(k_paged_clear<bf16>, grid, dim3(ATTEND_THREADS), 0, (hipStream_t)stream, (bf16*)out, n);
+    else
+      hipLaunchKernelGGL(k_paged_clear<float>, grid, dim3(ATTEND_THREADS), 0, (hipStream_t)stream, (float*)out, n);
+    return layer_launched();
+  }
+  return by_form(p->dtype, p->head_dim, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    const auto go = [&](auto kernel, int64_t groups, auto... more) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(ATTEND_THREADS), 0, (hipStream_t)stream, a, more...);
+      return layer_launched();
+    };
+    const int64_t lists = (int64_t)p->batch * p->kv_heads, groups = lists * x.tiles * x.pieces;
+    int rc = q->rel_weight ? x.ct == 1 ? go(k_paged_attention<T, D, 1, true>, groups) : go(k_paged_attention<T, D, 4, true>, groups)
+             : x.ct == 1   ? go(k_paged_attention<T, D, 1, false>, groups)
+                           : go(k_paged_attention<T, D, 4, false>, groups);
+    if (rc == LRAM_OK && x.part) {
+      const int64_t all = (int64_t)p->batch * p->heads;
+      const int64_t each = std::max<int64_t>(1, std::min({p->max_q, p->rows, MOST_GROUPS / all}));
+      rc = go(k_paged_join<T, D>, all * each, (int)each);
+    }
+    if (rc == LRAM_OK && q->weigh && p->pages) {
+      const int64_t keys = std::max<int64_t>(1, std::min(p->max_k, p->width * p->page));
+      const int64_t blocks = std::max<int64_t>(1, std::min(over(keys, ATTEND_WAVES * PageTile<T>::KEYS), MOST_GROUPS / lists));
+      rc = q->rel_weight ? go(k_paged_weigh<T, D, true>, lists * blocks, (int)blocks)
+                         : go(k_paged_weigh<T, D, false>, lists * blocks, (int)blocks);
+    }
+    return rc;
+  });
+}
+
+}  // extern "C"
