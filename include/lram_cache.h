@@ -43,7 +43,7 @@ int lram_positions(const int32_t* start, const int32_t* first, int32_t batch, in
  * lram_rotate -- q [rows][heads][head_dim] and k [rows][kv_heads][head_dim], with their strides in elements (multiples of 16
  * bytes), into dense q_out and k_out, at position [rows] (any int32).  backward != 0 turns the other way round, which takes
  * the results' gradients to the arguments'.  k is nullable (kv_heads = 0).  head_dim: a multiple of 8, at most
- * LRAM_ROTARY_MAX_HEAD_DIM.  A dense q or k may be its own result.
+ * LRAM_ROTARY_MAX_HEAD_DIM.  Results are not their arguments' own memory.
  */
 int lram_rotate(const lram_rotary* r, int dtype, int backward, int64_t rows, int32_t head_dim, const int32_t* position,
                 const void* q, int64_t q_row, int64_t q_head, int32_t heads, void* q_out, const void* k, int64_t k_row,

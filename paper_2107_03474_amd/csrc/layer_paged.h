@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "../../include/lram_cache.h"
 #include "layer_common.h"
@@ -98,6 +99,16 @@ inline Pool pool_of(const lram_paged& p) {
   x.rows = p.rows, x.width = p.width, x.pages = (int)p.pages, x.page = p.page, x.log_page = __builtin_ctz(p.page);
   x.batch = p.batch, x.heads = p.heads, x.kv_heads = p.kv_heads, x.group = p.heads / p.kv_heads;  // 0 where no queries are given
   return x;
+}
+
+template <typename F>
+int by_form(int dtype, int dim, F f) {
+  const auto of = [&](auto t) {
+    return dim == 128 ? f(t, std::integral_constant<int, 128>())
+           : dim == 64 ? f(t, std::integral_constant<int, 64>())
+                       : f(t, std::integral_constant<int, 32>());
+  };
+  return dtype == LRAM_BF16 ? of(bf16()) : of(float());
 }
 
 }  // namespace

@@ -1,61 +1,240 @@
 // layer_paged_append.hip -- part of liblram: new rows into the pages of the cache.
 //
-// One launch: workgroups that rotate q's rows, and workgroups that each take 32 key slots of a head, through LDS from
-// the rows' order into the pages' (keys are rotated on the way out).  Bound by HBM for prompts, by its launch for
-// single tokens.
+// One launch.  q: rows rotated as they lie (rotate_chunk).  k: a wave takes the rows of 16 key slots of a sequence and some of
+// their heads; a lane owns pairs of 16-byte chunks of single rows and forms their sines and cosines once for all of these
+// heads.  v: a wave takes 32 key slots; a lane takes 16 bytes of each of the 4 F keys that lie side by side in the page and
+// turns them round in its registers.  Nothing goes through LDS.  Bound by HBM for prompts, by its launch for single tokens.
 
 #include "layer_paged.h"
 #include "layer_rotary.h"
 
 namespace {
 
-constexpr int APPEND_THREADS = 256;
+constexpr int APPEND_WAVES = 4, APPEND_THREADS = APPEND_WAVES * WAVE;
 
 struct Append {
   Pool p;
-  const void *k, *v, *q;
-  void* q_out;
+  Rotate q;  // of q's rows; turns, pairs and magnitude are k's too
+  const void *k, *v;
   const float* given;
-  const int64_t* turns;  // null: nothing is rotated
-  int64_t k_row, k_head, v_row, v_head, q_row, q_head;
-  int pairs, interleaved;
-  float magnitude;
-  int tiles;         // workgroups of a sequence and key head
-  unsigned q_groups;  // workgroups of q's rows, the first ones of the grid
+  int64_t k_row, k_head, v_row, v_head;
+  int each;                 // heads that a wave takes
+  int64_t places, v_places;  // for tiles of 16 and of 32 slots
+  int64_t q_groups, waves;  // workgroups that take q, the first ones; waves that take k, the next ones
 };
 
-// x's E elements from e0 on, rotated; row: the head's whole row.
-template <typename T, int E>
-__device__ __forceinline__ void turned(const Append& a, const T* row, int e0, int position, float (&f)[E]) {
-  load_n<T, E>(row + e0, f);
-  if (!a.turns || e0 >= 2 * a.pairs) return;
-  if (a.interleaved) {
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      const int pair = (e0 + e) / 2;
-      if (pair >= a.pairs) break;
-      const Turn t = turn_of(a.turns[pair], position, a.magnitude, 1.0f);
-      const float u = f[e], v = f[e + 1];
-      f[e] = fmaf(u, t.c, -v * t.s);
-      f[e + 1] = fmaf(u, t.s, v * t.c);
+// Rows of a tile: row t of 16 or 32 is row at + t of the tensors, for from <= t < to, and has position + t.
+struct Tile {
+  int64_t at;
+  int from, to, position;
+};
+
+// A lane's chunks of a row, E elements each: units i = lane, lane + 64, ... of 16 rows times D / 2 E pairs of chunks.
+template <typename T, int D, Form FORM>
+struct Units {
+  static constexpr int E = PageTile<T>::E, OF_ROW = D / (2 * E), N = (16 * OF_ROW + WAVE - 1) / WAVE;
+  Turn turn[N][E];
+
+  // First elements of unit u's chunks.
+  static __device__ __forceinline__ void chunks(const Append& a, int u, int& x, int& y) {
+    if (FORM != HALVES || u * E >= a.q.pairs) {
+      x = u * 2 * E;
+      y = x + E;
+    } else {
+      x = u * E;
+      y = x + a.q.pairs;
     }
-  } else {
+  }
+  __device__ __forceinline__ void prepare(const Append& a, const Tile& tile) {
+    if constexpr (FORM == PLAIN) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = threadIdx.x % WAVE + n * WAVE, t = i / OF_ROW, u = i % OF_ROW;
+      if (t < tile.from || t >= tile.to || u * E >= a.q.pairs) continue;
+      const int position = tile.position + t;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        turn[n][e] = turn_of(a.q.turns[FORM == HALVES ? u * E + e : min(u * E + e, a.q.pairs - 1)], position, a.q.magnitude, 1.0f);
+    }
+  }
+  // Chunks x0 and y0 of unit n rotated.
+  using C = Chunk<T>;
+  __device__ __forceinline__ void rotate(const Append& a, int n, int u, typename C::type& x0, typename C::type& y0) const {
+    if (FORM == PLAIN || u * E >= a.q.pairs) return;
+    typename C::wide f = C::up(x0), g = C::up(y0);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int i = e0 + e;
-      if (i >= 2 * a.pairs) break;
-      const bool second = i >= a.pairs;
-      const int pair = second ? i - a.pairs : i;
-      const Turn t = turn_of(a.turns[pair], position, a.magnitude, 1.0f);
-      const float other = (float)row[second ? i - a.pairs : i + a.pairs];
-      f[e] = second ? fmaf(other, t.s, f[e] * t.c) : fmaf(f[e], t.c, -other * t.s);
+      if constexpr (FORM == HALVES) {
+        const float v = f[e], w = g[e];
+        f[e] = fmaf(v, turn[n][e].c, -w * turn[n][e].s);
+        g[e] = fmaf(v, turn[n][e].s, w * turn[n][e].c);
+      } else {
+        typename C::wide& x = e < E / 2 ? f : g;
+        const int i = 2 * e % E;
+        const bool turns = u * E + e < a.q.pairs;
+        const float v = x[i], w = x[i + 1];
+        x[i] = turns ? fmaf(v, turn[n][e].c, -w * turn[n][e].s) : v;
+        x[i + 1] = turns ? fmaf(v, turn[n][e].s, w * turn[n][e].c) : w;
+      }
+    }
+    x0 = C::down(f);
+    y0 = C::down(g);
+  }
+};
+
+// E elements from e0 on of a row whose halves do not start on a chunk.
+template <typename T, int E>
+__device__ __forceinline__ typename Chunk<T>::type turned(const Append& a, const T* row, int e0, int position) {
+  typename Chunk<T>::wide f = Chunk<T>::up(*(const typename Chunk<T>::type*)(row + e0));
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = e0 + e;
+    if (i >= 2 * a.q.pairs) break;
+    const bool second = i >= a.q.pairs;
+    const Turn t = turn_of(a.q.turns[second ? i - a.q.pairs : i], position, a.q.magnitude, 1.0f);
+    const float other = (float)row[second ? i - a.q.pairs : i + a.q.pairs];
+    f[e] = second ? fmaf(other, t.s, f[e] * t.c) : fmaf(f[e], t.c, -other * t.s);
+  }
+  return Chunk<T>::down(f);
+}
+
+// The chunks of one head of a tile.
+template <typename T, int D, Form FORM>
+struct Chunks {
+  using U = Units<T, D, FORM>;
+  typename Chunk<T>::type in[U::N][2];
+
+  __device__ __forceinline__ void load(const Append& a, const Tile& tile, const T* x, int64_t stride) {
+#pragma unroll
+    for (int n = 0; n < U::N; ++n) {
+      const int i = threadIdx.x % WAVE + n * WAVE, t = i / U::OF_ROW;
+      int c, d;
+      U::chunks(a, i % U::OF_ROW, c, d);
+      if (t < tile.from || t >= tile.to) continue;
+      in[n][0] = *(const typename Chunk<T>::type*)(x + (tile.at + t) * stride + c);
+      in[n][1] = *(const typename Chunk<T>::type*)(x + (tile.at + t) * stride + d);
+    }
+  }
+};
+
+// One head of a tile, rotated, into the page's block.
+template <typename T, int D, Form FORM>
+__device__ __forceinline__ void turn_head(const Append& a, const Units<T, D, FORM>& units, const Tile& tile, const T* x,
+                                          int64_t stride, const Chunks<T, D, FORM>& chunks, T* y) {
+  using U = Units<T, D, FORM>;
+  constexpr int E = U::E;
+  const int lane = threadIdx.x % WAVE;
+  const auto place = [](int t, int e0) { return (e0 / E * 16 + t) * E; };  // of the chunk from e0 on of row t
+  if constexpr (FORM != ODD_HALVES) {
+#pragma unroll
+    for (int n = 0; n < U::N; ++n) {
+      const int i = lane + n * WAVE, t = i / U::OF_ROW, u = i % U::OF_ROW;
+      int c, d;
+      U::chunks(a, u, c, d);
+      if (t < tile.from || t >= tile.to) continue;
+      typename Chunk<T>::type f = chunks.in[n][0], g = chunks.in[n][1];
+      units.rotate(a, n, u, f, g);
+      *(typename Chunk<T>::type*)(y + place(t, c)) = f;
+      *(typename Chunk<T>::type*)(y + place(t, d)) = g;
+    }
+  } else {
+    for (int i = lane; i < 16 * (D / E); i += WAVE) {
+      const int t = i / (D / E), e0 = i % (D / E) * E;
+      if (t < tile.from || t >= tile.to) continue;
+      *(typename Chunk<T>::type*)(y + place(t, e0)) =
+          turned<T, E>(a, x + (tile.at + t) * stride, e0, tile.position + t);
     }
   }
 }
 
+// One head of values into a page's block.
+template <typename T, int D>
+__device__ __forceinline__ void turn_values(const Tile& tile, const T* x, int64_t stride, T* y) {
+  using Ti = PageTile<T>;
+  constexpr int E = Ti::E, CH = D / E;
+  const int lane = threadIdx.x % WAVE;
+#pragma unroll
+  for (int n = 0; n < PAGE_BLOCK * D / (E * E) / WAVE + (PAGE_BLOCK * D / (E * E) < WAVE); ++n) {
+    const int i = lane + n * WAVE, c = i % CH, g = i / CH % 4, t1 = i / (4 * CH) * Ti::KEYS + 4 * g;
+    if (t1 >= PAGE_BLOCK) break;
+    typename Chunk<T>::type in[E];
+    bool whole = true, some = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int t = t1 + e / 4 * 16 + e % 4;
+      const bool mine = t >= tile.from && t < tile.to;
+      whole = whole && mine;
+      some = some || mine;
+      if (mine) in[e] = *(const typename Chunk<T>::type*)(x + (tile.at + t) * stride + c * E);
+    }
+    if (!some) continue;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const int d = c * E + j;
+      T* const to = y + ((t1 / Ti::KEYS * (D / 16) + d / 16) * 64 + g * 16 + d % 16) * E;
+      if (whole) {
+        typename Chunk<T>::type o;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = in[e][j];
+        *(typename Chunk<T>::type*)to = o;
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int t = t1 + e / 4 * 16 + e % 4;
+          if (t >= tile.from && t < tile.to) to[e] = in[e][j];
+        }
+      }
+    }
+  }
+}
+
+// Where the tiles of SLOTS slots lie.  Sequence b has the places from start[b] / SLOTS + 2 b on, as many as its n rows can
+// need ((n + SLOTS - 2) / SLOTS + 1 tiles), so that a wave finds its own by a search in the starts, 64 at a time.
+template <int SLOTS>
+struct Places {
+  static constexpr int64_t of(int64_t rows, int64_t batch) { return rows / SLOTS + 2 * batch + 1; }
+  int b;
+  int64_t nth;  // tile of the sequence, negative: none
+
+  __device__ __forceinline__ void find(const Pool& p, int64_t place) {
+    const int lane = threadIdx.x % WAVE;
+    const auto first = [&](int e) { return clamp_row(p.start[e], p.rows) / SLOTS + 2 * (int64_t)e; };
+    int lo = 0, n = p.batch;
+    while (n > 1) {
+      const int step = (n + WAVE - 1) / WAVE, e = lo + lane * step;
+      const uint64_t at = __builtin_amdgcn_ballot_w64(e < lo + n && first(e) <= place);
+      const int past = max(__popcll(at) - 1, 0) * step;
+      lo += past;
+      n = min(step, n - past);
+    }
+    b = __builtin_amdgcn_readfirstlane(lo);
+    nth = p.batch ? place - first(b) : -1;
+  }
+};
+
+// The rows of a tile that have a slot, from slot `slot` on, of the page `page`.
+template <int SLOTS>
+__device__ __forceinline__ Tile tile_of(const Pool& p, int64_t place, int& page, int64_t& slot) {
+  Places<SLOTS> at;
+  at.find(p, place);
+  Tile tile{};
+  if (at.nth < 0) return tile;
+  const CacheSeq s = cache_seq(p, at.b);
+  const int64_t first = (int64_t)s.used - (p.start[at.b + 1] - s.q0);  // slot of the row q0
+  slot = ((first >> (SLOTS == 16 ? 4 : 5)) + at.nth) * SLOTS;
+  if (slot < 0 || slot >= first + s.nq || slot >= s.nk) return tile;
+  page = page_of(p, at.b, (int)slot);
+  if (page < 0) return tile;
+  tile.at = s.q0 + slot - first;
+  tile.from = (int)max(first - slot, (int64_t)0);
+  tile.to = (int)min(min(first + s.nq, (int64_t)s.nk) - slot, (int64_t)SLOTS);
+  tile.position = s.at + (int)(slot - first);
+  return tile;
+}
+
 // The position of a row, 0 where it belongs to no sequence.
 __device__ __forceinline__ int position_of(const Pool& p, int64_t row) {
-  int lo = 0, hi = p.batch + 1;
+  int lo = 0, hi = p.batch + 1;  // start[lo - 1] <= row < start[hi]
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
     if (p.start[mid] <= row)
@@ -66,81 +245,61 @@ __device__ __forceinline__ int position_of(const Pool& p, int64_t row) {
   return lo == 0 || lo > p.batch ? 0 : p.seen[lo - 1] - (int)(p.start[lo] - row);
 }
 
-template <typename T, int D>
+template <typename T, int D, Form FORM>
 __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(Append a) {
-  using Ti = PageTile<T>;
-  constexpr int E = Ti::E, F = Ti::F, CH = D / E;
   const Pool& p = a.p;
-  if (blockIdx.x < a.q_groups) {
-    const int64_t id = (int64_t)blockIdx.x * APPEND_THREADS + threadIdx.x;
-    const int64_t at = id / CH, row = at / p.heads;
-    if (row >= p.rows) return;
-    const int h = (int)(at % p.heads), e0 = (int)(id % CH) * E;
-    float f[E];
-    turned<T, E>(a, (const T*)a.q + row * a.q_row + h * a.q_head, e0, position_of(p, row), f);
-    store_n<T, E>((T*)a.q_out + (row * p.heads + h) * D + e0, f);
+  if constexpr (FORM != PLAIN) {
+    if (blockIdx.x < a.q_groups) {
+      rotate_chunk<T, FORM>(a.q, blockIdx.x * APPEND_THREADS + threadIdx.x, [&](int64_t row) { return position_of(p, row); });
+      return;
+    }
+  }
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+  int64_t id = (blockIdx.x - a.q_groups) * APPEND_WAVES + wave;
+  const bool of_v = id >= a.waves;
+  if (of_v) id -= a.waves;
+  const int parts = (p.kv_heads + a.each - 1) / a.each;
+  const int head0 = (int)(id % parts) * a.each, head1 = min(head0 + a.each, p.kv_heads);
+  const int64_t place = id / parts;
+  if (place >= (of_v ? a.v_places : a.places)) return;
+  int page;
+  int64_t slot;
+  if (of_v) {
+    const Tile tile = tile_of<32>(p, place, page, slot);
+    if (tile.from >= tile.to) return;
+    for (int head = head0; head < head1; ++head) {
+      const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
+      turn_values<T, D>(tile, (const T*)a.v + head * a.v_head, a.v_row, (T*)p.v + keys * D);
+    }
     return;
   }
-  __shared__ __align__(16) T rows_k[PAGE_BLOCK][D], rows_v[PAGE_BLOCK][D + E];
-  const int64_t group = blockIdx.x - a.q_groups;
-  const int head = (int)(group % p.kv_heads), tile = (int)(group / p.kv_heads % a.tiles);
-  const int b = (int)(group / p.kv_heads / a.tiles);
-  const CacheSeq s = cache_seq(p, b);
-  const int first = s.used - (int)(p.start[b + 1] - s.q0);  // slot of the row q0
-  const int low = max(first, 0), high = min(first + s.nq, s.nk);
-  for (int64_t block = (low >> 5) + tile; block * PAGE_BLOCK < high; block += a.tiles) {
-    const int slot0 = (int)block * PAGE_BLOCK;
-    const int page = page_of(p, b, slot0);
-    if (page < 0) continue;  // all threads alike
-    const int t0 = slot0 & (p.page - 1);
-    const int from = max(low - slot0, 0), to = min(high - slot0, PAGE_BLOCK);
-    const int64_t keys = page_rows(p, page, head) + t0;
-    for (int i = threadIdx.x; i < PAGE_BLOCK * CH; i += APPEND_THREADS) {
-      const int t = i / CH, c = i % CH * E;
-      if (t < from || t >= to) continue;
-      const int64_t row = s.q0 + (slot0 + t - first);
-      *(Packed<T, E>*)&rows_k[t][c] = *(const Packed<T, E>*)((const T*)a.k + row * a.k_row + head * a.k_head + c);
-      *(Packed<T, E>*)&rows_v[t][c] = *(const Packed<T, E>*)((const T*)a.v + row * a.v_row + head * a.v_head + c);
-    }
-    if (threadIdx.x < PAGE_BLOCK && (int)threadIdx.x >= from && (int)threadIdx.x < to) {
-      const int row = slot0 + threadIdx.x - first;
-      p.position[keys + threadIdx.x] = s.at + row;
-      if (p.weight) p.weight[keys + threadIdx.x] = a.given ? a.given[(s.q0 + row) * p.kv_heads + head] : 0.0f;
-    }
-    __syncthreads();
-    T* const k = (T*)p.k + keys * D;
-    for (int i = threadIdx.x; i < PAGE_BLOCK * CH; i += APPEND_THREADS) {
-      const int half = i / (16 * CH), c = i / 16 % CH, t = half * 16 + i % 16;
-      if (t < from || t >= to) continue;
-      float f[E];
-      turned<T, E>(a, rows_k[t], c * E, s.at + slot0 + t - first, f);
-      store_n<T, E>(k + (int64_t)i * E, f);
-    }
-    T* const v = (T*)p.v + keys * D;
-    for (int i = threadIdx.x; i < PAGE_BLOCK * CH; i += APPEND_THREADS) {  // as many times E values
-      const int d16 = i % 16, g = i / 16 % 4, d = i / 64 % (D / 16) * 16 + d16, t1 = i / (4 * D) * Ti::KEYS + g * 4;
-      Packed<T, E> o;
-      bool whole = true;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int t = t1 + e / 4 * 16 + e % 4;
-        whole = whole && t >= from && t < to;
-        o.v[e] = rows_v[t][d];
-      }
-      if (whole) {
-        *(Packed<T, E>*)(v + (int64_t)i * E) = o;
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int t = t1 + e / 4 * 16 + e % 4;
-          if (t >= from && t < to) v[(int64_t)i * E + e] = o.v[e];
-        }
-      }
-    }
-    __syncthreads();
+  const Tile tile = tile_of<16>(p, place, page, slot);
+  if (tile.from >= tile.to) return;
+  // the next head's rows are on their way while one is rotated
+  Units<T, D, FORM> units;
+  Chunks<T, D, FORM> chunks, next;
+  if constexpr (FORM != ODD_HALVES) {
+    next.load(a, tile, (const T*)a.k + head0 * a.k_head, a.k_row);
+    units.prepare(a, tile);
   }
-  (void)F;
+  for (int head = head0; head < head1; ++head) {
+    const T* const rows = (const T*)a.k + head * a.k_head;
+    if constexpr (FORM != ODD_HALVES) {
+      chunks = next;
+      if (head + 1 < head1) next.load(a, tile, rows + a.k_head, a.k_row);
+    }
+    const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
+    turn_head<T, D, FORM>(a, units, tile, rows, a.k_row, chunks, (T*)p.k + keys * D);
+    if (lane >= tile.from && lane < tile.to) {
+      p.position[keys + lane] = tile.position + lane;
+      if (p.weight) p.weight[keys + lane] = a.given ? a.given[(tile.at + lane) * p.kv_heads + head] : 0.0f;
+    }
+  }
 }
+
+// Heads of a wave: as many as leave enough waves to fill the card.
+constexpr int KEY_HEADS_EACH = 16;
+constexpr int64_t MANY_WAVES = 4096;
 
 constexpr int EXTEND_THREADS = 256;
 __global__ __launch_bounds__(EXTEND_THREADS) void k_paged_extend(const int32_t* start, int batch, int32_t* used, int32_t* seen) {
@@ -180,29 +339,38 @@ int lram_paged_append(const lram_paged* p, const lram_rotary* r, const void* k, 
   if (!k || !v || off_align(k, 16) || off_align(v, 16) || off_align(given, 4)) return LRAM_EINVAL;
   Append a{};
   a.p = pool_of(*p);
-  a.k = k, a.v = v, a.q = q, a.q_out = q_out, a.given = given;
-  a.k_row = k_row, a.k_head = k_head, a.v_row = v_row, a.v_head = v_head, a.q_row = q_row, a.q_head = q_head;
-  if (r) a.turns = r->turns, a.pairs = r->pairs, a.interleaved = r->interleaved, a.magnitude = r->magnitude;
-  // n rows touch (n + 30) / 32 + 1 blocks at most; a grid holds fewer than 2^32 threads
-  const int64_t each = 16 / (int64_t)elem_size(p->dtype), expected = std::min(p->max_q, p->rows);
-  const int64_t groups_q = q ? (p->rows * p->heads * (p->head_dim / each) + APPEND_THREADS - 1) / APPEND_THREADS : 0;
-  const int64_t most = ((int64_t)1 << 32) / APPEND_THREADS - 1 - groups_q, lists = (int64_t)p->batch * p->kv_heads;
-  if (groups_q + lists >= ((int64_t)1 << 32) / APPEND_THREADS) return LRAM_EINVAL;
-  a.q_groups = (unsigned)groups_q;
-  if (lists) a.tiles = (int)std::max<int64_t>(1, std::min((expected + 30) / PAGE_BLOCK + 1, most / lists));
-  const int64_t grid = groups_q + lists * a.tiles;
-  if (grid == 0) return LRAM_OK;
+  a.k = k, a.v = v, a.given = given;
+  a.k_row = k_row, a.k_head = k_head, a.v_row = v_row, a.v_head = v_head;
+  a.q.q = q, a.q.q_out = q_out, a.q.q_row = q_row, a.q.q_head = q_head;
+  a.q.rows = p->rows, a.q.heads = p->heads, a.q.dim = p->head_dim;
+  if (r) {
+    const int64_t threads = divide(a.q, *r, p->dtype) * p->rows;
+    if (threads > (int64_t)1 << 31) return LRAM_EINVAL;
+    if (q) a.q_groups = (threads + APPEND_THREADS - 1) / APPEND_THREADS;
+  }
+  const int64_t most = (((int64_t)1 << 32) / APPEND_THREADS - 1 - a.q_groups) * APPEND_WAVES;  // a grid: below 2^32 threads
+  const auto parts = [&] { return (p->kv_heads + a.each - 1) / a.each; };
+  a.places = Places<16>::of(p->rows, p->batch), a.v_places = Places<32>::of(p->rows, p->batch);
+  const auto waves = [&] { return (a.places + a.v_places) * parts(); };
+  a.each = 1;
+  while (a.each < KEY_HEADS_EACH && p->rows / 16 * parts() >= 2 * MANY_WAVES) a.each *= 2;
+  while (waves() > most && a.each < p->kv_heads) a.each *= 2;
+  if (waves() > most) return LRAM_EINVAL;
+  a.waves = a.places * parts();
+  const int64_t grid = a.q_groups + (waves() + APPEND_WAVES - 1) / APPEND_WAVES;
   const auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(APPEND_THREADS), 0, (hipStream_t)stream, a);
     return layer_launched();
   };
-  if (p->dtype == LRAM_BF16)
-    return p->head_dim == 128 ? go(k_paged_append<bf16, 128>)
-           : p->head_dim == 64 ? go(k_paged_append<bf16, 64>)
-                               : go(k_paged_append<bf16, 32>);
-  return p->head_dim == 128 ? go(k_paged_append<float, 128>)
-         : p->head_dim == 64 ? go(k_paged_append<float, 64>)
-                             : go(k_paged_append<float, 32>);
+  const Form form = r ? form_of(*r, p->dtype) : PLAIN;
+  return by_form(p->dtype, p->head_dim, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    return form == PLAIN        ? go(k_paged_append<T, D, PLAIN>)
+           : form == NEIGHBOURS ? go(k_paged_append<T, D, NEIGHBOURS>)
+           : form == HALVES     ? go(k_paged_append<T, D, HALVES>)
+                                : go(k_paged_append<T, D, ODD_HALVES>);
+  });
 }
 
 }  // extern "C"

@@ -9,8 +9,6 @@
 // and has in its results the second operand of O^T += V^T P^T.  No value crosses lanes but the maximum, and LDS is met once,
 // when the four waves of a workgroup join what they have.  Long caches are cut into pieces, joined by a second kernel.
 
-#include <type_traits>
-
 #include "layer_paged.h"
 
 namespace {
@@ -444,16 +442,6 @@ int check_queries(const lram_paged& p, const lram_paged_queries& a) {
     if (off_align(a.rel_weight, elem_size(a.wdtype)) || off_align(a.rel_bucket, 4)) return LRAM_EINVAL;
   }
   return LRAM_OK;
-}
-
-template <typename F>
-int by_form(int dtype, int dim, F f) {
-  const auto of = [&](auto t) {
-    return dim == 128 ? f(t, std::integral_constant<int, 128>())
-           : dim == 64 ? f(t, std::integral_constant<int, 64>())
-                       : f(t, std::integral_constant<int, 32>());
-  };
-  return dtype == LRAM_BF16 ? of(bf16()) : of(float());
 }
 
 }  // namespace

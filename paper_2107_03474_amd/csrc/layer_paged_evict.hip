@@ -177,13 +177,7 @@ int lram_paged_evict(const lram_paged* p, int64_t budget, int64_t recent, void* 
     hipLaunchKernelGGL(kernel, dim3((unsigned)(p->batch * p->kv_heads)), dim3(EVICT_THREADS), 0, (hipStream_t)stream, a);
     return layer_launched();
   };
-  if (p->dtype == LRAM_BF16)
-    return p->head_dim == 128 ? go(k_paged_evict<bf16, 128>)
-           : p->head_dim == 64 ? go(k_paged_evict<bf16, 64>)
-                               : go(k_paged_evict<bf16, 32>);
-  return p->head_dim == 128 ? go(k_paged_evict<float, 128>)
-         : p->head_dim == 64 ? go(k_paged_evict<float, 64>)
-                             : go(k_paged_evict<float, 32>);
+  return by_form(p->dtype, p->head_dim, [&](auto t, auto d) { return go(k_paged_evict<decltype(t), decltype(d)::value>); });
 }
 
 }  // extern "C"
