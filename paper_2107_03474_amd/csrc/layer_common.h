@@ -39,6 +39,17 @@ __device__ __forceinline__ void store_n(T* p, const float (&f)[N]) {
   *reinterpret_cast<Packed<T, N>*>(p) = a;
 }
 
+// 16 bytes of elements as one value, so that they are moved by one instruction; `loose` where they start on any element.
+template <typename T>
+struct Chunk {
+  static constexpr int E = 16 / (int)sizeof(T);
+  typedef T type __attribute__((ext_vector_type(E)));
+  typedef T loose __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+  typedef float wide __attribute__((ext_vector_type(E)));
+  static __device__ __forceinline__ wide up(type x) { return __builtin_convertvector(x, wide); }
+  static __device__ __forceinline__ type down(wide x) { return __builtin_convertvector(x, type); }
+};
+
 // The sum of x over the wave, the same in every lane (a tree of fixed shape).
 __device__ __forceinline__ float wave_sum(float x) {
 #define LRAM_DPP_ADD(ctrl, rows) \

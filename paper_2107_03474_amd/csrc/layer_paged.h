@@ -64,6 +64,15 @@ __device__ __forceinline__ int page_of(const Pool& p, int b, int slot) {
   return page >= 0 && page < p.pages ? page : -1;
 }
 
+// The same for a slot that is one for the whole wave.  Through the scalar cache: a vector load here would wait for every load
+// that the wave has on its way.
+__device__ __forceinline__ int page_of_wave(const Pool& p, int b, int slot) {
+  const int at = __builtin_amdgcn_readfirstlane(slot >> p.log_page);
+  const auto* const row = (const __attribute__((address_space(4))) int32_t*)(p.table + (int64_t)b * p.width);
+  const int page = row[at];
+  return page >= 0 && page < p.pages ? page : -1;
+}
+
 // First element of a page's keys of a head (k and v alike), and of its positions.
 __device__ __forceinline__ int64_t page_rows(const Pool& p, int page, int head) {
   return ((int64_t)page * p.kv_heads + head) << p.log_page;

@@ -44,6 +44,9 @@ struct Attend {
   float* part;               // [piece][row][head][dim]
   float2* stat;              // [piece][row][head]: maximum and sum
   float2* whole;             // [row][head]: maximum and 1 / sum (weighing)
+  float* scores;             // [sequence][kv_head][score_cols][scored]: of few columns, kept for the weights; null: none are
+  int score_cols;
+  int64_t scored;
 };
 
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -90,6 +93,11 @@ struct Column {
   }
 };
 
+// Whether a sequence's scores are kept for its keys' weights: the host expects few columns, and the sequence has no more.
+__device__ __forceinline__ bool keeps_scores(const Attend& a, const CacheSeq& s) {
+  return a.scores && s.nk <= a.scored && (int64_t)s.nq * a.p.group <= a.score_cols;
+}
+
 // The bias of a group's heads by distance, in LDS.
 __device__ __forceinline__ void load_bias(const Attend& a, int kv_head, float* bias) {
   const int n = a.reach + 1;
@@ -126,7 +134,17 @@ __device__ __forceinline__ void scores(const Attend& a, const Column<T, D>& col,
   }
 }
 
-template <typename T, int D>
+// Keys that no other workgroup meets pass the caches by (ONCE): 32 tokens over caches of 256 to 8,192, 32/8 heads of 128, bf16:
+// 113 -> 100 us.
+template <bool ONCE, typename V>
+__device__ __forceinline__ V fetch(const V* x) {
+  if constexpr (ONCE)
+    return __builtin_nontemporal_load(x);
+  else
+    return *x;
+}
+
+template <typename T, int D, bool ONCE>
 __device__ __forceinline__ void load_keys(const Pool& p, int64_t keys,
                                           typename Operand<T>::type (&k)[PageTile<T>::F][Column<T, D>::CH],
                                           int4 (&at)[PageTile<T>::F]) {
@@ -137,16 +155,18 @@ __device__ __forceinline__ void load_keys(const Pool& p, int64_t keys,
   for (int h = 0; h < Ti::F; ++h) {
 #pragma unroll
     for (int c = 0; c < Column<T, D>::CH; ++c)
-      k[h][c] = *(const typename Operand<T>::type*)(x + h * 16 * D + c * WAVE * Ti::E);
+      k[h][c] = fetch<ONCE>((const typename Operand<T>::type*)(x + h * 16 * D + c * WAVE * Ti::E));
     at[h] = *(const int4*)(p.position + keys + h * 16 + lane / 16 * 4);
   }
 }
 
+// Two workgroups a compute unit, so that 256 registers hold everything and the matrix cores take them as they are: with more,
+// the compiler keeps the results in the other half of the register file and moves them to and fro.
 template <typename T, int D, int CT, bool BIAS>
-__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_attention(Attend a) {
+__global__ __launch_bounds__(ATTEND_THREADS, 2) void k_paged_attention(Attend a) {
   using Ti = PageTile<T>;
   using Op = typename Operand<T>::type;
-  constexpr int E = Ti::E, F = Ti::F, KEYS = Ti::KEYS, DB = D / 16, COLS = 16 * CT;
+  constexpr int E = Ti::E, F = Ti::F, KEYS = Ti::KEYS, DB = D / 16, COLS = 16 * CT, STEP = ATTEND_WAVES * KEYS;
   __shared__ __align__(16) float joined[ATTEND_WAVES][16][D + 4];
   __shared__ float2 stats[ATTEND_WAVES][COLS];
   __shared__ float bias[BIAS ? BIAS_MOST / 2 : 1];
@@ -159,18 +179,17 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_attention(Attend a) {
   id /= p.batch;
   const int tile0 = (int)(id % a.tiles), piece = (int)(id / a.tiles);
   const CacheSeq s = cache_seq(p, b);
-  if (piece == 0 && tile0 == 0) {  // rows of no sequence
-    const int64_t n = (int64_t)p.group * D;
-    const auto clear = [&](int64_t from, int64_t to) {
-      for (int64_t i = from * n + threadIdx.x; i < to * n; i += ATTEND_THREADS) {
-        const int64_t row = i / n;
-        ((T*)a.out)[(row * p.heads + head * p.group) * D + i % n] = (T)0.0f;
-      }
-    };
-    if (b == 0) clear(0, clamp_row(p.start[0], p.rows));
-    if (b == p.batch - 1) clear(clamp_row(p.start[p.batch], p.rows), p.rows);
+  {  // rows of no sequence, shared out over the workgroups of a head
+    const int64_t before = clamp_row(p.start[0], p.rows), behind = max(clamp_row(p.start[p.batch], p.rows), before);
+    const int all = gridDim.x / p.kv_heads;
+    for (int64_t i = blockIdx.x / p.kv_heads; i < before + (p.rows - behind); i += all) {
+      T* const row = (T*)a.out + ((i < before ? i : behind + (i - before)) * p.heads + head * p.group) * D;
+#pragma clang loop unroll(disable) vectorize(disable)
+      for (int d = threadIdx.x; d < p.group * D; d += ATTEND_THREADS) row[d] = (T)0.0f;
+    }
   }
   if (piece && (int64_t)piece * a.piece >= s.nk) return;
+  const bool keeps = keeps_scores(a, s);
   const bool alone = a.pieces == 1 || s.nk <= a.piece;  // no other piece has keys
   if constexpr (BIAS) {
     load_bias(a, head, bias);
@@ -186,17 +205,34 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_attention(Attend a) {
     for (int t = 0; t < CT; ++t) m[t] = -INFINITY, l[t] = 0;
     for (int64_t base = (int64_t)piece * a.piece; base < s.nk; base += (int64_t)a.pieces * a.piece) {
       const int end = (int)min(base + a.piece, (int64_t)s.nk);
-      for (int slot = (int)base + wave * KEYS; slot < end; slot += ATTEND_WAVES * KEYS) {
-        const int page = __builtin_amdgcn_readfirstlane(page_of(p, b, slot));
-        if (page < 0) continue;
-        const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
-        const int left = s.nk - slot;
-        Op k[F][Column<T, D>::CH], v[DB];
-        int4 at[F];
-        load_keys<T, D>(p, keys, k, at);
-        const T* const x = (const T*)p.v + keys * D + lane * E;
+      // A block's values are on their way while its scores are formed, and the next one's keys (of a page looked up a block
+      // before) while it is finished.  Loads are made whatever the table says, of page 0 where it names none: where some were
+      // left out, the wait for keys would be one for everything.
+      const auto look = [&](int at) { return page_of_wave(p, b, min(at, end - 1)); };
+      const auto keys_of = [&](int page, int at) { return page_rows(p, max(page, 0), head) + (at & (p.page - 1)); };
+      int slot = (int)base + wave * KEYS;
+      if (slot >= end) continue;
+      int page = look(slot), next = look(slot + STEP);
+      Op k[F][Column<T, D>::CH], v[DB];
+      int4 at[F];
+      load_keys<T, D, CT == 1>(p, keys_of(page, slot), k, at);
+      const auto block = [&](auto more) {
+        const int left = page < 0 ? 0 : s.nk - slot;  // 0: no key is met
+        const T* const x = (const T*)p.v + keys_of(page, slot) * D + lane * E;
 #pragma unroll
-        for (int d = 0; d < DB; ++d) v[d] = *(const Op*)(x + d * WAVE * E);
+        for (int d = 0; d < DB; ++d) v[d] = fetch<CT == 1>((const Op*)(x + d * WAVE * E));
+        __builtin_amdgcn_sched_barrier(0);  // first the values, then the next keys: they are waited for in this order
+        f32x4 z[CT][F];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) scores<T, D, BIAS>(a, col[t], k, at, left, bias, z[t]);
+        if constexpr (more.value) {
+          __builtin_amdgcn_sched_barrier(0);
+          load_keys<T, D, CT == 1>(p, keys_of(next, slot + STEP), k, at);
+          __builtin_amdgcn_sched_barrier(0);
+          page = next;
+          next = look(slot + 2 * STEP);
+        }
+        if (left == 0) return;
         if (left < KEYS) {  // what lies past the last key is never met, NaN or not
 #pragma unroll
           for (int d = 0; d < DB; ++d)
@@ -206,13 +242,16 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_attention(Attend a) {
         }
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-          f32x4 z[F];
-          scores<T, D, BIAS>(a, col[t], k, at, left, bias, z);
-          float top = z[0][0];
+          if (CT == 1 && keeps && lane % 16 < s.nq * p.group) {
+            float* const to = a.scores + ((int64_t)(b * p.kv_heads + head) * a.score_cols + lane % 16) * a.scored + slot + 4 * g;
+#pragma unroll
+            for (int h = 0; h < F; ++h) *(f32x4*)(to + 16 * h) = z[t][h];
+          }
+          float top = z[t][0][0];
 #pragma unroll
           for (int h = 0; h < F; ++h)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, z[h][r]);
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, z[t][h][r]);
           top = of_groups(top, false);
           if (__builtin_amdgcn_ballot_w64(top > m[t] + GROW)) {
             const float now = fmaxf(m[t], top), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - now);
@@ -227,14 +266,16 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_attention(Attend a) {
           for (int h = 0; h < F; ++h)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float e = __builtin_amdgcn_exp2f(z[h][r] - top_used);
+              const float e = __builtin_amdgcn_exp2f(z[t][h][r] - top_used);
               l[t] += e;
               w[h * 4 + r] = (T)e;
             }
 #pragma unroll
           for (int d = 0; d < DB; ++d) o[d][t] = mma(v[d], w, o[d][t]);
         }
-      }
+      };
+      for (; slot + STEP < end; slot += STEP) block(std::true_type());
+      block(std::false_type());
     }
     // the waves' parts, in their order
 #pragma unroll
@@ -336,55 +377,86 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_join(Attend a, int row
   }
 }
 
-// The weight that each key gathers: a wave keeps a block of keys and goes over the sequence's queries, in a fixed order.
+// The weight that each key gathers, in a fixed order.  Of a single token's few columns the scores were kept (16 bytes a key for
+// four heads that share it, beside the 256 of its k); a thread then takes a key.  Otherwise a wave keeps a block of keys and
+// forms their scores again, over all of the sequence's queries.
+constexpr int WEIGH_CHUNK = ATTEND_THREADS;  // keys of a workgroup
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int blocks) {
+__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int chunks, int chunk) {
   using Ti = PageTile<T>;
   using Op = typename Operand<T>::type;
   constexpr int F = Ti::F, KEYS = Ti::KEYS;
   __shared__ float bias[BIAS ? BIAS_MOST / 2 : 1];
+  __shared__ float2 whole[16];
   const Pool& p = a.p;
   const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int head = (int)(blockIdx.x % p.kv_heads), b = (int)(blockIdx.x / p.kv_heads % p.batch);
   const int64_t first = blockIdx.x / p.kv_heads / p.batch;
   const CacheSeq s = cache_seq(p, b);
-  if (s.nq == 0 || first * (ATTEND_WAVES * KEYS) >= s.nk) return;
+  if (s.nq == 0 || first * chunk >= s.nk) return;
+  if (keeps_scores(a, s)) {
+    const int cols = s.nq * p.group;
+    if ((int)threadIdx.x < cols)
+      whole[threadIdx.x] = a.whole[(s.q0 + threadIdx.x / p.group) * p.heads + head * p.group + threadIdx.x % p.group];
+    __syncthreads();
+    for (int64_t base = first * chunk; base < s.nk; base += (int64_t)chunks * chunk) {
+      const int end = (int)min(base + chunk, (int64_t)s.nk);
+      for (int slot = (int)base + threadIdx.x; slot < end; slot += ATTEND_THREADS) {
+        const int page = page_of(p, b, slot);
+        if (page < 0) continue;
+        const float* const z = a.scores + (int64_t)(b * p.kv_heads + head) * a.score_cols * a.scored + slot;
+        float* const w = p.weight + page_rows(p, page, head) + (slot & (p.page - 1));
+        const float had = *w;
+        float got = 0;
+#pragma unroll 8
+        for (int c = 0; c < cols; ++c) {
+          const float x = z[c * a.scored];
+          got += x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x - whole[c].x) * whole[c].y;
+        }
+        *w = had + got;
+      }
+    }
+    return;
+  }
   if constexpr (BIAS) {
     load_bias(a, head, bias);
     __syncthreads();
   }
-  for (int64_t slot = (first * ATTEND_WAVES + wave) * KEYS; slot < s.nk; slot += (int64_t)blocks * ATTEND_WAVES * KEYS) {
-    const int page = __builtin_amdgcn_readfirstlane(page_of(p, b, (int)slot));
-    if (page < 0) continue;
-    const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
-    const int left = s.nk - (int)slot;
-    Op k[F][Column<T, D>::CH];
-    int4 at[F];
-    load_keys<T, D>(p, keys, k, at);
-    f32x4 got[F] = {};
-    for (int64_t n = 0; n < (int64_t)s.nq * p.group; n += 16) {
-      Column<T, D> col;
-      col.load(a, s, head, n + lane % 16);
-      const float2 st = col.row < 0 ? float2{0, 0} : a.whole[col.row * p.heads + head * p.group + col.head];
-      f32x4 z[F];
-      scores<T, D, BIAS>(a, col, k, at, left, bias, z);
+  for (int64_t base = first * chunk; base < s.nk; base += (int64_t)chunks * chunk) {
+    const int end = (int)min(base + chunk, (int64_t)s.nk);
+    for (int slot = (int)base + wave * KEYS; slot < end; slot += ATTEND_WAVES * KEYS) {
+      const int page = page_of_wave(p, b, slot);
+      if (page < 0) continue;
+      const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
+      const int left = s.nk - slot;
+      Op k[F][Column<T, D>::CH];
+      int4 at[F];
+      load_keys<T, D, false>(p, keys, k, at);
+      f32x4 got[F] = {};
+      for (int64_t n = 0; n < (int64_t)s.nq * p.group; n += 16) {
+        Column<T, D> col;
+        col.load(a, s, head, n + lane % 16);
+        const float2 st = col.row < 0 ? float2{0, 0} : a.whole[col.row * p.heads + head * p.group + col.head];
+        f32x4 z[F];
+        scores<T, D, BIAS>(a, col, k, at, left, bias, z);
 #pragma unroll
-      for (int h = 0; h < F; ++h)
+        for (int h = 0; h < F; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          got[h][r] += z[h][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(z[h][r] - st.x) * st.y;
-    }
+          for (int r = 0; r < 4; ++r)
+            got[h][r] += z[h][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(z[h][r] - st.x) * st.y;
+      }
 #pragma unroll
-    for (int h = 0; h < F; ++h) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int o = 1; o < 16; o *= 2) got[h][r] += __shfl_xor(got[h][r], o);
-      if (lane % 16 == 0) {
-        float* const w = p.weight + keys + h * 16 + lane / 16 * 4;
+      for (int h = 0; h < F; ++h) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (h * 16 + lane / 16 * 4 + r < left) w[r] += got[h][r];
+#pragma unroll
+          for (int o = 1; o < 16; o *= 2) got[h][r] += __shfl_xor(got[h][r], o);
+        if (lane % 16 == 0) {
+          float* const w = p.weight + keys + h * 16 + lane / 16 * 4;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (h * 16 + lane / 16 * 4 + r < left) w[r] += got[h][r];
+        }
       }
     }
   }
@@ -399,10 +471,15 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_clear(T* out, int64_t 
 struct Plan {
   int ct;
   int64_t tiles, pieces, piece;
-  size_t part, stat, whole;  // bytes
+  int64_t cols, scored;              // of kept scores; 0: none
+  size_t part, scores, stat, whole;  // bytes
+  size_t all() const { return part + scores + stat + whole; }
 };
 
-constexpr int64_t PIECE_STEP = 128, PIECE_LEAST = 512, GROUPS_WANTED = 2048;
+// Pieces: a round of two workgroups a unit for a single sequence, and up to four rounds for several, which are rarely of one
+// length (us of one round / four: one token over 131,072 keys, 32/8 heads of 128 bf16 with weights, 123 / 130; 32 tokens over
+// 256 to 8,192 keys 107 / 97).
+constexpr int64_t PIECE_STEP = 128, PIECE_LEAST = 256, ROUND = 512, ROUNDS = 4;
 constexpr int64_t MOST_GROUPS = ((int64_t)1 << 32) / ATTEND_THREADS - 1;
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -413,9 +490,9 @@ Plan plan_of(const lram_paged& p, bool weigh) {
   // a plan that understates the rows is found out by how many there are
   const int64_t tokens = std::max({std::min(p.max_q, p.rows), over(p.rows, std::max(p.batch, 1)), (int64_t)1});
   const int64_t keys = std::max<int64_t>(1, std::min(p.max_k, p.width * p.page));
-  x.ct = tokens * G > 16 ? 4 : 1;
+  x.ct = tokens * G > 16 ? 2 : 1;
   x.tiles = std::max<int64_t>(1, std::min(over(tokens * G, 16 * x.ct), MOST_GROUPS / lists));
-  const int64_t wanted = std::min(over(GROUPS_WANTED, lists * x.tiles), MOST_GROUPS / (lists * x.tiles));
+  const int64_t wanted = std::min(over(ROUND * std::min<int64_t>(std::max(p.batch, 1), ROUNDS), lists * x.tiles), MOST_GROUPS / (lists * x.tiles));
   x.piece = over(over(keys, std::max<int64_t>(1, wanted)), PIECE_STEP) * PIECE_STEP;
   x.piece = std::max(x.piece, PIECE_LEAST);
   x.pieces = over(keys, x.piece);
@@ -425,6 +502,11 @@ Plan plan_of(const lram_paged& p, bool weigh) {
     x.stat = (size_t)x.pieces * places * sizeof(float2);
   }
   if (weigh) x.whole = places * sizeof(float2);
+  if (weigh && tokens * G <= 16) {
+    x.cols = tokens * G;
+    x.scored = x.pieces * x.piece;
+    x.scores = (size_t)lists * x.cols * x.scored * sizeof(float);
+  }
   return x;
 }
 
@@ -452,7 +534,7 @@ int lram_paged_attention_workspace_bytes(const lram_paged* p, const lram_paged_q
   if (!p || !q || !bytes) return LRAM_EINVAL;
   if (int rc = check_queries(*p, *q)) return rc;
   const Plan x = plan_of(*p, q->weigh);
-  *bytes = x.part + x.stat + x.whole;
+  *bytes = x.all();
   return LRAM_OK;
 }
 
@@ -463,7 +545,7 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void*
   if (p->rows == 0) return LRAM_OK;
   if (!q->q || !out || off_align(q->q, 16) || off_align(out, 16)) return LRAM_EINVAL;
   const Plan x = plan_of(*p, q->weigh);
-  const size_t need = x.part + x.stat + x.whole;
+  const size_t need = x.all();
   if (need && (!workspace || off_align(workspace, 16) || ws_bytes < need)) return LRAM_EWORKSPACE;
   Attend a{};
   a.p = pool_of(*p);
@@ -473,9 +555,10 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void*
   a.rel_bf16 = q->wdtype == LRAM_BF16;
   a.tiles = (int)x.tiles, a.pieces = (int)x.pieces, a.piece = (int)x.piece;
   char* const ws = (char*)workspace;
-  if (x.part) a.part = (float*)ws, a.stat = (float2*)(ws + x.part);
-  if (x.whole) a.whole = (float2*)(ws + x.part + x.stat);
-  if (p->batch == 0) {
+  if (x.part) a.part = (float*)ws, a.stat = (float2*)(ws + x.part + x.scores);
+  if (x.scores) a.scores = (float*)(ws + x.part), a.score_cols = (int)x.cols, a.scored = x.scored;
+  if (x.whole) a.whole = (float2*)(ws + x.part + x.scores + x.stat);
+  if (p->batch == 0 || p->pages == 0) {
     const int64_t n = p->rows * p->heads * p->head_dim;
     const dim3 grid((unsigned)std::min<int64_t>(over(n, ATTEND_THREADS), 4096));
     if (p->dtype == LRAM_BF16)
@@ -492,19 +575,20 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void*
       return layer_launched();
     };
     const int64_t lists = (int64_t)p->batch * p->kv_heads, groups = lists * x.tiles * x.pieces;
-    int rc = q->rel_weight ? x.ct == 1 ? go(k_paged_attention<T, D, 1, true>, groups) : go(k_paged_attention<T, D, 4, true>, groups)
+    int rc = q->rel_weight ? x.ct == 1 ? go(k_paged_attention<T, D, 1, true>, groups) : go(k_paged_attention<T, D, 2, true>, groups)
              : x.ct == 1   ? go(k_paged_attention<T, D, 1, false>, groups)
-                           : go(k_paged_attention<T, D, 4, false>, groups);
+                           : go(k_paged_attention<T, D, 2, false>, groups);
     if (rc == LRAM_OK && x.part) {
       const int64_t all = (int64_t)p->batch * p->heads;
       const int64_t each = std::max<int64_t>(1, std::min({p->max_q, p->rows, MOST_GROUPS / all}));
       rc = go(k_paged_join<T, D>, all * each, (int)each);
     }
-    if (rc == LRAM_OK && q->weigh && p->pages) {
+    if (rc == LRAM_OK && q->weigh) {
       const int64_t keys = std::max<int64_t>(1, std::min(p->max_k, p->width * p->page));
-      const int64_t blocks = std::max<int64_t>(1, std::min(over(keys, ATTEND_WAVES * PageTile<T>::KEYS), MOST_GROUPS / lists));
-      rc = q->rel_weight ? go(k_paged_weigh<T, D, true>, lists * blocks, (int)blocks)
-                         : go(k_paged_weigh<T, D, false>, lists * blocks, (int)blocks);
+      const int64_t chunk = x.scores ? WEIGH_CHUNK : ATTEND_WAVES * PageTile<T>::KEYS;
+      const int64_t chunks = std::max<int64_t>(1, std::min(over(keys, chunk), MOST_GROUPS / lists));
+      rc = q->rel_weight ? go(k_paged_weigh<T, D, true>, lists * chunks, (int)chunks, (int)chunk)
+                         : go(k_paged_weigh<T, D, false>, lists * chunks, (int)chunks, (int)chunk);
     }
     return rc;
   });

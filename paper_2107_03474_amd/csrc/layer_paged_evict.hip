@@ -3,7 +3,8 @@
 // Of n keys of a head the `budget` of the highest rank stay: (newest ones first, weight, lowest position) as one 64-bit number
 // whose order is theirs, found by a radix selection from the top digit down.  Attention asks for no order of its keys (their
 // positions are stored beside them), so only keys that stay and lie past the budget move, into the slots below it that
-// are left: budget - n moves at most, and one where a step adds one key.
+// are left: budget - n moves at most, and one where a step adds one key.  A workgroup to a head selects, from ranks that it
+// keeps in registers; it moves a few keys itself, and leaves many to a second kernel that fills the card.
 
 #include "layer_paged.h"
 
@@ -11,11 +12,16 @@ namespace {
 
 constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / WAVE;
 
+constexpr int KEPT = 16;        // ranks that a thread keeps: 16,384 of a head; those of the slots behind are formed again
+constexpr int MOVED_HERE = 64;  // keys that the selecting workgroup moves itself
+constexpr int MOVE_WAVES = 4, MOVE_EACH = 16;  // of the second kernel: waves of a workgroup and keys of a wave
+
 struct Evict {
   Pool p;
   int64_t budget, recent;
-  int64_t most;   // entries of a list
-  int32_t* lists; // [batch][kv_heads][2][most]: slots that move, and where they go
+  int64_t most;    // entries of a list
+  int32_t* lists;  // [batch][kv_heads][2][most]: slots that move, and where they go
+  int32_t* counts; // [batch][kv_heads]: keys that are left to the second kernel
 };
 
 // A slot of no page below the budget counts as taken: nothing can move there.
@@ -47,77 +53,217 @@ __device__ __forceinline__ int before(bool yes, int* sums, int& all) {
   return n;
 }
 
-// One key to another slot, by a wave.
+// n <= 64 keys of a head to other slots, by a wave.
 template <typename T, int D>
-__device__ __forceinline__ void move_key(const Pool& p, int b, int head, int from, int to) {
+__device__ __forceinline__ void move_keys(const Pool& p, int b, int head, const int32_t* from, const int32_t* to, int n) {
   using Ti = PageTile<T>;
-  constexpr int E = Ti::E;
+  constexpr int E = Ti::E, CH = D / E, AT_ONCE = 4;
   const int lane = threadIdx.x % WAVE;
-  const int pf = page_of(p, b, from), pt = page_of(p, b, to);
-  if (pf < 0 || pt < 0) return;
-  const int tf = from & (p.page - 1), tt = to & (p.page - 1);
-  const int64_t f = page_rows(p, pf, head), t = page_rows(p, pt, head);
-  if (lane < D / E)
-    *(uint4*)((T*)p.k + t * D + ((int64_t)(tt / 16 * (D / E) + lane) * 16 + tt % 16) * E) =
-        *(const uint4*)((const T*)p.k + f * D + ((int64_t)(tf / 16 * (D / E) + lane) * 16 + tf % 16) * E);
-  const auto place = [](int t, int d) {
-    return ((t / Ti::KEYS * (D / 16) + d / 16) * 64 + t % 16 / 4 * 16 + d % 16) * E + t % Ti::KEYS / 16 * 4 + t % 4;
+  // lane i: the rows of the pool that key i leaves and takes, and whether it has both
+  int64_t f = 0, t = 0;
+  bool moves = false;
+  if (lane < n) {
+    const int sf = from[lane], st = to[lane], pf = page_of(p, b, sf), pt = page_of(p, b, st);
+    moves = pf >= 0 && pt >= 0;
+    f = page_rows(p, max(pf, 0), head) + (sf & (p.page - 1));
+    t = page_rows(p, max(pt, 0), head) + (st & (p.page - 1));
+    if (moves) {
+      const int position = p.position[f];
+      const float weight = p.weight[f];
+      p.position[t] = position;
+      p.weight[t] = weight;
+    }
+  }
+  const auto key_at = [](int64_t row, int c) {  // pages hold whole blocks, so that a row's place in its block is its own
+    return ((row >> 4 << 4) * D) + (int64_t)(c * 16 + (int)(row & 15)) * E;
   };
-  for (int d = lane; d < D; d += WAVE) ((T*)p.v)[t * D + place(tt, d)] = ((const T*)p.v)[f * D + place(tf, d)];
-  if (lane == 0) {
-    p.position[t + tt] = p.position[f + tf];
-    p.weight[t + tt] = p.weight[f + tf];
+  const auto value_at = [](int64_t row, int d) {
+    const int r = (int)(row & (Ti::KEYS - 1));
+    return (row - r) * D + (int64_t)((d / 16 * 4 + r % 16 / 4) * 16 + d % 16) * E + r / 16 * 4 + r % 4;
+  };
+  for (int i0 = 0; i0 < n * CH; i0 += AT_ONCE * WAVE) {
+    typename Chunk<T>::type x[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int i = i0 + j * WAVE + lane, key = min(i / CH, WAVE - 1);
+      const int64_t row = __shfl(f, key);
+      if (__shfl(moves, key) && i < n * CH) x[j] = *(const typename Chunk<T>::type*)((const T*)p.k + key_at(row, i % CH));
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int i = i0 + j * WAVE + lane, key = min(i / CH, WAVE - 1);
+      const int64_t row = __shfl(t, key);
+      if (__shfl(moves, key) && i < n * CH) *(typename Chunk<T>::type*)((T*)p.k + key_at(row, i % CH)) = x[j];
+    }
+  }
+  for (int i0 = 0; i0 < n * D; i0 += 2 * AT_ONCE * WAVE) {
+    T x[2 * AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < 2 * AT_ONCE; ++j) {
+      const int i = i0 + j * WAVE + lane, key = min(i / D, WAVE - 1);
+      const int64_t row = __shfl(f, key);
+      if (__shfl(moves, key) && i < n * D) x[j] = ((const T*)p.v)[value_at(row, i % D)];
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * AT_ONCE; ++j) {
+      const int i = i0 + j * WAVE + lane, key = min(i / D, WAVE - 1);
+      const int64_t row = __shfl(t, key);
+      if (__shfl(moves, key) && i < n * D) ((T*)p.v)[value_at(row, i % D)] = x[j];
+    }
   }
 }
 
 template <typename T, int D>
 __global__ __launch_bounds__(EVICT_THREADS) void k_paged_evict(Evict a) {
-  __shared__ int bins[256], sums[EVICT_WAVES], chosen[3];
+  constexpr int BINS = 2048;
+  __shared__ int bins[BINS], sums[EVICT_WAVES], chosen[3];
+  __shared__ int votes[2][KEPT * EVICT_WAVES];
+  __shared__ int32_t near[2][MOVED_HERE];
   const Pool& p = a.p;
-  const int head = blockIdx.x % p.kv_heads, b = blockIdx.x / p.kv_heads;
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+  const int list = blockIdx.x, head = list % p.kv_heads, b = list / p.kv_heads;
   const int64_t most = p.width << p.log_page;
   const int n = (int)min((int64_t)max(p.used[b], 0), most);
-  if (n <= a.budget) return;
+  if (n <= a.budget) {
+    if (threadIdx.x == 0) a.counts[list] = 0;
+    return;
+  }
   const int budget = (int)a.budget;
   const int64_t newest = (int64_t)p.seen[b] - a.recent;
-  // the digits of the lowest rank that stays, from the top
+  uint64_t rank[KEPT];
+#pragma unroll
+  for (int j = 0; j < KEPT; ++j) {
+    const int slot = j * EVICT_THREADS + threadIdx.x;
+    if (j * EVICT_THREADS >= n) break;
+    rank[j] = slot < n ? rank_of(p, b, head, slot, newest, budget) : 0;
+  }
+  if (n - budget == 1) {  // a step that adds one key: the lowest rank goes, of equal ones the last
+    uint64_t lowest = ~(uint64_t)0;
+    int at = -1;
+    const auto look = [&](uint64_t r, int slot) {
+      if (r < lowest || (r == lowest && slot > at)) lowest = r, at = slot;
+    };
+#pragma unroll
+    for (int j = 0; j < KEPT; ++j) {
+      if (j * EVICT_THREADS >= n) break;
+      const int slot = j * EVICT_THREADS + threadIdx.x;
+      if (slot < n) look(rank[j], slot);
+    }
+    for (int slot = KEPT * EVICT_THREADS + threadIdx.x; slot < n; slot += EVICT_THREADS)
+      look(rank_of(p, b, head, slot, newest, budget), slot);
+#pragma unroll
+    for (int o = WAVE / 2; o; o /= 2) {
+      const uint64_t r = __shfl_xor(lowest, o);
+      const int slot = __shfl_xor(at, o);
+      look(r, slot);
+    }
+    __shared__ uint64_t low_rank[EVICT_WAVES];
+    if (lane == 0) low_rank[wave] = lowest, sums[wave] = at;
+    __syncthreads();
+    if (threadIdx.x == 0) a.counts[list] = 0;
+    if (wave) return;
+    for (int w = 0; w < EVICT_WAVES; ++w) look(low_rank[w], sums[w]);
+    if (at < budget) {  // the last slot's key takes its place
+      near[0][0] = budget;
+      near[1][0] = at;
+      move_keys<T, D>(p, b, head, near[0], near[1], 1);
+    }
+    return;
+  }
+  // the digits of the lowest rank that stays, from the top: 11, 11 and 10 bits of either half
   uint64_t mask = 0, prefix = 0;
   int want = budget;  // of the ranks that begin with prefix
   bool all = false;   // these are all there are
-  for (int shift = 56; shift >= 0 && !all; shift -= 8) {
-    if (threadIdx.x < 256) bins[threadIdx.x] = 0;
+  for (int i = 0; i < 6 && !all; ++i) {
+    const int shift = i == 0 ? 53 : i == 1 ? 42 : i == 2 ? 32 : i == 3 ? 21 : i == 4 ? 10 : 0;
+    const int size = i == 2 || i == 5 ? 1023 : 2047;
+    for (int k = threadIdx.x; k < BINS; k += EVICT_THREADS) bins[k] = 0;
     __syncthreads();
-    for (int slot = threadIdx.x; slot < n; slot += EVICT_THREADS) {
+#pragma unroll
+    for (int j = 0; j < KEPT; ++j)
+      if (j * EVICT_THREADS + (int)threadIdx.x < n && (rank[j] & mask) == prefix) atomicAdd(&bins[rank[j] >> shift & size], 1);
+    for (int slot = KEPT * EVICT_THREADS + threadIdx.x; slot < n; slot += EVICT_THREADS) {
       const uint64_t r = rank_of(p, b, head, slot, newest, budget);
-      if ((r & mask) == prefix) atomicAdd(&bins[r >> shift & 255], 1);
+      if ((r & mask) == prefix) atomicAdd(&bins[r >> shift & size], 1);
     }
     __syncthreads();
-    if (threadIdx.x < WAVE) {  // lane l: the bins 255 - 4 l and the three below
-      int sum = 0;
+    // thread t: the bins 2047 - 2 t and the one below
+    const int high = bins[BINS - 1 - 2 * threadIdx.x], low = bins[BINS - 2 - 2 * threadIdx.x];
+    int above = high + low;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum += bins[255 - 4 * threadIdx.x - i];
-      int above = sum;
+    for (int o = 1; o < WAVE; o *= 2) {
+      const int x = __shfl_up(above, o);
+      above += lane >= o ? x : 0;
+    }
+    if (lane == WAVE - 1) sums[wave] = above;
+    __syncthreads();
 #pragma unroll
-      for (int o = 1; o < WAVE; o *= 2) {
-        const int x = __shfl_up(above, o);
-        above += (int)threadIdx.x >= o ? x : 0;
-      }
-      if (above >= want && above - sum < want) {  // one lane
-        int left = want - (above - sum), bin = 255 - 4 * threadIdx.x;
-        while (bins[bin] < left) left -= bins[bin--];
-        chosen[0] = bin, chosen[1] = left, chosen[2] = bins[bin];
-      }
+    for (int w = 0; w < EVICT_WAVES; ++w) above += w < wave ? sums[w] : 0;
+    above -= high + low;  // of the bins above both
+    if (above < want && want <= above + high + low) {  // one thread
+      const bool upper = want <= above + high;
+      chosen[0] = BINS - 1 - 2 * (int)threadIdx.x - !upper;
+      chosen[1] = want - above - (upper ? 0 : high);
+      chosen[2] = upper ? high : low;
     }
     __syncthreads();
     prefix |= (uint64_t)chosen[0] << shift;
-    mask |= (uint64_t)255 << shift;
+    mask |= (uint64_t)size << shift;
     want = chosen[1];
     all = want == chosen[2];
   }
-  int32_t* const from = a.lists + ((int64_t)b * p.kv_heads + head) * 2 * a.most;
+  int32_t* const from = a.lists + (int64_t)list * 2 * a.most;
   int32_t* const to = from + a.most;
-  int equal = 0, sources = 0, holes = 0;
-  for (int base = 0; base < n; base += EVICT_THREADS) {
+  const auto put = [&](bool moves, int i, bool hole, int j, int slot) {
+    if (moves && i < a.most) from[i] = slot;
+    if (hole && j < a.most) to[j] = slot;
+    if (moves && i < MOVED_HERE) near[0][i] = slot;
+    if (hole && j < MOVED_HERE) near[1][j] = slot;
+  };
+  int sources = 0, holes = 0, done = 0;
+  if (all) {  // every rank that begins with prefix stays: the order of the kept slots in two steps
+    uint64_t moving[KEPT], leaving[KEPT];
+#pragma unroll
+    for (int j = 0; j < KEPT; ++j) {
+      const int slot = j * EVICT_THREADS + threadIdx.x;
+      const bool stays = slot < n && (rank[j] & mask) >= prefix;
+      moving[j] = __builtin_amdgcn_ballot_w64(stays && slot >= budget);
+      leaving[j] = __builtin_amdgcn_ballot_w64(!stays && slot < budget);
+      if (lane == 0) {
+        votes[0][j * EVICT_WAVES + wave] = __popcll(moving[j]);
+        votes[1][j * EVICT_WAVES + wave] = __popcll(leaving[j]);
+      }
+    }
+    __syncthreads();
+    if (wave < 2) {  // sums of all before, four entries a lane
+      static_assert(KEPT * EVICT_WAVES == 4 * WAVE, "four entries a lane");
+      int v[4], sum = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum += v[k] = votes[wave][lane * 4 + k];
+      int up = sum;
+#pragma unroll
+      for (int o = 1; o < WAVE; o *= 2) {
+        const int x = __shfl_up(up, o);
+        up += lane >= o ? x : 0;
+      }
+      if (lane == WAVE - 1) chosen[wave] = up;
+      up -= sum;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        votes[wave][lane * 4 + k] = up;
+        up += v[k];
+      }
+    }
+    __syncthreads();
+    const uint64_t earlier = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+    for (int j = 0; j < KEPT; ++j)
+      put(moving[j] >> lane & 1, votes[0][j * EVICT_WAVES + wave] + __popcll(moving[j] & earlier), leaving[j] >> lane & 1,
+          votes[1][j * EVICT_WAVES + wave] + __popcll(leaving[j] & earlier), j * EVICT_THREADS + threadIdx.x);
+    sources = chosen[0], holes = chosen[1], done = KEPT * EVICT_THREADS;
+  }
+  int equal = 0;
+  for (int base = done; base < n; base += EVICT_THREADS) {
     const int slot = base + threadIdx.x;
     const uint64_t r = slot < n ? rank_of(p, b, head, slot, newest, budget) & mask : 0;
     bool stays = slot < n && r >= prefix;
@@ -133,22 +279,48 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_paged_evict(Evict a) {
     sources += more;
     const int j = holes + before(hole, sums, more);
     holes += more;
-    if (moves && i < a.most) from[i] = slot;
-    if (hole && j < a.most) to[j] = slot;
+    put(moves, i, hole, j, slot);
   }
   __syncthreads();
   const int count = (int)min((int64_t)min(sources, holes), a.most);
-  for (int i = threadIdx.x / WAVE; i < count; i += EVICT_WAVES) move_key<T, D>(p, b, head, from[i], to[i]);
+  const bool here = count <= MOVED_HERE;
+  if (threadIdx.x == 0) a.counts[list] = here ? 0 : count;
+  if (here) {
+    constexpr int EACH = MOVED_HERE / EVICT_WAVES;
+    const int i = wave * EACH;
+    if (i < count) move_keys<T, D>(p, b, head, near[0] + i, near[1] + i, min(EACH, count - i));
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(MOVE_WAVES* WAVE) void k_paged_move(Evict a, int lists) {
+  const int list = blockIdx.x % lists, i = ((int)(blockIdx.x / lists) * MOVE_WAVES + threadIdx.x / WAVE) * MOVE_EACH;
+  const int n = min(a.counts[list] - i, MOVE_EACH);
+  if (n <= 0) return;
+  const int32_t* const from = a.lists + (int64_t)list * 2 * a.most + i;
+  move_keys<T, D>(a.p, list / a.p.kv_heads, list % a.p.kv_heads, from, from + a.most, n);
 }
 
 int64_t list_of(const lram_paged& p, int64_t budget) {
   return std::max<int64_t>(0, std::min(budget, p.width * p.page - budget));
 }
 
+// Workgroups of the second kernel.
+int64_t groups_of(const lram_paged& p, int64_t budget) {
+  const int64_t most = list_of(p, budget), each = MOVE_WAVES * MOVE_EACH;
+  return most <= MOVED_HERE ? 0 : (int64_t)p.batch * p.kv_heads * ((most + each - 1) / each);
+}
+
+size_t workspace_of(const lram_paged& p, int64_t budget) {
+  const int64_t most = list_of(p, budget), lists = (int64_t)p.batch * p.kv_heads;
+  return most ? (size_t)(lists * (2 * most + 1)) * sizeof(int32_t) : 0;
+}
+
 int check_evict(const lram_paged& p, int64_t budget, int64_t recent) {
   if (int rc = check_pool(p, false)) return rc;
   if (budget < 1 || recent < 0 || recent > budget || (p.pages && !p.weight)) return LRAM_EINVAL;
   if ((int64_t)p.batch * p.kv_heads > ((int64_t)1 << 32) / EVICT_THREADS - 1) return LRAM_EINVAL;
+  if (groups_of(p, budget) > ((int64_t)1 << 32) / (MOVE_WAVES * WAVE) - 1) return LRAM_EINVAL;
   return LRAM_OK;
 }
 
@@ -159,7 +331,7 @@ extern "C" {
 int lram_paged_evict_workspace_bytes(const lram_paged* p, int64_t budget, size_t* bytes) {
   if (!p || !bytes) return LRAM_EINVAL;
   if (int rc = check_evict(*p, budget, 0)) return rc;
-  *bytes = (size_t)p->batch * p->kv_heads * 2 * list_of(*p, budget) * sizeof(int32_t);
+  *bytes = workspace_of(*p, budget);
   return LRAM_OK;
 }
 
@@ -170,14 +342,23 @@ int lram_paged_evict(const lram_paged* p, int64_t budget, int64_t recent, void* 
   a.p = pool_of(*p);
   a.budget = budget, a.recent = recent, a.most = list_of(*p, budget);
   if (p->batch == 0 || a.most == 0) return LRAM_OK;  // nothing can be over the budget
-  const size_t need = (size_t)p->batch * p->kv_heads * 2 * a.most * sizeof(int32_t);
+  const size_t need = workspace_of(*p, budget);
   if (!workspace || off_align(workspace, 16) || ws_bytes < need) return LRAM_EWORKSPACE;
+  const int lists = p->batch * p->kv_heads;
   a.lists = (int32_t*)workspace;
-  const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p->batch * p->kv_heads)), dim3(EVICT_THREADS), 0, (hipStream_t)stream, a);
-    return layer_launched();
-  };
-  return by_form(p->dtype, p->head_dim, [&](auto t, auto d) { return go(k_paged_evict<decltype(t), decltype(d)::value>); });
+  a.counts = a.lists + (int64_t)lists * 2 * a.most;
+  const int64_t groups = groups_of(*p, budget);
+  return by_form(p->dtype, p->head_dim, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    hipLaunchKernelGGL((k_paged_evict<T, D>), dim3((unsigned)lists), dim3(EVICT_THREADS), 0, (hipStream_t)stream, a);
+    int rc = layer_launched();
+    if (rc == LRAM_OK && groups) {
+      hipLaunchKernelGGL((k_paged_move<T, D>), dim3((unsigned)groups), dim3(MOVE_WAVES * WAVE), 0, (hipStream_t)stream, a, lists);
+      rc = layer_launched();
+    }
+    return rc;
+  });
 }
 
 }  // extern "C"

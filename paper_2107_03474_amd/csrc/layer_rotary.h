@@ -38,17 +38,6 @@ inline Form form_of(const lram_rotary& r, int dtype) {
   return r.interleaved ? NEIGHBOURS : r.pairs % (16 / (int)elem_size(dtype)) == 0 ? HALVES : ODD_HALVES;
 }
 
-// 16 bytes of elements as one value, so that they are moved by one instruction; `loose` where they start on any element.
-template <typename T>
-struct Chunk {
-  static constexpr int E = 16 / (int)sizeof(T);
-  typedef T type __attribute__((ext_vector_type(E)));
-  typedef T loose __attribute__((ext_vector_type(E), aligned(sizeof(T))));
-  typedef float wide __attribute__((ext_vector_type(E)));
-  static __device__ __forceinline__ wide up(type x) { return __builtin_convertvector(x, wide); }
-  static __device__ __forceinline__ type down(wide x) { return __builtin_convertvector(x, type); }
-};
-
 inline int check_rotary(const lram_rotary& r, int64_t head_dim) {
   if (r.pairs < 1 || 2 * (int64_t)r.pairs > head_dim || (r.interleaved & ~1) || !(r.magnitude - r.magnitude == 0))
     return LRAM_EINVAL;

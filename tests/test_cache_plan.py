@@ -155,10 +155,10 @@ def test_evict_refuses(lib):
     for budget, recent in ((0, 0), (-1, 0), (10, 11), (10, -1)):
         assert lib.lram_paged_evict(_pool(), budget, recent, P, 1 << 40, None) == EINVAL
     assert lib.lram_paged_evict(_pool(weight=None), 100, 10, P, 1 << 40, None) == EINVAL
-    assert lib.lram_paged_evict_workspace_bytes(_pool(), 100, n) == 0 and n.value == 2 * 4 * 2 * 100 * 4
+    assert lib.lram_paged_evict_workspace_bytes(_pool(), 100, n) == 0 and n.value == 2 * 4 * (2 * 100 + 1) * 4
     for bad in ((None, 1 << 40), (P + 4, 1 << 40), (P, n.value - 1)):
         assert lib.lram_paged_evict(_pool(), 100, 10, *bad, None) == EWORKSPACE, bad
-    assert lib.lram_paged_evict_workspace_bytes(_pool(), 2550, n) == 0 and n.value == 2 * 4 * 2 * 10 * 4  # 40 pages hold 2560
+    assert lib.lram_paged_evict_workspace_bytes(_pool(), 2550, n) == 0 and n.value == 2 * 4 * (2 * 10 + 1) * 4  # 40 pages hold 2560
     assert lib.lram_paged_evict(_pool(), 2560, 10, None, 0, None) == 0  # nothing can be over the budget
     assert lib.lram_paged_evict(_pool(), 1 << 60, 10, None, 0, None) == 0
     assert lib.lram_paged_evict(_pool(batch=0), 100, 10, None, 0, None) == 0

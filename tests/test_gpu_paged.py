@@ -338,6 +338,8 @@ EVICT = [
     ([500, 129, 1], [700, 200, 1], 1, 1, 3, 64, 32, F32),
     ([1500], [100000], 700, 700, 2, 64, 256, F32),
     ([5000, 1025], [5000, 1025], 513, 100, 2, 32, 128, BF16),
+    ([20000, 16390], [50000, 16390], 16385, 100, 1, 32, 256, F32),
+    ([17500, 70], [17500, 70], 64, 64, 1, 64, 256, BF16),
 ]
 
 
