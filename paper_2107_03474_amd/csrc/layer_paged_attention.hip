@@ -43,7 +43,6 @@ struct Attend {
   int tiles, pieces, piece;  // workgroups along a sequence's columns, along its keys, and keys of one of these
   float* part;               // [piece][row][head][dim]
   float2* stat;              // [piece][row][head]: maximum and sum
-  float2* whole;             // [row][head]: maximum and 1 / sum (weighing)
   float* scores;             // [sequence][kv_head][score_cols][scored]: of few columns, kept for the weights; null: none are
   int score_cols;
   int64_t scored;
@@ -314,7 +313,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, 2) void k_paged_attention(Attend a)
           const float inv = sum == 0 ? 0.0f : 1.0f / sum;
           const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
           store_n<T, 4>((T*)a.out + place * D + d, y);
-          if (a.whole && d == 0) a.whole[place] = {top, inv};
+          if (a.stat && d == 0) a.stat[place] = {top, sum};
         } else {
           const int64_t to = (int64_t)piece * p.rows * p.heads + place;
           *(f32x4*)(a.part + to * D + d) = x;
@@ -326,19 +325,23 @@ __global__ __launch_bounds__(ATTEND_THREADS, 2) void k_paged_attention(Attend a)
   }
 }
 
+// Pieces that hold a part of a sequence's results; 1: the results themselves are there.
+__device__ __forceinline__ int pieces_of(const Attend& a, const CacheSeq& s) {
+  return (int)max(min(((int64_t)s.nk + a.piece - 1) / a.piece, (int64_t)a.pieces), (int64_t)1);
+}
+
 // The pieces' parts of a query and head joined.
 template <typename T, int D>
-__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_join(Attend a, int rows_each) {
+__device__ __forceinline__ void join_rows(const Attend& a, int64_t id, int rows_each) {
   constexpr int LANES = D / 4, TEAMS = ATTEND_THREADS / LANES;
   __shared__ float tops[ATTEND_WAVES];
   __shared__ __align__(16) float parts[TEAMS][D];
   __shared__ float sums[TEAMS];
   const Pool& p = a.p;
-  const int h = (int)(blockIdx.x % p.heads), b = (int)(blockIdx.x / p.heads % p.batch);
-  const int first = (int)(blockIdx.x / p.heads / p.batch);
+  const int h = (int)(id % p.heads), b = (int)(id / p.heads % p.batch), first = (int)(id / p.heads / p.batch);
   const CacheSeq s = cache_seq(p, b);
-  if (s.nk <= a.piece) return;
-  const int pieces = (int)min(((int64_t)s.nk + a.piece - 1) / a.piece, (int64_t)a.pieces);
+  const int pieces = pieces_of(a, s);
+  if (pieces == 1) return;
   const int team = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
   const int64_t step = p.rows * p.heads;
   for (int i = first; i < s.nq; i += rows_each) {
@@ -371,49 +374,82 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_join(Attend a, int row
       const float inv = sum == 0 ? 0.0f : 1.0f / sum;
       const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
       store_n<T, 4>((T*)a.out + place * D + d, y);
-      if (a.whole && d == 0) a.whole[place] = {top, inv};
     }
     __syncthreads();
   }
 }
 
-// The weight that each key gathers, in a fixed order.  Of a single token's few columns the scores were kept (16 bytes a key for
-// four heads that share it, beside the 256 of its k); a thread then takes a key.  Otherwise a wave keeps a block of keys and
-// forms their scores again, over all of the sequence's queries.
-constexpr int WEIGH_CHUNK = ATTEND_THREADS;  // keys of a workgroup
+template <typename T, int D>
+__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_join(Attend a, int rows_each) {
+  join_rows<T, D>(a, blockIdx.x, rows_each);
+}
+
+// The maximum and 1 / sum of a row and head, by the `step` neighbouring lanes that share it (a power of 2; first: this one's).
+__device__ __forceinline__ float2 whole_of(const Attend& a, int64_t place, int pieces, int first, int step) {
+  const int64_t all = a.p.rows * a.p.heads;
+  float top = -INFINITY, sum = 0;
+  for (int n = first; n < pieces; n += step) top = fmaxf(top, a.stat[n * all + place].x);
+  for (int o = 1; o < step; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+  for (int n = first; n < pieces; n += step) {
+    const float2 st = a.stat[n * all + place];
+    sum += st.x == -INFINITY ? st.y : st.y * __builtin_amdgcn_exp2f(st.x - top);
+  }
+  for (int o = 1; o < step; o *= 2) sum += __shfl_xor(sum, o);
+  return {top, sum == 0 ? 0.0f : 1.0f / sum};
+}
+
+// The weight that each key gathers, in a fixed order, beside the join.  Of a single token's few columns the scores were kept (16
+// bytes a key for four heads that share it, beside the 256 of its k); a thread then takes four keys.  Otherwise a wave keeps
+// a block of keys and forms their scores again, over all of the sequence's queries.
+constexpr int WEIGH_CHUNK = 4 * ATTEND_THREADS;  // keys of a workgroup
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int chunks, int chunk) {
+__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int joins, int rows_each, int chunks, int chunk) {
   using Ti = PageTile<T>;
   using Op = typename Operand<T>::type;
   constexpr int F = Ti::F, KEYS = Ti::KEYS;
   __shared__ float bias[BIAS ? BIAS_MOST / 2 : 1];
   __shared__ float2 whole[16];
+  if (blockIdx.x < (unsigned)joins) {
+    join_rows<T, D>(a, blockIdx.x, rows_each);
+    return;
+  }
   const Pool& p = a.p;
   const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int head = (int)(blockIdx.x % p.kv_heads), b = (int)(blockIdx.x / p.kv_heads % p.batch);
-  const int64_t first = blockIdx.x / p.kv_heads / p.batch;
+  const unsigned id = blockIdx.x - joins;
+  const int head = (int)(id % p.kv_heads), b = (int)(id / p.kv_heads % p.batch);
+  const int64_t first = id / p.kv_heads / p.batch;
   const CacheSeq s = cache_seq(p, b);
   if (s.nq == 0 || first * chunk >= s.nk) return;
+  const int pieces = pieces_of(a, s);
   if (keeps_scores(a, s)) {
-    const int cols = s.nq * p.group;
-    if ((int)threadIdx.x < cols)
-      whole[threadIdx.x] = a.whole[(s.q0 + threadIdx.x / p.group) * p.heads + head * p.group + threadIdx.x % p.group];
+    const int cols = s.nq * p.group, mine = threadIdx.x / 16;
+    if (mine < cols) {
+      const int64_t place = (s.q0 + mine / p.group) * p.heads + head * p.group + mine % p.group;
+      const float2 st = whole_of(a, place, pieces, threadIdx.x % 16, 16);
+      if (threadIdx.x % 16 == 0) whole[mine] = st;
+    }
     __syncthreads();
     for (int64_t base = first * chunk; base < s.nk; base += (int64_t)chunks * chunk) {
       const int end = (int)min(base + chunk, (int64_t)s.nk);
-      for (int slot = (int)base + threadIdx.x; slot < end; slot += ATTEND_THREADS) {
+      for (int slot = (int)base + 4 * threadIdx.x; slot < end; slot += 4 * ATTEND_THREADS) {
         const int page = page_of(p, b, slot);
         if (page < 0) continue;
         const float* const z = a.scores + (int64_t)(b * p.kv_heads + head) * a.score_cols * a.scored + slot;
-        float* const w = p.weight + page_rows(p, page, head) + (slot & (p.page - 1));
-        const float had = *w;
-        float got = 0;
+        f32x4* const w = (f32x4*)(p.weight + page_rows(p, page, head) + (slot & (p.page - 1)));
+        const f32x4 had = *w;
+        f32x4 got = {0, 0, 0, 0};
 #pragma unroll 8
         for (int c = 0; c < cols; ++c) {
-          const float x = z[c * a.scored];
-          got += x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x - whole[c].x) * whole[c].y;
+          const f32x4 x = *(const f32x4*)(z + c * a.scored);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            got[r] += x[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x[r] - whole[c].x) * whole[c].y;
         }
-        *w = had + got;
+        if (slot + 4 <= s.nk) {
+          *w = had + got;
+        } else {
+          for (int r = 0; slot + r < s.nk; ++r) ((float*)w)[r] = had[r] + got[r];
+        }
       }
     }
     return;
@@ -436,7 +472,8 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int ch
       for (int64_t n = 0; n < (int64_t)s.nq * p.group; n += 16) {
         Column<T, D> col;
         col.load(a, s, head, n + lane % 16);
-        const float2 st = col.row < 0 ? float2{0, 0} : a.whole[col.row * p.heads + head * p.group + col.head];
+        const float2 st = col.row < 0 ? float2{0, 0}
+                                     : whole_of(a, col.row * p.heads + head * p.group + col.head, pieces, 0, 1);
         f32x4 z[F];
         scores<T, D, BIAS>(a, col, k, at, left, bias, z);
 #pragma unroll
@@ -472,8 +509,8 @@ struct Plan {
   int ct;
   int64_t tiles, pieces, piece;
   int64_t cols, scored;              // of kept scores; 0: none
-  size_t part, scores, stat, whole;  // bytes
-  size_t all() const { return part + scores + stat + whole; }
+  size_t part, scores, stat;  // bytes
+  size_t all() const { return part + scores + stat; }
 };
 
 // Pieces: a round of two workgroups a unit for a single sequence, and up to four rounds for several, which are rarely of one
@@ -497,11 +534,8 @@ Plan plan_of(const lram_paged& p, bool weigh) {
   x.piece = std::max(x.piece, PIECE_LEAST);
   x.pieces = over(keys, x.piece);
   const size_t places = (size_t)p.rows * p.heads;
-  if (x.pieces > 1) {
-    x.part = (size_t)x.pieces * places * p.head_dim * sizeof(float);
-    x.stat = (size_t)x.pieces * places * sizeof(float2);
-  }
-  if (weigh) x.whole = places * sizeof(float2);
+  if (x.pieces > 1) x.part = (size_t)x.pieces * places * p.head_dim * sizeof(float);
+  if (x.pieces > 1 || weigh) x.stat = (size_t)x.pieces * places * sizeof(float2);
   if (weigh && tokens * G <= 16) {
     x.cols = tokens * G;
     x.scored = x.pieces * x.piece;
@@ -515,7 +549,7 @@ int check_queries(const lram_paged& p, const lram_paged_queries& a) {
   const int64_t G = p.heads / p.kv_heads;
   if (!(a.scale > 0) || !(a.scale < INFINITY) || (a.weigh & ~1) || (a.weigh && p.pages && !p.weight)) return LRAM_EINVAL;
   if (bad_strides(a.q_row, a.q_head, p.heads, p.head_dim, p.dtype)) return LRAM_EINVAL;
-  if ((int64_t)p.batch * p.heads > MOST_GROUPS) return LRAM_EINVAL;
+  if ((int64_t)p.batch * p.heads > MOST_GROUPS / 2) return LRAM_EINVAL;
   if (a.rel_weight) {
     if (a.wdtype != LRAM_F32 && !(a.wdtype == LRAM_BF16 && p.dtype == LRAM_BF16)) return LRAM_EDTYPE;
     if (!a.rel_bucket || a.rel_buckets < 1 || a.rel_buckets > 256 || a.rel_reach < 0 || a.rel_reach > BIAS_MOST ||
@@ -555,9 +589,9 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void*
   a.rel_bf16 = q->wdtype == LRAM_BF16;
   a.tiles = (int)x.tiles, a.pieces = (int)x.pieces, a.piece = (int)x.piece;
   char* const ws = (char*)workspace;
-  if (x.part) a.part = (float*)ws, a.stat = (float2*)(ws + x.part + x.scores);
+  if (x.part) a.part = (float*)ws;
   if (x.scores) a.scores = (float*)(ws + x.part), a.score_cols = (int)x.cols, a.scored = x.scored;
-  if (x.whole) a.whole = (float2*)(ws + x.part + x.scores + x.stat);
+  if (x.stat) a.stat = (float2*)(ws + x.part + x.scores);
   if (p->batch == 0 || p->pages == 0) {
     const int64_t n = p->rows * p->heads * p->head_dim;
     const dim3 grid((unsigned)std::min<int64_t>(over(n, ATTEND_THREADS), 4096));
@@ -578,18 +612,16 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void*
     int rc = q->rel_weight ? x.ct == 1 ? go(k_paged_attention<T, D, 1, true>, groups) : go(k_paged_attention<T, D, 2, true>, groups)
              : x.ct == 1   ? go(k_paged_attention<T, D, 1, false>, groups)
                            : go(k_paged_attention<T, D, 2, false>, groups);
-    if (rc == LRAM_OK && x.part) {
-      const int64_t all = (int64_t)p->batch * p->heads;
-      const int64_t each = std::max<int64_t>(1, std::min({p->max_q, p->rows, MOST_GROUPS / all}));
-      rc = go(k_paged_join<T, D>, all * each, (int)each);
-    }
-    if (rc == LRAM_OK && q->weigh) {
-      const int64_t keys = std::max<int64_t>(1, std::min(p->max_k, p->width * p->page));
-      const int64_t chunk = x.scores ? WEIGH_CHUNK : ATTEND_WAVES * PageTile<T>::KEYS;
-      const int64_t chunks = std::max<int64_t>(1, std::min(over(keys, chunk), MOST_GROUPS / lists));
-      rc = q->rel_weight ? go(k_paged_weigh<T, D, true>, lists * chunks, (int)chunks, (int)chunk)
-                         : go(k_paged_weigh<T, D, false>, lists * chunks, (int)chunks, (int)chunk);
-    }
+    if (rc != LRAM_OK || (!x.part && !q->weigh)) return rc;
+    const int64_t all = (int64_t)p->batch * p->heads;
+    const int64_t each = std::max<int64_t>(1, std::min({p->max_q, p->rows, MOST_GROUPS / 2 / all}));
+    const int64_t joins = x.part ? all * each : 0;
+    if (!q->weigh) return go(k_paged_join<T, D>, joins, (int)each);
+    const int64_t keys = std::max<int64_t>(1, std::min(p->max_k, p->width * p->page));
+    const int64_t chunk = x.scores ? WEIGH_CHUNK : ATTEND_WAVES * PageTile<T>::KEYS;
+    const int64_t chunks = std::max<int64_t>(1, std::min(over(keys, chunk), (MOST_GROUPS - joins) / lists));
+    rc = q->rel_weight ? go(k_paged_weigh<T, D, true>, joins + lists * chunks, (int)joins, (int)each, (int)chunks, (int)chunk)
+                       : go(k_paged_weigh<T, D, false>, joins + lists * chunks, (int)joins, (int)each, (int)chunks, (int)chunk);
     return rc;
   });
 }
