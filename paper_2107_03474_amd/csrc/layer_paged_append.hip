@@ -3,7 +3,8 @@
 // One launch.  q: rows rotated as they lie (rotate_chunk).  k: a wave takes the rows of 16 key slots of a sequence and some of
 // their heads; a lane owns pairs of 16-byte chunks of single rows and forms their sines and cosines once for all of these
 // heads.  v: a wave takes 32 key slots; a lane takes 16 bytes of each of the 4 F keys that lie side by side in the page and
-// turns them round in its registers.  Nothing goes through LDS.  Bound by HBM for prompts, by its launch for single tokens.
+// turns them round in its registers, and a whole block goes out by way of LDS.  Bound by HBM for prompts, by its launch for
+// single tokens.
 
 #include "layer_paged.h"
 #include "layer_rotary.h"
@@ -147,45 +148,57 @@ __device__ __forceinline__ void turn_head(const Append& a, const Units<T, D, FOR
   }
 }
 
-// One head of values into a page's block.
+// One head of values into a page's block.  In bf16 a whole block goes by way of `lds` (32 rows of the wave's own): a lane's
+// 16-byte results lie 128 bytes from the next one's, and go out side by side (28,654 rows of 32/8 heads of 128: 179 -> 146
+// us).  In fp32 a lane has 64 bytes in one piece.
 template <typename T, int D>
-__device__ __forceinline__ void turn_values(const Tile& tile, const T* x, int64_t stride, T* y) {
+__device__ __forceinline__ void turn_values(const Tile& tile, const T* x, int64_t stride, T* y, typename Chunk<T>::type* lds) {
   using Ti = PageTile<T>;
-  constexpr int E = Ti::E, CH = D / E;
+  constexpr int E = Ti::E, CH = D / E, ITEMS = PAGE_BLOCK * D / (E * E), N = (ITEMS + WAVE - 1) / WAVE;
   const int lane = threadIdx.x % WAVE;
+  const bool all = E == 8 && tile.from == 0 && tile.to == PAGE_BLOCK;
+  // chunk i of the block, 16 bytes each, spread over the banks
+  const auto spread = [](int i) { return i ^ (i >> 3 & 7); };
 #pragma unroll
-  for (int n = 0; n < PAGE_BLOCK * D / (E * E) / WAVE + (PAGE_BLOCK * D / (E * E) < WAVE); ++n) {
+  for (int n = 0; n < N; ++n) {
     const int i = lane + n * WAVE, c = i % CH, g = i / CH % 4, t1 = i / (4 * CH) * Ti::KEYS + 4 * g;
     if (t1 >= PAGE_BLOCK) break;
     typename Chunk<T>::type in[E];
-    bool whole = true, some = false;
+    bool some = false, whole = true;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int t = t1 + e / 4 * 16 + e % 4;
       const bool mine = t >= tile.from && t < tile.to;
-      whole = whole && mine;
       some = some || mine;
+      whole = whole && mine;
       if (mine) in[e] = *(const typename Chunk<T>::type*)(x + (tile.at + t) * stride + c * E);
     }
     if (!some) continue;
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      const int d = c * E + j;
-      T* const to = y + ((t1 / Ti::KEYS * (D / 16) + d / 16) * 64 + g * 16 + d % 16) * E;
-      if (whole) {
-        typename Chunk<T>::type o;
+      const int d = c * E + j, place = (t1 / Ti::KEYS * (D / 16) + d / 16) * 64 + g * 16 + d % 16;
+      typename Chunk<T>::type o;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = in[e][j];
-        *(typename Chunk<T>::type*)to = o;
+      for (int e = 0; e < E; ++e) o[e] = in[e][j];
+      if (all) {
+        lds[spread(place)] = o;
+      } else if (whole) {
+        *(typename Chunk<T>::type*)(y + place * E) = o;
       } else {
+        T* const to = y + place * E;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const int t = t1 + e / 4 * 16 + e % 4;
-          if (t >= tile.from && t < tile.to) to[e] = in[e][j];
+          if (t >= tile.from && t < tile.to) to[e] = o[e];
         }
       }
     }
   }
+  if constexpr (E != 8) return;
+  if (!all) return;
+#pragma unroll
+  for (int n = 0; n < PAGE_BLOCK * CH / WAVE; ++n)
+    *(typename Chunk<T>::type*)(y + (lane + n * WAVE) * E) = lds[spread(lane + n * WAVE)];
 }
 
 // Where the tiles of SLOTS slots lie.  Sequence b has the places from start[b] / SLOTS + 2 b on, as many as its n rows can
@@ -254,6 +267,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(Append a) {
       return;
     }
   }
+  __shared__ typename Chunk<T>::type lds[APPEND_WAVES][Chunk<T>::E == 8 ? PAGE_BLOCK * D / 8 : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
   int64_t id = (blockIdx.x - a.q_groups) * APPEND_WAVES + wave;
   const bool of_v = id >= a.waves;
@@ -269,7 +283,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(Append a) {
     if (tile.from >= tile.to) return;
     for (int head = head0; head < head1; ++head) {
       const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
-      turn_values<T, D>(tile, (const T*)a.v + head * a.v_head, a.v_row, (T*)p.v + keys * D);
+      turn_values<T, D>(tile, (const T*)a.v + head * a.v_head, a.v_row, (T*)p.v + keys * D, lds[wave]);
     }
     return;
   }
