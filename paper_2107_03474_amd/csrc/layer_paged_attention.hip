@@ -516,7 +516,12 @@ struct Plan {
 // Pieces: a round of two workgroups a unit for a single sequence, and up to four rounds for several, which are rarely of one
 // length (us of one round / four: one token over 131,072 keys, 32/8 heads of 128 bf16 with weights, 123 / 130; 32 tokens over
 // 256 to 8,192 keys 107 / 97).
+// Few keys take one piece, which needs no join (us of a call / of its kernels, one piece and pieces of 256: one token over 777
+// keys, 8 heads of 64 bf16, 15.9 / 8.3 and 19.9 / 9.0; four over 300, 32/8 heads of 128, 13.9 / 7.4 and 17.8 / 9.7, with
+// weights 17.9 / 12.1 and 18.0 / 11.0; over 777 of these 13.9 / 12.0 and 17.8 / 10.3).  Results are the same with weights
+// and without.
 constexpr int64_t PIECE_STEP = 128, PIECE_LEAST = 256, ROUND = 512, ROUNDS = 4;
+constexpr int64_t FEW_BYTES = 256 << 10;  // of a sequence's keys and values of a head
 constexpr int64_t MOST_GROUPS = ((int64_t)1 << 32) / ATTEND_THREADS - 1;
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -532,6 +537,7 @@ Plan plan_of(const lram_paged& p, bool weigh) {
   const int64_t wanted = std::min(over(ROUND * std::min<int64_t>(std::max(p.batch, 1), ROUNDS), lists * x.tiles), MOST_GROUPS / (lists * x.tiles));
   x.piece = over(over(keys, std::max<int64_t>(1, wanted)), PIECE_STEP) * PIECE_STEP;
   x.piece = std::max(x.piece, PIECE_LEAST);
+  if (keys * p.head_dim * 2 * (int64_t)elem_size(p.dtype) <= FEW_BYTES) x.piece = over(keys, PIECE_STEP) * PIECE_STEP;
   x.pieces = over(keys, x.piece);
   const size_t places = (size_t)p.rows * p.heads;
   if (x.pieces > 1) x.part = (size_t)x.pieces * places * p.head_dim * sizeof(float);

@@ -99,6 +99,13 @@ def page_table(batch: int, width: int, device="cuda") -> PageTable:
     return PageTable(torch.full((batch, width), -1, **i32), torch.zeros(batch, **i32), torch.zeros(batch, **i32))
 
 
+def _at(t: torch.Tensor, name: str, dtype: torch.dtype, shape, like: torch.Tensor, index: int) -> int:
+    """Device address of a contiguous tensor of this type and shape on like's device, whose index this is."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+        return t.data_ptr()
+    return _ptr(t, name, dtype, shape, like)  # says what is wrong
+
+
 def _describe(keys: PagedKeys, table: PageTable, heads: int = 0, rows: int = 0, seqs: Optional[Packed] = None) -> _Paged:
     k, v, position, weight = keys
     if k.dim() != 6 or position.dim() != 3:
@@ -113,16 +120,17 @@ def _describe(keys: PagedKeys, table: PageTable, heads: int = 0, rows: int = 0, 
         raise LramError("table must be [batch, width], used and seen [batch]")
     width, i32 = table.table.shape[1], torch.int32
     a = _Paged(_type(k, "k"), heads or kv, kv, dim, batch, page, pages, width)
-    a.k = _ptr(k, "k", k.dtype, (pages, kv, page // 16, dim // e, 16, e), k)
-    a.v = _ptr(v, "v", k.dtype, (pages, kv, page // (4 * e), dim // 16, 4, 16, e), k)
-    a.position = _ptr(position, "position", i32, (pages, kv, page), k)
+    on = k.get_device()
+    a.k = _at(k, "k", k.dtype, (pages, kv, page // 16, dim // e, 16, e), k, on)
+    a.v = _at(v, "v", k.dtype, (pages, kv, page // (4 * e), dim // 16, 4, 16, e), k, on)
+    a.position = _at(position, "position", i32, (pages, kv, page), k, on)
     if weight is not None:
-        a.weight = _ptr(weight, "weight", torch.float32, (pages, kv, page), k)
-    a.table = _ptr(table.table, "table", i32, (batch, width), k)
-    a.used = _ptr(table.used, "used", i32, (batch,), k)
-    a.seen = _ptr(table.seen, "seen", i32, (batch,), k)
+        a.weight = _at(weight, "weight", torch.float32, (pages, kv, page), k, on)
+    a.table = _at(table.table, "table", i32, (batch, width), k, on)
+    a.used = _at(table.used, "used", i32, (batch,), k, on)
+    a.seen = _at(table.seen, "seen", i32, (batch,), k, on)
     if seqs is not None:
-        a.start = _ptr(seqs.start_q, "start_q", i32, (batch + 1,), k)
+        a.start = _at(seqs.start_q, "start_q", i32, (batch + 1,), k, on)
         a.rows, a.max_q, a.max_k = rows, seqs.max_q, seqs.max_k
     return a
 
