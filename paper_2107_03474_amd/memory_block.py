@@ -3,19 +3,21 @@ dense feed-forward part of one layer of a BERT-style model).
 
     a = attention(x);  x = norm(x + a);  x = norm(x + memory(x))
 
-over packed sequences of different lengths, in both directions or causal, with a learned relative position bias.  The
-attention, its bias, the norms with their residual adds and the lookup run in liblram's kernels; the projections are
-library GEMMs.
+over packed sequences of different lengths, in both directions or causal, with a learned relative position bias or rotary
+positions.  The attention, its bias, the rotation, the caches' pages, the norms with their residual adds and the lookup run in
+liblram's kernels; the projections are library GEMMs.
 """
 from __future__ import annotations
 
-from typing import Optional, Sequence
+from typing import Optional, Sequence, Union
 
 import torch
 
 from .layer import (HEAD_DIMS, Packed, RelativeBias, attention, attention_forward, bias_refusal, layer_norm,
                     relative_buckets)
 from .memory_layer import MemorySubnetwork
+from .paged import PagedCache, paged_append, paged_attention
+from .positions import Rotary, packed_positions, rotary as rotate, rotary_forward
 
 
 class KeyValueCache:
@@ -69,24 +71,33 @@ class KeyValueCache:
 
 
 class MemoryBlock(torch.nn.Module):
+    """rotary: positions by rotation (of the plan's pairs of every head) in place of the learned bias."""
+
     def __init__(self, w: int, heads: int, K: Sequence[int], kv_heads: Optional[int] = None, causal: bool = False,
                  buckets: int = 32, reach: int = 128, eps: float = 1e-5, table_dtype=torch.bfloat16,
-                 dtype=torch.float32, device="cuda", memory: Optional[MemorySubnetwork] = None):
+                 dtype=torch.float32, device="cuda", memory: Optional[MemorySubnetwork] = None, rotary: Optional[Rotary] = None):
         super().__init__()
         kv_heads = heads if kv_heads is None else kv_heads
         if w % heads or heads % kv_heads:
             raise ValueError("w must be a multiple of heads, and heads of kv_heads")
         if w // heads not in HEAD_DIMS:
             raise ValueError("w / heads must be 32, 64 or 128")
-        refusal = bias_refusal(heads, kv_heads, w // heads, dtype, buckets, reach)
+        refusal = bias_refusal(heads, kv_heads, w // heads, dtype, buckets, reach) if rotary is None else None
         if refusal:
             raise ValueError(refusal)
+        if rotary is not None and not 1 <= rotary.turns.numel() <= w // heads // 2:
+            raise ValueError("a rotation has 1 to head_dim / 2 pairs")
         self.heads, self.kv_heads, self.head_dim, self.causal, self.eps = heads, kv_heads, w // heads, causal, eps
         new = dict(device=device, dtype=dtype)
         self.qkv = torch.nn.Linear(w, (heads + 2 * kv_heads) * self.head_dim, **new)
         self.proj = torch.nn.Linear(w, w, **new)
-        self.bias = torch.nn.Parameter(torch.zeros((heads, buckets), **new))
-        self.register_buffer("bucket", relative_buckets(buckets, reach, both=not causal, device=device))
+        self.rotates = rotary is not None
+        if rotary is not None:
+            self.register_buffer("turns", rotary.turns.to(device))
+            self.interleaved, self.magnitude = rotary.interleaved, rotary.magnitude
+        else:
+            self.bias = torch.nn.Parameter(torch.zeros((heads, buckets), **new))
+            self.register_buffer("bucket", relative_buckets(buckets, reach, both=not causal, device=device))
         self.norm_w = torch.nn.ParameterList([torch.ones(w, **new) for _ in range(2)])
         self.norm_b = torch.nn.ParameterList([torch.zeros(w, **new) for _ in range(2)])
         self.memory = memory if memory is not None else MemorySubnetwork(w, K, table_dtype, dtype, device=device)
@@ -97,23 +108,40 @@ class MemoryBlock(torch.nn.Module):
         return (x[:, :a].unflatten(1, (self.heads, self.head_dim)), x[:, a:b].unflatten(1, (self.kv_heads, self.head_dim)),
                 x[:, b:].unflatten(1, (self.kv_heads, self.head_dim)))
 
-    def forward(self, x: torch.Tensor, seqs: Packed) -> torch.Tensor:
-        """x [rows, w], its sequences packed by seqs."""
-        q, k, v = self._heads(x)
-        a = attention(q, k, v, seqs, self.causal, rel=RelativeBias(self.bias, self.bucket))
+    def _positions(self):
+        """(rotation, bias), one of them None."""
+        if self.rotates:
+            return Rotary(self.turns, self.interleaved, self.magnitude), None
+        return None, RelativeBias(self.bias, self.bucket)
+
+    def _rest(self, a: torch.Tensor, x: torch.Tensor) -> torch.Tensor:
         x, _ = layer_norm(self.proj(a.flatten(1)), self.norm_w[0], self.norm_b[0], self.eps, residual=x)
         x, _ = layer_norm(self.memory(x), self.norm_w[1], self.norm_b[1], self.eps, residual=x)
         return x
 
+    def forward(self, x: torch.Tensor, seqs: Packed, position: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x [rows, w], its sequences packed by seqs; position (of a rotation): ``packed_positions`` of them by default, which
+        several layers can share."""
+        q, k, v = self._heads(x)
+        plan, rel = self._positions()
+        if plan is not None:
+            q, k = rotate(q, k, packed_positions(seqs, x.shape[0]) if position is None else position, plan)
+        return self._rest(attention(q, k, v, seqs, self.causal, rel=rel), x)
+
     @torch.no_grad()
-    def serve(self, x: torch.Tensor, seqs: Packed, cache: KeyValueCache) -> torch.Tensor:
+    def serve(self, x: torch.Tensor, seqs: Packed, cache: Union[KeyValueCache, PagedCache], layer: int = 0) -> torch.Tensor:
         """The next rows of every sequence (whole prompts, pieces of them or single tokens; causal layers): their keys and
-        values join the cache, and they attend over all of it."""
+        values join the cache, and they attend over all of it.  A ``KeyValueCache`` is the layer's own; of a ``PagedCache`` it is
+        layer ``layer``, seqs is what ``cache.extend`` returned for the step, and keys gather weights where the cache has them."""
         if not self.causal:
             raise ValueError("only a causal layer can be served piece by piece")
         q, k, v = self._heads(x)
+        plan, rel = self._positions()
+        if isinstance(cache, PagedCache):
+            keys = cache.keys[layer]
+            q = paged_append(k, v, keys, cache.table, seqs, q=q, rotary=plan)
+            return self._rest(paged_attention(q, keys, cache.table, seqs, rel=rel, weigh=keys.weight is not None), x)
+        if plan is not None:
+            q, k = rotary_forward(q, k, packed_positions(seqs, x.shape[0], cache.used), plan)
         seqs = cache.append(k, v, seqs)
-        a, _ = attention_forward(q, cache.k, cache.v, seqs, True, rel=RelativeBias(self.bias, self.bucket))
-        x, _ = layer_norm(self.proj(a.flatten(1)), self.norm_w[0], self.norm_b[0], self.eps, residual=x)
-        x, _ = layer_norm(self.memory(x), self.norm_w[1], self.norm_b[1], self.eps, residual=x)
-        return x
+        return self._rest(attention_forward(q, cache.k, cache.v, seqs, True, rel=rel)[0], x)
