@@ -63,7 +63,8 @@ int lram_rotate(const lram_rotary* r, int dtype, int backward, int64_t rows, int
  * one piece and no value is moved between lanes.  With E = 16 bytes of elements and F = E / 4, slot t of the page is
  *     k [page][kv_head][t / 16][d / E][t % 16][d % E]
  *     v [page][kv_head][t / (16 F)][d / 16][t % 16 / 4][d % 16][t % (16 F) / 16 * 4 + t % 4]
- * and position, weight [page][kv_head][t]: the key's position in its text, the attention weight that it has gathered.
+ * and position, weight [page][kv_head][t]: the key's position in its text, the attention weight that it has gathered.  As long
+ * as used[b] = seen[b], which says that no key was evicted, slot t holds the key of position t.
  */
 typedef struct {
   int32_t dtype;

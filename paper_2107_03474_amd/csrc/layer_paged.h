@@ -27,10 +27,11 @@ struct PageTile {
 constexpr int PAGE_BLOCK = 32;  // every page size is a multiple: 2 blocks of 16 keys
 
 // A sequence of the cache: nq new rows from q0 on (those that lie in the tensor: from row `skip` of the sequence's own on), nk
-// keys that pages can hold, and the position of the sequence's row 0.
+// keys that pages can hold, the position of the row q0, and whether every token's key is there.
 struct CacheSeq {
   int64_t q0;
   int nq, nk, used, at;
+  bool whole;
 };
 
 struct Pool {
@@ -54,7 +55,9 @@ __device__ __forceinline__ CacheSeq cache_seq(const Pool& p, int b) {
   const int64_t most = p.width << p.log_page;
   s.used = p.used[b];
   s.nk = s.used < 0 ? 0 : s.used > most ? (int)most : s.used;
-  s.at = p.seen[b] - (int)(s1 - s.q0);  // of the row q0
+  const int seen = p.seen[b];
+  s.at = seen - (int)(s1 - s.q0);
+  s.whole = s.used == seen;
   return s;
 }
 

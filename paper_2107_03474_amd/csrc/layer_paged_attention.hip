@@ -69,6 +69,12 @@ __device__ __forceinline__ float of_groups(float x, bool sum) {
   return sum ? w + z : fmaxf(w, z);
 }
 
+// Keys that queries up to the token-th may meet: of a sequence that has lost none (used = seen) those up to its own, since slot t
+// then has position t.
+__device__ __forceinline__ int64_t keys_met(const CacheSeq& s, int64_t token) {
+  return s.whole ? min((int64_t)s.nk, max((int64_t)s.at + min(token, (int64_t)s.nq - 1) + 1, (int64_t)0)) : (int64_t)s.nk;
+}
+
 // The columns of a tile that a lane holds: its query's operand, position and place.
 template <typename T, int D>
 struct Column {
@@ -77,12 +83,15 @@ struct Column {
   int position, head;  // head: of the group
   int64_t row;         // -1: none
 
-  __device__ __forceinline__ void load(const Attend& a, const CacheSeq& s, int kv_head, int64_t n) {
+  __device__ __forceinline__ void load(const Attend& a, const CacheSeq& s, int kv_head, int64_t n) {  // n < 2^31
+    const uint32_t i = (uint32_t)n / (uint32_t)a.p.group;
+    load(a, s, kv_head, (int)i, (int)((uint32_t)n - i * (uint32_t)a.p.group));
+  }
+  __device__ __forceinline__ void load(const Attend& a, const CacheSeq& s, int kv_head, int i, int of_group) {
     const int lane = threadIdx.x % WAVE;
-    const int64_t i = n / a.p.group;
-    head = (int)(n - i * a.p.group);
+    head = of_group;
     row = i < s.nq ? s.q0 + i : -1;
-    position = i < s.nq ? s.at + (int)i : INT32_MIN;
+    position = i < s.nq ? s.at + i : INT32_MIN;
     const T* const x = (const T*)a.q + (row < 0 ? 0 : row * a.q_row + (kv_head * a.p.group + head) * a.q_head);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -95,6 +104,11 @@ struct Column {
 // Whether a sequence's scores are kept for its keys' weights: the host expects few columns, and the sequence has no more.
 __device__ __forceinline__ bool keeps_scores(const Attend& a, const CacheSeq& s) {
   return a.scores && s.nk <= a.scored && (int64_t)s.nq * a.p.group <= a.score_cols;
+}
+
+// Pieces that hold a part of a sequence's results; 1: the results themselves are there.
+__device__ __forceinline__ int pieces_of(const Attend& a, const CacheSeq& s) {
+  return (int)max(min(((int64_t)s.nk + a.piece - 1) / a.piece, (int64_t)a.pieces), (int64_t)1);
 }
 
 // The bias of a group's heads by distance, in LDS.
@@ -159,6 +173,51 @@ __device__ __forceinline__ void load_keys(const Pool& p, int64_t keys,
   }
 }
 
+// A block's scores of column t and its values into the results: the maximum moves only when it grows by more than 2^GROW.
+template <typename T, int D, int CT>
+__device__ __forceinline__ void absorb(int t, const f32x4 (&z)[PageTile<T>::F], const typename Operand<T>::type (&v)[D / 16],
+                                       f32x4 (&o)[D / 16][CT], float (&m)[CT], float (&l)[CT]) {
+  constexpr int F = PageTile<T>::F, DB = D / 16;
+  float top = z[0][0];
+#pragma unroll
+  for (int h = 0; h < F; ++h)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) top = fmaxf(top, z[h][r]);
+  top = of_groups(top, false);
+  if (__builtin_amdgcn_ballot_w64(top > m[t] + GROW)) {
+    const float now = fmaxf(m[t], top), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - now);
+    m[t] = now;
+    l[t] *= f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d][t] *= f;
+  }
+  const float used = m[t] == -INFINITY ? 0.0f : m[t];
+  typename Operand<T>::type w;
+#pragma unroll
+  for (int h = 0; h < F; ++h)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float e = __builtin_amdgcn_exp2f(z[h][r] - used);
+      l[t] += e;
+      w[h * 4 + r] = (T)e;
+    }
+#pragma unroll
+  for (int d = 0; d < DB; ++d) o[d][t] = mma(v[d], w, o[d][t]);
+}
+
+// Rows of no sequence get zeros, shared out over the workgroups of a head.
+template <typename T, int D>
+__device__ __forceinline__ void clear_rows(const Attend& a, int head) {
+  const Pool& p = a.p;
+  const int64_t before = clamp_row(p.start[0], p.rows), behind = max(clamp_row(p.start[p.batch], p.rows), before);
+  const int all = gridDim.x / p.kv_heads;
+  for (int64_t i = blockIdx.x / p.kv_heads; i < before + (p.rows - behind); i += all) {
+    T* const row = (T*)a.out + ((i < before ? i : behind + (i - before)) * p.heads + head * p.group) * D;
+#pragma clang loop unroll(disable) vectorize(disable)
+    for (int d = threadIdx.x; d < p.group * D; d += ATTEND_THREADS) row[d] = (T)0.0f;
+  }
+}
+
 // Two workgroups a compute unit, so that 256 registers hold everything and the matrix cores take them as they are: with more,
 // the compiler keeps the results in the other half of the register file and moves them to and fro.
 template <typename T, int D, int CT, bool BIAS>
@@ -176,20 +235,12 @@ __global__ __launch_bounds__(ATTEND_THREADS, 2) void k_paged_attention(Attend a)
   id /= p.kv_heads;
   const int b = (int)(id % p.batch);
   id /= p.batch;
-  const int tile0 = (int)(id % a.tiles), piece = (int)(id / a.tiles);
+  const int tile0 = a.tiles - 1 - (int)(id % a.tiles), piece = (int)(id / a.tiles);  // a prompt's longest tiles first
   const CacheSeq s = cache_seq(p, b);
-  {  // rows of no sequence, shared out over the workgroups of a head
-    const int64_t before = clamp_row(p.start[0], p.rows), behind = max(clamp_row(p.start[p.batch], p.rows), before);
-    const int all = gridDim.x / p.kv_heads;
-    for (int64_t i = blockIdx.x / p.kv_heads; i < before + (p.rows - behind); i += all) {
-      T* const row = (T*)a.out + ((i < before ? i : behind + (i - before)) * p.heads + head * p.group) * D;
-#pragma clang loop unroll(disable) vectorize(disable)
-      for (int d = threadIdx.x; d < p.group * D; d += ATTEND_THREADS) row[d] = (T)0.0f;
-    }
-  }
+  clear_rows<T, D>(a, head);
   if (piece && (int64_t)piece * a.piece >= s.nk) return;
   const bool keeps = keeps_scores(a, s);
-  const bool alone = a.pieces == 1 || s.nk <= a.piece;  // no other piece has keys
+  const bool alone = pieces_of(a, s) == 1;
   if constexpr (BIAS) {
     load_bias(a, head, bias);
     __syncthreads();
@@ -202,8 +253,9 @@ __global__ __launch_bounds__(ATTEND_THREADS, 2) void k_paged_attention(Attend a)
     float m[CT], l[CT];
 #pragma unroll
     for (int t = 0; t < CT; ++t) m[t] = -INFINITY, l[t] = 0;
-    for (int64_t base = (int64_t)piece * a.piece; base < s.nk; base += (int64_t)a.pieces * a.piece) {
-      const int end = (int)min(base + a.piece, (int64_t)s.nk);
+    const int64_t met = keys_met(s, (tile * COLS + COLS - 1) / p.group);
+    for (int64_t base = (int64_t)piece * a.piece; base < met; base += (int64_t)a.pieces * a.piece) {
+      const int end = (int)min(base + a.piece, met);
       // A block's values are on their way while its scores are formed, and the next one's keys (of a page looked up a block
       // before) while it is finished.  Loads are made whatever the table says, of page 0 where it names none: where some were
       // left out, the wait for keys would be one for everything.
@@ -246,31 +298,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, 2) void k_paged_attention(Attend a)
 #pragma unroll
             for (int h = 0; h < F; ++h) *(f32x4*)(to + 16 * h) = z[t][h];
           }
-          float top = z[t][0][0];
-#pragma unroll
-          for (int h = 0; h < F; ++h)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, z[t][h][r]);
-          top = of_groups(top, false);
-          if (__builtin_amdgcn_ballot_w64(top > m[t] + GROW)) {
-            const float now = fmaxf(m[t], top), f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[t] - now);
-            m[t] = now;
-            l[t] *= f;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) o[d][t] *= f;
-          }
-          const float top_used = m[t] == -INFINITY ? 0.0f : m[t];
-          Op w;
-#pragma unroll
-          for (int h = 0; h < F; ++h)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float e = __builtin_amdgcn_exp2f(z[t][h][r] - top_used);
-              l[t] += e;
-              w[h * 4 + r] = (T)e;
-            }
-#pragma unroll
-          for (int d = 0; d < DB; ++d) o[d][t] = mma(v[d], w, o[d][t]);
+          absorb<T, D, CT>(t, z[t], v, o, m, l);
         }
       };
       for (; slot + STEP < end; slot += STEP) block(std::true_type());
@@ -323,11 +351,6 @@ __global__ __launch_bounds__(ATTEND_THREADS, 2) void k_paged_attention(Attend a)
       __syncthreads();
     }
   }
-}
-
-// Pieces that hold a part of a sequence's results; 1: the results themselves are there.
-__device__ __forceinline__ int pieces_of(const Attend& a, const CacheSeq& s) {
-  return (int)max(min(((int64_t)s.nk + a.piece - 1) / a.piece, (int64_t)a.pieces), (int64_t)1);
 }
 
 // The pieces' parts of a query and head joined.
@@ -399,11 +422,11 @@ __device__ __forceinline__ float2 whole_of(const Attend& a, int64_t place, int p
 }
 
 // The weight that each key gathers, in a fixed order, beside the join.  Of a single token's few columns the scores were kept (16
-// bytes a key for four heads that share it, beside the 256 of its k); a thread then takes four keys.  Otherwise a wave keeps
-// a block of keys and forms their scores again, over all of the sequence's queries.
+// bytes a key for four heads that share it, beside the 256 of its k); a thread then takes four keys.  Otherwise a workgroup
+// keeps a block of keys and forms their scores again, its waves sharing out the sequence's queries.
 constexpr int WEIGH_CHUNK = 4 * ATTEND_THREADS;  // keys of a workgroup
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int joins, int rows_each, int chunks, int chunk) {
+__global__ __launch_bounds__(ATTEND_THREADS, 2) void k_paged_weigh(Attend a, int joins, int rows_each, int chunks, int chunk) {
   using Ti = PageTile<T>;
   using Op = typename Operand<T>::type;
   constexpr int F = Ti::F, KEYS = Ti::KEYS;
@@ -429,8 +452,9 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int jo
       if (threadIdx.x % 16 == 0) whole[mine] = st;
     }
     __syncthreads();
-    for (int64_t base = first * chunk; base < s.nk; base += (int64_t)chunks * chunk) {
-      const int end = (int)min(base + chunk, (int64_t)s.nk);
+    const int64_t met = keys_met(s, s.nq - 1);  // scores were kept of these
+    for (int64_t base = first * chunk; base < met; base += (int64_t)chunks * chunk) {
+      const int end = (int)min(base + chunk, met);
       for (int slot = (int)base + 4 * threadIdx.x; slot < end; slot += 4 * ATTEND_THREADS) {
         const int page = page_of(p, b, slot);
         if (page < 0) continue;
@@ -445,10 +469,10 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int jo
           for (int r = 0; r < 4; ++r)
             got[r] += x[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x[r] - whole[c].x) * whole[c].y;
         }
-        if (slot + 4 <= s.nk) {
+        if (slot + 4 <= met) {
           *w = had + got;
         } else {
-          for (int r = 0; slot + r < s.nk; ++r) ((float*)w)[r] = had[r] + got[r];
+          for (int r = 0; slot + r < met; ++r) ((float*)w)[r] = had[r] + got[r];
         }
       }
     }
@@ -458,43 +482,87 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_weigh(Attend a, int jo
     load_bias(a, head, bias);
     __syncthreads();
   }
+  constexpr uint32_t STEP = ATTEND_WAVES * 16;
+  __shared__ float sums[ATTEND_WAVES][KEYS];
+  const uint32_t group = p.group, all = (uint32_t)s.nq * group;  // columns
   for (int64_t base = first * chunk; base < s.nk; base += (int64_t)chunks * chunk) {
     const int end = (int)min(base + chunk, (int64_t)s.nk);
-    for (int slot = (int)base + wave * KEYS; slot < end; slot += ATTEND_WAVES * KEYS) {
+    for (int slot = (int)base; slot < end; slot += KEYS) {
       const int page = page_of_wave(p, b, slot);
-      if (page < 0) continue;
+      if (page < 0) continue;  // all waves alike
       const int64_t keys = page_rows(p, page, head) + (slot & (p.page - 1));
       const int left = s.nk - slot;
       Op k[F][Column<T, D>::CH];
       int4 at[F];
       load_keys<T, D, false>(p, keys, k, at);
+      // queries before the lowest position meet none of these keys
+      int lowest = INT32_MAX;
+#pragma unroll
+      for (int h = 0; h < F; ++h) {
+        const int x[4] = {at[h].x, at[h].y, at[h].z, at[h].w}, key = h * 16 + lane / 16 * 4;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) lowest = key + r < left ? min(lowest, x[r]) : lowest;
+      }
+      lowest = min(lowest, __shfl_xor(lowest, 16));
+      lowest = min(lowest, __shfl_xor(lowest, 32));
+      const int64_t skipped = min(max((int64_t)__builtin_amdgcn_readfirstlane(lowest) - s.at, (int64_t)0), (int64_t)s.nq);
+      // this lane's columns: one of each 16, every fourth 16 of them the wave's; the next one's query is on its way
+      const uint32_t tile0 = ((uint32_t)skipped * group & ~15u) + wave * 16;
+      uint32_t i = (tile0 + lane % 16) / group, h0 = tile0 + lane % 16 - i * group;
+      const uint32_t step_i = STEP / group, step_h = STEP - step_i * group;
+      const T* query = (const T*)a.q + (s.q0 + i) * a.q_row + (int64_t)(head * group + h0) * a.q_head + lane / 16 * Ti::E;
+      const float2* stat = a.stat + (s.q0 + i) * p.heads + head * group + h0;
+      const int64_t query_step = step_i * a.q_row + step_h * a.q_head, query_wrap = a.q_row - (int64_t)group * a.q_head;
       f32x4 got[F] = {};
-      for (int64_t n = 0; n < (int64_t)s.nq * p.group; n += 16) {
-        Column<T, D> col;
-        col.load(a, s, head, n + lane % 16);
-        const float2 st = col.row < 0 ? float2{0, 0}
-                                     : whole_of(a, col.row * p.heads + head * p.group + col.head, pieces, 0, 1);
+      Column<T, D> col;
+      float2 st;
+      const auto get = [&] {
+        const bool has = i < (uint32_t)s.nq;
+        col.head = (int)h0;
+        col.position = has ? s.at + (int)i : INT32_MIN;
+        st = {0, 0};
+#pragma unroll
+        for (int c = 0; c < Column<T, D>::CH; ++c) col.q[c] = {};
+        if (has) {
+#pragma unroll
+          for (int c = 0; c < Column<T, D>::CH; ++c) col.q[c] = *(const Op*)(query + c * 4 * Ti::E);
+          st = pieces == 1 ? *stat : whole_of(a, stat - a.stat, pieces, 0, 1);
+        }
+      };
+      get();
+      for (uint32_t tile = tile0; tile < all; tile += STEP) {
+        const Column<T, D> mine = col;
+        const float2 mine_st = {st.x, pieces > 1 ? st.y : st.y == 0 ? 0.0f : __builtin_amdgcn_rcpf(st.y)};
+        const bool wraps = h0 + step_h >= group;
+        i += step_i + wraps;
+        h0 += step_h - (wraps ? group : 0);
+        query += query_step + (wraps ? query_wrap : 0);
+        stat += (int64_t)step_i * p.heads + step_h + (wraps ? p.heads - (int64_t)group : 0);
+        if (tile + STEP < all) get();
         f32x4 z[F];
-        scores<T, D, BIAS>(a, col, k, at, left, bias, z);
+        scores<T, D, BIAS>(a, mine, k, at, left, bias, z);
 #pragma unroll
         for (int h = 0; h < F; ++h)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            got[h][r] += z[h][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(z[h][r] - st.x) * st.y;
+            got[h][r] += z[h][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(z[h][r] - mine_st.x) * mine_st.y;
       }
 #pragma unroll
-      for (int h = 0; h < F; ++h) {
+      for (int h = 0; h < F; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r) {
 #pragma unroll
           for (int o = 1; o < 16; o *= 2) got[h][r] += __shfl_xor(got[h][r], o);
-        if (lane % 16 == 0) {
-          float* const w = p.weight + keys + h * 16 + lane / 16 * 4;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (h * 16 + lane / 16 * 4 + r < left) w[r] += got[h][r];
+          if (lane % 16 == 0) sums[wave][h * 16 + lane / 16 * 4 + r] = got[h][r];
         }
+      __syncthreads();
+      if ((int)threadIdx.x < min(KEYS, left)) {
+        float sum = 0;
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) sum += sums[w][threadIdx.x];
+        p.weight[keys + threadIdx.x] += sum;
       }
+      __syncthreads();
     }
   }
 }
@@ -506,9 +574,9 @@ __global__ __launch_bounds__(ATTEND_THREADS) void k_paged_clear(T* out, int64_t 
 }
 
 struct Plan {
-  int ct;
+  int cols;  // of a tile: 16 or 32
   int64_t tiles, pieces, piece;
-  int64_t cols, scored;              // of kept scores; 0: none
+  int64_t score_cols, scored;        // of kept scores; 0: none
   size_t part, scores, stat;  // bytes
   size_t all() const { return part + scores + stat; }
 };
@@ -532,8 +600,8 @@ Plan plan_of(const lram_paged& p, bool weigh) {
   // a plan that understates the rows is found out by how many there are
   const int64_t tokens = std::max({std::min(p.max_q, p.rows), over(p.rows, std::max(p.batch, 1)), (int64_t)1});
   const int64_t keys = std::max<int64_t>(1, std::min(p.max_k, p.width * p.page));
-  x.ct = tokens * G > 16 ? 2 : 1;
-  x.tiles = std::max<int64_t>(1, std::min(over(tokens * G, 16 * x.ct), MOST_GROUPS / lists));
+  x.cols = tokens * G <= 16 ? 16 : 32;
+  x.tiles = std::max<int64_t>(1, std::min(over(tokens * G, x.cols), MOST_GROUPS / lists));
   const int64_t wanted = std::min(over(ROUND * std::min<int64_t>(std::max(p.batch, 1), ROUNDS), lists * x.tiles), MOST_GROUPS / (lists * x.tiles));
   x.piece = over(over(keys, std::max<int64_t>(1, wanted)), PIECE_STEP) * PIECE_STEP;
   x.piece = std::max(x.piece, PIECE_LEAST);
@@ -543,9 +611,9 @@ Plan plan_of(const lram_paged& p, bool weigh) {
   if (x.pieces > 1) x.part = (size_t)x.pieces * places * p.head_dim * sizeof(float);
   if (x.pieces > 1 || weigh) x.stat = (size_t)x.pieces * places * sizeof(float2);
   if (weigh && tokens * G <= 16) {
-    x.cols = tokens * G;
+    x.score_cols = tokens * G;
     x.scored = x.pieces * x.piece;
-    x.scores = (size_t)lists * x.cols * x.scored * sizeof(float);
+    x.scores = (size_t)lists * x.score_cols * x.scored * sizeof(float);
   }
   return x;
 }
@@ -596,7 +664,7 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void*
   a.tiles = (int)x.tiles, a.pieces = (int)x.pieces, a.piece = (int)x.piece;
   char* const ws = (char*)workspace;
   if (x.part) a.part = (float*)ws;
-  if (x.scores) a.scores = (float*)(ws + x.part), a.score_cols = (int)x.cols, a.scored = x.scored;
+  if (x.scores) a.scores = (float*)(ws + x.part), a.score_cols = (int)x.score_cols, a.scored = x.scored;
   if (x.stat) a.stat = (float2*)(ws + x.part + x.scores);
   if (p->batch == 0 || p->pages == 0) {
     const int64_t n = p->rows * p->heads * p->head_dim;
@@ -615,16 +683,18 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void*
       return layer_launched();
     };
     const int64_t lists = (int64_t)p->batch * p->kv_heads, groups = lists * x.tiles * x.pieces;
-    int rc = q->rel_weight ? x.ct == 1 ? go(k_paged_attention<T, D, 1, true>, groups) : go(k_paged_attention<T, D, 2, true>, groups)
-             : x.ct == 1   ? go(k_paged_attention<T, D, 1, false>, groups)
-                           : go(k_paged_attention<T, D, 2, false>, groups);
+    const auto of = [&](auto bias) {
+      constexpr bool BIAS = decltype(bias)::value;
+      return x.cols == 16 ? go(k_paged_attention<T, D, 1, BIAS>, groups) : go(k_paged_attention<T, D, 2, BIAS>, groups);
+    };
+    int rc = q->rel_weight ? of(std::true_type()) : of(std::false_type());
     if (rc != LRAM_OK || (!x.part && !q->weigh)) return rc;
     const int64_t all = (int64_t)p->batch * p->heads;
     const int64_t each = std::max<int64_t>(1, std::min({p->max_q, p->rows, MOST_GROUPS / 2 / all}));
     const int64_t joins = x.part ? all * each : 0;
     if (!q->weigh) return go(k_paged_join<T, D>, joins, (int)each);
     const int64_t keys = std::max<int64_t>(1, std::min(p->max_k, p->width * p->page));
-    const int64_t chunk = x.scores ? WEIGH_CHUNK : ATTEND_WAVES * PageTile<T>::KEYS;
+    const int64_t chunk = x.scores ? WEIGH_CHUNK : PageTile<T>::KEYS;
     const int64_t chunks = std::max<int64_t>(1, std::min(over(keys, chunk), (MOST_GROUPS - joins) / lists));
     rc = q->rel_weight ? go(k_paged_weigh<T, D, true>, joins + lists * chunks, (int)joins, (int)each, (int)chunks, (int)chunk)
                        : go(k_paged_weigh<T, D, false>, joins + lists * chunks, (int)joins, (int)each, (int)chunks, (int)chunk);
