@@ -263,7 +263,11 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(Append a) {
   const Pool& p = a.p;
   if constexpr (FORM != PLAIN) {
     if (blockIdx.x < a.q_groups) {
-      rotate_chunk<T, FORM>(a.q, blockIdx.x * APPEND_THREADS + threadIdx.x, [&](int64_t row) { return position_of(p, row); });
+      const auto position = [&](int64_t row) { return position_of(p, row); };
+      if (a.q.past)
+        rotate_chunk<T, FORM, true>(a.q, blockIdx.x * APPEND_THREADS + threadIdx.x, position);
+      else
+        rotate_chunk<T, FORM, false>(a.q, blockIdx.x * APPEND_THREADS + threadIdx.x, position);
       return;
     }
   }

@@ -64,11 +64,12 @@ struct Rotate {
   int pair_chunks;  // of them rotated, the first ones
   int teams;        // threads that share a row's heads for one chunk
   float magnitude, sign;
+  bool past;        // results go past the caches
 };
 
 // A region of a head that is not whole chunks ends in one that overlaps the one before (both write the same values); one
 // shorter than a chunk goes element by element.
-template <typename T, Form FORM, typename F>
+template <typename T, Form FORM, bool PAST, typename F>
 __device__ __forceinline__ void rotate_chunk(const Rotate& a, uint32_t id, F position_of) {
   using C = Chunk<T>;
   constexpr int E = C::E;
@@ -119,6 +120,12 @@ __device__ __forceinline__ void rotate_chunk(const Rotate& a, uint32_t id, F pos
       t[e] = turn_of(a.turns[FORM == NEIGHBOURS ? min(pair, a.pairs - 1) : pair], position, a.magnitude, a.sign);
     }
   }
+  const auto put = [](V* at, typename C::type value) {
+    if constexpr (PAST)
+      __builtin_nontemporal_store((V)value, at);
+    else
+      *at = value;
+  };
   for (int head1 = head0; head1 < all; head1 += AT_ONCE * a.teams) {
     typename C::type x[AT_ONCE], z[AT_ONCE];
 #pragma unroll
@@ -149,11 +156,11 @@ __device__ __forceinline__ void rotate_chunk(const Rotate& a, uint32_t id, F pos
             f[e] = fmaf(u, t[e].c, -v * t[e].s);
             g[e] = fmaf(u, t[e].s, v * t[e].c);
           }
-          *(V*)(to(head) + a.pairs + first) = C::down(g);
+          put((V*)(to(head) + a.pairs + first), C::down(g));
         }
         x[j] = C::down(f);
       }
-      *(V*)(to(head) + first) = x[j];
+      put((V*)(to(head) + first), x[j]);
     }
   }
 }
@@ -168,12 +175,16 @@ int teams_of(int64_t rows, int chunks, int heads) {
   return heads;
 }
 
+// Results that the L2s cannot hold go past them (16,384 rows of 32/8 heads of 128 bf16: 65 -> 53 us).
+constexpr int64_t CACHED_BYTES = 32 << 20;
+
 // What a thread does where rows are rotated as they lie; the threads of a row.
 inline int64_t divide(Rotate& a, const lram_rotary& r, int dtype) {
   const int per = 16 / (int)elem_size(dtype), turned = r.interleaved ? 2 * r.pairs : r.pairs;
   a.turns = r.turns, a.pairs = r.pairs, a.magnitude = r.magnitude, a.sign = 1.0f;
   a.pair_chunks = (turned + per - 1) / per;
   a.chunks = r.interleaved ? a.dim / per : a.pair_chunks + (a.dim - 2 * r.pairs + per - 1) / per;
+  a.past = a.rows * (a.heads + a.kv_heads) * a.dim * (int64_t)elem_size(dtype) > CACHED_BYTES;
   a.teams = teams_of(a.rows, a.chunks, a.heads + a.kv_heads);
   return (int64_t)a.chunks * a.teams;
 }

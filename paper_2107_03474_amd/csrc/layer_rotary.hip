@@ -10,7 +10,11 @@ namespace {
 
 template <typename T, Form FORM>
 __global__ __launch_bounds__(ROTATE_THREADS) void k_rotate(Rotate a) {
-  rotate_chunk<T, FORM>(a, blockIdx.x * ROTATE_THREADS + threadIdx.x, [&](int64_t row) { return a.position[row]; });
+  const auto position_of = [&](int64_t row) { return a.position[row]; };
+  if (a.past)
+    rotate_chunk<T, FORM, true>(a, blockIdx.x * ROTATE_THREADS + threadIdx.x, position_of);
+  else
+    rotate_chunk<T, FORM, false>(a, blockIdx.x * ROTATE_THREADS + threadIdx.x, position_of);
 }
 
 __global__ __launch_bounds__(ROTATE_THREADS) void k_positions(const int32_t* start, const int32_t* first, int batch,
