@@ -21,7 +21,8 @@ struct Append {
   int64_t k_row, k_head, v_row, v_head;
   int each;                 // heads that a wave takes
   int64_t places, v_places;  // for tiles of 16 and of 32 slots
-  int64_t q_groups, waves;  // workgroups that take q, the first ones; waves that take k, the next ones
+  int64_t waves;             // that take k, the first ones
+  int64_t groups;            // workgroups that take k and v, the first ones (their way is the longer one); the others take q
 };
 
 // Rows of a tile: row t of 16 or 32 is row at + t of the tensors, for from <= t < to, and has position + t.
@@ -262,18 +263,19 @@ template <typename T, int D, Form FORM>
 __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(Append a) {
   const Pool& p = a.p;
   if constexpr (FORM != PLAIN) {
-    if (blockIdx.x < a.q_groups) {
+    if (blockIdx.x >= a.groups) {
+      const uint32_t id = (uint32_t)(blockIdx.x - a.groups) * APPEND_THREADS + threadIdx.x;
       const auto position = [&](int64_t row) { return position_of(p, row); };
       if (a.q.past)
-        rotate_chunk<T, FORM, true>(a.q, blockIdx.x * APPEND_THREADS + threadIdx.x, position);
+        rotate_chunk<T, FORM, true>(a.q, id, position);
       else
-        rotate_chunk<T, FORM, false>(a.q, blockIdx.x * APPEND_THREADS + threadIdx.x, position);
+        rotate_chunk<T, FORM, false>(a.q, id, position);
       return;
     }
   }
   __shared__ typename Chunk<T>::type lds[APPEND_WAVES][Chunk<T>::E == 8 ? PAGE_BLOCK * D / 8 : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
-  int64_t id = (blockIdx.x - a.q_groups) * APPEND_WAVES + wave;
+  int64_t id = (int64_t)blockIdx.x * APPEND_WAVES + wave;
   const bool of_v = id >= a.waves;
   if (of_v) id -= a.waves;
   const int parts = (p.kv_heads + a.each - 1) / a.each;
@@ -361,12 +363,13 @@ int lram_paged_append(const lram_paged* p, const lram_rotary* r, const void* k, 
   a.k_row = k_row, a.k_head = k_head, a.v_row = v_row, a.v_head = v_head;
   a.q.q = q, a.q.q_out = q_out, a.q.q_row = q_row, a.q.q_head = q_head;
   a.q.rows = p->rows, a.q.heads = p->heads, a.q.dim = p->head_dim;
+  int64_t q_groups = 0;
   if (r) {
     const int64_t threads = divide(a.q, *r, p->dtype) * p->rows;
     if (threads > (int64_t)1 << 31) return LRAM_EINVAL;
-    if (q) a.q_groups = (threads + APPEND_THREADS - 1) / APPEND_THREADS;
+    if (q) q_groups = (threads + APPEND_THREADS - 1) / APPEND_THREADS;
   }
-  const int64_t most = (((int64_t)1 << 32) / APPEND_THREADS - 1 - a.q_groups) * APPEND_WAVES;  // a grid: below 2^32 threads
+  const int64_t most = (((int64_t)1 << 32) / APPEND_THREADS - 1 - q_groups) * APPEND_WAVES;  // a grid: below 2^32 threads
   const auto parts = [&] { return (p->kv_heads + a.each - 1) / a.each; };
   a.places = Places<16>::of(p->rows, p->batch), a.v_places = Places<32>::of(p->rows, p->batch);
   const auto waves = [&] { return (a.places + a.v_places) * parts(); };
@@ -375,7 +378,8 @@ int lram_paged_append(const lram_paged* p, const lram_rotary* r, const void* k, 
   while (waves() > most && a.each < p->kv_heads) a.each *= 2;
   if (waves() > most) return LRAM_EINVAL;
   a.waves = a.places * parts();
-  const int64_t grid = a.q_groups + (waves() + APPEND_WAVES - 1) / APPEND_WAVES;
+  a.groups = (waves() + APPEND_WAVES - 1) / APPEND_WAVES;
+  const int64_t grid = a.groups + q_groups;
   const auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(APPEND_THREADS), 0, (hipStream_t)stream, a);
     return layer_launched();
