@@ -21,7 +21,7 @@ struct Append {
   int64_t k_row, k_head, v_row, v_head;
   int each;                 // heads that a wave takes
   int64_t places, v_places;  // for tiles of 16 and of 32 slots
-  int64_t waves;             // that take k, the first ones
+  int64_t waves;             // that take v, the first ones (us of 8,200 prompt rows, 16/8 heads of 128: 28, k first 34)
   int64_t groups;            // workgroups that take k and v, the first ones (their way is the longer one); the others take q
 };
 
@@ -276,8 +276,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(Append a) {
   __shared__ typename Chunk<T>::type lds[APPEND_WAVES][Chunk<T>::E == 8 ? PAGE_BLOCK * D / 8 : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
   int64_t id = (int64_t)blockIdx.x * APPEND_WAVES + wave;
-  const bool of_v = id >= a.waves;
-  if (of_v) id -= a.waves;
+  const bool of_v = id < a.waves;
+  if (!of_v) id -= a.waves;
   const int parts = (p.kv_heads + a.each - 1) / a.each;
   const int head0 = (int)(id % parts) * a.each, head1 = min(head0 + a.each, p.kv_heads);
   const int64_t place = id / parts;
@@ -377,7 +377,7 @@ int lram_paged_append(const lram_paged* p, const lram_rotary* r, const void* k, 
   while (a.each < KEY_HEADS_EACH && p->rows / 16 * parts() >= 2 * MANY_WAVES) a.each *= 2;
   while (waves() > most && a.each < p->kv_heads) a.each *= 2;
   if (waves() > most) return LRAM_EINVAL;
-  a.waves = a.places * parts();
+  a.waves = a.v_places * parts();
   a.groups = (waves() + APPEND_WAVES - 1) / APPEND_WAVES;
   const int64_t grid = a.groups + q_groups;
   const auto go = [&](auto kernel) {
