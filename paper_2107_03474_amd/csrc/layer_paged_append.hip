@@ -366,7 +366,7 @@ int lram_paged_append(const lram_paged* p, const lram_rotary* r, const void* k, 
   int64_t q_groups = 0;
   if (r) {
     const int64_t threads = divide(a.q, *r, p->dtype) * p->rows;
-    if (threads > (int64_t)1 << 31) return LRAM_EINVAL;
+    if (q && threads > (int64_t)1 << 31) return LRAM_EINVAL;
     if (q) q_groups = (threads + APPEND_THREADS - 1) / APPEND_THREADS;
   }
   const int64_t most = (((int64_t)1 << 32) / APPEND_THREADS - 1 - q_groups) * APPEND_WAVES;  // a grid: below 2^32 threads

@@ -14,7 +14,7 @@ import torch
 
 from . import F32, LramError
 from . import load as _load_library
-from .layer import HEAD_DIMS, Packed, RelativeBias, _check, _heads, _ptr, _scratch, _type
+from .layer import HEAD_DIMS, Packed, RelativeBias, _check, _heads, _ptr, _records, _scratch, _type
 from .positions import Rotary, _launch, _refusal, _Rotary, _rotary
 
 __all__ = ["PagedKeys", "PageTable", "paged_keys", "page_table", "paged_extend", "paged_append", "paged_attention",
@@ -186,6 +186,8 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, keys: PagedKeys, table: PageT
     weight [rows, kv_heads] fp32 they begin with these weights, not with 0.  Returns q [rows, heads, head_dim] rotated (q
     itself without a rotation, None without q).  Only start_q and max_q of seqs are used."""
     lib = _library()
+    if _records(k, v, q):
+        raise LramError("a cache has no gradients: append to it under torch.no_grad()")
     rows = k.shape[0]
     a = _describe(keys, table, q.shape[1] if q is not None and q.dim() == 3 else 0, rows, seqs)
     dim = a.head_dim
@@ -222,6 +224,8 @@ def paged_attention(q: torch.Tensor, keys: PagedKeys, table: PageTable, seqs: Pa
     1 / sqrt(head_dim) by default.  weigh: the weights that each key is given, summed over queries and the heads that share
     it, are added to keys.weight.  Of seqs start_q, max_q and max_k are used."""
     lib = _library()
+    if _records(q, None if rel is None else rel.weight):
+        raise LramError("attention over a cache has no gradients: call it under torch.no_grad()")
     if q.dim() != 3:
         raise LramError("q must be [rows, heads, head_dim]")
     rows, heads, dim = q.shape
@@ -261,7 +265,8 @@ def paged_evict(keys: PagedKeys, table: PageTable, budget: int, recent: int = 0,
     """Cuts every sequence that uses more than ``budget`` keys down to it, each key head by itself: its keys of the ``recent``
     newest positions stay, and of the others those that have gathered the largest weights (at equal weights the lowest
     position; NaN is less than any).  Keys that stay past slot ``budget`` move into the slots that are left below it.  The
-    lengths stay as they are, for the other layers: ``paged_shrink`` follows the last of them."""
+    lengths stay as they are, for the other layers: ``paged_shrink`` follows the last of them, before anything else is done
+    with the cache."""
     lib = _library()
     if keys.weight is None:
         raise LramError("the cache gathers no weights")
@@ -307,8 +312,8 @@ class PagedCache:
         for each layer i: paged_append(k, v, cache.keys[i], cache.table, seqs, ...); paged_attention(q, cache.keys[i], ...)
         cache.evict(budget, recent)      # where the cache has weights and a budget
 
-    The lengths are on the device.  The host keeps bounds of them, by which pages are given out: a captured step takes only what
-    was reserved before, and after its replays ``refresh`` reads the lengths back."""
+    The lengths are on the device.  The host keeps bounds of them, by which pages are given out.  A captured step takes only
+    what was reserved before; once there was one, the host's calls read the lengths back first (``refresh``)."""
 
     def __init__(self, batch: int, pages: int, kv_heads: int, head_dim: int, page: int = 64, capacity: int = 0, layers: int = 1,
                  dtype=torch.bfloat16, weigh: bool = False, device="cuda"):
@@ -322,6 +327,7 @@ class PagedCache:
         self._free = list(range(pages - 1, -1, -1))
         self._own: List[List[int]] = [[] for _ in range(batch)]
         self._used = [0] * batch  # no sequence uses more keys
+        self._captured = False    # a step was captured, so that its replays may have changed the lengths
 
     def free_pages(self) -> int:
         return len(self._free)
@@ -344,6 +350,8 @@ class PagedCache:
         lengths = [int(n) for n in lengths]
         if len(lengths) != self.batch or any(n < 0 for n in lengths):
             raise ValueError("lengths must be those of the cache's %d sequences" % self.batch)
+        if self._captured:
+            self.refresh()
         why, more = self._missing(lengths)
         if why:  # the bounds may be too high
             self.refresh()
@@ -363,15 +371,15 @@ class PagedCache:
         lengths: the numbers of them, where the host knows them (else every sequence is taken to have max_q)."""
         if seqs.start_q.numel() != self.batch + 1:
             raise ValueError("the plan must be of the cache's %d sequences" % self.batch)
-        if not torch.cuda.is_current_stream_capturing():
-            lengths = [seqs.max_q] * self.batch if lengths is None else lengths
-            self.reserve(lengths)
-            self._used = [u + int(n) for u, n in zip(self._used, lengths)]
-            longest = max(self._used, default=0)
-        else:
-            longest = self.capacity
+        if torch.cuda.is_current_stream_capturing():
+            self._captured = True
+            paged_extend(self.table, seqs)
+            return seqs._replace(max_k=self.capacity)
+        lengths = [seqs.max_q] * self.batch if lengths is None else lengths
+        self.reserve(lengths)
         paged_extend(self.table, seqs)
-        return seqs._replace(max_k=longest)
+        self._used = [u + int(n) for u, n in zip(self._used, lengths)]
+        return seqs._replace(max_k=max(self._used, default=0))
 
     def evict(self, budget: int, recent: int = 0) -> None:
         """``paged_evict`` in every layer; the pages past the budget stay the sequences' own (``trim`` gives them back)."""
@@ -388,7 +396,8 @@ class PagedCache:
         self.table.table.copy_(self._host)
 
     def trim(self) -> None:
-        """Pages that hold no key go back to the pool."""
+        """Pages that hold no key go back to the pool (waits for the device)."""
+        self.refresh()
         self._give_back([-(-u // self.page) for u in self._used])
 
     def release(self, sequences: Sequence[int]) -> None:

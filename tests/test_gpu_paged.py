@@ -99,6 +99,8 @@ APPEND = [
     ([200, 0, 3], [0, 0, 250], 6, 2, 64, 256, 17, False, F32),
     ([31, 64, 1], [1, 0, 64], 3, 3, 128, 128, 5, True, F32),
     ([40, 9], [10, 0], 4, 1, 64, 64, 0, False, BF16),
+    ([1, 0, 2] * 100, [7, 40, 31] * 100, 2, 1, 32, 32, 16, False, BF16),  # more sequences than a wave has lanes
+    ([70, 1] * 40, [0, 5] * 40, 4, 2, 64, 32, 9, True, F32),
 ]
 
 
@@ -245,6 +247,44 @@ def test_attention(new, used, heads, kv, dim, page, dtype, bias, evicted):
         ref.check(lram.paged_attention(q, keys, table, s, scale, rel), want["out"])
     lram.paged_attention(q, keys, table, seqs, scale, rel, weigh=True)
     assert _same(keys.weight, first)  # the same bits on every call
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols", [1, 4])
+def test_rows_that_the_tensor_does_not_hold(cols, dtype):
+    """Starts past q's end: the rows that are there, in their places, and weights of these alone."""
+    g = _gen(21)
+    new, used, heads = [5, 3, 4], [300, 200, 40], cols
+    keys, table = _cache(g, used, 1, 64, 32, dtype)
+    q = torch.randn((6, heads, 64), generator=g, device=DEV).to(dtype)  # 5 rows, one of three, and none of four
+    seqs = _plan(new, max_k=300)
+    store = ref.Store(keys)
+    want, more, bound = ref.attention(store, q, table.table, used, [300, 198, 36], [0, 5, 6, 6], 0.125)
+    out = lram.paged_attention(q, keys, table, seqs, weigh=True)
+    ref.check(out, want["out"])
+    got, met = ref.Store(keys).weight, bound > 0
+    total = store.weight.double() + more
+    assert ((got.double() - total).abs() <= bound + 2 * E * total.abs())[met].all()
+    assert _same(got[~met], store.weight[~met])
+    k, v = (torch.randn((6, 1, 64), generator=g, device=DEV).to(dtype) for _ in range(2))
+    lram.paged_append(k, v, keys, table, seqs)
+    after = ref.Store(keys)
+    p, s = store.places(table.table[0], 300)
+    store.k[p[295:], s[295:]] = k[:5]
+    p, s = store.places(table.table[1], 200)
+    store.k[p[197], s[197]] = k[5]
+    assert _same(after.k, store.k)
+
+
+def test_gradients_are_refused():
+    g = _gen(22)
+    keys, table = _cache(g, [10], 2, 64, 32, F32)
+    q = torch.randn((1, 2, 64), device=DEV, requires_grad=True)
+    for call in (lambda: lram.paged_attention(q, keys, table, _plan([1])), lambda: lram.paged_append(q, q, keys, table, _plan([1]))):
+        with pytest.raises(lram.LramError, match="no gradients"):
+            call()
+        with torch.no_grad():
+            call()
 
 
 def test_no_sequences_and_no_pages():
@@ -486,7 +526,13 @@ def test_a_captured_step_replayed():
         assert torch.equal(captured.table.used, eager.table.used) and torch.equal(captured.table.seen, eager.table.seen)
         for a, b in zip(captured.keys[0], eager.keys[0]):
             assert _same(a, b)
-    assert captured.refresh() == eager.refresh() == eager.table.used.tolist()
+    # once a step was captured, the host's calls go by the real lengths
+    used = eager.table.used.tolist()
+    captured.reserve([5, 5, 5])
+    assert captured._used == used
+    captured.trim()
+    assert captured.free_pages() == 9 - sum(-(-n // 32) for n in used)
+    assert captured.refresh() == eager.refresh() == used
 
 
 def test_two_streams_at_once():

@@ -1,6 +1,7 @@
 """Rotary positions against the rotation in 64 bits, with bounds from the arithmetic that the header states."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import cache_reference as ref
 import paper_2107_03474_amd as lram
@@ -106,6 +107,31 @@ def test_second_derivatives_are_refused():
     first, = torch.autograd.grad((y * y).sum(), q, create_graph=True)
     with pytest.raises(RuntimeError):
         torch.autograd.grad(first.sum(), q)
+
+
+def test_forward_mode_is_refused():
+    q = torch.randn((3, 2, 16), device=DEV)
+    at, plan = torch.arange(3, dtype=torch.int32, device=DEV), lram.rotary_plan(16)
+    with forward_ad.dual_level():
+        with pytest.raises(NotImplementedError):
+            lram.rotary(forward_ad.make_dual(q, torch.ones_like(q)), None, at, plan)
+        lram.rotary(q, None, at, plan)  # no tangent: nothing to refuse
+
+
+@pytest.mark.parametrize("interleaved,pairs,dtype", [(False, 32, BF16), (True, 30, BF16), (False, 13, F32)])
+def test_many_rows_are_rotated_as_few(interleaved, pairs, dtype):
+    """Results past the caches, and threads that go over several heads: the bits of the same rows by themselves."""
+    g = _gen(5)
+    rows = 18000 if dtype == BF16 else 9000
+    q, k = _randn(g, rows, 12, 64, dtype=dtype), _randn(g, rows, 5, 64, dtype=dtype)
+    at = torch.randint(-(1 << 31), (1 << 31) - 1, (rows,), generator=g, device=DEV).to(torch.int32)
+    plan = lram.rotary_plan(2 * pairs, interleaved=interleaved)
+    a, b = lram.rotary_forward(q, k, at, plan)
+    assert a.numel() * a.element_size() + b.numel() * b.element_size() > 32 << 20
+    for first in (0, 777, rows - 40):
+        part = slice(first, first + 40)
+        x, y = lram.rotary_forward(q[part], k[part], at[part], plan)
+        assert torch.equal(a[part], x) and torch.equal(b[part], y)
 
 
 @pytest.mark.parametrize("lengths,before,after", [([5, 0, 17, 1], 2, 3), ([1] * 300, 0, 0), ([0], 3, 0), ([], 0, 4)])
