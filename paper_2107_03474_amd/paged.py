@@ -119,20 +119,16 @@ def _describe(keys: PagedKeys, table: PageTable, heads: int = 0, rows: int = 0, 
     if table.table.dim() != 2 or batch < 0:
         raise LramError("table must be [batch, width], used and seen [batch]")
     width, i32 = table.table.shape[1], torch.int32
-    a = _Paged(_type(k, "k"), heads or kv, kv, dim, batch, page, pages, width)
-    on = k.get_device()
-    a.k = _at(k, "k", k.dtype, (pages, kv, page // 16, dim // e, 16, e), k, on)
-    a.v = _at(v, "v", k.dtype, (pages, kv, page // (4 * e), dim // 16, 4, 16, e), k, on)
-    a.position = _at(position, "position", i32, (pages, kv, page), k, on)
-    if weight is not None:
-        a.weight = _at(weight, "weight", torch.float32, (pages, kv, page), k, on)
-    a.table = _at(table.table, "table", i32, (batch, width), k, on)
-    a.used = _at(table.used, "used", i32, (batch,), k, on)
-    a.seen = _at(table.seen, "seen", i32, (batch,), k, on)
-    if seqs is not None:
-        a.start = _at(seqs.start_q, "start_q", i32, (batch + 1,), k, on)
-        a.rows, a.max_q, a.max_k = rows, seqs.max_q, seqs.max_k
-    return a
+    on, dt = k.get_device(), k.dtype
+    return _Paged(_type(k, "k"), heads or kv, kv, dim, batch, page, pages, width,
+                  _at(k, "k", dt, (pages, kv, page // 16, dim // e, 16, e), k, on),
+                  _at(v, "v", dt, (pages, kv, page // (4 * e), dim // 16, 4, 16, e), k, on),
+                  _at(position, "position", i32, (pages, kv, page), k, on),
+                  None if weight is None else _at(weight, "weight", torch.float32, (pages, kv, page), k, on),
+                  _at(table.table, "table", i32, (batch, width), k, on), _at(table.used, "used", i32, (batch,), k, on),
+                  _at(table.seen, "seen", i32, (batch,), k, on),
+                  *((None, 0, 0, 0) if seqs is None else
+                    (_at(seqs.start_q, "start_q", i32, (batch + 1,), k, on), rows, seqs.max_q, seqs.max_k)))
 
 
 def _like_keys(t: torch.Tensor, name: str, keys: PagedKeys, dim: int):
@@ -204,7 +200,7 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, keys: PagedKeys, table: PageT
         if rotary is None:
             pq = (None, 0, 0)
         else:
-            out = q.new_empty(q.shape)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
     given = None
     if weight is not None:
         if keys.weight is None:
@@ -246,7 +242,7 @@ def paged_attention(q: torch.Tensor, keys: PagedKeys, table: PageTable, seqs: Pa
         x.rel_weight = _ptr(w, "rel.weight", w.dtype, (heads, w.shape[1]), q)
         x.rel_bucket = _ptr(bucket, "rel.bucket", torch.int32, (bucket.shape[0],), q)
         x.wdtype, x.rel_buckets, x.rel_reach = _type(w, "rel.weight"), w.shape[1], bucket.shape[0] // 2
-    out = q.new_empty(q.shape)
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
     n = ctypes.c_size_t(0)
     rc = 0
     if workspace is None:

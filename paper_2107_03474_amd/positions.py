@@ -44,7 +44,7 @@ def _library():
 
 def _launch(device: torch.device, call, *args) -> int:
     """call(*args, the device's current stream), with the device as the current one."""
-    if device.index == torch.cuda.current_device():
+    if device.index == torch._C._cuda_getDevice():
         return call(*args, torch._C._cuda_getCurrentRawStream(device.index))
     with torch.cuda.device(device):
         return call(*args, torch._C._cuda_getCurrentRawStream(device.index))
@@ -141,8 +141,9 @@ def _rotate(q, k, position, plan: Rotary, backward: bool):
             raise LramError("q and k must have the same rows")
     at = _ptr(position, "position", torch.int32, (rows,), q)
     r = _rotary(plan, q)
-    out_q = q.new_empty(q.shape)
-    out_k = None if k is None else k.new_empty(k.shape)
+    # (new_empty takes half a microsecond longer)
+    out_q = torch.empty_like(q, memory_format=torch.contiguous_format)
+    out_k = None if k is None else torch.empty_like(k, memory_format=torch.contiguous_format)
     kv = 0 if k is None else k.shape[1]
     if not heads or k is not None and not kv:
         raise LramError("q and k must have heads")
