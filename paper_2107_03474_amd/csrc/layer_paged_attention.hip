@@ -590,6 +590,8 @@ struct Plan {
 // and without.
 constexpr int64_t PIECE_STEP = 128, PIECE_LEAST = 256, ROUND = 512, ROUNDS = 4;
 constexpr int64_t FEW_BYTES = 256 << 10;  // of a sequence's keys and values of a head
+constexpr int64_t SCORE_BYTES = 256 << 20;
+constexpr int64_t WEIGH_GROUPS = 8192;  // more go over several stretches each: where few keys are met of many expected, they only start
 constexpr int64_t MOST_GROUPS = ((int64_t)1 << 32) / ATTEND_THREADS - 1;
 
 int64_t over(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -612,7 +614,9 @@ Plan plan_of(const lram_paged& p, bool weigh) {
   if (x.pieces > 1 || weigh) x.stat = (size_t)x.pieces * places * sizeof(float2);
   if (weigh && tokens * G <= 16) {
     x.score_cols = tokens * G;
-    x.scored = x.pieces * x.piece;
+    // longer sequences' scores, of a plan that expects the whole of a large cache, are formed again
+    const int64_t most = SCORE_BYTES / (lists * x.score_cols * (int64_t)sizeof(float)) / PIECE_STEP * PIECE_STEP;
+    x.scored = std::min(x.pieces * x.piece, most);
     x.scores = (size_t)lists * x.score_cols * x.scored * sizeof(float);
   }
   return x;
@@ -695,7 +699,7 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* q, void*
     if (!q->weigh) return go(k_paged_join<T, D>, joins, (int)each);
     const int64_t keys = std::max<int64_t>(1, std::min(p->max_k, p->width * p->page));
     const int64_t chunk = x.scores ? WEIGH_CHUNK : PageTile<T>::KEYS;
-    const int64_t chunks = std::max<int64_t>(1, std::min(over(keys, chunk), (MOST_GROUPS - joins) / lists));
+    const int64_t chunks = std::max<int64_t>(1, std::min({over(keys, chunk), over(WEIGH_GROUPS, lists), (MOST_GROUPS - joins) / lists}));
     rc = q->rel_weight ? go(k_paged_weigh<T, D, true>, joins + lists * chunks, (int)joins, (int)each, (int)chunks, (int)chunk)
                        : go(k_paged_weigh<T, D, false>, joins + lists * chunks, (int)joins, (int)each, (int)chunks, (int)chunk);
     return rc;

@@ -314,21 +314,22 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_paged_evict(Evict a) {
 
 template <typename T, int D>
 __global__ __launch_bounds__(MOVE_WAVES* WAVE) void k_paged_move(Evict a, int lists) {
-  const int list = blockIdx.x % lists, i = ((int)(blockIdx.x / lists) * MOVE_WAVES + threadIdx.x / WAVE) * MOVE_EACH;
-  const int n = min(a.counts[list] - i, MOVE_EACH);
-  if (n <= 0) return;
-  const int32_t* const from = a.lists + (int64_t)list * 2 * a.most + i;
-  move_keys<T, D>(a.p, list / a.p.kv_heads, list % a.p.kv_heads, from, from + a.most, n);
+  const int list = blockIdx.x % lists, count = a.counts[list], step = (int)(gridDim.x / lists) * MOVE_WAVES * MOVE_EACH;
+  const int32_t* const from = a.lists + (int64_t)list * 2 * a.most;
+  for (int i = ((int)(blockIdx.x / lists) * MOVE_WAVES + threadIdx.x / WAVE) * MOVE_EACH; i < count; i += step)
+    move_keys<T, D>(a.p, list / a.p.kv_heads, list % a.p.kv_heads, from + i, from + a.most + i, min(count - i, MOVE_EACH));
 }
 
 int64_t list_of(const lram_paged& p, int64_t budget) {
   return std::max<int64_t>(0, std::min(budget, p.width * p.page - budget));
 }
 
-// Workgroups of the second kernel.
+// Workgroups of the second kernel: no more than fill the card, since a step that moves a few keys leaves it nothing.
+constexpr int64_t MOVE_GROUPS = 4096;
 int64_t groups_of(const lram_paged& p, int64_t budget) {
-  const int64_t most = list_of(p, budget), each = MOVE_WAVES * MOVE_EACH;
-  return most <= MOVED_HERE ? 0 : (int64_t)p.batch * p.kv_heads * ((most + each - 1) / each);
+  const int64_t most = list_of(p, budget), each = MOVE_WAVES * MOVE_EACH, lists = (int64_t)p.batch * p.kv_heads;
+  if (most <= MOVED_HERE || lists == 0) return 0;
+  return lists * std::max<int64_t>(1, std::min((most + each - 1) / each, MOVE_GROUPS / lists));
 }
 
 size_t workspace_of(const lram_paged& p, int64_t budget) {

@@ -370,7 +370,7 @@ class PagedCache:
         if torch.cuda.is_current_stream_capturing():
             self._captured = True
             paged_extend(self.table, seqs)
-            return seqs._replace(max_k=self.capacity)
+            return seqs._replace(max_k=min(self.capacity, max(map(len, self._own), default=0) * self.page))
         lengths = [seqs.max_q] * self.batch if lengths is None else lengths
         self.reserve(lengths)
         paged_extend(self.table, seqs)

@@ -143,7 +143,10 @@ def test_workspaces_of_odd_expectations(lib, rows, max_q, max_k, batch):
     n = ctypes.c_size_t(0)
     a = _pool(rows=rows, max_q=max_q, max_k=max_k, batch=batch, width=1 << 20)
     assert lib.lram_paged_attention_workspace_bytes(a, _queries(), n) == 0
-    assert n.value <= 2 * max(2048 * 64, rows * 8) * (64 + 2) * 4
+    most = 2 * max(2048 * 64, rows * 8) * (64 + 2) * 4
+    assert n.value <= most
+    assert lib.lram_paged_attention_workspace_bytes(a, _queries(weigh=1), n) == 0
+    assert n.value <= most + (256 << 20)  # and the scores of single tokens
 
 
 def test_evict_refuses(lib):

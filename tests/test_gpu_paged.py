@@ -244,7 +244,10 @@ def test_attention(new, used, heads, kv, dim, page, dtype, bias, evicted):
     keys.weight.copy_(before[3])
     for wrong in ((1, 1), (1, 10 ** 9), (10 ** 6, 1), (0, 0)):  # expectations that say little: other divisions of the work
         s = seqs._replace(max_q=wrong[0], max_k=wrong[1])
-        ref.check(lram.paged_attention(q, keys, table, s, scale, rel), want["out"])
+        ref.check(lram.paged_attention(q, keys, table, s, scale, rel, weigh=True), want["out"])
+        got = ref.Store(keys).weight
+        assert ((got.double() - total).abs() <= more_bound + 2 * E * total.abs())[met].all() and _same(got[~met], store.weight[~met])
+        keys.weight.copy_(before[3])
     lram.paged_attention(q, keys, table, seqs, scale, rel, weigh=True)
     assert _same(keys.weight, first)  # the same bits on every call
 
