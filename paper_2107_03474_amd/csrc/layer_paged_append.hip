@@ -159,7 +159,7 @@ __device__ __forceinline__ void turn_values(const Tile& tile, const T* x, int64_
   const int lane = threadIdx.x % WAVE;
   const bool all = E == 8 && tile.from == 0 && tile.to == PAGE_BLOCK;
   // chunk i of the block, 16 bytes each, spread over the banks
-  const auto spread = [](int i) { return i ^ (i >> 3 & 7); };
+  const auto spread = [](int i) { return i ^ (i >> 6 & 7); };
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int i = lane + n * WAVE, c = i % CH, g = i / CH % 4, t1 = i / (4 * CH) * Ti::KEYS + 4 * g;
