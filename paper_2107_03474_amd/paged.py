@@ -133,8 +133,13 @@ def _describe(keys: PagedKeys, table: PageTable, heads: int = 0, rows: int = 0, 
 
 def _like_keys(t: torch.Tensor, name: str, keys: PagedKeys, dim: int):
     """(address, row stride, head stride) of new rows that go with the cache."""
-    place = _heads(t, name, t)
-    if t.dtype is not keys.k.dtype or t.device != keys.k.device or t.shape[2] != dim:
+    k, shape = keys.k, t.shape
+    if len(shape) == 3 and shape[2] == dim and t.dtype is k.dtype and t.get_device() == k.get_device() and t.is_cuda:
+        row, head, one = t.stride()
+        if one == 1:  # a dimension of size 1 has no stride to speak of
+            return t.data_ptr(), row if shape[0] > 1 else shape[1] * dim, head if shape[1] > 1 else dim
+    place = _heads(t, name, t)  # says what is wrong
+    if t.dtype is not k.dtype or t.device != k.device or shape[2] != dim:
         raise LramError("%s must have the cache's device, type and head_dim" % name)
     return place
 

@@ -110,9 +110,11 @@ def packed_positions(seqs: Packed, rows: int, first: Optional[torch.Tensor] = No
 
 
 def _rotary(plan: Rotary, like: torch.Tensor) -> _Rotary:
-    turns = plan.turns
-    return _Rotary(turns.numel(), 1 if plan.interleaved else 0, plan.magnitude,
-                   _ptr(turns, "turns", torch.int64, (turns.numel(),), like))
+    turns, interleaved, magnitude = plan
+    n = turns.numel()
+    if turns.dtype is torch.int64 and turns.dim() == 1 and turns.get_device() == like.get_device() and turns.is_contiguous():
+        return _Rotary(n, 1 if interleaved else 0, magnitude, turns.data_ptr())
+    return _Rotary(n, 1 if interleaved else 0, magnitude, _ptr(turns, "turns", torch.int64, (n,), like))  # says what is wrong
 
 
 def _refusal(dtype, dim: int, plan: Rotary, tensors) -> Optional[str]:
