@@ -3,8 +3,9 @@
 // One launch.  q: rows rotated as they lie (rotate_chunk).  k: a wave takes the rows of 16 key slots of a sequence and some of
 // their heads; a lane owns pairs of 16-byte chunks of single rows and forms their sines and cosines once for all of these
 // heads.  v: a wave takes 32 key slots; a lane takes 16 bytes of each of the 4 F keys that lie side by side in the page and
-// turns them round in its registers, and a whole block goes out by way of LDS.  Bound by HBM for prompts, by its launch for
-// single tokens.
+// turns them round in its registers, and a whole block goes out by way of LDS.  Bound by HBM for prompts (28,654 rows of 32/8
+// heads of 128 bf16, 704 MB in 150 us, 4.7 TB/s where a large copy reaches 5.1; keys and values alone 51 us, 4.6 TB/s), by its
+// launch for single tokens (32: 5.5 us).
 
 #include "layer_paged.h"
 #include "layer_rotary.h"

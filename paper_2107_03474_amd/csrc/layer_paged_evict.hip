@@ -3,8 +3,10 @@
 // Of n keys of a head the `budget` of the highest rank stay: (newest ones first, weight, lowest position) as one 64-bit number
 // whose order is theirs, found by a radix selection from the top digit down.  Attention asks for no order of its keys (their
 // positions are stored beside them), so only keys that stay and lie past the budget move, into the slots below it that
-// are left: budget - n moves at most, and one where a step adds one key.  A workgroup to a head selects, from ranks that it
-// keeps in registers; it moves a few keys itself, and leaves many to a second kernel that fills the card.
+// are left: n - budget moves at most, and one where a step adds one key.  A workgroup to a head selects, from ranks that it
+// keeps in registers; it moves a few keys itself, and leaves many to a second kernel that fills the card.  Bound by the chain of
+// dependent steps: 9 us for 256 heads of 2,049 keys, of which one goes; 26 us for 64 heads of 512 to 8,192 keys, many of equal
+// weight, and 35 us for the 31,000 keys that move (16 bytes of k and 2 of v lie together, so that a move touches 2 KiB of each).
 
 #include "layer_paged.h"
 
@@ -14,7 +16,7 @@ constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / WAVE;
 
 constexpr int KEPT = 16;        // ranks that a thread keeps: 16,384 of a head; those of the slots behind are formed again
 constexpr int MOVED_HERE = 64;  // keys that the selecting workgroup moves itself
-constexpr int MOVE_WAVES = 4, MOVE_EACH = 4;  // of the second kernel: waves of a workgroup and keys of a wave (16: 10 us more for 57,000 keys)
+constexpr int MOVE_WAVES = 4, MOVE_EACH = 4;  // of the second kernel: waves of a workgroup and keys of a wave (16: 10 us more for 31,000 keys)
 
 struct Evict {
   Pool p;
@@ -59,26 +61,25 @@ __device__ __forceinline__ int before(bool yes, int* sums, int& all) {
   return n;
 }
 
-// n <= 64 keys of a head to other slots, by a wave.
+// n <= MOVE_EACH keys of a head to other slots, by a wave: everything is on its way before the first is stored.
 template <typename T, int D>
 __device__ __forceinline__ void move_keys(const Pool& p, int b, int head, const int32_t* from, const int32_t* to, int n) {
   using Ti = PageTile<T>;
-  constexpr int E = Ti::E, CH = D / E, AT_ONCE = 4;
+  using C = typename Chunk<T>::type;
+  constexpr int E = Ti::E, CH = D / E, OF_K = (MOVE_EACH * CH + WAVE - 1) / WAVE, OF_V = MOVE_EACH * D / WAVE;
   const int lane = threadIdx.x % WAVE;
   // lane i: the rows of the pool that key i leaves and takes, and whether it has both
   int64_t f = 0, t = 0;
   bool moves = false;
+  int position = 0;
+  float weight = 0;
   if (lane < n) {
     const int sf = from[lane], st = to[lane], pf = page_of(p, b, sf), pt = page_of(p, b, st);
     moves = pf >= 0 && pt >= 0;
     f = page_rows(p, max(pf, 0), head) + (sf & (p.page - 1));
     t = page_rows(p, max(pt, 0), head) + (st & (p.page - 1));
-    if (moves) {
-      const int position = p.position[f];
-      const float weight = p.weight[f];
-      p.position[t] = position;
-      p.weight[t] = weight;
-    }
+    position = p.position[f];
+    weight = p.weight[f];
   }
   const auto key_at = [](int64_t row, int c) {  // pages hold whole blocks, so that a row's place in its block is its own
     return ((row >> 4 << 4) * D) + (int64_t)(c * 16 + (int)(row & 15)) * E;
@@ -87,35 +88,35 @@ __device__ __forceinline__ void move_keys(const Pool& p, int b, int head, const 
     const int r = (int)(row & (Ti::KEYS - 1));
     return (row - r) * D + (int64_t)((d / 16 * 4 + r % 16 / 4) * 16 + d % 16) * E + r / 16 * 4 + r % 4;
   };
-  for (int i0 = 0; i0 < n * CH; i0 += AT_ONCE * WAVE) {
-    typename Chunk<T>::type x[AT_ONCE];
+  C k[OF_K];
+  T v[OF_V];
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      const int i = i0 + j * WAVE + lane, key = min(i / CH, WAVE - 1);
-      const int64_t row = __shfl(f, key);
-      if (__shfl(moves, key) && i < n * CH) x[j] = *(const typename Chunk<T>::type*)((const T*)p.k + key_at(row, i % CH));
-    }
-#pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      const int i = i0 + j * WAVE + lane, key = min(i / CH, WAVE - 1);
-      const int64_t row = __shfl(t, key);
-      if (__shfl(moves, key) && i < n * CH) *(typename Chunk<T>::type*)((T*)p.k + key_at(row, i % CH)) = x[j];
-    }
+  for (int j = 0; j < OF_K; ++j) {
+    const int i = j * WAVE + lane, key = min(i / CH, MOVE_EACH - 1);
+    const int64_t row = __shfl(f, key);
+    if (__shfl(moves, key) && i < MOVE_EACH * CH) k[j] = *(const C*)((const T*)p.k + key_at(row, i % CH));
   }
-  for (int i0 = 0; i0 < n * D; i0 += 2 * AT_ONCE * WAVE) {
-    T x[2 * AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < 2 * AT_ONCE; ++j) {
-      const int i = i0 + j * WAVE + lane, key = min(i / D, WAVE - 1);
-      const int64_t row = __shfl(f, key);
-      if (__shfl(moves, key) && i < n * D) x[j] = ((const T*)p.v)[value_at(row, i % D)];
-    }
+  for (int j = 0; j < OF_V; ++j) {
+    const int i = j * WAVE + lane, key = i / D;
+    const int64_t row = __shfl(f, key);
+    if (__shfl(moves, key)) v[j] = ((const T*)p.v)[value_at(row, i % D)];
+  }
+  if (moves) {
+    p.position[t] = position;
+    p.weight[t] = weight;
+  }
 #pragma unroll
-    for (int j = 0; j < 2 * AT_ONCE; ++j) {
-      const int i = i0 + j * WAVE + lane, key = min(i / D, WAVE - 1);
-      const int64_t row = __shfl(t, key);
-      if (__shfl(moves, key) && i < n * D) ((T*)p.v)[value_at(row, i % D)] = x[j];
-    }
+  for (int j = 0; j < OF_K; ++j) {
+    const int i = j * WAVE + lane, key = min(i / CH, MOVE_EACH - 1);
+    const int64_t row = __shfl(t, key);
+    if (__shfl(moves, key) && i < MOVE_EACH * CH) *(C*)((T*)p.k + key_at(row, i % CH)) = k[j];
+  }
+#pragma unroll
+  for (int j = 0; j < OF_V; ++j) {
+    const int i = j * WAVE + lane, key = i / D;
+    const int64_t row = __shfl(t, key);
+    if (__shfl(moves, key)) ((T*)p.v)[value_at(row, i % D)] = v[j];
   }
 }
 
@@ -307,6 +308,7 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_paged_evict(Evict a) {
   if (threadIdx.x == 0) a.counts[list] = here ? 0 : count;
   if (here) {
     constexpr int EACH = MOVED_HERE / EVICT_WAVES;
+    static_assert(EACH <= MOVE_EACH, "a wave moves so many at once");
     const int i = wave * EACH;
     if (i < count) move_keys<T, D>(p, b, head, near[0] + i, near[1] + i, min(EACH, count - i));
   }
