@@ -4,8 +4,8 @@
 // their heads; a lane owns pairs of 16-byte chunks of single rows and forms their sines and cosines once for all of these
 // heads.  v: a wave takes 32 key slots; a lane takes 16 bytes of each of the 4 F keys that lie side by side in the page and
 // turns them round in its registers, and a whole block goes out by way of LDS.  Bound by HBM for prompts (28,654 rows of 32/8
-// heads of 128 bf16, 704 MB in 150 us, 4.7 TB/s where a large copy reaches 5.1; keys and values alone 51 us, 4.6 TB/s), by its
-// launch for single tokens (32: 5.5 us).
+// heads of 128 bf16, 704 MB in 143 us, 4.9 TB/s where a large copy reaches 5.1; q and the others in launches of their own took
+// 9 us more), by its launch for single tokens (32: 5.5 us).
 
 #include "layer_paged.h"
 #include "layer_rotary.h"
@@ -31,6 +31,14 @@ struct Tile {
   int64_t at;
   int from, to, position;
 };
+
+// A chunk into a page.  Pages are next read by other launches, most of them from other L2s, so it goes past the cache (28,654
+// rows of 32/8 heads of 128 bf16: 149 -> 143 us, keys and values alone 48 -> 40; 32,768 of 8 heads of 64 fp32 58 -> 46, of 128
+// 136 -> 143; one token of 32 sequences is as fast).  Pieces of 64 bytes of a lane lose by it (fp32 values: 136 -> 243).
+template <typename T>
+__device__ __forceinline__ void put(T* to, typename Chunk<T>::type x) {
+  __builtin_nontemporal_store(x, (typename Chunk<T>::type*)to);
+}
 
 // A lane's chunks of a row, E elements each: units i = lane, lane + 64, ... of 16 rows times D / 2 E pairs of chunks.
 template <typename T, int D, Form FORM>
@@ -137,15 +145,14 @@ __device__ __forceinline__ void turn_head(const Append& a, const Units<T, D, FOR
       if (t < tile.from || t >= tile.to) continue;
       typename Chunk<T>::type f = chunks.in[n][0], g = chunks.in[n][1];
       units.rotate(a, n, u, f, g);
-      *(typename Chunk<T>::type*)(y + place(t, c)) = f;
-      *(typename Chunk<T>::type*)(y + place(t, d)) = g;
+      put<T>(y + place(t, c), f);
+      put<T>(y + place(t, d), g);
     }
   } else {
     for (int i = lane; i < 16 * (D / E); i += WAVE) {
       const int t = i / (D / E), e0 = i % (D / E) * E;
       if (t < tile.from || t >= tile.to) continue;
-      *(typename Chunk<T>::type*)(y + place(t, e0)) =
-          turned<T, E>(a, x + (tile.at + t) * stride, e0, tile.position + t);
+      put<T>(y + place(t, e0), turned<T, E>(a, x + (tile.at + t) * stride, e0, tile.position + t));
     }
   }
 }
@@ -200,7 +207,7 @@ __device__ __forceinline__ void turn_values(const Tile& tile, const T* x, int64_
   if (!all) return;
 #pragma unroll
   for (int n = 0; n < PAGE_BLOCK * CH / WAVE; ++n)
-    *(typename Chunk<T>::type*)(y + (lane + n * WAVE) * E) = lds[spread(lane + n * WAVE)];
+    put<T>(y + (lane + n * WAVE) * E, lds[spread(lane + n * WAVE)]);
 }
 
 // Where the tiles of SLOTS slots lie.  Sequence b has the places from start[b] / SLOTS + 2 b on, as many as its n rows can
