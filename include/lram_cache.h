@@ -124,13 +124,16 @@ int lram_paged_attention(const lram_paged* p, const lram_paged_queries* a, void*
 /*
  * lram_paged_evict -- cuts the sequences that use more than `budget` keys down to it, for each key head by itself.  What stays:
  * the keys of the positions from seen - recent on, and of the others those of the largest weight; of equal weights the lowest
- * position, of equal positions the lowest slot.  A weight
- * that is NaN counts as less than any, and a slot below the budget that lies in no page is taken.  Those that stay past slot `budget` move, in their order, into the slots below that
- * are left, with their positions and weights; used is left as it is (every layer's pool is cut by the same lengths) and is
- * min(used, budget) from then on.  1 <= budget, 0 <= recent <= budget.  rows, start, max_q are not read.
+ * position, of equal positions the lowest slot.  A weight that is NaN counts as less than any, and a slot below the budget that
+ * lies in no page is taken.  Those that stay past slot `budget` move, in their order, into the slots below that are left, with
+ * their positions and weights.  used is left as it is, since every layer's pool is cut by the same lengths: lram_paged_shrink
+ * follows the last of them.  1 <= budget, 0 <= recent <= budget.  rows, start, max_q are not read.
  */
 int lram_paged_evict_workspace_bytes(const lram_paged* p, int64_t budget, size_t* bytes);
 int lram_paged_evict(const lram_paged* p, int64_t budget, int64_t recent, void* workspace, size_t ws_bytes, void* stream);
+
+/* lram_paged_shrink -- used[b] = min(used[b], budget), budget >= 1. */
+int lram_paged_shrink(int64_t budget, int32_t batch, int32_t* used, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,6 +1,6 @@
-// layer_paged_append.hip -- part of liblram: new rows into the pages of the cache.
+// layer_paged_append.hip -- part of liblram: new rows into the pages of the cache, and the lengths of its sequences.
 //
-// One launch.  q: rows rotated as they lie (rotate_chunk).  k: a wave takes the rows of 16 key slots of a sequence and some of
+// Append is one launch.  q: rows rotated as they lie (rotate_chunk).  k: a wave takes the rows of 16 key slots of a sequence and some of
 // their heads; a lane owns pairs of 16-byte chunks of single rows and forms their sines and cosines once for all of these
 // heads.  v: a wave takes 32 key slots; a lane takes 16 bytes of each of the 4 F keys that lie side by side in the page and
 // turns them round in its registers, and a whole block goes out by way of LDS.  Bound by HBM for prompts (28,654 rows of 32/8
@@ -337,6 +337,10 @@ __global__ __launch_bounds__(EXTEND_THREADS) void k_paged_extend(const int32_t* 
   used[b] += n;
   seen[b] += n;
 }
+__global__ __launch_bounds__(EXTEND_THREADS) void k_paged_shrink(int budget, int batch, int32_t* used) {
+  const int b = blockIdx.x * EXTEND_THREADS + threadIdx.x;
+  if (b < batch && used[b] > budget) used[b] = budget;
+}
 
 }  // namespace
 
@@ -348,6 +352,15 @@ int lram_paged_extend(const int32_t* start, int32_t batch, int32_t* used, int32_
   if (!start || !used || !seen || off_align(start, 4) || off_align(used, 4) || off_align(seen, 4)) return LRAM_EINVAL;
   hipLaunchKernelGGL(k_paged_extend, dim3((unsigned)((batch + EXTEND_THREADS - 1) / EXTEND_THREADS)), dim3(EXTEND_THREADS), 0,
                      (hipStream_t)stream, start, (int)batch, used, seen);
+  return layer_launched();
+}
+
+int lram_paged_shrink(int64_t budget, int32_t batch, int32_t* used, void* stream) {
+  if (budget < 1 || batch < 0 || batch > 1 << 20) return LRAM_EINVAL;
+  if (batch == 0) return LRAM_OK;
+  if (!used || off_align(used, 4)) return LRAM_EINVAL;
+  hipLaunchKernelGGL(k_paged_shrink, dim3((unsigned)((batch + EXTEND_THREADS - 1) / EXTEND_THREADS)), dim3(EXTEND_THREADS), 0,
+                     (hipStream_t)stream, (int)std::min<int64_t>(budget, INT32_MAX), (int)batch, used);
   return layer_launched();
 }
 

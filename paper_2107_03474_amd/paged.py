@@ -53,6 +53,7 @@ def _library():
         lib.lram_paged_attention.argtypes = [A, Q, _P, _P, SZ, _P]
         lib.lram_paged_evict_workspace_bytes.argtypes = [A, _I64, SZP]
         lib.lram_paged_evict.argtypes = [A, _I64, _I64, _P, SZ, _P]
+        lib.lram_paged_shrink.argtypes = [_I64, _I32, _P, _P]
         _lib = lib
     return _lib
 
@@ -110,6 +111,8 @@ def _describe(keys: PagedKeys, table: PageTable, heads: int = 0, rows: int = 0, 
     k, v, position, weight = keys
     if k.dim() != 6 or position.dim() != 3:
         raise LramError("keys must be PagedKeys: k [pages, kv_heads, page / 16, head_dim / e, 16, e]")
+    if not k.is_cuda:
+        raise LramError("keys must be GPU tensors")
     pages, kv, page = position.shape
     e = 16 // k.element_size()
     dim = k.shape[3] * e
@@ -286,9 +289,13 @@ def paged_evict(keys: PagedKeys, table: PageTable, budget: int, recent: int = 0,
 
 def paged_shrink(table: PageTable, budget: int) -> None:
     """used = min(used, budget): once every layer's pages are cut down to the budget."""
-    if budget < 1:
+    if not 1 <= budget < 1 << 62:
         raise LramError("a budget is at least 1")
-    table.used.clamp_(max=min(budget, 2 ** 31 - 1))
+    used = table.used
+    batch = used.numel()
+    rc = _launch(used.device, _library().lram_paged_shrink, budget, batch, _ptr(used, "used", torch.int32, (batch,), used))
+    if rc:
+        _check(rc)
 
 
 def paged_read(keys: PagedKeys, table: PageTable, b: int) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:

@@ -26,7 +26,7 @@ def lib():
 def test_every_declared_symbol_is_exported(lib):
     txt = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "lram_cache.h")).read(), flags=re.S)
     names = set(re.findall(r"\b(lram_[a-z_0-9]+)\s*\(", txt))
-    assert len(names) == 8
+    assert len(names) == 9
     out = subprocess.run(["nm", "-D", "--defined-only", lram.library_path()], capture_output=True, text=True, check=True).stdout
     assert names <= set(re.findall(r"\bT (lram_[a-z_0-9]+)", out))
 
@@ -165,6 +165,19 @@ def test_evict_refuses(lib):
     assert lib.lram_paged_evict(_pool(), 2560, 10, None, 0, None) == 0  # nothing can be over the budget
     assert lib.lram_paged_evict(_pool(), 1 << 60, 10, None, 0, None) == 0
     assert lib.lram_paged_evict(_pool(batch=0), 100, 10, None, 0, None) == 0
+    for bad in ((0, 3, P), (10, -1, P), (10, (1 << 20) + 1, P), (10, 3, None), (10, 3, P + 2)):
+        assert lib.lram_paged_shrink(*bad, None) == EINVAL, bad
+    assert lib.lram_paged_shrink(10, 0, None, None) == 0
+
+
+def test_tensors_of_the_host_are_refused(lib):
+    keys, table = lram.paged_keys(4, 2, 32, weigh=True, device="cpu"), lram.page_table(2, 2, device="cpu")
+    seqs, rows = lram.pack([1, 1], device="cpu"), torch.zeros((2, 2, 32), dtype=torch.bfloat16)
+    for call in (lambda: lram.paged_evict(keys, table, 1), lambda: lram.paged_shrink(table, 1), lambda: lram.paged_extend(table, seqs),
+                 lambda: lram.paged_append(rows, rows, keys, table, seqs), lambda: lram.paged_attention(rows, keys, table, seqs),
+                 lambda: lram.rotary_forward(rows, None, table.used, lram.rotary_plan(32, device="cpu"))):
+        with pytest.raises(lram.LramError, match="GPU tensor"):
+            call()
 
 
 def test_frequencies():

@@ -366,6 +366,8 @@ def test_keys_past_four_gigabytes():
         assert torch.equal(got[2], torch.arange(n, device=DEV, dtype=torch.int32)[:, None].expand(n, kv))
         assert ((got[3].sum(0) - n).abs() < 1e-2).all()  # each query gives away 1
     lram.paged_evict(keys, table, 200, 10)
+    lram.paged_shrink(table, 1 << 40)
+    assert table.used.tolist() == new
     lram.paged_shrink(table, 200)
     assert [len(lram.paged_read(keys, table, b)[0]) for b in (0, 1)] == [200, 200]
 
