@@ -341,9 +341,15 @@ class PagedCache:
         return len(self._free)
 
     def refresh(self) -> List[int]:
-        """The sequences' lengths, read back (waits for the device)."""
-        self._used = self.table.used.clamp(max=self.capacity).tolist()
-        return list(self._used)
+        """The sequences' lengths, read back (waits for the device).  Refused where captured steps have counted rows past what
+        was reserved, which are not in the cache: ``release`` ends such sequences."""
+        used = self.table.used.tolist()
+        for b, (n, own) in enumerate(zip(used, self._own)):
+            if n > min(self.capacity, len(own) * self.page):
+                raise LramError("sequence %d has counted %d keys, and %d were reserved" %
+                                (b, n, min(self.capacity, len(own) * self.page)))
+        self._used = used
+        return list(used)
 
     def _missing(self, lengths) -> Tuple[Optional[str], List[int]]:
         more = [max(0, -(-(u + n) // self.page) - len(own)) for u, n, own in zip(self._used, lengths, self._own)]
@@ -376,7 +382,8 @@ class PagedCache:
 
     def extend(self, seqs: Packed, lengths: Optional[Sequence[int]] = None) -> Packed:
         """Counts the new rows that seqs packs (start_q), with pages for them; the plan of the step's appends and attention.
-        lengths: the numbers of them, where the host knows them (else every sequence is taken to have max_q)."""
+        lengths: the numbers of them, where the host knows them (else every sequence is taken to have max_q, which must then
+        be no less)."""
         if seqs.start_q.numel() != self.batch + 1:
             raise ValueError("the plan must be of the cache's %d sequences" % self.batch)
         if torch.cuda.is_current_stream_capturing():
@@ -394,7 +401,10 @@ class PagedCache:
         for keys in self.keys:
             paged_evict(keys, self.table, budget, recent)
         paged_shrink(self.table, budget)
-        self._used = [min(u, budget) for u in self._used]
+        if torch.cuda.is_current_stream_capturing():  # nothing is cut yet
+            self._captured = True
+        else:
+            self._used = [min(u, budget) for u in self._used]
 
     def _give_back(self, keep: Sequence[int]) -> None:
         for b, n in enumerate(keep):

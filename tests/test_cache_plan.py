@@ -231,6 +231,19 @@ def test_pages_are_given_out_and_back():
     assert c._used == [33, 0, 1]
     c.release([0, 2])
     assert c.free_pages() == 10 and (c.table.table < 0).all() and c.table.used.tolist() == [0, 0, 0]
+    c.reserve([32, 0, 70])
+    c.table.used.copy_(torch.tensor([33, 0, 70]))  # a replayed step went on past what was reserved
+    c._captured = True
+    for call in (c.refresh, c.trim, lambda: c.reserve([0, 0, 0])):
+        with pytest.raises(lram.LramError, match="sequence 0 has counted 33 keys, and 32 were reserved"):
+            call()
+    c.release([0])
+    c.reserve([0, 0, 30])
+    assert c.free_pages() == 6 and c.refresh() == [0, 0, 70]
+    c.table.used[2] = 101
+    with pytest.raises(lram.LramError, match="101 keys, and 100 were"):
+        c.refresh()
+    c.release([0, 2])
     for bad in ([1, 2], [1, 2, -3]):
         with pytest.raises(ValueError, match="lengths"):
             c.reserve(bad)

@@ -540,6 +540,31 @@ def test_a_captured_step_replayed():
     assert captured.refresh() == eager.refresh() == used
 
 
+def test_a_captured_eviction_is_no_cut_yet():
+    """Only the eviction is captured: until it is replayed the host gives pages out by the lengths as they are."""
+    cache = lram.PagedCache(1, 4, 1, 32, page=32, dtype=BF16, weigh=True)
+    rows = torch.randn((60, 1, 32), generator=_gen(21), device=DEV).to(BF16)
+
+    def append(n):
+        lram.paged_append(rows[:n], rows[:n], cache.keys[0], cache.table, cache.extend(lram.pack([n])))
+
+    append(60)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        lram.paged_evict(cache.keys[0], cache.table, 60)  # the first call of the kernels: nothing is over the budget
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.evict(30)
+    append(10)
+    assert len(lram.paged_read(cache.keys[0], cache.table, 0)[0]) == 70  # refuses where a page is missing
+    graph.replay()
+    append(5)
+    assert cache.refresh() == [35]
+    assert lram.paged_read(cache.keys[0], cache.table, 0)[2].flatten().tolist()[30:] == list(range(70, 75))
+
+
 def test_two_streams_at_once():
     """Two readers of a cache and a writer of another, each on a stream of its own."""
     g = _gen(15)
