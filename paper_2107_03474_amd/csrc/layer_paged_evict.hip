@@ -6,7 +6,7 @@
 // are left: n - budget moves at most, and one where a step adds one key.  A workgroup to a head selects, from ranks that it
 // keeps in registers; it moves a few keys itself, and leaves many to a second kernel that fills the card.  Bound by the chain of
 // dependent steps: 9 us for 256 heads of 2,049 keys, of which one goes; 26 us for 64 heads of 512 to 8,192 keys, many of equal
-// weight, and 35 us for the 31,000 keys that move (16 bytes of k and 2 of v lie together, so that a move touches 2 KiB of each).
+// weight, and 34 us for the 31,000 keys that move (16 bytes of k and 2 of v lie together, so that a move touches 2 KiB of each).
 
 #include "layer_paged.h"
 
