@@ -100,38 +100,47 @@ def page_table(batch: int, width: int, device="cuda") -> PageTable:
     return PageTable(torch.full((batch, width), -1, **i32), torch.zeros(batch, **i32), torch.zeros(batch, **i32))
 
 
-def _at(t: torch.Tensor, name: str, dtype: torch.dtype, shape, like: torch.Tensor, index: int) -> int:
-    """Device address of a contiguous tensor of this type and shape on like's device, whose index this is."""
-    if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
-        return t.data_ptr()
-    return _ptr(t, name, dtype, shape, like)  # says what is wrong
-
-
 def _describe(keys: PagedKeys, table: PageTable, heads: int = 0, rows: int = 0, seqs: Optional[Packed] = None) -> _Paged:
     k, v, position, weight = keys
-    if k.dim() != 6 or position.dim() != 3:
+    where, used, seen = table
+    of_k, of_position, of_table, of_used = k.shape, position.shape, where.shape, used.shape
+    if len(of_k) != 6 or len(of_position) != 3:
         raise LramError("keys must be PagedKeys: k [pages, kv_heads, page / 16, head_dim / e, 16, e]")
     if not k.is_cuda:
         raise LramError("keys must be GPU tensors")
-    pages, kv, page = position.shape
-    e = 16 // k.element_size()
-    dim = k.shape[3] * e
+    dt, i32, on = k.dtype, torch.int32, k.get_device()
+    code, e = _type(k, "k"), 8 if dt is torch.bfloat16 else 4
+    pages, kv, page = of_position
+    dim = of_k[3] * e
     if page not in PAGE_SIZES or dim not in HEAD_DIMS:
         raise LramError("pages hold 32, 64, 128 or 256 keys of head_dim 32, 64 or 128")
-    batch = table.used.shape[0] if table.used.dim() == 1 else -1
-    if table.table.dim() != 2 or batch < 0:
+    if len(of_table) != 2 or len(of_used) != 1:
         raise LramError("table must be [batch, width], used and seen [batch]")
-    width, i32 = table.table.shape[1], torch.int32
-    on, dt = k.get_device(), k.dtype
-    return _Paged(_type(k, "k"), heads or kv, kv, dim, batch, page, pages, width,
-                  _at(k, "k", dt, (pages, kv, page // 16, dim // e, 16, e), k, on),
-                  _at(v, "v", dt, (pages, kv, page // (4 * e), dim // 16, 4, 16, e), k, on),
-                  _at(position, "position", i32, (pages, kv, page), k, on),
-                  None if weight is None else _at(weight, "weight", torch.float32, (pages, kv, page), k, on),
-                  _at(table.table, "table", i32, (batch, width), k, on), _at(table.used, "used", i32, (batch,), k, on),
-                  _at(table.seen, "seen", i32, (batch,), k, on),
-                  *((None, 0, 0, 0) if seqs is None else
-                    (_at(seqs.start_q, "start_q", i32, (batch + 1,), k, on), rows, seqs.max_q, seqs.max_k)))
+    batch, width = of_used[0], of_table[1]
+    as_k, as_v = (pages, kv, page // 16, of_k[3], 16, e), (pages, kv, page // (4 * e), dim // 16, 4, 16, e)
+    # one test for what is right, since small calls are bound by the host: a call for each tensor takes 1.5 us more
+    if not (of_k == as_k and k.is_contiguous() and
+            v.shape == as_v and v.dtype is dt and v.get_device() == on and v.is_contiguous() and
+            position.dtype is i32 and position.get_device() == on and position.is_contiguous() and
+            (weight is None or weight.shape == of_position and weight.dtype is torch.float32 and weight.get_device() == on and
+             weight.is_contiguous()) and
+            of_table[0] == batch and where.dtype is i32 and where.get_device() == on and where.is_contiguous() and
+            used.dtype is i32 and used.get_device() == on and used.is_contiguous() and
+            seen.shape == of_used and seen.dtype is i32 and seen.get_device() == on and seen.is_contiguous()):
+        _ptr(k, "k", dt, as_k, k)  # one of these says what is wrong
+        _ptr(v, "v", dt, as_v, k)
+        _ptr(position, "position", i32, of_position, k)
+        if weight is not None:
+            _ptr(weight, "weight", torch.float32, of_position, k)
+        _ptr(where, "table", i32, (batch, width), k)
+        _ptr(used, "used", i32, (batch,), k)
+        _ptr(seen, "seen", i32, (batch,), k)
+    start = max_q = max_k = 0
+    if seqs is not None:
+        start, max_q, max_k = _ptr(seqs.start_q, "start_q", i32, (batch + 1,), k), seqs.max_q, seqs.max_k
+    return _Paged(code, heads or kv, kv, dim, batch, page, pages, width, k.data_ptr(), v.data_ptr(), position.data_ptr(),
+                  None if weight is None else weight.data_ptr(), where.data_ptr(), used.data_ptr(), seen.data_ptr(), start or None,
+                  rows, max_q, max_k)
 
 
 def _like_keys(t: torch.Tensor, name: str, keys: PagedKeys, dim: int):
