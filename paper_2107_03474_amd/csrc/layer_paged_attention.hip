@@ -376,8 +376,13 @@ __device__ __forceinline__ void join_rows(const Attend& a, int64_t id, int rows_
   const int64_t step = p.rows * p.heads;
   for (int i = first; i < s.nq; i += rows_each) {
     const int64_t place = (s.q0 + i) * p.heads + h;
-    float top = -INFINITY;
-    for (int n = threadIdx.x; n < pieces; n += ATTEND_THREADS) top = fmaxf(top, a.stat[n * step + place].x);
+    const auto stat = [&](int n) { return a.stat[n * step + place]; };
+    const auto part = [&](int n) { return *(const f32x4*)(a.part + (n * step + place) * D + d); };
+    float top = stat(min((int)threadIdx.x, pieces - 1)).x;
+    const int own = min(team, pieces - 1);
+    const float2 st0 = stat(own);  // on their way while the maximum is found
+    const f32x4 y0 = part(own);
+    for (int n = threadIdx.x + ATTEND_THREADS; n < pieces; n += ATTEND_THREADS) top = fmaxf(top, stat(n).x);
 #pragma unroll
     for (int o = WAVE / 2; o; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
     if (threadIdx.x % WAVE == 0) tops[threadIdx.x / WAVE] = top;
@@ -385,14 +390,14 @@ __device__ __forceinline__ void join_rows(const Attend& a, int64_t id, int rows_
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     float sum = 0;
     f32x4 x = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int n = team; n < pieces; n += TEAMS) {
-      const float2 st = a.stat[n * step + place];
-      const f32x4 y = *(const f32x4*)(a.part + (n * step + place) * D + d);
+    const auto add = [&](float2 st, f32x4 y) {
       const float f = st.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.x - top);
       sum += st.x == -INFINITY ? st.y : st.y * f;
       x += y * f;
-    }
+    };
+    if (team < pieces) add(st0, y0);
+#pragma unroll 4
+    for (int n = team + TEAMS; n < pieces; n += TEAMS) add(stat(n), part(n));
     *(f32x4*)&parts[team][d] = x;
     if (d == 0) sums[team] = sum;
     __syncthreads();
@@ -429,7 +434,7 @@ __device__ __forceinline__ float2 whole_of(const Attend& a, int64_t place, int p
 }
 
 // The weight that each key gathers, in a fixed order, beside the join.  Of a single token's few columns the scores were kept (16
-// bytes a key for four heads that share it, beside the 256 of its k); a thread then takes four keys.  Otherwise a workgroup
+// bytes a key for four heads that share it, beside the 256 of its k); a thread then takes four keys of each stretch.  Otherwise a workgroup
 // keeps a block of keys and forms their scores again, its waves sharing out the sequence's queries.
 constexpr int WEIGH_CHUNK = 4 * ATTEND_THREADS;  // keys of a workgroup
 template <typename T, int D, bool BIAS>
@@ -453,35 +458,44 @@ __global__ __launch_bounds__(ATTEND_THREADS, sizeof(T) * D == 512 ? 3 : 4) void 
   const int pieces = pieces_of(a, s);
   if (keeps_scores(a, s)) {
     const int cols = s.nq * p.group, mine = threadIdx.x / 16;
+    const int64_t met = keys_met(s, s.nq - 1);  // scores were kept of these
+    f32x4 x[16], had, *w = nullptr;
+    const auto load = [&](int64_t slot) {
+      w = nullptr;
+      const int page = slot < met ? page_of(p, b, (int)slot) : -1;
+      if (page < 0) return;
+      w = (f32x4*)(p.weight + page_rows(p, page, head) + (slot & (p.page - 1)));
+      had = *w;
+      const float* const z = a.scores + (int64_t)(b * p.kv_heads + head) * a.score_cols * a.scored + slot;
+#pragma unroll
+      for (int c = 0; c < 16; ++c)
+        if (c < cols) x[c] = *(const f32x4*)(z + c * a.scored);
+    };
+    int64_t slot = first * chunk + 4 * threadIdx.x;
+    load(slot);  // on its way while the sums are formed
     if (mine < cols) {
       const int64_t place = (s.q0 + mine / p.group) * p.heads + head * p.group + mine % p.group;
       const float2 st = whole_of(a, place, pieces, threadIdx.x % 16, 16);
       if (threadIdx.x % 16 == 0) whole[mine] = st;
     }
     __syncthreads();
-    const int64_t met = keys_met(s, s.nq - 1);  // scores were kept of these
-    for (int64_t base = first * chunk; base < met; base += (int64_t)chunks * chunk) {
-      const int end = (int)min(base + chunk, met);
-      for (int slot = (int)base + 4 * threadIdx.x; slot < end; slot += 4 * ATTEND_THREADS) {
-        const int page = page_of(p, b, slot);
-        if (page < 0) continue;
-        const float* const z = a.scores + (int64_t)(b * p.kv_heads + head) * a.score_cols * a.scored + slot;
-        f32x4* const w = (f32x4*)(p.weight + page_rows(p, page, head) + (slot & (p.page - 1)));
-        const f32x4 had = *w;
+    while (slot < met) {
+      if (w) {
         f32x4 got = {0, 0, 0, 0};
-#pragma unroll 8
-        for (int c = 0; c < cols; ++c) {
-          const f32x4 x = *(const f32x4*)(z + c * a.scored);
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            got[r] += x[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x[r] - whole[c].x) * whole[c].y;
-        }
+        for (int c = 0; c < 16; ++c)
+          if (c < cols)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              got[r] += x[c][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x[c][r] - whole[c].x) * whole[c].y;
         if (slot + 4 <= met) {
           *w = had + got;
         } else {
           for (int r = 0; slot + r < met; ++r) ((float*)w)[r] = had[r] + got[r];
         }
       }
+      slot += (int64_t)chunks * chunk;
+      load(slot);
     }
     return;
   }
@@ -591,11 +605,15 @@ struct Plan {
 // Pieces: a round of two workgroups a unit for a single sequence, and up to four rounds for several, which are rarely of one
 // length (us of one round / four: one token over 131,072 keys, 32/8 heads of 128 bf16 with weights, 123 / 130; 32 tokens over
 // 256 to 8,192 keys 107 / 97).
+// The least piece is 128 keys where workgroups are fewer than units even so, and few parts are joined (us of kernels, 256 / 128:
+// one token over 4,000 keys, 32/8 heads of 128 fp32 with weights 15.5 / 13.0, over 1,500 in bf16 10.9 / 10.2; 50 over 1,000, 16/8
+// heads of 64 fp32, 16.6 / 14.3; with more of them: four over 1,500, 32/8 heads of 128 bf16, 9.8 / 10.7; one over 20,000 of one
+// head of 64 10.1 / 11.0, for its join), otherwise 256.
 // Few keys take one piece, which needs no join (us of a call / of its kernels, one piece and pieces of 256: one token over 777
 // keys, 8 heads of 64 bf16, 15.9 / 8.3 and 19.9 / 9.0; four over 300, 32/8 heads of 128, 13.9 / 7.4 and 17.8 / 9.7, with
 // weights 17.9 / 12.1 and 18.0 / 11.0; over 777 of these 13.9 / 12.0 and 17.8 / 10.3).  Results are the same with weights
 // and without.
-constexpr int64_t PIECE_STEP = 128, PIECE_LEAST = 256, ROUND = 512, ROUNDS = 4;
+constexpr int64_t PIECE_STEP = 128, PIECE_LEAST = 256, ROUND = 512, ROUNDS = 4, UNITS = 256, JOINED = 64;
 constexpr int64_t FEW_BYTES = 256 << 10;  // of a sequence's keys and values of a head
 constexpr int64_t SCORE_BYTES = 256 << 20;
 constexpr int64_t WEIGH_GROUPS = 8192;  // more go over several stretches each: where few keys are met of many expected, they only start
@@ -613,7 +631,8 @@ Plan plan_of(const lram_paged& p, bool weigh) {
   x.tiles = std::max<int64_t>(1, std::min(over(tokens * G, x.cols), MOST_GROUPS / lists));
   const int64_t wanted = std::min(over(ROUND * std::min<int64_t>(std::max(p.batch, 1), ROUNDS), lists * x.tiles), MOST_GROUPS / (lists * x.tiles));
   x.piece = over(over(keys, std::max<int64_t>(1, wanted)), PIECE_STEP) * PIECE_STEP;
-  x.piece = std::max(x.piece, PIECE_LEAST);
+  const int64_t most_pieces = over(keys, PIECE_STEP);
+  x.piece = std::max(x.piece, most_pieces <= JOINED && lists * x.tiles * most_pieces <= UNITS ? PIECE_STEP : PIECE_LEAST);
   if (keys * p.head_dim * 2 * (int64_t)elem_size(p.dtype) <= FEW_BYTES) x.piece = over(keys, PIECE_STEP) * PIECE_STEP;
   x.pieces = over(keys, x.piece);
   const size_t places = (size_t)p.rows * p.heads;
