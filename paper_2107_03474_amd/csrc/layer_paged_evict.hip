@@ -5,8 +5,8 @@
 // positions are stored beside them), so only keys that stay and lie past the budget move, into the slots below it that
 // are left: n - budget moves at most, and one where a step adds one key.  A workgroup to a head selects, from ranks that it
 // keeps in registers; it moves a few keys itself, and leaves many to a second kernel that fills the card.  Bound by the chain of
-// dependent steps: 9 us for 256 heads of 2,049 keys, of which one goes; 26 us for 64 heads of 512 to 8,192 keys, many of equal
-// weight, and 34 us for the 31,000 keys that move (16 bytes of k and 2 of v lie together, so that a move touches 2 KiB of each).
+// dependent steps: 8 us for 256 heads of 2,049 keys, of which one goes; 26 us for 64 heads of 512 to 8,192 keys, many of equal
+// weight, and 32 us for the 31,000 keys that move (16 bytes of k and 2 of v lie together, so that a move touches 2 KiB of each).
 
 #include "layer_paged.h"
 
@@ -61,63 +61,86 @@ __device__ __forceinline__ int before(bool yes, int* sums, int& all) {
   return n;
 }
 
-// n <= MOVE_EACH keys of a head to other slots, by a wave: everything is on its way before the first is stored.
+// n <= MOVE_EACH keys of a head on their way to other slots, by a wave: all are read before the first is stored.  Lane i holds
+// the place of key i.
 template <typename T, int D>
-__device__ __forceinline__ void move_keys(const Pool& p, int b, int head, const int32_t* from, const int32_t* to, int n) {
+struct Moving {
   using Ti = PageTile<T>;
   using C = typename Chunk<T>::type;
-  constexpr int E = Ti::E, CH = D / E, OF_K = (MOVE_EACH * CH + WAVE - 1) / WAVE, OF_V = MOVE_EACH * D / WAVE;
-  const int lane = threadIdx.x % WAVE;
-  // lane i: the rows of the pool that key i leaves and takes, and whether it has both
-  int64_t f = 0, t = 0;
-  bool moves = false;
-  int position = 0;
-  float weight = 0;
-  if (lane < n) {
-    const int sf = from[lane], st = to[lane], pf = page_of(p, b, sf), pt = page_of(p, b, st);
-    moves = pf >= 0 && pt >= 0;
-    f = page_rows(p, max(pf, 0), head) + (sf & (p.page - 1));
-    t = page_rows(p, max(pt, 0), head) + (st & (p.page - 1));
-    position = p.position[f];
-    weight = p.weight[f];
-  }
-  const auto key_at = [](int64_t row, int c) {  // pages hold whole blocks, so that a row's place in its block is its own
-    return ((row >> 4 << 4) * D) + (int64_t)(c * 16 + (int)(row & 15)) * E;
-  };
-  const auto value_at = [](int64_t row, int d) {
-    const int r = (int)(row & (Ti::KEYS - 1));
-    return (row - r) * D + (int64_t)((d / 16 * 4 + r % 16 / 4) * 16 + d % 16) * E + r / 16 * 4 + r % 4;
-  };
+  static constexpr int E = Ti::E, CH = D / E, OF_K = (MOVE_EACH * CH + WAVE - 1) / WAVE, OF_V = MOVE_EACH * D / WAVE;
   C k[OF_K];
   T v[OF_V];
+  int position;
+  float weight;
+  bool has;  // the key lies in a page
+
+  static __device__ __forceinline__ int64_t key_at(int64_t row, int c) {  // pages hold whole blocks, so that a row's place in
+    return ((row >> 4 << 4) * D) + (int64_t)(c * 16 + (int)(row & 15)) * E;  // its block is its own
+  }
+  static __device__ __forceinline__ int64_t value_at(int64_t row, int d) {
+    const int r = (int)(row & (Ti::KEYS - 1));
+    return (row - r) * D + (int64_t)((d / 16 * 4 + r % 16 / 4) * 16 + d % 16) * E + r / 16 * 4 + r % 4;
+  }
+  static __device__ __forceinline__ int64_t row_of(const Pool& p, int page, int head, int slot) {
+    return page_rows(p, max(page, 0), head) + (slot & (p.page - 1));
+  }
+
+  __device__ __forceinline__ void load(const Pool& p, int b, int head, int slot, int n) {
+    const int lane = threadIdx.x % WAVE;
+    int64_t f = 0;
+    has = false;
+    if (lane < n) {
+      const int page = page_of(p, b, slot);
+      has = page >= 0;
+      f = row_of(p, page, head, slot);
+      position = p.position[f];
+      weight = p.weight[f];
+    }
 #pragma unroll
-  for (int j = 0; j < OF_K; ++j) {
-    const int i = j * WAVE + lane, key = min(i / CH, MOVE_EACH - 1);
-    const int64_t row = __shfl(f, key);
-    if (__shfl(moves, key) && i < MOVE_EACH * CH) k[j] = *(const C*)((const T*)p.k + key_at(row, i % CH));
-  }
+    for (int j = 0; j < OF_K; ++j) {
+      const int i = j * WAVE + lane, key = min(i / CH, MOVE_EACH - 1);
+      const int64_t row = __shfl(f, key);
+      if (__shfl(has, key) && i < MOVE_EACH * CH) k[j] = *(const C*)((const T*)p.k + key_at(row, i % CH));
+    }
 #pragma unroll
-  for (int j = 0; j < OF_V; ++j) {
-    const int i = j * WAVE + lane, key = i / D;
-    const int64_t row = __shfl(f, key);
-    if (__shfl(moves, key)) v[j] = ((const T*)p.v)[value_at(row, i % D)];
+    for (int j = 0; j < OF_V; ++j) {
+      const int i = j * WAVE + lane, key = i / D;
+      const int64_t row = __shfl(f, key);
+      if (__shfl(has, key)) v[j] = ((const T*)p.v)[value_at(row, i % D)];
+    }
   }
-  if (moves) {
-    p.position[t] = position;
-    p.weight[t] = weight;
-  }
+  __device__ __forceinline__ void store(const Pool& p, int b, int head, int slot, int n) {
+    const int lane = threadIdx.x % WAVE;
+    int64_t t = 0;
+    if (lane < n) {
+      const int page = page_of(p, b, slot);
+      has = has && page >= 0;
+      t = row_of(p, page, head, slot);
+      if (has) {
+        p.position[t] = position;
+        p.weight[t] = weight;
+      }
+    }
 #pragma unroll
-  for (int j = 0; j < OF_K; ++j) {
-    const int i = j * WAVE + lane, key = min(i / CH, MOVE_EACH - 1);
-    const int64_t row = __shfl(t, key);
-    if (__shfl(moves, key) && i < MOVE_EACH * CH) *(C*)((T*)p.k + key_at(row, i % CH)) = k[j];
-  }
+    for (int j = 0; j < OF_K; ++j) {
+      const int i = j * WAVE + lane, key = min(i / CH, MOVE_EACH - 1);
+      const int64_t row = __shfl(t, key);
+      if (__shfl(has, key) && i < MOVE_EACH * CH) *(C*)((T*)p.k + key_at(row, i % CH)) = k[j];
+    }
 #pragma unroll
-  for (int j = 0; j < OF_V; ++j) {
-    const int i = j * WAVE + lane, key = i / D;
-    const int64_t row = __shfl(t, key);
-    if (__shfl(moves, key)) ((T*)p.v)[value_at(row, i % D)] = v[j];
+    for (int j = 0; j < OF_V; ++j) {
+      const int i = j * WAVE + lane, key = i / D;
+      const int64_t row = __shfl(t, key);
+      if (__shfl(has, key)) ((T*)p.v)[value_at(row, i % D)] = v[j];
+    }
   }
+};
+template <typename T, int D>
+__device__ __forceinline__ void move_keys(const Pool& p, int b, int head, const int32_t* from, const int32_t* to, int n) {
+  const int i = min((int)threadIdx.x % WAVE, n - 1), f = from[i], t = to[i];
+  Moving<T, D> keys;
+  keys.load(p, b, head, f, n);
+  keys.store(p, b, head, t, n);
 }
 
 template <typename T, int D>
@@ -157,6 +180,8 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_paged_evict(Evict a) {
       rank[j0 + j] = Ranks{newest, budget}(page[j], (j0 + j) * EVICT_THREADS + (int)threadIdx.x, position[j], weight[j]);
   }
   if (n - budget == 1) {  // a step that adds one key: the lowest rank goes, of equal ones the last
+    Moving<T, D> last;  // the key of the last slot, which takes its place, is on its way
+    if (wave == 0) last.load(p, b, head, budget, 1);
     uint64_t lowest = ~(uint64_t)0;
     int at = -1;
     const auto look = [&](uint64_t r, int slot) {
@@ -182,11 +207,7 @@ __global__ __launch_bounds__(EVICT_THREADS) void k_paged_evict(Evict a) {
     if (threadIdx.x == 0) a.counts[list] = 0;
     if (wave) return;
     for (int w = 0; w < EVICT_WAVES; ++w) look(low_rank[w], sums[w]);
-    if (at < budget) {  // the last slot's key takes its place
-      near[0][0] = budget;
-      near[1][0] = at;
-      move_keys<T, D>(p, b, head, near[0], near[1], 1);
-    }
+    if (at < budget) last.store(p, b, head, at, 1);
     return;
   }
   // the digits of the lowest rank that stays, from the top: 11, 11 and 10 bits of either half
