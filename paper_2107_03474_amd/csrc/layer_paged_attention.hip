@@ -614,7 +614,10 @@ struct Plan {
 // weights 17.9 / 12.1 and 18.0 / 11.0; over 777 of these 13.9 / 12.0 and 17.8 / 10.3).  Results are the same with weights
 // and without.
 constexpr int64_t PIECE_STEP = 128, PIECE_LEAST = 256, ROUND = 512, ROUNDS = 4, UNITS = 256, JOINED = 64;
-constexpr int64_t FEW_BYTES = 256 << 10;  // of a sequence's keys and values of a head
+// So do more keys where heads of sequences fill a round by themselves (us, four rounds / one piece, all sequences as long as
+// said or of lengths from 16 on: 64 tokens over 1,024 keys, 32/8 heads of 128 bf16, 50.7 / 41.3 and 22.5 / 16.9, over 2,048
+// 92.7 / 81.6 and 30.2 / 27.3; over 4,096 174 / 160 and 43.3 / 46.2, which stays in pieces).
+constexpr int64_t FEW_BYTES = 256 << 10, ALONE_BYTES = 1 << 20;  // of a sequence's keys and values of a head
 constexpr int64_t SCORE_BYTES = 256 << 20;
 constexpr int64_t WEIGH_GROUPS = 8192;  // more go over several stretches each: where few keys are met of many expected, they only start
 constexpr int64_t MOST_GROUPS = ((int64_t)1 << 32) / ATTEND_THREADS - 1;
@@ -633,7 +636,8 @@ Plan plan_of(const lram_paged& p, bool weigh) {
   x.piece = over(over(keys, std::max<int64_t>(1, wanted)), PIECE_STEP) * PIECE_STEP;
   const int64_t most_pieces = over(keys, PIECE_STEP);
   x.piece = std::max(x.piece, most_pieces <= JOINED && lists * x.tiles * most_pieces <= UNITS ? PIECE_STEP : PIECE_LEAST);
-  if (keys * p.head_dim * 2 * (int64_t)elem_size(p.dtype) <= FEW_BYTES) x.piece = over(keys, PIECE_STEP) * PIECE_STEP;
+  if (keys * p.head_dim * 2 * (int64_t)elem_size(p.dtype) <= (lists * x.tiles >= ROUND ? ALONE_BYTES : FEW_BYTES))
+    x.piece = over(keys, PIECE_STEP) * PIECE_STEP;
   x.pieces = over(keys, x.piece);
   const size_t places = (size_t)p.rows * p.heads;
   if (x.pieces > 1) x.part = (size_t)x.pieces * places * p.head_dim * sizeof(float);
