@@ -197,6 +197,10 @@ ATTEND = [
     ([2, 1], [600, 70], 64, 1, 32, 32, BF16),
     ([1] * 70, list(range(70)), 4, 2, 32, 32, F32),
     ([30], [513], 3, 3, 32, 64, F32),
+    ([1], [1100], 32, 8, 128, 64, BF16),  # the least pieces
+    ([3], [1501], 8, 4, 64, 32, F32),
+    ([1] * 136, [600] + [7 * i % 41 for i in range(135)], 4, 4, 128, 64, BF16),   # heads of sequences that fill the card
+    ([1] * 136, [2100] + [7 * i % 41 for i in range(135)], 4, 4, 128, 64, BF16),  # and keys past one piece
 ]
 
 
