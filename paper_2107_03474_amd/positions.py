@@ -197,6 +197,7 @@ class Rotate(torch.autograd.Function):
     def backward(ctx, gq, gk):
         position, turns = ctx.saved_tensors
         plan = Rotary(turns, *ctx.rest)
+        gq, gk = gq if ctx.needs_input_grad[0] else None, gk if ctx.needs_input_grad[1] else None
         if gq is None and gk is None:
             return (None,) * 6
         if gq is None:

@@ -94,6 +94,11 @@ def test_gradients(interleaved):
         y.backward((ga, gb)[only].transpose(0, 1).contiguous().transpose(0, 1))  # a gradient of other strides
         assert (q.grad is None) == bool(only) and (k.grad is None) == (not only)
         ref.check((k if only else q).grad, ref.rotated((gb if only else ga), at, plan.turns, interleaved, plan.magnitude, True))
+    for only in (0, 1):  # one of the two is trained
+        x = [t.detach().requires_grad_(i == only) for i, t in enumerate((q, k))]
+        torch.autograd.backward(lram.rotary(*x, at, plan), (ga, gb))
+        assert x[1 - only].grad is None
+        ref.check(x[only].grad, ref.rotated((ga, gb)[only], at, plan.turns, interleaved, plan.magnitude, True))
     x = _randn(g, 11, 1, 32).requires_grad_()  # a gradient that is broadcast, of an odd start
     lram.rotary(x, None, at, plan)[0].sum().backward()
     ref.check(x.grad, ref.rotated(torch.ones_like(x), at, plan.turns, interleaved, plan.magnitude, True))
