@@ -192,3 +192,36 @@ def test_a_captured_call_and_a_side_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_a_captured_training_step():
+    """Forward and backward in one graph, of leaves that no other graph holds, over other values at every replay."""
+    g = _gen(5)
+    q, k = (_randn(g, 37, h, 64, dtype=BF16).requires_grad_() for h in (4, 2))
+    gq, gk = _randn(g, 37, 4, 64, dtype=BF16), _randn(g, 37, 2, 64, dtype=BF16)
+    at = torch.arange(37, dtype=torch.int32, device=DEV)
+    plan = lram.rotary_plan(48, interleaved=True)
+
+    def step():
+        a, b = lram.rotary(q, k, at, plan)
+        return (a.detach(), b.detach(), *torch.autograd.grad((a, b), (q, k), (gq, gk)))
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for _ in range(2):
+            step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for i in range(4):
+        with torch.no_grad():
+            q.copy_(_randn(g, 37, 4, 64, dtype=BF16))
+            gk.copy_(_randn(g, 37, 2, 64, dtype=BF16))
+            at.add_(77 * i)
+        eager = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, eager))
