@@ -64,6 +64,14 @@ __device__ __forceinline__ float wave_sum(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
+// Orders LDS traffic between the lanes of one wave: its LDS operations execute in the order of their issue, so that the compiler
+// is all there is to hold back.
+__device__ __forceinline__ void wave_lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 constexpr float LOG2E = 1.4426950408889634f;
 
 // A bias's weights far past any score.  From 2^24 on (a weight of 1.2e7, times log2 e) fp32 holds no digit behind the point,

@@ -205,9 +205,11 @@ __device__ __forceinline__ void turn_values(const Tile& tile, const T* x, int64_
   }
   if constexpr (E != 8) return;
   if (!all) return;
+  wave_lds_sync();  // a lane reads what others wrote
 #pragma unroll
   for (int n = 0; n < PAGE_BLOCK * CH / WAVE; ++n)
     put<T>(y + (lane + n * WAVE) * E, lds[spread(lane + n * WAVE)]);
+  wave_lds_sync();  // and the next head's block takes its place
 }
 
 // Where the tiles of SLOTS slots lie.  Sequence b has the places from start[b] / SLOTS + 2 b on, as many as its n rows can
