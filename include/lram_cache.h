@@ -6,8 +6,10 @@
  * The conventions are those of lram.h and lram_layer.h: the caller's memory and stream, status codes, checks on the host
  * before any launch, nothing kept between calls, results that have the same bits on every call.  dtype is LRAM_F32 or
  * LRAM_BF16.  Angles are exact to 2^-32 of a turn, their sines and cosines fp32; a rotated value is rounded once.  Attention's
- * sums, statistics, weights and partial results are fp32; in bf16 the softmax's weights are rounded to bf16 before
- * the product with the values (their sums, and the weights that keys gather, are of the unrounded ones).
+ * sums, statistics, weights and partial results are fp32.  In bf16 the softmax's weights enter the product with the values
+ * with 16 bits (less than 2^-15 of one is lost) where a call expects at most 16 new rows times heads / kv_heads of a sequence
+ * (by max_q and by rows / batch), otherwise rounded to bf16; their sums, and the weights that keys gather, are of the
+ * unrounded ones.
  */
 #ifndef LRAM_CACHE_H
 #define LRAM_CACHE_H
