@@ -2,12 +2,14 @@
 the text, forward and backward.
 
 As in the package's other calls, this module only marshals torch tensors and the current HIP stream into the C ABI
-(``include/lram_cache.h``); there is no fallback.  Angles are exact to 2^-32 of a turn at any position, and a rotated value is
-rounded once.
+(``include/lram_cache.h``); there is no fallback.  Angles of a plan's turns are exact to 2^-32 of a turn at any position, those
+turns are its frequencies rounded to the nearest 2^-64 (2^-34 of a turn at the farthest position), and a rotated value is rounded
+once.
 """
 from __future__ import annotations
 
 import ctypes
+import decimal
 import math
 from typing import NamedTuple, Optional, Tuple
 
@@ -28,6 +30,8 @@ class _Rotary(ctypes.Structure):
     _fields_ = [("pairs", _I32), ("interleaved", _I32), ("magnitude", ctypes.c_float), ("turns", _P)]
 
 
+TWO_PI = decimal.Decimal("6.28318530717958647692528676655900576839433879875021164194988918461563"
+                         "2812572417997256069650684234135964296173")
 _lib = None
 
 
@@ -76,17 +80,21 @@ def rotary_plan(dim: int, base: float = 10000.0, interleaved: bool = False, scal
         raise LramError("scaling 'parts' needs length > 0 and 0 <= low < high")
     if scaling == "base" and dim < 4:
         raise LramError("scaling 'base' needs at least 4 dimensions")
-    magnitude = 1.0
-    if scaling == "base":
-        base = base * factor ** (dim / (dim - 2))
-    turns = [base ** (-2 * i / dim) / (2 * math.pi) for i in range(dim // 2)]
-    if scaling == "linear":
-        turns = [t / factor for t in turns]
-    elif scaling == "parts":
-        stays = [min(max((length * t - low) / (high - low), 0.0), 1.0) for t in turns]
-        turns = [t * (s + (1 - s) / factor) for t, s in zip(turns, stays)]
-        magnitude = 0.1 * math.log(factor) + 1
-    bits = [int(t * 2.0 ** 64) % (1 << 64) for t in turns]
+    magnitude = 0.1 * math.log(factor) + 1 if scaling == "parts" else 1.0
+    # a double's 53 bits of a frequency would leave 2^-25 of a turn at the farthest positions, so decimal digits: 64 bits are 20,
+    # and what is left holds whole turns
+    with decimal.localcontext(decimal.Context(prec=100, rounding=decimal.ROUND_HALF_EVEN, traps=[])):
+        base, factor, length, low, high = (decimal.Decimal(float(x)) for x in (base, factor, length, low, high))
+        size = decimal.Decimal(int(dim))
+        if scaling == "base":
+            base = base * factor ** (size / (size - 2))
+        turns = [base ** (-2 * i / size) / TWO_PI for i in range(dim // 2)]
+        if scaling == "linear":
+            turns = [t / factor for t in turns]
+        elif scaling == "parts":
+            stays = [min(max((length * t - low) / (high - low), 0), 1) for t in turns]
+            turns = [t * (s + (1 - s) / factor) for t, s in zip(turns, stays)]
+        bits = [int((t * (1 << 64)).to_integral_value()) % (1 << 64) for t in turns]
     return Rotary(torch.tensor([b - (1 << 64) if b >> 63 else b for b in bits]).to(device), bool(interleaved), magnitude)
 
 
