@@ -71,7 +71,8 @@ class KeyValueCache:
 
 
 class MemoryBlock(torch.nn.Module):
-    """rotary: positions by rotation (of the plan's pairs of every head) in place of the learned bias."""
+    """rotary: positions by rotation (of the plan's pairs of every head) in place of the learned bias.  The state holds the
+    rotation whole (turns, and rotation: layout and magnitude), so that a loaded one takes the place of the constructor's."""
 
     def __init__(self, w: int, heads: int, K: Sequence[int], kv_heads: Optional[int] = None, causal: bool = False,
                  buckets: int = 32, reach: int = 128, eps: float = 1e-5, table_dtype=torch.bfloat16,
@@ -93,7 +94,7 @@ class MemoryBlock(torch.nn.Module):
         self.proj = torch.nn.Linear(w, w, **new)
         self.rotates = rotary is not None
         if rotary is not None:
-            self.register_buffer("turns", rotary.turns.to(device))
+            self.register_buffer("turns", rotary.turns.to(device).clone())  # its own: a loaded state replaces it
             self.interleaved, self.magnitude = rotary.interleaved, rotary.magnitude
         else:
             self.bias = torch.nn.Parameter(torch.zeros((heads, buckets), **new))
@@ -101,6 +102,30 @@ class MemoryBlock(torch.nn.Module):
         self.norm_w = torch.nn.ParameterList([torch.ones(w, **new) for _ in range(2)])
         self.norm_b = torch.nn.ParameterList([torch.zeros(w, **new) for _ in range(2)])
         self.memory = memory if memory is not None else MemorySubnetwork(w, K, table_dtype, dtype, device=device)
+
+    def _save_to_state_dict(self, destination, prefix, keep_vars):
+        super()._save_to_state_dict(destination, prefix, keep_vars)
+        if self.rotates:  # with turns, the whole rotation
+            destination[prefix + "rotation"] = torch.tensor([float(self.interleaved), self.magnitude], dtype=torch.float64)
+
+    def _load_from_state_dict(self, state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, error_msgs):
+        own = self.turns.clone() if self.rotates else None
+        super()._load_from_state_dict(state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, error_msgs)
+        if not self.rotates:
+            return
+        name, turns = prefix + "rotation", state_dict.get(prefix + "turns")
+        rest = state_dict.get(name)
+        if name in unexpected_keys:
+            unexpected_keys.remove(name)
+        if rest is not None and rest.shape != (2,):
+            error_msgs.append("%s must hold a rotation's layout and magnitude" % name)
+        elif rest is not None and turns is not None and turns.shape == own.shape:
+            self.interleaved, self.magnitude = bool(rest[0]), float(rest[1])
+        elif strict:
+            # turns alone go with the block's layout and magnitude only where they are the block's own, to what a double rounds
+            off = None if turns is None or turns.shape != own.shape or own.is_meta else turns.to(own.device) - own
+            if off is None or not bool(((off < 1 << 14) & (off > -(1 << 14))).all()):
+                missing_keys.append(name)
 
     def _heads(self, x: torch.Tensor):
         a, b = self.heads * self.head_dim, (self.heads + self.kv_heads) * self.head_dim
