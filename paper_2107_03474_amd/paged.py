@@ -11,10 +11,11 @@ import math
 from typing import List, NamedTuple, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import F32, LramError
 from . import load as _load_library
-from .layer import HEAD_DIMS, Packed, RelativeBias, _check, _heads, _ptr, _records, _scratch, _type
+from .layer import HEAD_DIMS, Packed, RelativeBias, _check, _heads, _ptr, _scratch, _type
 from .positions import Rotary, _launch, _refusal, _Rotary, _rotary
 
 __all__ = ["PagedKeys", "PageTable", "paged_keys", "page_table", "paged_extend", "paged_append", "paged_attention",
@@ -143,6 +144,13 @@ def _describe(keys: PagedKeys, table: PageTable, heads: int = 0, rows: int = 0, 
                   rows, max_q, max_k)
 
 
+def _differentiated(*inputs: Optional[torch.Tensor]) -> bool:
+    """Whether a derivative of these inputs is asked for, backward or by a tangent (no_grad leaves tangents as they are)."""
+    inputs = [t for t in inputs if t is not None]
+    return (torch.is_grad_enabled() and any(t.requires_grad for t in inputs) or
+            forward_ad._current_level >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in inputs))
+
+
 def _like_keys(t: torch.Tensor, name: str, keys: PagedKeys, dim: int):
     """(address, row stride, head stride) of new rows that go with the cache."""
     k, shape = keys.k, t.shape
@@ -199,7 +207,7 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, keys: PagedKeys, table: PageT
     weight [rows, kv_heads] fp32 they begin with these weights, not with 0.  Returns q [rows, heads, head_dim] rotated (q
     itself without a rotation, None without q).  Only start_q and max_q of seqs are used."""
     lib = _library()
-    if _records(k, v, q):
+    if _differentiated(k, v, q):
         raise LramError("a cache has no gradients: append to it under torch.no_grad()")
     rows = k.shape[0]
     a = _describe(keys, table, q.shape[1] if q is not None and q.dim() == 3 else 0, rows, seqs)
@@ -237,7 +245,7 @@ def paged_attention(q: torch.Tensor, keys: PagedKeys, table: PageTable, seqs: Pa
     1 / sqrt(head_dim) by default.  weigh: the weights that each key is given, summed over queries and the heads that share
     it, are added to keys.weight.  Of seqs start_q, max_q and max_k are used."""
     lib = _library()
-    if _records(q, None if rel is None else rel.weight):
+    if _differentiated(q, None if rel is None else rel.weight):
         raise LramError("attention over a cache has no gradients: call it under torch.no_grad()")
     if q.dim() != 3:
         raise LramError("q must be [rows, heads, head_dim]")
