@@ -9,6 +9,7 @@ liblram's kernels; the projections are library GEMMs.
 """
 from __future__ import annotations
 
+import math
 from typing import Optional, Sequence, Union
 
 import torch
@@ -86,8 +87,15 @@ class MemoryBlock(torch.nn.Module):
         refusal = bias_refusal(heads, kv_heads, w // heads, dtype, buckets, reach) if rotary is None else None
         if refusal:
             raise ValueError(refusal)
-        if rotary is not None and not 1 <= rotary.turns.numel() <= w // heads // 2:
-            raise ValueError("a rotation has 1 to head_dim / 2 pairs")
+        if heads > 64 * kv_heads:
+            raise ValueError("heads must be at most 64 times kv_heads")
+        if rotary is not None:
+            if rotary.turns.dtype != torch.int64 or rotary.turns.dim() != 1:
+                raise ValueError("a rotation's turns must be [pairs] int64")
+            if not 1 <= rotary.turns.numel() <= w // heads // 2:
+                raise ValueError("a rotation has 1 to head_dim / 2 pairs")
+            if not math.isfinite(rotary.magnitude):
+                raise ValueError("a rotation's magnitude must be finite")
         self.heads, self.kv_heads, self.head_dim, self.causal, self.eps = heads, kv_heads, w // heads, causal, eps
         new = dict(device=device, dtype=dtype)
         self.qkv = torch.nn.Linear(w, (heads + 2 * kv_heads) * self.head_dim, **new)
