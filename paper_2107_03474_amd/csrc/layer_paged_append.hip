@@ -4,7 +4,7 @@
 // their heads; a lane owns pairs of 16-byte chunks of single rows and forms their sines and cosines once for all of these
 // heads.  v: a wave takes 32 key slots; a lane takes 16 bytes of each of the 4 F keys that lie side by side in the page and
 // turns them round in its registers, and a whole block goes out by way of LDS.  Bound by HBM for prompts (28,654 rows of 32/8
-// heads of 128 bf16, 704 MB in 143 us, 4.9 TB/s where a large copy reaches 5.1; q and the others in launches of their own took
+// heads of 128 bf16, 704 MB in 145 us, 4.9 TB/s where a large copy reaches 5.1; q and the others in launches of their own took
 // 9 us more), by its launch for single tokens (32: 5.5 us).
 
 #include "layer_paged.h"
@@ -32,9 +32,10 @@ struct Tile {
   int from, to, position;
 };
 
-// A chunk into a page.  Pages are next read by other launches, most of them from other L2s, so it goes past the cache (28,654
-// rows of 32/8 heads of 128 bf16: 149 -> 143 us, keys and values alone 48 -> 40; 32,768 of 8 heads of 64 fp32 58 -> 46, of 128
-// 136 -> 143; one token of 32 sequences is as fast).  Pieces of 64 bytes of a lane lose by it (fp32 values: 136 -> 243).
+// A chunk into a page.  Pages are next read by other launches, most of them from other L2s, so it goes past the cache (us over two
+// sets of data in turn: 28,654 rows of 32/8 heads of 128 bf16 150 -> 145, 8,200 of 16/8 27.2 -> 26.8, keys and values of 32,768
+// rows of 8 heads of 64 fp32 68 -> 67; of 128 fp32 it costs, 142 -> 150; one token of 32 sequences is as fast).  Pieces of 64 bytes
+// of a lane lose by it (fp32 values of heads of 128: 136 -> 243).
 template <typename T>
 __device__ __forceinline__ void put(T* to, typename Chunk<T>::type x) {
   __builtin_nontemporal_store(x, (typename Chunk<T>::type*)to);

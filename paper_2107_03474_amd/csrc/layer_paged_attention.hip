@@ -9,11 +9,14 @@
 // and has in its results the second operand of O^T += V^T P^T.  No value crosses lanes but the maximum, and LDS is met once,
 // when the four waves of a workgroup join what they have.  Long caches are cut into pieces, joined by a second kernel, which
 // also adds up the weights that keys gather.  Measured: 32 tokens over caches of 256 to 8,192, 32/8 heads of 128 bf16, 531 MB
-// in 88 us, 6.0 TB/s where a plain read reaches 6.9; one token over 131,072 keys 99 us, 5.4 TB/s.
+// in 88 us, 6.0 TB/s where a plain read reaches 6.9; one token over 131,072 keys 84 us, 6.4 TB/s, and 100 where scores are kept
+// for the weights.
 //
-// Prompts and pieces of them take tiles of 32 columns, so that a load serves two products.  4,096 causal tokens, 32/8 heads of
-// 128 bf16: 230 us, 600 TFLOP/s of what is met; a form with 128 columns a workgroup, whose waves shared keys through LDS, took
-// 272 us, and 174 for 4 x 100 tokens over 101 to 12,345 keys, for 146.
+// Prompts and pieces of them take tiles of 32 columns, so that a load serves two products, and leave out keys that no query of
+// the tile may meet.  4,096 causal tokens, 32/8 heads of 128 bf16: 207 to 232 us, 590 to 660 TFLOP/s of what is met, bound by the
+// softmax's vector instructions (0.61 of a unit's issue) and by waits for keys; 4 x 100 tokens over 101 to 12,345 keys 126 us and
+// a join of 17.  A form with 128 columns a workgroup, whose waves shared keys through LDS, was timed without leaving keys out:
+// there it took 272 us for the prompt, this one 398, and for the pieces 174, this one 146.  With it, it was not built.
 
 #include "layer_paged.h"
 

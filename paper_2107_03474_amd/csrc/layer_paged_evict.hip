@@ -7,6 +7,8 @@
 // keeps in registers; it moves a few keys itself, and leaves many to a second kernel that fills the card.  Bound by the chain of
 // dependent steps: 8 us for 256 heads of 2,049 keys, of which one goes; 26 us for 64 heads of 512 to 8,192 keys, many of equal
 // weight, and 32 us for the 31,000 keys that move (16 bytes of k and 2 of v lie together, so that a move touches 2 KiB of each).
+// Past KEPT ranks a thread a head's workgroup forms them again for every digit: 8 heads of 131,072 keys cut to 4,096 take 453 us,
+// and the moves 27, where the ranks' bytes are worth a launch.
 
 #include "layer_paged.h"
 

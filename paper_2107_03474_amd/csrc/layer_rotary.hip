@@ -1,8 +1,8 @@
 // layer_rotary.hip -- part of liblram: rotary positions for gfx950.
 //
-// Bound by HBM: every element is read and written once (rotate_chunk).  16,384 rows of 32/8 heads of 128 bf16: 51 to 61 us,
-// 5.5 to 6.5 TB/s; 8,192 rows of 8/8 heads of 64 7.4 us, 4.5 TB/s; 17 pairs of 64 dimensions in fp32, 5,003 rows of 12/4 heads,
-// 10 us, 4.1 TB/s.
+// Bound by HBM: every element is read and written once (rotate_chunk).  16,384 rows of 32/8 heads of 128 bf16: 61 us, 5.5 TB/s
+// (52 where the same rows are rotated again and again); 8,192 rows of 8/8 heads of 64 7.7 us, 4.4 TB/s; 17 pairs of 64 dimensions
+// in fp32, 5,003 rows of 12/4 heads, 10 us, 4.0 TB/s.
 
 #include <algorithm>
 

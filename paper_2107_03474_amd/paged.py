@@ -2,7 +2,9 @@
 of new tokens over it, and eviction from it by accumulated attention weight.
 
 As in the package's other calls, this module only marshals torch tensors and the current HIP stream into the C ABI
-(``include/lram_cache.h``, which says where a key lies in its page); there is no fallback.
+(``include/lram_cache.h``, which says where a key lies in its page); there is no fallback.  Sums, statistics and weights are fp32.
+In bf16 attention's softmax weights enter the product with the values with 16 bits where a call expects at most 16 new rows times
+heads / kv_heads of a sequence, otherwise rounded to bf16.
 """
 from __future__ import annotations
 
@@ -243,7 +245,8 @@ def paged_attention(q: torch.Tensor, keys: PagedKeys, table: PageTable, seqs: Pa
     """softmax(scale q k^T + bias) v of each sequence's new rows (q [rows, heads, head_dim], packed by seqs.start_q) over the
     keys in its pages whose positions are not past theirs; the bias is that of the distance between positions, the scale
     1 / sqrt(head_dim) by default.  weigh: the weights that each key is given, summed over queries and the heads that share
-    it, are added to keys.weight.  Of seqs start_q, max_q and max_k are used."""
+    it, are added to keys.weight.  Of seqs start_q, max_q and max_k are used; the work is divided by the longest, so that single
+    tokens over long texts are served faster in a call without prompts."""
     lib = _library()
     if _differentiated(q, None if rel is None else rel.weight):
         raise LramError("attention over a cache has no gradients: call it under torch.no_grad()")
