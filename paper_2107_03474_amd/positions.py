@@ -84,15 +84,17 @@ def rotary_plan(dim: int, base: float = 10000.0, interleaved: bool = False, scal
     # a double's 53 bits of a frequency would leave 2^-25 of a turn at the farthest positions, so decimal digits: 64 bits are 20,
     # and what is left holds whole turns
     with decimal.localcontext(decimal.Context(prec=100, rounding=decimal.ROUND_HALF_EVEN, traps=[])):
-        base, factor, length, low, high = (decimal.Decimal(float(x)) for x in (base, factor, length, low, high))
-        size = decimal.Decimal(int(dim))
+        def of(x):
+            return decimal.Decimal(float(x))
+
+        base, factor, size = of(base), of(factor) if scaling else None, decimal.Decimal(int(dim))
         if scaling == "base":
             base = base * factor ** (size / (size - 2))
         turns = [base ** (-2 * i / size) / TWO_PI for i in range(dim // 2)]
         if scaling == "linear":
             turns = [t / factor for t in turns]
         elif scaling == "parts":
-            stays = [min(max((length * t - low) / (high - low), 0), 1) for t in turns]
+            stays = [min(max((of(length) * t - of(low)) / (of(high) - of(low)), 0), 1) for t in turns]
             turns = [t * (s + (1 - s) / factor) for t, s in zip(turns, stays)]
         bits = [int((t * (1 << 64)).to_integral_value()) % (1 << 64) for t in turns]
     return Rotary(torch.tensor([b - (1 << 64) if b >> 63 else b for b in bits]).to(device), bool(interleaved), magnitude)

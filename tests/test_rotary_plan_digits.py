@@ -88,6 +88,13 @@ def test_every_bit_of_a_frequency(plan):
         assert abs(off) <= Fraction(1, 2) + Fraction(1, 1 << 40), (i, float(off))
 
 
+def test_what_no_scaling_needs_is_not_read():
+    plain = lram.rotary_plan(8, device="cpu").turns.tolist()
+    assert lram.rotary_plan(8, factor=None, length=None, low=None, high=None, device="cpu").turns.tolist() == plain
+    linear = lram.rotary_plan(8, scaling="linear", factor=2, length=None, low=None, high=None, device="cpu").turns.tolist()
+    assert linear == lram.rotary_plan(8, scaling="linear", factor=2.0, device="cpu").turns.tolist()
+
+
 def test_angles_at_the_farthest_position():
     """What a frequency's rounding leaves of an angle at position 2^31: at most 2^-34 of a turn."""
     got = [t % (1 << 64) for t in lram.rotary_plan(128, device="cpu").turns.tolist()]
